@@ -7,8 +7,12 @@
  *
  *   kvq_pack         append the step's new K/V to a KbVb cache (Sec. 3.1)
  *   kvq_decode_attn  softmax(q K^T / sqrt(d)) V over that cache (Sec. 1)
+ *   kvq_chunk_attn   the same for the newest n_q tokens of each sequence (prompt
+ *                    chunks, draft tokens), with a sliding window and sinks
  *   dgap_restore     features, detector, gate, top-K corrector, sparse merge
  *                    on the step's logits (Sec. 4.1-4.3, Eqs. 2, 6, 11-13)
+ *   kvq_sample       the next token of each row of logits by temperature,
+ *                    top-k, top-p and min-p from given random numbers
  *   kvq_drift_*      offline drift metrics on paired FP16 / low-bit logits and
  *                    the recovery-window rule (Sec. 4.1, Sec. 4.2)
  *
@@ -358,6 +362,51 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
                                    void* stream);
 
 /*
+ * kvq_chunk_attn — attention of the n_q newest tokens of each sequence over
+ * its cache, causal, with an optional sliding window.  The tokens are in the
+ * cache already (kvq_pack of n_new = n_q first): with L = seq_len[b], query t
+ * of sequence b stands at position p = L - n_q + t and sees token j when
+ *   0 <= j <= p  and  (window == 0  or  j > p - window  or  j < sinks),
+ * packed tokens in quantized form and the residual window in fp16, as
+ * kvq_decode_attn does (n_q = 1 without a window is the same operator).
+ *   out[b, t, i] = softmax_j(q[b, t, i] . K_hat[b, g(i), j] * softmax_scale)
+ *                  V_hat[b, g(i), j]
+ * A query that stands before the first token (L < n_q) gets a zero output.
+ * Dequantized keys and values are rounded once to fp16 (zero + scale * code in
+ * one fused multiply-add), the softmax weights too; scores, the running
+ * maximum and sum, and the output accumulate in fp32, and the result is
+ * rounded once to fp16.
+ *   q, out       device fp16, element (b, t, i, d) at b * stride[0] + t *
+ *                stride[1] + i * stride[2] + d for sequence batch_begin + b;
+ *                16-byte aligned.
+ *   params       below.
+ *   workspace    device, >= kvq_chunk_workspace_bytes(cfg, n_q, batch_count),
+ *                zeroed once by kvq_workspace_init; calls sharing it must not
+ *                overlap on the GPU.
+ * Lengths are read on the device; the call can be captured in a CUDA graph.
+ */
+typedef struct kvq_chunk_params {
+  int32_t n_q;           /* queries per sequence, 1 .. max_len */
+  int32_t window;        /* newest tokens seen, the query's own included; 0: all */
+  int32_t sinks;         /* with a window: first tokens that stay visible, >= 0 */
+  float softmax_scale;   /* 0 selects 1/sqrt(128) */
+  int64_t q_stride[3];   /* elements between sequences, tokens, heads: multiples
+                            of 8, >= 0 (0 repeats the same queries) */
+  int64_t out_stride[3]; /* the same for out; >= 128 where the size is over 1,
+                            and no two rows may overlap */
+} kvq_chunk_params;
+
+/* Workspace bytes of kvq_chunk_attn (0 on an invalid config, n_q outside
+ * [1, max_len] or batch_count outside [1, batch]). */
+size_t kvq_chunk_workspace_bytes(const kvq_config* cfg, int32_t n_q, int32_t batch_count);
+
+kvq_status kvq_chunk_attn(const kvq_config* cfg, const kvq_cache* cache,
+                          const uint16_t* q, uint16_t* out,
+                          const kvq_chunk_params* params, int32_t batch_begin,
+                          int32_t batch_count, void* workspace, size_t ws_bytes,
+                          void* stream);
+
+/*
  * DGAP parameters (Sec. 4.2 detector, Sec. 4.3 corrector).  Weights are
  * device fp32, row-major [out][in]; H = hidden.
  *   detector  f = w2 . relu(W1 phi + b1) + b2, r = sigmoid(f)   (Eq. 6)
@@ -418,6 +467,43 @@ kvq_status dgap_restore(const dgap_params* params, float* logits,
                         float* topk_val, float* risk, uint8_t* gate,
                         int32_t* next_token, float* features, void* workspace,
                         size_t ws_bytes, void* stream);
+
+/* Largest vocab kvq_sample accepts (262144). */
+int32_t kvq_sample_max_vocab(void);
+
+/*
+ * kvq_sample — the next token of each row z (fp32; finite or -inf, a forbidden
+ * token) from given random numbers.  With T, k, p, m the row's temperature,
+ * top_k, top_p, min_p, the order of the tokens being value descending, lowest
+ * index first among equal values, d_i = (z_i - max z) / T and e_i = exp(d_i):
+ *   K     the first k tokens of the order (k <= 0: all of them);
+ *   P     those of K whose predecessors in K hold less than p times the e-sum
+ *         of K (p >= 1: all of K; p <= 0: its first);
+ *   M     the tokens with e_i >= m (m <= 0: all);
+ *   kept  P and M, and the first token of the order in any case; never -inf;
+ *   token the kept i with the largest d_i - ln(-ln u_i), lowest index on ties:
+ *         with u uniform in [0, 1) an exact draw from the kept tokens'
+ *         renormalised probabilities.
+ * T <= 0 (or NaN) takes the first token of the order.
+ *   logits       device fp32, row b at b * logits_stride, read only.
+ *   noise        device fp32 u, row b at b * noise_stride; only kept tokens'
+ *                numbers are read.  NULL: every row takes its first token.
+ *   temperature, top_k, top_p, min_p
+ *                device arrays [batch], each NULL for "no such limit" (T = 1).
+ *   token        device int32 [batch]; -1 for a row of -inf alone.
+ *   logprob      device fp32 [batch] or NULL: d_token - ln(sum of all e_i), the
+ *                token's log-probability at temperature T (1 where T <= 0)
+ *                before any limit; -inf for a row of -inf alone.
+ * The e_i are summed as multiples of 2^-40 in integers, so the kept set does
+ * not depend on any order of summation and repeats bit for bit.
+ * No workspace; calls on different outputs may overlap.
+ */
+kvq_status kvq_sample(const float* logits, int64_t logits_stride,
+                      const float* noise, int64_t noise_stride, int32_t batch,
+                      int32_t vocab, const float* temperature,
+                      const int32_t* top_k, const float* top_p,
+                      const float* min_p, int32_t* token, float* logprob,
+                      void* stream);
 
 /*
  * kvq_selftest_wait_timeout — checks on the device that a bounded wait gives

@@ -457,6 +457,112 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
                      "kvq_decode_attn_noalloc launch");
 }
 
+static kvq_status check_chunk_sizes(const kvq_config* cfg, int32_t n_q, int32_t batch_count) {
+  kvq_status s = check_config(cfg);
+  if (s != KVQ_OK) return s;
+  if (n_q < 1 || n_q > cfg->max_len)
+    return fail(KVQ_ERR_ARG, "n_q must be in [1, max_len] (got %d)", n_q);
+  if (batch_count < 1 || batch_count > cfg->batch)
+    return fail(KVQ_ERR_SHAPE, "batch_count must be in [1, %d] (got %d)", cfg->batch, batch_count);
+  if ((long long)n_q * cfg->n_q_heads * batch_count > (1LL << 30))
+    return fail(KVQ_ERR_SHAPE, "batch_count * n_q * n_q_heads must be <= 2^30");
+  return KVQ_OK;
+}
+
+size_t kvq_chunk_workspace_bytes(const kvq_config* cfg, int32_t n_q, int32_t batch_count) {
+  if (check_chunk_sizes(cfg, n_q, batch_count) != KVQ_OK) return 0;
+  return chunk_workspace_bytes(make_dims(*cfg), n_q, batch_count, sm_count());
+}
+
+kvq_status kvq_chunk_attn(const kvq_config* cfg, const kvq_cache* cache, const uint16_t* q,
+                          uint16_t* out, const kvq_chunk_params* p, int32_t batch_begin,
+                          int32_t batch_count, void* workspace, size_t ws_bytes, void* stream) {
+  kvq_status s = check_config(cfg);
+  if (s != KVQ_OK) return s;
+  if ((s = check_cache(*cfg, cache)) != KVQ_OK) return s;
+  if (!q || !out || !p) return fail(KVQ_ERR_ARG, "q, out or params is NULL");
+  if (!aligned16(q) || !aligned16(out))
+    return fail(KVQ_ERR_ALIGN, "q / out must be 16-byte aligned");
+  if ((s = check_chunk_sizes(cfg, p->n_q, batch_count)) != KVQ_OK) return s;
+  if (batch_begin < 0 || batch_begin > cfg->batch - batch_count)
+    return fail(KVQ_ERR_SHAPE, "batch range begins at %d and holds %d of %d sequences",
+                batch_begin, batch_count, cfg->batch);
+  if (p->window < 0 || p->sinks < 0)
+    return fail(KVQ_ERR_ARG, "window and sinks must be >= 0 (got %d, %d)", p->window, p->sinks);
+  if (!(p->softmax_scale >= 0.0f) || isinf(p->softmax_scale))
+    return fail(KVQ_ERR_ARG, "softmax_scale must be finite and >= 0");
+  const int sizes[3] = {batch_count, p->n_q, cfg->n_q_heads};
+  ChunkCall call;
+  for (int i = 0; i < 3; ++i) {
+    if (p->q_stride[i] < 0 || p->out_stride[i] < 0)
+      return fail(KVQ_ERR_ARG, "strides must be >= 0");
+    if ((p->q_stride[i] | p->out_stride[i]) & 7)
+      return fail(KVQ_ERR_ALIGN, "strides must be multiples of 8 elements");
+    if (sizes[i] > 1 && p->out_stride[i] < kHeadDim)
+      return fail(KVQ_ERR_ARG, "out_stride[%d] must be >= 128 (got %lld)", i,
+                  (long long)p->out_stride[i]);
+    call.q_stride[i] = p->q_stride[i];
+    call.out_stride[i] = p->out_stride[i];
+  }
+  const Dims d = make_dims(*cfg);
+  const size_t need = chunk_workspace_bytes(d, p->n_q, batch_count, sm_count());
+  if (!workspace) return fail(KVQ_ERR_ARG, "workspace is NULL");
+  if (!aligned16(workspace)) return fail(KVQ_ERR_ALIGN, "workspace must be 16-byte aligned");
+  if (ws_bytes < need)
+    return fail(KVQ_ERR_CAPACITY, "workspace too small: %zu < %zu bytes", ws_bytes, need);
+  const float scale =
+      p->softmax_scale == 0.0f ? 1.0f / sqrtf((float)kHeadDim) : p->softmax_scale;
+  call.scale_log2 = scale * 1.4426950408889634f;
+  call.n_q = p->n_q;
+  call.window = p->window;
+  call.sinks = p->window ? p->sinks : 0;
+  call.batch_begin = batch_begin;
+  call.batch_count = batch_count;
+  trace("kvq_chunk_attn batch [%d, %d) n_q %d window %d sinks %d heads %d/%d bits K%dV%d",
+        batch_begin, batch_begin + batch_count, call.n_q, call.window, call.sinks, d.hq, d.hkv,
+        d.bits_k, d.bits_v);
+  return cuda_status(launch_chunk_attn(d, *cache, reinterpret_cast<const __half*>(q),
+                                       reinterpret_cast<__half*>(out), call, sm_count(),
+                                       workspace, static_cast<cudaStream_t>(stream)),
+                     "kvq_chunk_attn launch");
+}
+
+int32_t kvq_sample_max_vocab(void) { return sample_max_vocab(); }
+
+kvq_status kvq_sample(const float* logits, int64_t logits_stride, const float* noise,
+                      int64_t noise_stride, int32_t batch, int32_t vocab,
+                      const float* temperature, const int32_t* top_k, const float* top_p,
+                      const float* min_p, int32_t* token, float* logprob, void* stream) {
+  if (!logits || !token) return fail(KVQ_ERR_ARG, "logits or token is NULL");
+  if (batch < 1 || batch > 65535)
+    return fail(KVQ_ERR_SHAPE, "batch must be in [1, 65535] (got %d)", batch);
+  if (vocab < 1) return fail(KVQ_ERR_SHAPE, "vocab must be >= 1 (got %d)", vocab);
+  if (vocab > sample_max_vocab())
+    return fail(KVQ_ERR_UNSUPPORTED, "vocab must be <= %d (got %d)", sample_max_vocab(), vocab);
+  if (batch > 1 && (logits_stride < vocab || (noise && noise_stride < 0)))
+    return fail(KVQ_ERR_ARG, "logits_stride must be >= vocab and noise_stride >= 0");
+  for (const void* p : {(const void*)logits, (const void*)noise, (const void*)temperature,
+                        (const void*)top_k, (const void*)top_p, (const void*)min_p,
+                        (const void*)token, (const void*)logprob})
+    if (reinterpret_cast<uintptr_t>(p) & 3u)
+      return fail(KVQ_ERR_ALIGN, "pointers must be 4-byte aligned");
+  SampleCall c;
+  c.logits = logits;
+  c.noise = noise;
+  c.logits_stride = batch > 1 ? logits_stride : 0;
+  c.noise_stride = batch > 1 ? noise_stride : 0;
+  c.batch = batch;
+  c.vocab = vocab;
+  c.temperature = temperature;
+  c.top_k = top_k;
+  c.top_p = top_p;
+  c.min_p = min_p;
+  c.token = token;
+  c.logprob = logprob;
+  trace("kvq_sample batch %d vocab %d", batch, vocab);
+  return cuda_status(launch_sample(c, static_cast<cudaStream_t>(stream)), "kvq_sample launch");
+}
+
 static kvq_status check_dgap(const dgap_params* p, int32_t batch, int32_t vocab) {
   if (!p) return fail(KVQ_ERR_ARG, "params is NULL");
   if (batch < 1 || vocab < 1) return fail(KVQ_ERR_SHAPE, "batch and vocab must be >= 1");

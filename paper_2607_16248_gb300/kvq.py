@@ -30,7 +30,8 @@ EXPORTS = (
     "kvq_attn_workspace_bytes", "kvq_attn_default_splits", "kvq_attn_splits_for_lengths",
     "kvq_workspace_init",
     "kvq_decode_attn", "kvq_decode_attn_f32", "kvq_decode_step", "kvq_decode_step_f32",
-    "kvq_decode_attn_noalloc", "dgap_workspace_bytes",
+    "kvq_decode_attn_noalloc", "kvq_chunk_workspace_bytes", "kvq_chunk_attn",
+    "kvq_sample_max_vocab", "kvq_sample", "dgap_workspace_bytes",
     "dgap_restore", "kvq_drift_max_vocab", "kvq_drift_metrics", "kvq_drift_window",
     "kvq_selftest_wait_timeout",
 )
@@ -60,6 +61,12 @@ class _DriftParams(ctypes.Structure):
                 ("eps", ctypes.c_float), ("rho_c", ctypes.c_float)]
 
 
+class _ChunkParams(ctypes.Structure):
+    _fields_ = [("n_q", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 3),
+                ("out_stride", ctypes.c_int64 * 3)]
+
+
 class _DgapParams(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("hidden", ctypes.c_int32), ("tau", ctypes.c_float)] + [
         (n, ctypes.c_void_p) for n in ("det_w1", "det_b1", "det_w2", "det_b2",
@@ -75,6 +82,7 @@ def lib():
                                "paper_2607_16248_gb300.build.build()")
         L = ctypes.CDLL(str(_LIB_PATH))
         P, I32, SZ, F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
+        I64 = ctypes.c_int64
         cfg_p = ctypes.POINTER(_Config)
         cache_p = ctypes.POINTER(_Cache)
         par_p = ctypes.POINTER(_DgapParams)
@@ -100,6 +108,11 @@ def lib():
             "kvq_decode_step": (I32, [cfg_p, cache_p, P, P, P, P, F32, I32, P, SZ, P]),
             "kvq_decode_step_f32": (I32, [cfg_p, cache_p, P, P, P, P, F32, I32, P, SZ, P]),
             "kvq_decode_attn_noalloc": (I32, [cfg_p, cache_p, P, P, F32, I32, P]),
+            "kvq_chunk_workspace_bytes": (SZ, [cfg_p, I32, I32]),
+            "kvq_chunk_attn": (I32, [cfg_p, cache_p, P, P, ctypes.POINTER(_ChunkParams), I32,
+                                     I32, P, SZ, P]),
+            "kvq_sample_max_vocab": (I32, []),
+            "kvq_sample": (I32, [P, I64, P, I64, I32, I32, P, P, P, P, P, P, P]),
             "dgap_workspace_bytes": (SZ, [I32, I32, par_p]),
             "dgap_restore": (I32, [par_p, P, I32, I32, P, P, P, P, P, P, P, SZ, P]),
             "kvq_drift_max_vocab": (I32, []),
@@ -417,6 +430,111 @@ def kvq_decode_attn_noalloc(cache: QuantKVCache, q, out, softmax_scale=0.0, n_sp
                                          _dev(out, torch.float32, "out"), float(softmax_scale),
                                          n_splits, _stream(stream)))
     return out
+
+
+def chunk_workspace(cfg: CacheConfig, n_q, batch_count=None, device="cuda"):
+    """A zeroed workspace for kvq_chunk_attn of n_q queries per sequence."""
+    c = cfg.c()
+    n = lib().kvq_chunk_workspace_bytes(ctypes.byref(c), n_q,
+                                        cfg.batch if batch_count is None else batch_count)
+    if n == 0:
+        raise KvqError(1, last_error())
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _rows(t, name):
+    """The pointer of an fp16 CUDA tensor [..., 128] whose last dimension is
+    contiguous (the others may have any strides)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != torch.float16:
+        raise TypeError(f"{name} must be torch.float16, got {t.dtype}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_scale=0.0,
+                   batch_begin=0, workspace=None, stream=None):
+    """Causal attention of the n_q newest tokens of sequences [batch_begin,
+    batch_begin + batch_count), which kvq_pack has appended before: q fp16
+    [batch_count, n_q, n_q_heads, 128] (strided views too) -> out fp16 of that
+    shape.  window > 0: each query sees the ``window`` newest tokens up to its
+    own and the first ``sinks`` tokens.  n_q = 1 is the windowed form of a
+    decode step."""
+    cfg = cache.cfg
+    if q.dim() != 4 or q.shape[2] != cfg.n_q_heads or q.shape[3] != cfg.head_dim:
+        raise ValueError(f"q must be [batch_count, n_q, {cfg.n_q_heads}, {cfg.head_dim}]")
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    batch_count, n_q = q.shape[:2]
+    if workspace is None:
+        workspace = chunk_workspace(cfg, n_q, batch_count, q.device)
+    # the stride of a dimension of size 1 says nothing
+    strides = [[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)] for t in (q, out)]
+    p = _ChunkParams(n_q, int(window), int(sinks), float(softmax_scale),
+                     (ctypes.c_int64 * 3)(*strides[0]), (ctypes.c_int64 * 3)(*strides[1]))
+    c = cfg.c()
+    _check(lib().kvq_chunk_attn(ctypes.byref(c), ctypes.byref(cache._c), _rows(q, "q"),
+                                _rows(out, "out"), ctypes.byref(p), batch_begin, batch_count,
+                                _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Sampling
+# ---------------------------------------------------------------------------
+
+
+def sample_outputs(batch, device="cuda"):
+    """The result tensors of kvq_sample."""
+    return dict(token=torch.empty(batch, dtype=torch.int32, device=device),
+                logprob=torch.empty(batch, dtype=torch.float32, device=device))
+
+
+def _logit_rows(t, shape, name):
+    """Pointer and row stride of an fp32 CUDA tensor [batch, vocab]."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+
+
+def kvq_sample(logits, noise=None, temperature=None, top_k=None, top_p=None, min_p=None,
+               outputs=None, stream=None):
+    """The next token of each row of fp32 logits [batch, vocab] (rows may be
+    strided) from ``noise``, fp32 uniform numbers in [0, 1) of the same shape.
+    temperature, top_p, min_p (fp32) and top_k (int32) are device tensors
+    [batch] or None; noise None is greedy.  Returns a dict of device tensors:
+    token (int32) and logprob (fp32, may be None in ``outputs``)."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [batch, vocab]")
+    B, V = logits.shape
+    o = sample_outputs(B, logits.device) if outputs is None else outputs
+
+    def row(t, dt, name):
+        if t is None:
+            return ctypes.c_void_p(None)
+        if t.shape != (B,):
+            raise ValueError(f"{name} must be [{B}]")
+        return _dev(t, dt, name)
+
+    z, zs = _logit_rows(logits, (B, V), "logits")
+    u, us = (ctypes.c_void_p(None), 0) if noise is None else _logit_rows(noise, (B, V), "noise")
+    f32 = torch.float32
+    _check(lib().kvq_sample(z, zs, u, us, B, V, row(temperature, f32, "temperature"),
+                            row(top_k, torch.int32, "top_k"), row(top_p, f32, "top_p"),
+                            row(min_p, f32, "min_p"), row(o["token"], torch.int32, "token"),
+                            row(o.get("logprob"), f32, "logprob"), _stream(stream)))
+    return o
 
 
 # ---------------------------------------------------------------------------
