@@ -464,8 +464,12 @@ static kvq_status check_chunk_sizes(const kvq_config* cfg, int32_t n_q, int32_t 
     return fail(KVQ_ERR_ARG, "n_q must be in [1, max_len] (got %d)", n_q);
   if (batch_count < 1 || batch_count > cfg->batch)
     return fail(KVQ_ERR_SHAPE, "batch_count must be in [1, %d] (got %d)", cfg->batch, batch_count);
-  if ((long long)n_q * cfg->n_q_heads * batch_count > (1LL << 30))
-    return fail(KVQ_ERR_SHAPE, "batch_count * n_q * n_q_heads must be <= 2^30");
+  if ((long long)n_q * cfg->n_q_heads * batch_count > (1LL << 28))
+    return fail(KVQ_ERR_SHAPE, "batch_count * n_q * n_q_heads must be <= 2^28");
+  // key tiles over all row tiles, counted in 32 bits
+  const long long row_tiles = ((long long)n_q * (cfg->n_q_heads / cfg->n_kv_heads) + 127) / 128;
+  if (row_tiles * cfg->n_kv_heads * batch_count * (cfg->max_len / 128 + 2) >= (1LL << 31))
+    return fail(KVQ_ERR_SHAPE, "too many tiles in one call: split the chunk or the batch");
   return KVQ_OK;
 }
 

@@ -48,6 +48,7 @@ cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __hal
   p.c = call;
   p.tiles = plan.tiles;
   p.streams_rows = plan.streams_rows;
+  p.gq_inverse = (uint32_t)((1ull << 32) / d.gq + 1);
   char* w = static_cast<char*>(workspace);
   p.part_o = reinterpret_cast<float*>(w);
   p.part_ml = reinterpret_cast<float2*>(w + plan.o_bytes);

@@ -23,7 +23,7 @@
 //   warps 0-3, 4-7  softmax of streams 0 and 1 (and queries in, results out)
 //   warps 8-11      keys: one 32-token block each, codes -> fp16 tile
 //   warps 12-15     values, the same
-//   warp 16         issues the products
+//   warp 16         issues the products (17-19 idle)
 // The running maximum of a row moves only when a score is more than 8 (in log2)
 // above it, so the accumulator is rescaled rarely; weights stay below 2^8.
 //
@@ -47,8 +47,14 @@ constexpr int kTile = 128;                  // tokens of a key / value tile, row
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;  // 64 elements of the contiguous axis
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 8;
-constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps + 1);
-constexpr long long kWaitLimit = 4000000000LL;  // cycles of a bounded wait (~2 s)
+constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps + 4);
+// Registers a thread: at launch, then by warpgroup.  The shares must not exceed
+// what the launch got.
+constexpr int kRegsLaunch = 96, kRegsSoftmax = 104, kRegsLoad = 104, kRegsIssue = 64;
+static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kLoadWarps * kRegsLoad + 4 * kRegsIssue) <=
+                  kThreads * kRegsLaunch,
+              "register shares exceed the launch's");
+constexpr uint32_t kWaitLimit = 2000000000u;  // cycles of a bounded wait (~1 s)
 constexpr float kRescaleLog2 = 8.0f;
 
 struct Smem {
@@ -57,12 +63,12 @@ struct Smem {
   unsigned char v[2][kTileBytes];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_full;
   uint64_t meet, drained;
-  long long scan[32];
-  long long start_unit;
-  int start_group, start_head, start_step;
+  int scan[32];
+  int start_seq, start_tile, start_head, start_step;
   uint32_t tmem;
   int abort, last;
-  float m[kTile], l[kTile];
+  float m[kTile], l[kTile];            // stream 1's statistics of a shared row tile
+  float row_m[2 * kTile], row_f[2 * kTile];
 };
 
 struct Params {
@@ -72,6 +78,7 @@ struct Params {
   __half* out;
   ChunkCall c;
   int tiles;         // row tiles per (sequence, kv-head)
+  uint32_t gq_inverse;  // floor(2^32 / gq) + 1
   int streams_rows;  // 1: items of 256 rows (a row tile per stream), 0: of 128
   float* part_o;     // [2 * CTAs][rows of an item][128]
   float2* part_ml;   // [2 * CTAs][rows of an item]
@@ -106,10 +113,10 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
 // false; every role then leaves its loop.
 __device__ __forceinline__ bool bar_wait(Smem& s, uint64_t* b, uint32_t parity) {
   if (bar_try(b, parity)) return true;
-  const long long t0 = clock64();
+  const uint32_t t0 = (uint32_t)clock();
+#pragma unroll 1
   while (!bar_try(b, parity)) {
-    if (*reinterpret_cast<volatile int*>(&s.abort)) return false;
-    if (clock64() - t0 > kWaitLimit) {
+    if (*reinterpret_cast<volatile int*>(&s.abort) || (uint32_t)clock() - t0 > kWaitLimit) {
       *reinterpret_cast<volatile int*>(&s.abort) = 1;
       return false;
     }
@@ -172,17 +179,6 @@ __device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t (&r)[32]) {
 __device__ __forceinline__ void tm_load_wait() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,"
-      "%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-      "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-      "r"(r[30]), "r"(r[31]), "r"(addr)
-      : "memory");
-}
 __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,"
@@ -192,6 +188,18 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16
       "r"(addr)
       : "memory");
 }
+__device__ __forceinline__ void tm_load8(uint32_t addr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+                 "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tm_store8(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
+      : "memory");
+}
 __device__ __forceinline__ void tm_store_wait() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
@@ -199,6 +207,33 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// Two fp32 numbers in one 64-bit register, for the packed instructions.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -233,6 +268,12 @@ __host__ __device__ constexpr uint32_t instr_desc(bool b_mn) {
 // Items
 // ---------------------------------------------------------------------------
 
+// Row r of an item's sequence: its token.  Rows stay below 2^28 (checked on the
+// host), where the product with gq_inverse gives the exact quotient.
+__device__ __forceinline__ int token_of_row(const Params& p, int r) {
+  return p.d.gq == 1 ? r : (int)__umulhi((uint32_t)r, p.gq_inverse);
+}
+
 // What one row tile of a sequence sees: key tiles 0 .. n_sink - 1, then from
 // first on; n of them in all.
 struct Span {
@@ -244,37 +285,50 @@ struct Span {
 
 __device__ __forceinline__ Span span_of(const Params& p, int bl, int tile) {
   Span s;
-  const int gq = p.d.gq, tr = kTile << p.streams_rows;
   s.L = p.cache.seq_len[p.c.batch_begin + bl];
-  const int r0 = tile * tr, r1 = min(r0 + tr, p.c.n_q * gq) - 1;
-  s.p0 = s.L - p.c.n_q + r0 / gq;
-  s.p1 = s.L - p.c.n_q + r1 / gq;
+  const int shift = 7 + p.streams_rows;
+  const int r1 = min((tile + 1) << shift, p.c.n_q * p.d.gq) - 1;
+  s.p0 = s.L - p.c.n_q + token_of_row(p, tile << shift);
+  s.p1 = s.L - p.c.n_q + token_of_row(p, r1);
   s.lo = p.c.window ? max(0, max(s.p0, 0) - p.c.window + 1) : 0;
-  s.first = s.lo / kTile;
-  s.n_sink = p.c.window ? min((p.c.sinks + kTile - 1) / kTile, s.first) : 0;
-  s.n = s.n_sink + max(s.p1, 0) / kTile - s.first + 1;
+  s.first = s.lo >> 7;
+  s.n_sink = min((p.c.sinks + kTile - 1) >> 7, s.first);  // sinks is 0 without a window
+  s.n = s.n_sink + (max(s.p1, 0) >> 7) - s.first + 1;
   return s;
 }
 
-// The items of this CTA's share of the units, in order; every role walks them.
+// CTA c's share of the units: [begin(c), begin(c + 1)), equal to within one.
+struct Shares {
+  int q, r, n;  // units = n q + r over n CTAs
+  __device__ __forceinline__ int begin(int c) const { return c * q + min(c, r); }
+  __device__ __forceinline__ int owner(int u) const {
+    const int wide = (q + 1) * r;  // units of the CTAs that have q + 1
+    return u < wide ? (int)((uint32_t)u / (uint32_t)(q + 1))
+                    : r + (int)((uint32_t)(u - wide) / (uint32_t)q);
+  }
+};
+
+// The items of this CTA's share of the units, in order (sequence, row tile,
+// kv-head); every role walks them.
 struct Walk {
-  long long u, end, base;  // next unit, end of the share, first unit of the item
-  int group, head, step;   // group = sequence * tiles + row tile
+  int u, end, base;        // next unit, end of the share, first unit of the item
+  int bl, row_tile, head, step;
   Span s;
   int i0, i1;              // the item's units in this share
-  __device__ __forceinline__ void begin(const Smem& sm, long long u0, long long u1) {
+  __device__ __forceinline__ void begin(const Smem& sm, int u0, int u1) {
     u = u0;
     end = u1;
-    group = sm.start_group;
+    bl = sm.start_seq;
+    row_tile = sm.start_tile;
     head = sm.start_head;
     step = sm.start_step;
     base = u0 - step;
   }
   __device__ __forceinline__ bool next(const Params& p) {
     if (u >= end) return false;
-    s = span_of(p, group / p.tiles, group % p.tiles);
+    s = span_of(p, bl, row_tile);
     i0 = step;
-    i1 = (int)min((long long)s.n, step + (end - u));
+    i1 = min(s.n, step + (end - u));
     return true;
   }
   __device__ __forceinline__ void advance(const Params& p) {
@@ -283,7 +337,10 @@ struct Walk {
     step = 0;
     if (++head == p.d.hkv) {
       head = 0;
-      ++group;
+      if (++row_tile == p.tiles) {
+        row_tile = 0;
+        ++bl;
+      }
     }
   }
 };
@@ -366,236 +423,230 @@ __device__ __forceinline__ uint4 run_order(uint4 v) {
 // Row of the value tile (channel-major, 1-bit) that holds channel c.
 __device__ __forceinline__ int value_row(int c) { return (c & ~7) + run_pos(c & 7); }
 
-// A packed block's codes and scales on their way to a tile (registers).
-// 1-bit: 16 bytes of codes and the pairs of scales and zeros they meet;
-// others: four groups of B words with a scale and a zero each.
+// Keys and values share one body of code per width (`key` is a runtime flag):
+// the hot loops of all roles have to stay in the instruction cache together.
+
+// A part (a quarter) of a packed block on its way to a tile, in registers.
+// B >= 2: part k is group k, B words with a scale and a zero a lane.  1 bit:
+// word k of the lane's 16 bytes and the pairs of scales and zeros it meets.
 template <int B>
-struct Codes {
-  uint32_t w[4][B];
-  uint32_t sz[4];
+struct Part {
+  uint32_t w[B], sz;
 };
 template <>
-struct Codes<1> {
-  uint32_t w[4];
-  uint32_t s[16], z[16];
+struct Part<1> {
+  uint32_t w[1], s[4], z[4];
 };
 
-template <int B, bool kKey>
-__device__ __forceinline__ void load_codes(Codes<B>& c, const char* codes, const __half* meta) {
-  const int lane = threadIdx.x & 31;
+template <int B>
+__device__ __forceinline__ void load_part(Part<B>& c, int k, const char* codes, bool key) {
+  const int lane = threadIdx.x & 31, tig = lane & 3;
+  const __half* meta = reinterpret_cast<const __half*>(codes + 512 * B) + 32 * k;
   if constexpr (B == 1) {
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(codes) + lane);
-    c.w[0] = w.x, c.w[1] = w.y, c.w[2] = w.z, c.w[3] = w.w;
-    if constexpr (kKey) {
-      const int tig = lane & 3;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const uint2 a = __ldg(reinterpret_cast<const uint2*>(meta + 16 * ks + 4 * tig));
-        const uint2 b = __ldg(reinterpret_cast<const uint2*>(meta + kHeadDim + 16 * ks + 4 * tig));
-        c.s[2 * ks] = a.x, c.s[2 * ks + 1] = a.y;
-        c.z[2 * ks] = b.x, c.z[2 * ks + 1] = b.y;
-      }
-    } else {
-      const int tig = lane & 3;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(meta + 32 * g + 8 * tig));
-        const uint4 b = __ldg(reinterpret_cast<const uint4*>(meta + kHeadDim + 32 * g + 8 * tig));
-        c.s[4 * g] = a.x, c.s[4 * g + 1] = a.y, c.s[4 * g + 2] = a.z, c.s[4 * g + 3] = a.w;
-        c.z[4 * g] = b.x, c.z[4 * g + 1] = b.y, c.z[4 * g + 2] = b.z, c.z[4 * g + 3] = b.w;
-      }
-    }
+    c.w[0] = __ldg(reinterpret_cast<const uint32_t*>(codes) + 4 * lane + k);
+    meta += key ? 4 * tig : 8 * tig;
+    const __half* second = meta + (key ? 16 : 4);
+    const uint2 a = __ldg(reinterpret_cast<const uint2*>(meta));
+    const uint2 b = __ldg(reinterpret_cast<const uint2*>(second));
+    const uint2 d = __ldg(reinterpret_cast<const uint2*>(meta + kHeadDim));
+    const uint2 e = __ldg(reinterpret_cast<const uint2*>(second + kHeadDim));
+    c.s[0] = a.x, c.s[1] = a.y, c.s[2] = b.x, c.s[3] = b.y;
+    c.z[0] = d.x, c.z[1] = d.y, c.z[2] = e.x, c.z[3] = e.y;
   } else {
+    const char* src = codes + (32 * k + lane) * (4 * B);
+    if constexpr (B == 2) {
+      const uint2 a = __ldg(reinterpret_cast<const uint2*>(src));
+      c.w[0] = a.x, c.w[1] = a.y;
+    } else {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const char* src = codes + (32 * g + lane) * (4 * B);
-      if constexpr (B == 2) {
-        const uint2 a = __ldg(reinterpret_cast<const uint2*>(src));
-        c.w[g][0] = a.x, c.w[g][1] = a.y;
-      } else {
-#pragma unroll
-        for (int i = 0; i < B / 4; ++i) {
-          const uint4 a = __ldg(reinterpret_cast<const uint4*>(src) + i);
-          c.w[g][4 * i] = a.x, c.w[g][4 * i + 1] = a.y;
-          c.w[g][4 * i + 2] = a.z, c.w[g][4 * i + 3] = a.w;
-        }
+      for (int i = 0; i < B / 4; ++i) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(src) + i);
+        c.w[4 * i] = a.x, c.w[4 * i + 1] = a.y, c.w[4 * i + 2] = a.z, c.w[4 * i + 3] = a.w;
       }
-      const int mi = kKey ? 32 * g + lane : vmeta_index(g, lane);
-      const __half2 sz = __halves2half2(meta[mi], meta[kHeadDim + mi]);
-      c.sz[g] = as_u32(sz);
     }
+    const __half* m = meta + (key ? lane : vmeta_index(0, lane));
+    c.sz = as_u32(__halves2half2(m[0], m[kHeadDim]));
   }
 }
 
-// The block's part of a tile: tokens 32 j .. 32 j + 31 of its 128.
-template <int B, bool kKey>
-__device__ __forceinline__ void restore_block(const Codes<B>& c, unsigned char* tile, int j) {
+template <int B>
+__device__ __forceinline__ void restore_part(const Part<B>& c, int k, unsigned char* tile, int j,
+                                             bool key) {
   const int lane = threadIdx.x & 31;
   if constexpr (B == 1) {
     const int gid = lane >> 2, tig = lane & 3;
-    if constexpr (kKey) {
+    // keys: token 4 gid + n; values: channel 4 gid + n of the group, the odd
+    // gids in another order so that a store phase meets eight banks
+    const int flip = key ? 0 : (gid & 1) << 1;
+    const int half = key ? tig >> 1 : j >> 1;
+    const int chunk = key ? (tig & 1) * 4 + (k ^ (tig & 2)) : (j & 1) * 4 + tig;
+    const int row = 32 * (key ? j : k) + 8 * (gid >> 1) + (gid & 1);
+    unsigned char* base = tile + half * kHalfBytes + row * 128;
+    const uint32_t x0 = (uint32_t)(chunk ^ (gid & 1)) << 4;
+    __half2 s[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        __half2 s[4];
+    for (int r = 0; r < 4; ++r) s[r] = __hmul2(as_half2(c.s[r]), __float2half2_rn(0.5f));
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          s[r] = __hmul2(as_half2(c.s[4 * k + r]), __float2half2_rn(0.5f));
+    for (int i = 0; i < 4; ++i) {
+      const int n = i ^ flip;
+      const uint32_t w = __funnelshift_l(c.w[0], c.w[0], 4 - n);
+      uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t o[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            // the token's two codes at bits 14 and 30: 0 or 2.0
-            const uint32_t x = __funnelshift_l(c.w[k], c.w[k], 4 * r + 4 - i) & 0x40004000u;
-            o[r] = as_u32(__hfma2(as_half2(x), s[r], as_half2(c.z[4 * k + r])));
-          }
-          const int t = 4 * gid + i, row = 32 * j + (t & 24) + run_pos(t & 7), half = tig >> 1;
-          st16(tile, tile_at(half, row, (tig & 1) * 4 + (k ^ (half << 1))),
-               make_uint4(o[0], o[1], o[2], o[3]));
-        }
+      for (int r = 0; r < 4; ++r) {
+        // two codes at bits 14 and 30: 0 or 2.0
+        const uint32_t x = __funnelshift_l(w, w, 4 * r) & 0x40004000u;
+        o[r] = as_u32(__hfma2(as_half2(x), s[r], as_half2(c.z[r])));
       }
-    } else {
-      const int flip = (gid & 1) << 1;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        __half2 s[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          s[r] = __hmul2(as_half2(c.s[4 * g + r]), __float2half2_rn(0.5f));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ch = i ^ flip;  // so that a store phase meets eight banks
-          const uint32_t w = __funnelshift_l(c.w[g], c.w[g], 4 - ch);
-          uint32_t o[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const uint32_t x = __funnelshift_l(w, w, 4 * r) & 0x40004000u;
-            o[r] = as_u32(__hfma2(as_half2(x), s[r], as_half2(c.z[4 * g + r])));
-          }
-          st16(tile, tile_at(j >> 1, 32 * g + 8 * (gid >> 1) + 2 * ch + (gid & 1), (j & 1) * 4 + tig),
-               make_uint4(o[0], o[1], o[2], o[3]));
-        }
-      }
+      st16(base, n * 256 + (x0 ^ (n << 5)), make_uint4(o[0], o[1], o[2], o[3]));
     }
   } else {
+    const __half2 s = __low2half2(as_half2(c.sz)), z = __high2half2(as_half2(c.sz));
+    const int row = key ? 32 * k + lane : 32 * j + (lane & 24) + run_pos(lane & 7);
+    const uint32_t at = key ? tile_at(j >> 1, row, (j & 1) * 4) : tile_at(k >> 1, row, (k & 1) * 4);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const __half2 s = __low2half2(as_half2(c.sz[g])), z = __high2half2(as_half2(c.sz[g]));
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint4 v = restore8<B>(c.w[g], k, s, z);
-        if constexpr (kKey) {
-          st16(tile, tile_at(j >> 1, 32 * g + lane, (j & 1) * 4 + k), v);
-        } else {
-          const int row = 32 * j + (lane & 24) + run_pos(lane & 7);
-          st16(tile, tile_at(g >> 1, row, (g & 1) * 4 + k), v);
-        }
-      }
-    }
+    for (int q = 0; q < 4; ++q) st16(tile, at ^ (q << 4), restore8<B>(c.w, q, s, z));
   }
 }
 
-// The same for a block of the fp16 window, whose token t is at rows + slot *
-// 128, slot = (t0 + t) mod ring; tokens from `valid` on are zero.
-template <int B, bool kKey>
-__device__ __noinline__ void window_block(const __half* rows, int t0, int ring, int valid,
-                                          unsigned char* tile, int j) {
+// The same for a block of the fp16 window: `rows` is its first token's row (the
+// ring holds a whole number of blocks, so a block does not wrap); tokens from
+// `valid` on are zero.
+template <int B>
+__device__ __forceinline__ void window_block(const __half* rows, int valid, unsigned char* tile,
+                                             int j, bool key) {
   const int lane = threadIdx.x & 31;
-  if constexpr ((B == 1) == kKey) {  // rows of the tile are tokens
+  if ((B == 1) == key) {  // rows of the tile are tokens
     const int row = 32 * j + (lane & 24) + run_pos(lane & 7);
-    const uint4* src =
-        reinterpret_cast<const uint4*>(rows + (long long)((t0 + lane) % ring) * kHeadDim);
-#pragma unroll 4
-    for (int m = 0; m < 16; ++m) {
-      const uint4 v = lane < valid ? src[m] : make_uint4(0u, 0u, 0u, 0u);
-      if constexpr (kKey) put_key_row<1>(tile, row, m, v);
-      else st16(tile, tile_at(m >> 3, row, m & 7), run_order(v));
+    const uint4* src = reinterpret_cast<const uint4*>(rows + lane * kHeadDim);
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+      uint4 v[8];
+#pragma unroll
+      for (int m = 0; m < 8; ++m) v[m] = lane < valid ? src[8 * h + m] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        if constexpr (B == 1) put_key_row<1>(tile, row, 8 * h + m, v[m]);
+        else st16(tile, tile_at(h, row, m), run_order(v[m]));
+      }
     }
-  } else {  // rows are channels
-    const unsigned short* src = reinterpret_cast<const unsigned short*>(rows);
-    for (int g = 0; g < 4; ++g) {
-      const int c = 32 * g + lane, row = kKey ? c : value_row(c);
+  } else {  // rows are channels, two a lane
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(rows) + lane;
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {  // 64 channels and 16 tokens at a time
+      const int c = 64 * (g >> 1) + 2 * lane, h = g & 1;
+      uint32_t x[16];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t x[8];
+      for (int t = 0; t < 16; ++t)
+        x[t] = 16 * h + t < valid ? src[(16 * h + t) * (kHeadDim / 2) + 32 * (g >> 1)] : 0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int t = 8 * k + i;
-          x[i] = t < valid ? src[(long long)((t0 + t) % ring) * kHeadDim + c] : 0u;
+      for (int e = 0; e < 2; ++e) {
+        const int row = key ? c + e : value_row(c + e);
+        const uint32_t sel = e ? 0x7632 : 0x5410;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t* y = x + 8 * k;
+          st16(tile, tile_at(j >> 1, row, (j & 1) * 4 + 2 * h + k),
+               make_uint4(__byte_perm(y[0], y[4], sel), __byte_perm(y[1], y[5], sel),
+                          __byte_perm(y[2], y[6], sel), __byte_perm(y[3], y[7], sel)));
         }
-        st16(tile, tile_at(j >> 1, row, (j & 1) * 4 + k),
-             make_uint4(x[0] | x[4] << 16, x[1] | x[5] << 16, x[2] | x[6] << 16, x[3] | x[7] << 16));
       }
     }
   }
 }
-template <int B, bool kKey>
-__device__ __noinline__ void zero_block(unsigned char* tile, int j) {
+template <int B>
+__device__ __forceinline__ void zero_block(unsigned char* tile, int j, bool key) {
   const int lane = threadIdx.x & 31;
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  if constexpr ((B == 1) == kKey) {
-    for (int m = 0; m < 16; ++m) st16(tile, tile_at(m >> 3, 32 * j + lane, m & 7), zero);
-  } else {
-    for (int i = 0; i < 16; ++i)
-      st16(tile, tile_at(j >> 1, 32 * (i >> 2) + lane, (j & 1) * 4 + (i & 3)), zero);
-  }
+  const bool tokens = (B == 1) == key;
+#pragma unroll 1
+  for (int i = 0; i < 16; ++i)
+    st16(tile, tokens ? tile_at(i >> 3, 32 * j + lane, i & 7)
+                      : tile_at(j >> 1, 32 * (i >> 2) + lane, (j & 1) * 4 + (i & 3)),
+         make_uint4(0u, 0u, 0u, 0u));
 }
 
-// A loading warp: block j of every key (or value) tile of the CTA's share.
-template <int B, bool kKey>
-__device__ __forceinline__ void load_role(const Params& p, Smem& s, long long u0, long long u1,
-                                          int j) {
+// A loading warp: block j of every key (or value) tile of the CTA's share.  As
+// soon as a part of a block is restored, the same part of the next block is
+// loaded into its registers; the block after that is brought into L2, and the
+// table entry of the one after that is on its way.
+template <int B>
+__device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int u1, int j,
+                                          bool key) {
   const int lane = threadIdx.x & 31;
-  unsigned char(*tiles)[kTileBytes] = kKey ? s.k : s.v;
-  uint64_t* full = kKey ? s.k_full : s.v_full;
-  uint64_t* empty = kKey ? s.k_empty : s.v_empty;
+  unsigned char(*tiles)[kTileBytes] = key ? s.k : s.v;
+  uint64_t* full = key ? s.k_full : s.v_full;
+  uint64_t* empty = key ? s.k_empty : s.v_empty;
+  const int codes = key ? 0 : page_off_vcodes(p.d.bits_k);
   uint32_t n = 0;
   Walk w;
   w.begin(s, u0, u1);
   for (; w.next(p); w.advance(p)) {
-    const int b = p.c.batch_begin + w.group / p.tiles;
-    const PageMap pm = page_map(p.d, p.cache, b, w.head);
-    const __half* rows =
-        reinterpret_cast<const __half*>(kKey ? p.cache.k_resid : p.cache.v_resid) +
-        ((long long)b * p.d.hkv + w.head) * p.d.ring * kHeadDim;
+    const int b = p.c.batch_begin + w.bl;
+    // block n at base + index * stride: its number, or its entry of the table
+    const int32_t* table =
+        p.cache.block_table ? p.cache.block_table + (long long)b * p.d.max_blocks : nullptr;
+    const int page = (int)p.d.page_bytes, stride = table ? page * p.d.hkv : page;
+    const int limit = table ? p.cache.n_pages : p.d.max_blocks;
+    const char* base = static_cast<const char*>(p.cache.pages) + codes +
+                       (table ? (long long)w.head * page
+                              : ((long long)b * p.d.hkv + w.head) * p.d.max_blocks * page);
     const int lq = packed_len(w.s.L, p.d.residual);
-    const int codes = kKey ? 0 : page_off_vcodes(p.d.bits_k);
-    const int meta = kKey ? page_off_kmeta(p.d.bits_k) : page_off_vmeta(p.d.bits_k, p.d.bits_v);
-    // the block of unit i, by kind: 0 nothing to see, 1 packed, 2 window
-    const auto kind_of = [&](int t0) {
-      const bool seen = t0 <= w.s.p1 && (t0 + kGroup > w.s.lo || t0 < p.c.sinks);
-      return !seen ? 0 : t0 < lq ? 1 : 2;
+    const auto seen = [&](int t0) {
+      return t0 <= w.s.p1 && (t0 + kGroup > w.s.lo || t0 < p.c.sinks);
     };
-    Codes<B> c;
-    const auto fetch = [&](int i) {
-      const int t0 = w.s.tile(i) * kTile + j * kGroup;
-      int kind = kind_of(t0);
-      if (kind == 1) {
-        const char* page = pm.at(t0 / kGroup);
-        if (page) {
-          load_codes<B, kKey>(c, page + codes, reinterpret_cast<const __half*>(page + meta));
-        } else {
-          kind = 0;
-          if (lane == 0)
-            atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_BAD_PAGE);
+    const auto token = [&](int i) { return w.s.tile(i) * kTile + j * kGroup; };
+    // index of unit i's block; kNone where there is nothing to restore
+    constexpr int kNone = -0x7fffffff - 1;
+    const auto index = [&](int i) {
+      const int t0 = token(i);
+      if (i >= w.i1 || t0 >= lq || !seen(t0)) return kNone;
+      return table ? __ldg(table + (t0 >> 5)) : t0 >> 5;
+    };
+    const auto address = [&](int e) -> const char* {
+      if (e >= 0 && e < limit) return base + (long long)e * stride;
+      if (e != kNone && lane == 0)
+        atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_BAD_PAGE);
+      return nullptr;
+    };
+    Part<B> c[4];
+    const char* at0 = nullptr;
+    const char* at1 = address(index(w.i0));
+    int e1 = index(w.i0 + 1), e2 = index(w.i0 + 2);
+    // i = i0 - 1 only loads the first block
+#pragma unroll 1
+    for (int i = w.i0 - 1; i < w.i1; ++i) {
+      const int buf = n & 1, e3 = index(i + 4);
+      unsigned char* tile = tiles[buf];
+      if (i >= w.i0) {
+        if (!warp_wait(s, &empty[buf], ((n >> 1) & 1) ^ 1)) return;
+        if (!at0) {
+          const int ta = token(i);
+          if (ta >= lq && seen(ta)) {
+            const __half* rows =
+                reinterpret_cast<const __half*>(key ? p.cache.k_resid : p.cache.v_resid) +
+                (((long long)b * p.d.hkv + w.head) * p.d.ring + ta % p.d.ring) * kHeadDim;
+            window_block<B>(rows, w.s.L - ta, tile, j, key);
+          } else {
+            zero_block<B>(tile, j, key);
+          }
         }
       }
-      return kind;
-    };
-    int kind = fetch(w.i0);
-    for (int i = w.i0; i < w.i1; ++i, ++n) {
-      const int buf = n & 1;
-      if (!warp_wait(s, &empty[buf], ((n >> 1) & 1) ^ 1)) return;
-      const int t0 = w.s.tile(i) * kTile + j * kGroup;
-      if (kind == 1) restore_block<B, kKey>(c, tiles[buf], j);
-      else if (kind == 2)
-        window_block<B, kKey>(rows, t0, p.d.ring, w.s.L - t0, tiles[buf], j);
-      else
-        zero_block<B, kKey>(tiles[buf], j);
-      fence_async();
-      __syncwarp();
-      if (lane == 0) bar_arrive(&full[buf]);
-      if (i + 1 < w.i1) kind = fetch(i + 1);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (at0) restore_part<B>(c[k], k, tile, j, key);
+        if (at1) load_part<B>(c[k], k, at1, key);
+      }
+      if (i >= w.i0) {
+        fence_async();
+        __syncwarp();
+        if (lane == 0) bar_arrive(&full[buf]);
+        ++n;
+      }
+      at0 = at1;
+      at1 = address(e1);
+      if (at1 && lane < 4 * B + 4)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(at1 + 128 * lane));
+      e1 = e2;
+      e2 = e3;
     }
   }
 }
@@ -607,7 +658,7 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, long long u0
 constexpr uint32_t kColS = 0, kColO = 256;  // tensor memory columns: S0 S1 O0 O1, 128 each
 
 template <int BK, int BV>
-__device__ __forceinline__ void mma_role(const Params& p, Smem& s, long long u0, long long u1) {
+__device__ __forceinline__ void mma_role(const Params& p, Smem& s, int u0, int u1) {
   constexpr uint32_t kIdS = instr_desc(BK != 1), kIdO = instr_desc(BV != 1);
   const uint32_t tm = s.tmem;
   uint32_t nk = 0, nv = 0, ns[2] = {0, 0}, items = 0;
@@ -618,44 +669,45 @@ __device__ __forceinline__ void mma_role(const Params& p, Smem& s, long long u0,
     const int steps = (w.i1 - w.i0) << two;
     if (!bar_wait(s, &s.q_full, items & 1)) return;
     tc_after();
-    const auto scores = [&](int st) {
-      const int x = st & 1, buf = nk & 1;
-      if (!two || x == 0) {
-        if (!bar_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return false;
+    // scores run two steps ahead of the weights times the values
+#pragma unroll 1
+    for (int st = -2; st < steps; ++st) {
+      const int x = st & 1;
+      if (st >= 0) {
+        const int buf = nv & 1;
+        if (!bar_wait(s, &s.p_ready[x], ns[x] & 1)) return;
+        ++ns[x];
+        if ((!two || x == 0) && !bar_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
         tc_after();
-      }
-      const uint64_t a = tile_desc(sptr(s.q[two ? x : 0]), false),
-                     b = tile_desc(sptr(s.k[buf]), BK != 1);
+        const uint64_t b = tile_desc(sptr(s.v[buf]), BV != 1);
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks)
-        mma_ss(tm + kColS + 128 * x, a + step_major_k(ks),
-               b + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdS, ks > 0);
-      tc_commit(&s.s_full[x]);
-      if (!two || x == 1) {
-        tc_commit(&s.k_empty[buf]);
-        ++nk;
+        for (int ks = 0; ks < 8; ++ks)
+          mma_ts(tm + kColO + 128 * x, tm + kColS + 128 * x + 8 * ks,
+                 b + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 1 || ks > 0);
+        if (!two || x == 1) {
+          tc_commit(&s.v_empty[buf]);
+          ++nv;
+        }
+        if (st + 2 >= steps) tc_commit(&s.o_full[x]);
       }
-      return true;
-    };
-    if (!scores(0)) return;
-    if (steps > 1 && !scores(1)) return;
-    for (int st = 0; st < steps; ++st) {
-      const int x = st & 1, buf = nv & 1;
-      if (!bar_wait(s, &s.p_ready[x], ns[x] & 1)) return;
-      ++ns[x];
-      if ((!two || x == 0) && !bar_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
-      tc_after();
-      const uint64_t b = tile_desc(sptr(s.v[buf]), BV != 1);
+      if (st + 2 < steps) {
+        const int buf = nk & 1;
+        if (!two || x == 0) {
+          if (!bar_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return;
+          tc_after();
+        }
+        const uint64_t a = tile_desc(sptr(s.q[two ? x : 0]), false),
+                       b = tile_desc(sptr(s.k[buf]), BK != 1);
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks)
-        mma_ts(tm + kColO + 128 * x, tm + kColS + 128 * x + 8 * ks,
-               b + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 1 || ks > 0);
-      if (!two || x == 1) {
-        tc_commit(&s.v_empty[buf]);
-        ++nv;
+        for (int ks = 0; ks < 8; ++ks)
+          mma_ss(tm + kColS + 128 * x, a + step_major_k(ks),
+                 b + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdS, ks > 0);
+        tc_commit(&s.s_full[x]);
+        if (!two || x == 1) {
+          tc_commit(&s.k_empty[buf]);
+          ++nk;
+        }
       }
-      if (st + 2 >= steps) tc_commit(&s.o_full[x]);
-      else if (!scores(st + 2)) return;
     }
   }
 }
@@ -676,37 +728,57 @@ __device__ __forceinline__ void load_queries(const Params& p, const __half* src,
                                              unsigned char* tile, int row) {
   (void)p;
   const uint4* q = reinterpret_cast<const uint4*>(src);
+#pragma unroll 1
+  for (int h = 0; h < 16; h += 8) {
+    uint4 v[8];
 #pragma unroll
-  for (int m = 0; m < 16; ++m)
-    put_key_row<BK>(tile, row, m, src ? q[m] : make_uint4(0u, 0u, 0u, 0u));
+    for (int m = 0; m < 8; ++m) v[m] = src ? q[h + m] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) put_key_row<BK>(tile, row, h + m, v[m]);
+  }
 }
 
-// Scores at columns [32 c, 32 c + 32) of the thread's row, masked: column n is
+// The thread's row of scores with -inf where a column is not seen: column n is
 // seen when its token (less the tile's first) is at most hi and above lo, or
-// below sink.
-__device__ __forceinline__ void mask32(uint32_t (&r)[32], int c, int hi, int lo, int sink) {
+// below sink.  Only tiles at an edge come here; the scores are rewritten in
+// tensor memory by a short loop to keep the code of the others small.
+__device__ __forceinline__ void mask_row(uint32_t ts, int hi, int lo, int sink) {
+#pragma unroll 1
+  for (int c = 0; c < 128; c += 8) {
+    uint32_t r[8];
+    tm_load8(ts + c, r);
+    tm_load_wait();
 #pragma unroll
-  for (int n = 0; n < 32; ++n) {
-    const int t = 32 * c + (n & ~7) + run_token(n & 7);
-    if (t > hi || (t <= lo && t >= sink)) r[n] = 0xff800000u;
+    for (int n = 0; n < 8; ++n) {
+      const int t = c + run_token(n);
+      if (t > hi || (t <= lo && t >= sink)) r[n] = 0xff800000u;
+    }
+    tm_store8(ts + c, r);
   }
+  tm_store_wait();
 }
 
 // One step of a stream's softmax for a row (a thread); `first`: no accumulator
-// yet.
+// yet.  The scores are read twice, 32 at a time (holding all 128 would take
+// the registers that the loading warps need more); the next 32 are on their
+// way while 32 are worked on.
 __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sl2, bool first,
-                                             bool masked, int hi, int lo, int sink, Row& row) {
-  float mx = -INFINITY;
+                                             Row& row) {
+  uint32_t r[2][32];
+  float mc[4];
+  tm_load32(ts, r[0]);
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    uint32_t r[32];
-    tm_load32(ts + 32 * c, r);
+    const uint32_t(&x)[32] = r[c & 1];
     tm_load_wait();
-    if (masked) mask32(r, c, hi, lo, sink);
+    tm_load32(ts + 32 * ((c + 1) & 3), r[(c + 1) & 1]);  // at the end: the first again
+    mc[c] = __uint_as_float(x[0]);
 #pragma unroll
-    for (int n = 0; n < 32; ++n) mx = fmaxf(mx, __uint_as_float(r[n]));
+    for (int n = 1; n < 31; n += 2)
+      mc[c] = fmaxf(fmaxf(mc[c], __uint_as_float(x[n])), __uint_as_float(x[n + 1]));
+    mc[c] = fmaxf(mc[c], __uint_as_float(x[31]));
   }
-  mx *= sl2;
+  const float mx = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])) * sl2;
   if (first) {
     row.m = mx;
     row.l = 0.0f;
@@ -717,35 +789,39 @@ __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sl2
       if (up) row.m = mx;
       row.l *= f;
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        uint32_t r[32];
-        tm_load32(to + 32 * c, r);
+      for (int c = 0; c < 16; ++c) {
+        uint32_t o[8];
+        tm_load8(to + 8 * c, o);
         tm_load_wait();
 #pragma unroll
-        for (int n = 0; n < 32; ++n) r[n] = __float_as_uint(__uint_as_float(r[n]) * f);
-        tm_store32(to + 32 * c, r);
+        for (int n = 0; n < 8; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
+        tm_store8(to + 8 * c, o);
       }
     }
   }
   const float off = row.m == -INFINITY ? 0.0f : -row.m;
-  float l0 = 0.0f, l1 = 0.0f;
+  const uint64_t sl = pair(sl2, sl2), of = pair(off, off);
+  uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    uint32_t r[32], h[16];
-    tm_load32(ts + 32 * c, r);
+    const uint32_t(&x)[32] = r[c & 1];
+    uint32_t w[16];
     tm_load_wait();
-    if (masked) mask32(r, c, hi, lo, sink);
+    if (c < 3) tm_load32(ts + 32 * (c + 1), r[(c + 1) & 1]);
 #pragma unroll
     for (int n = 0; n < 16; ++n) {
-      const float a = exp2_fast(fmaf(__uint_as_float(r[2 * n]), sl2, off));
-      const float b = exp2_fast(fmaf(__uint_as_float(r[2 * n + 1]), sl2, off));
-      l0 += a;
-      l1 += b;
-      h[n] = pack_half2(a, b);
+      float a, b;
+      unpair(fma2(pair(__uint_as_float(x[2 * n]), __uint_as_float(x[2 * n + 1])), sl, of), a, b);
+      a = exp2_fast(a);
+      b = exp2_fast(b);
+      sum[n & 1] = add2(sum[n & 1], pair(a, b));
+      w[n] = pack_half2(a, b);
     }
-    tm_store16(ts + 16 * c, h);
+    tm_store16(ts + 16 * c, w);  // columns that have been read
   }
-  row.l += l0 + l1;
+  float a, b;
+  unpair(add2(sum[0], sum[1]), a, b);
+  row.l += a + b;
   tm_store_wait();
 }
 
@@ -773,9 +849,76 @@ __device__ __forceinline__ void put_float(float* dst, int c, const float (&o)[32
   }
 }
 
+// The partials of CTAs c0 .. c1 to results, by all softmax threads: first each
+// row's maximum and sum (256 / rows threads a row share the CTAs), then a warp
+// per row, four channels a lane.
+// `inside`: c0's share begins in an earlier item, so this one is in its slot 1;
+// every other CTA's share begins here (slot 0).
+__device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk& w, int c0, int c1,
+                                           bool inside, uint32_t& met) {
+  const int tr = kTile << p.streams_rows, gq = p.d.gq, tid = threadIdx.x, tile = w.row_tile;
+  const int n_rows = min(tr, p.c.n_q * gq - tile * tr);
+  const auto slot_of = [&](int c) {
+    return (long long)(2 * c + (inside && c == c0 ? 1 : 0)) * tr;
+  };
+  int parts = 1;
+  while (parts < 32 && 2 * parts * n_rows <= 32 * kSoftmaxWarps) parts *= 2;
+  for (int r0 = 0; r0 < n_rows; r0 += 32 * kSoftmaxWarps / parts) {
+    const int r = r0 + tid / parts, q = tid % parts;
+    float m = -INFINITY, l = 0.0f;
+    if (r < n_rows) {
+#pragma unroll 4
+      for (int c = c0 + q; c <= c1; c += parts) {
+        const float2 ml = __ldcg(&p.part_ml[slot_of(c) + r]);
+        if (ml.y > 0.0f) {
+          const float mm = fmaxf(m, ml.x);
+          l = l * exp2_fast(m - mm) + ml.y * exp2_fast(ml.x - mm);
+          m = mm;
+        }
+      }
+    }
+    for (int o = 1; o < parts; o *= 2) {
+      const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o);
+      const float mm = fmaxf(m, m1);
+      if (mm > -INFINITY) l = l * exp2_fast(m - mm) + l1 * exp2_fast(m1 - mm);
+      m = mm;
+    }
+    if (r < n_rows && q == 0) {
+      s.row_m[r] = m > -INFINITY ? m : 0.0f;
+      s.row_f[r] = l > 0.0f ? 1.0f / l : 0.0f;
+    }
+  }
+  if (!meet_softmax(s, met)) return false;
+  const int ch = 4 * (tid & 31), bl = w.bl;
+#pragma unroll 2
+  for (int r = tid >> 5; r < n_rows; r += kSoftmaxWarps) {
+    const float m = s.row_m[r], f = s.row_f[r];
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+      const long long pr = slot_of(c) + r;
+      const float2 ml = __ldcg(&p.part_ml[pr]);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + pr * kHeadDim + ch));
+      const float x = exp2_fast(ml.x - m);
+      if (ml.y > 0.0f) {
+        o.x = fmaf(v.x, x, o.x);
+        o.y = fmaf(v.y, x, o.y);
+        o.z = fmaf(v.z, x, o.z);
+        o.w = fmaf(v.w, x, o.w);
+      }
+    }
+    const int g = tile * tr + r, t = token_of_row(p, g), head = w.head * gq + g - t * gq;
+    __half* dst = p.out + bl * p.c.out_stride[0] + t * p.c.out_stride[1] +
+                  head * p.c.out_stride[2] + ch;
+    *reinterpret_cast<uint2*>(dst) =
+        make_uint2(pack_half2(o.x * f, o.y * f), pack_half2(o.z * f, o.w * f));
+  }
+  return true;
+}
+
 template <int BK>
-__device__ __forceinline__ void softmax_role(const Params& p, Smem& s, long long u0, long long u1,
-                                             long long total, long long n_cta) {
+__device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, int u1,
+                                             const Shares& shares) {
   const int warp = threadIdx.x >> 5, x = warp >> 2, lane_row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes a warp, in bits 16 up
   const uint32_t ts = s.tmem + lanes + kColS + 128 * x, to = s.tmem + lanes + kColO + 128 * x;
@@ -784,11 +927,11 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, long long
   Walk w;
   w.begin(s, u0, u1);
   for (; w.next(p); w.advance(p)) {
-    const int bl = w.group / p.tiles, tile = w.group % p.tiles;
+    const int bl = w.bl, tile = w.row_tile;
     const int tr_row = (two ? kTile * x : 0) + lane_row;  // row in the item
     const int g = tile * tr + tr_row;
     const bool valid = g < rows;
-    const int t = g / gq, head = w.head * gq + g % gq;
+    const int t = token_of_row(p, g), head = w.head * gq + g - t * gq;
     const int pos = w.s.L - p.c.n_q + t;
     if (two || x == 0) {
       const long long off = bl * p.c.q_stride[0] + t * p.c.q_stride[1] + head * p.c.q_stride[2];
@@ -808,8 +951,10 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, long long
         // every token of the tile is seen by every row of the item
         const bool whole = w.s.p0 >= t0 + kTile - 1 &&
                            (!p.c.window || t0 > w.s.p1 - p.c.window || t0 + kTile <= p.c.sinks);
-        softmax_step(ts, to, p.c.scale_log2, first, !whole, (valid ? pos : -1) - t0,
-                     p.c.window ? pos - p.c.window - t0 : -1 - t0, p.c.sinks - t0, row);
+        if (!whole)
+          mask_row(ts, (valid ? pos : -1) - t0, p.c.window ? pos - p.c.window - t0 : -1 - t0,
+                   p.c.sinks - t0);
+        softmax_step(ts, to, p.c.scale_log2, first, row);
       }
       tc_before();
       bar_arrive(&s.p_ready[x]);
@@ -876,9 +1021,8 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, long long
     if (!direct) {
       // the last of the item's CTAs merges its partials, in the order of the
       // tokens
-      const long long a = w.base, z = w.base + w.s.n - 1;
-      const int c0 = (int)(((a + 1) * n_cta - 1) / total), c1 = (int)(((z + 1) * n_cta - 1) / total);
-      const long long item = (long long)w.group * p.d.hkv + w.head;
+      const int c0 = shares.owner(w.base), c1 = shares.owner(w.base + w.s.n - 1);
+      const int item = (w.bl * p.tiles + w.row_tile) * p.d.hkv + w.head;
       __threadfence();
       if (!meet_softmax(s, met)) return;
       if (threadIdx.x == 0) {
@@ -888,33 +1032,7 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, long long
       if (!meet_softmax(s, met)) return;
       if (s.last) {
         if (threadIdx.x == 0) p.tickets[item] = 0u;
-        const int n_rows = min(tr, rows - tile * tr);
-        // a CTA's slot 0 holds the item its share begins in
-        const auto slot_of = [&](int c) { return 2 * c + (c * total / n_cta < a ? 1 : 0); };
-        for (int r = threadIdx.x >> 5; r < n_rows; r += kSoftmaxWarps) {
-          const int ch = 4 * (threadIdx.x & 31);
-          float m = -INFINITY, l = 0.0f;
-          float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int c = c0; c <= c1; ++c) {
-            const long long pr = (long long)slot_of(c) * tr + r;
-            const float2 ml = __ldcg(&p.part_ml[pr]);
-            if (!(ml.y > 0.0f)) continue;
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + pr * kHeadDim + ch));
-            const float mm = fmaxf(m, ml.x), fa = exp2_fast(m - mm), fb = exp2_fast(ml.x - mm);
-            m = mm;
-            l = l * fa + ml.y * fb;
-            o.x = o.x * fa + v.x * fb;
-            o.y = o.y * fa + v.y * fb;
-            o.z = o.z * fa + v.z * fb;
-            o.w = o.w * fa + v.w * fb;
-          }
-          const float f = l > 0.0f ? 1.0f / l : 0.0f;
-          const int gr = tile * tr + r, tt = gr / gq, hh = w.head * gq + gr % gq;
-          __half* dst = p.out + bl * p.c.out_stride[0] + tt * p.c.out_stride[1] +
-                        hh * p.c.out_stride[2] + ch;
-          *reinterpret_cast<uint2*>(dst) =
-              make_uint2(pack_half2(o.x * f, o.y * f), pack_half2(o.z * f, o.w * f));
-        }
+        if (!merge_item(p, s, w, c0, c1, shares.begin(c0) < w.base, met)) return;
       }
     }
     if (!meet_softmax(s, met)) return;  // s.m, s.last and both accumulators may be written again
@@ -933,14 +1051,19 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
 
   // Units of every (sequence, row tile), summed over the threads in order.
   const int groups = p.c.batch_count * p.tiles;
-  const int per = (groups + kThreads - 1) / kThreads;
+  const int per = (int)((uint32_t)(groups + kThreads - 1) / kThreads);
   const int g0 = min(groups, tid * per), g1 = min(groups, g0 + per);
-  long long mine = 0;
-  for (int g = g0; g < g1; ++g) mine += (long long)span_of(p, g / p.tiles, g % p.tiles).n * p.d.hkv;
-  long long inc = mine;
+  const int seq0 = (int)((uint32_t)g0 / (uint32_t)p.tiles), tile0 = g0 - seq0 * p.tiles;
+  int mine = 0;
+#pragma unroll 1
+  for (int g = g0, sq = seq0, tl = tile0; g < g1; ++g) {
+    mine += span_of(p, sq, tl).n * p.d.hkv;
+    if (++tl == p.tiles) tl = 0, ++sq;
+  }
+  int inc = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+    const int y = __shfl_up_sync(0xffffffffu, inc, o);
     if (lane >= o) inc += y;
   }
   if (lane == 31) s.scan[warp] = inc;
@@ -961,26 +1084,32 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  long long before = 0, total = 0;
+  int before = 0, total = 0;
+#pragma unroll 1
   for (int i = 0; i < kThreads / 32; ++i) {
     if (i < warp) before += s.scan[i];
     total += s.scan[i];
   }
   before += inc - mine;
-  const long long n_cta = min((long long)gridDim.x, total);
-  if (blockIdx.x >= n_cta) return;  // fewer units than CTAs
-  const long long u0 = blockIdx.x * total / n_cta, u1 = (blockIdx.x + 1) * total / n_cta;
+  Shares shares;
+  shares.n = min((int)gridDim.x, total);
+  if ((int)blockIdx.x >= shares.n) return;  // fewer units than CTAs
+  shares.q = (int)((uint32_t)total / (uint32_t)shares.n);
+  shares.r = total - shares.q * shares.n;
+  const int u0 = shares.begin(blockIdx.x), u1 = shares.begin(blockIdx.x + 1);
   if (before <= u0 && u0 < before + mine) {
-    long long at = before;
-    for (int g = g0; g < g1; ++g) {
-      const int n = span_of(p, g / p.tiles, g % p.tiles).n;
-      if (u0 < at + (long long)n * p.d.hkv) {
-        s.start_group = g;
-        s.start_head = (int)((u0 - at) / n);
-        s.start_step = (int)((u0 - at) % n);
+#pragma unroll 1
+    for (int at = before, sq = seq0, tl = tile0;;) {
+      const int n = span_of(p, sq, tl).n;
+      if (u0 < at + n * p.d.hkv) {
+        s.start_seq = sq;
+        s.start_tile = tl;
+        s.start_head = (int)((uint32_t)(u0 - at) / (uint32_t)n);
+        s.start_step = u0 - at - s.start_head * n;
         break;
       }
-      at += (long long)n * p.d.hkv;
+      at += n * p.d.hkv;
+      if (++tl == p.tiles) tl = 0, ++sq;
     }
   }
   if (warp == kSoftmaxWarps + kLoadWarps) {
@@ -995,19 +1124,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(&s.tmem);
 
   if (warp < kSoftmaxWarps) {
-    softmax_role<BK>(p, s, u0, u1, total, n_cta);
-  } else if (warp < kSoftmaxWarps + 4) {
-    load_role<BK, true>(p, s, u0, u1, warp - kSoftmaxWarps);
-  } else if (warp < kSoftmaxWarps + 8) {
-    load_role<BV, false>(p, s, u0, u1, warp - kSoftmaxWarps - 4);
+    regs_up<kRegsSoftmax>();
+    softmax_role<BK>(p, s, u0, u1, shares);
+  } else if (warp < kSoftmaxWarps + kLoadWarps) {
+    regs_up<kRegsLoad>();
+    const bool key = warp < kSoftmaxWarps + 4;
+    if constexpr (BK == BV) load_role<BK>(p, s, u0, u1, warp & 3, key);
+    else if (key) load_role<BK>(p, s, u0, u1, warp & 3, true);
+    else load_role<BV>(p, s, u0, u1, warp & 3, false);
   } else {
-    if (lane == 0) {
+    regs_down<kRegsIssue>();
+    if (warp == kSoftmaxWarps + kLoadWarps && lane == 0) {
       mma_role<BK, BV>(p, s, u0, u1);
       if (*reinterpret_cast<volatile int*>(&s.abort)) {
         // products in flight end before the tile memory is given back
         tc_commit(&s.drained);
-        const long long t0 = clock64();
-        while (!bar_try(&s.drained, 0) && clock64() - t0 < kWaitLimit) {
+        const uint32_t t0 = (uint32_t)clock();
+        while (!bar_try(&s.drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
         }
         atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
       }
@@ -1027,6 +1160,11 @@ cudaError_t launch_widths(const Params& p, int ctas, cudaStream_t stream) {
       cudaFuncSetAttribute(chunk_attn_kernel<BK, BV>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            (int)sizeof(Smem));
   if (e != cudaSuccess) return e;
+  // the register shares below wait for registers that a smaller launch lacks
+  cudaFuncAttributes attr;
+  const cudaError_t ea = cudaFuncGetAttributes(&attr, chunk_attn_kernel<BK, BV>);
+  if (ea != cudaSuccess) return ea;
+  if (attr.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
   chunk_attn_kernel<BK, BV><<<ctas, kThreads, sizeof(Smem), stream>>>(p);
   return cudaGetLastError();
 }
