@@ -141,29 +141,40 @@ __device__ __forceinline__ void tc_before() {
 __device__ __forceinline__ void tc_after() {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 }
-__device__ __forceinline__ void tc_commit(uint64_t* b) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                   sptr(b))
-               : "memory");
+__device__ __forceinline__ void tc_commit(uint32_t leader, uint64_t* b) {
+  asm volatile(
+      "{\n .reg .pred e;\n setp.ne.b32 e, %1, 0;\n"
+      " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(
+          sptr(b)),
+      "r"(leader)
+      : "memory");
 }
 
-// D[128 x 128] (+)= A B, fp16 in, fp32 out, K = 16.  A in shared memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t acc) {
+// D[128 x 128] (+)= A B, fp16 in, fp32 out, K = 16, by the warp's elected lane
+// (`leader`); all lanes run it, so that the descriptors stay uniform.
+// A in shared memory.
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b,
+                                       uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
       : "memory");
 }
 // The same with A in tensor memory.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t acc) {
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b,
+                                       uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
       : "memory");
+}
+__device__ __forceinline__ uint32_t elect_lane() {
+  uint32_t e;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(e));
+  return e;
 }
 __device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
@@ -660,14 +671,14 @@ constexpr uint32_t kColS = 0, kColO = 256;  // tensor memory columns: S0 S1 O0 O
 template <int BK, int BV>
 __device__ __forceinline__ void mma_role(const Params& p, Smem& s, int u0, int u1) {
   constexpr uint32_t kIdS = instr_desc(BK != 1), kIdO = instr_desc(BV != 1);
-  const uint32_t tm = s.tmem;
+  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0), leader = elect_lane();
   uint32_t nk = 0, nv = 0, ns[2] = {0, 0}, items = 0;
   const int two = p.streams_rows;  // a key tile serves two steps
   Walk w;
   w.begin(s, u0, u1);
   for (; w.next(p); w.advance(p), ++items) {
     const int steps = (w.i1 - w.i0) << two;
-    if (!bar_wait(s, &s.q_full, items & 1)) return;
+    if (!warp_wait(s, &s.q_full, items & 1)) return;
     tc_after();
     // scores run two steps ahead of the weights times the values
 #pragma unroll 1
@@ -675,36 +686,36 @@ __device__ __forceinline__ void mma_role(const Params& p, Smem& s, int u0, int u
       const int x = st & 1;
       if (st >= 0) {
         const int buf = nv & 1;
-        if (!bar_wait(s, &s.p_ready[x], ns[x] & 1)) return;
+        if (!warp_wait(s, &s.p_ready[x], ns[x] & 1)) return;
         ++ns[x];
-        if ((!two || x == 0) && !bar_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
+        if ((!two || x == 0) && !warp_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
         tc_after();
         const uint64_t b = tile_desc(sptr(s.v[buf]), BV != 1);
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
-          mma_ts(tm + kColO + 128 * x, tm + kColS + 128 * x + 8 * ks,
+          mma_ts(leader, tm + kColO + 128 * x, tm + kColS + 128 * x + 8 * ks,
                  b + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 1 || ks > 0);
         if (!two || x == 1) {
-          tc_commit(&s.v_empty[buf]);
+          tc_commit(leader, &s.v_empty[buf]);
           ++nv;
         }
-        if (st + 2 >= steps) tc_commit(&s.o_full[x]);
+        if (st + 2 >= steps) tc_commit(leader, &s.o_full[x]);
       }
       if (st + 2 < steps) {
         const int buf = nk & 1;
         if (!two || x == 0) {
-          if (!bar_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return;
+          if (!warp_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return;
           tc_after();
         }
         const uint64_t a = tile_desc(sptr(s.q[two ? x : 0]), false),
                        b = tile_desc(sptr(s.k[buf]), BK != 1);
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
-          mma_ss(tm + kColS + 128 * x, a + step_major_k(ks),
+          mma_ss(leader, tm + kColS + 128 * x, a + step_major_k(ks),
                  b + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdS, ks > 0);
-        tc_commit(&s.s_full[x]);
+        tc_commit(leader, &s.s_full[x]);
         if (!two || x == 1) {
-          tc_commit(&s.k_empty[buf]);
+          tc_commit(leader, &s.k_empty[buf]);
           ++nk;
         }
       }
@@ -1134,15 +1145,16 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     else load_role<BV>(p, s, u0, u1, warp & 3, false);
   } else {
     regs_down<kRegsIssue>();
-    if (warp == kSoftmaxWarps + kLoadWarps && lane == 0) {
+    if (warp == kSoftmaxWarps + kLoadWarps) {
       mma_role<BK, BV>(p, s, u0, u1);
-      if (*reinterpret_cast<volatile int*>(&s.abort)) {
+      if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort))) {
         // products in flight end before the tile memory is given back
-        tc_commit(&s.drained);
+        tc_commit(elect_lane(), &s.drained);
         const uint32_t t0 = (uint32_t)clock();
         while (!bar_try(&s.drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
         }
-        atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
+        if (lane == 0)
+          atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
       }
     }
     __syncwarp();
