@@ -378,7 +378,7 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  * rounded once to fp16.
  *   q, out       device fp16, element (b, t, i, d) at b * stride[0] + t *
  *                stride[1] + i * stride[2] + d for sequence batch_begin + b;
- *                16-byte aligned.
+ *                16-byte aligned; they must not overlap.
  *   params       below.
  *   workspace    device, >= kvq_chunk_workspace_bytes(cfg, n_q, batch_count),
  *                zeroed once by kvq_workspace_init; calls sharing it must not

@@ -20,10 +20,10 @@
 // alternate, so that one's softmax runs under the other's products: two row
 // tiles on the same key tiles, or (items of at most 128 rows) the same row
 // tile on alternate key tiles, joined at the end.
-//   warps 0-3, 4-7  softmax of streams 0 and 1 (and queries in, results out)
+//   warps 0-3, 4-7  softmax of streams 0 and 1, queries in, results out; the
+//                   first warp of each issues its stream's products
 //   warps 8-11      keys: one 32-token block each, codes -> fp16 tile
 //   warps 12-15     values, the same
-//   warp 16         issues the products (17-19 idle)
 // The running maximum of a row moves only when a score is more than 8 (in log2)
 // above it, so the accumulator is rescaled rarely; weights stay below 2^8.
 //
@@ -47,14 +47,22 @@ constexpr int kTile = 128;                  // tokens of a key / value tile, row
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;  // 64 elements of the contiguous axis
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 8;
-constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps + 4);
-// Registers a thread: at launch, then by warpgroup.  The shares must not exceed
-// what the launch got.
-constexpr int kRegsLaunch = 96, kRegsSoftmax = 104, kRegsLoad = 104, kRegsIssue = 64;
-static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kLoadWarps * kRegsLoad + 4 * kRegsIssue) <=
-                  kThreads * kRegsLaunch,
-              "register shares exceed the launch's");
+constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps);
+// Registers a thread: at launch, then by role: softmax holds a row's 128
+// scores, a loading warp four parts of a block (those of 1 and 8 bits are the
+// largest).  Together the roles have what the launch got.
+constexpr int kRegsLaunch = 128;
+template <int BK, int BV>
+constexpr int regs_load() {
+  return BK == 1 || BV == 1 || BK == 8 || BV == 8 ? 112 : 96;
+}
+template <int BK, int BV>
+constexpr int regs_softmax() {
+  return 2 * kRegsLaunch - regs_load<BK, BV>();
+}
+static_assert(kSoftmaxWarps == kLoadWarps, "the two shares are of equal size");
 constexpr uint32_t kWaitLimit = 2000000000u;  // cycles of a bounded wait (~1 s)
+constexpr int kAhead = 2;  // blocks behind the next whose table entry (and L2 copy) is on its way
 constexpr float kRescaleLog2 = 8.0f;
 
 struct Smem {
@@ -62,7 +70,7 @@ struct Smem {
   unsigned char k[2][kTileBytes];
   unsigned char v[2][kTileBytes];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_full;
-  uint64_t meet, drained;
+  uint64_t meet, drained[2];
   int scan[32];
   int start_seq, start_tile, start_head, start_step;
   uint32_t tmem;
@@ -98,11 +106,13 @@ __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(sptr(b)) : "memory");
 }
+// One try, suspended for up to ~10 us in hardware: a warp that polls takes
+// issue slots from the others on its scheduler.
 __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n .reg .pred p;\n"
-      " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 10000;\n"
       " selp.u32 %0, 1, 0, p;\n}"
       : "=r"(ok)
       : "r"(sptr(b)), "r"(parity)
@@ -127,9 +137,15 @@ __device__ __forceinline__ bool bar_wait(Smem& s, uint64_t* b, uint32_t parity) 
 __device__ __forceinline__ bool warp_wait(Smem& s, uint64_t* b, uint32_t parity) {
   return __all_sync(0xffffffffu, bar_wait(s, b, parity));
 }
+// One arrival for a warp, behind what all its lanes did (32 arrivals on one
+// barrier are served one by one).
+__device__ __forceinline__ void warp_arrive(uint64_t* b) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) bar_arrive(b);
+}
 // All softmax threads meet (bounded, unlike a hardware barrier).
 __device__ __forceinline__ bool meet_softmax(Smem& s, uint32_t& n) {
-  bar_arrive(&s.meet);
+  warp_arrive(&s.meet);
   return warp_wait(s, &s.meet, n++ & 1);
 }
 __device__ __forceinline__ void fence_async() {
@@ -189,6 +205,17 @@ __device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tm_load_wait() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,"
+      "%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+      "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+      "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+      "r"(r[30]), "r"(r[31]), "r"(addr)
+      : "memory");
 }
 __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -442,7 +469,8 @@ __device__ __forceinline__ int value_row(int c) { return (c & ~7) + run_pos(c & 
 // word k of the lane's 16 bytes and the pairs of scales and zeros it meets.
 template <int B>
 struct Part {
-  uint32_t w[B], sz;
+  uint32_t w[B];
+  __half s, z;  // kept apart: packing them would wait for the loads
 };
 template <>
 struct Part<1> {
@@ -476,7 +504,8 @@ __device__ __forceinline__ void load_part(Part<B>& c, int k, const char* codes, 
       }
     }
     const __half* m = meta + (key ? lane : vmeta_index(0, lane));
-    c.sz = as_u32(__halves2half2(m[0], m[kHeadDim]));
+    c.s = m[0];
+    c.z = m[kHeadDim];
   }
 }
 
@@ -511,7 +540,7 @@ __device__ __forceinline__ void restore_part(const Part<B>& c, int k, unsigned c
       st16(base, n * 256 + (x0 ^ (n << 5)), make_uint4(o[0], o[1], o[2], o[3]));
     }
   } else {
-    const __half2 s = __low2half2(as_half2(c.sz)), z = __high2half2(as_half2(c.sz));
+    const __half2 s = __half2half2(c.s), z = __half2half2(c.z);
     const int row = key ? 32 * k + lane : 32 * j + (lane & 24) + run_pos(lane & 7);
     const uint32_t at = key ? tile_at(j >> 1, row, (j & 1) * 4) : tile_at(k >> 1, row, (k & 1) * 4);
 #pragma unroll
@@ -543,20 +572,19 @@ __device__ __forceinline__ void window_block(const __half* rows, int valid, unsi
   } else {  // rows are channels, two a lane
     const uint32_t* src = reinterpret_cast<const uint32_t*>(rows) + lane;
 #pragma unroll 1
-    for (int g = 0; g < 4; ++g) {  // 64 channels and 16 tokens at a time
-      const int c = 64 * (g >> 1) + 2 * lane, h = g & 1;
-      uint32_t x[16];
+    for (int g = 0; g < 2; ++g) {  // 64 channels at a time
+      const int c = 64 * g + 2 * lane;
+      uint32_t x[32];
 #pragma unroll
-      for (int t = 0; t < 16; ++t)
-        x[t] = 16 * h + t < valid ? src[(16 * h + t) * (kHeadDim / 2) + 32 * (g >> 1)] : 0u;
+      for (int t = 0; t < 32; ++t) x[t] = t < valid ? src[t * (kHeadDim / 2) + 32 * g] : 0u;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int row = key ? c + e : value_row(c + e);
         const uint32_t sel = e ? 0x7632 : 0x5410;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < 4; ++k) {
           const uint32_t* y = x + 8 * k;
-          st16(tile, tile_at(j >> 1, row, (j & 1) * 4 + 2 * h + k),
+          st16(tile, tile_at(j >> 1, row, (j & 1) * 4 + k),
                make_uint4(__byte_perm(y[0], y[4], sel), __byte_perm(y[1], y[5], sel),
                           __byte_perm(y[2], y[6], sel), __byte_perm(y[3], y[7], sel)));
         }
@@ -618,14 +646,22 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
         atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_BAD_PAGE);
       return nullptr;
     };
+    const auto prefetch = [&](int e) {
+      if (e >= 0 && e < limit && lane < 4 * B + 4)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(base + (long long)e * stride + 128 * lane));
+    };
     Part<B> c[4];
     const char* at0 = nullptr;
     const char* at1 = address(index(w.i0));
-    int e1 = index(w.i0 + 1), e2 = index(w.i0 + 2);
+    int e[kAhead];  // indexes of the blocks behind at1's
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) e[k] = index(w.i0 + 1 + k);
+#pragma unroll
+    for (int k = 0; k < kAhead - 1; ++k) prefetch(e[k]);
     // i = i0 - 1 only loads the first block
 #pragma unroll 1
     for (int i = w.i0 - 1; i < w.i1; ++i) {
-      const int buf = n & 1, e3 = index(i + 4);
+      const int buf = n & 1, far = index(i + 2 + kAhead);
       unsigned char* tile = tiles[buf];
       if (i >= w.i0) {
         if (!warp_wait(s, &empty[buf], ((n >> 1) & 1) ^ 1)) return;
@@ -648,16 +684,15 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
       }
       if (i >= w.i0) {
         fence_async();
-        __syncwarp();
-        if (lane == 0) bar_arrive(&full[buf]);
+        warp_arrive(&full[buf]);
         ++n;
       }
       at0 = at1;
-      at1 = address(e1);
-      if (at1 && lane < 4 * B + 4)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(at1 + 128 * lane));
-      e1 = e2;
-      e2 = e3;
+      at1 = address(e[0]);
+      prefetch(e[kAhead - 1]);
+#pragma unroll
+      for (int k = 0; k < kAhead - 1; ++k) e[k] = e[k + 1];
+      e[kAhead - 1] = far;
     }
   }
 }
@@ -668,59 +703,25 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
 
 constexpr uint32_t kColS = 0, kColO = 256;  // tensor memory columns: S0 S1 O0 O1, 128 each
 
-template <int BK, int BV>
-__device__ __forceinline__ void mma_role(const Params& p, Smem& s, int u0, int u1) {
-  constexpr uint32_t kIdS = instr_desc(BK != 1), kIdO = instr_desc(BV != 1);
-  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0), leader = elect_lane();
-  uint32_t nk = 0, nv = 0, ns[2] = {0, 0}, items = 0;
-  const int two = p.streams_rows;  // a key tile serves two steps
-  Walk w;
-  w.begin(s, u0, u1);
-  for (; w.next(p); w.advance(p), ++items) {
-    const int steps = (w.i1 - w.i0) << two;
-    if (!warp_wait(s, &s.q_full, items & 1)) return;
-    tc_after();
-    // scores run two steps ahead of the weights times the values
-#pragma unroll 1
-    for (int st = -2; st < steps; ++st) {
-      const int x = st & 1;
-      if (st >= 0) {
-        const int buf = nv & 1;
-        if (!warp_wait(s, &s.p_ready[x], ns[x] & 1)) return;
-        ++ns[x];
-        if ((!two || x == 0) && !warp_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
-        tc_after();
-        const uint64_t b = tile_desc(sptr(s.v[buf]), BV != 1);
+// Scores of a row tile: S = Q K^T.
+template <int BK>
+__device__ __forceinline__ void issue_scores(uint32_t leader, uint32_t ts, const unsigned char* q,
+                                             const unsigned char* k) {
+  const uint64_t a = tile_desc(sptr(q), false), b = tile_desc(sptr(k), BK != 1);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          mma_ts(leader, tm + kColO + 128 * x, tm + kColS + 128 * x + 8 * ks,
-                 b + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 1 || ks > 0);
-        if (!two || x == 1) {
-          tc_commit(leader, &s.v_empty[buf]);
-          ++nv;
-        }
-        if (st + 2 >= steps) tc_commit(leader, &s.o_full[x]);
-      }
-      if (st + 2 < steps) {
-        const int buf = nk & 1;
-        if (!two || x == 0) {
-          if (!warp_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return;
-          tc_after();
-        }
-        const uint64_t a = tile_desc(sptr(s.q[two ? x : 0]), false),
-                       b = tile_desc(sptr(s.k[buf]), BK != 1);
+  for (int ks = 0; ks < 8; ++ks)
+    mma_ss(leader, ts, a + step_major_k(ks), b + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)),
+           instr_desc(BK != 1), ks > 0);
+}
+// Weights times values: O (+)= P V, P in the columns of S.
+template <int BV>
+__device__ __forceinline__ void issue_values(uint32_t leader, uint32_t to, uint32_t ts,
+                                             const unsigned char* v, bool add) {
+  const uint64_t b = tile_desc(sptr(v), BV != 1);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          mma_ss(leader, tm + kColS + 128 * x, a + step_major_k(ks),
-                 b + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdS, ks > 0);
-        tc_commit(leader, &s.s_full[x]);
-        if (!two || x == 1) {
-          tc_commit(leader, &s.k_empty[buf]);
-          ++nk;
-        }
-      }
-    }
-  }
+  for (int ks = 0; ks < 8; ++ks)
+    mma_ts(leader, to, ts + 8 * ks, b + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)),
+           instr_desc(BV != 1), add || ks > 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -734,18 +735,32 @@ struct Row {
   float m, l;    // running maximum (of scores times scale, log2 domain) and sum
 };
 
+// Row r (of the sequence's n_q * gq) of a [sequence][token][head] array.
+__device__ __forceinline__ long long row_offset(const Params& p, const long long (&stride)[3],
+                                                int bl, int kv_head, int r) {
+  const int t = token_of_row(p, r);
+  return bl * stride[0] + t * stride[1] + (kv_head * p.d.gq + r - t * p.d.gq) * stride[2];
+}
+
+// A warp's 32 rows, from row r0 of the sequence and row `row` of the tile on:
+// 16 lanes a row.
 template <int BK>
-__device__ __forceinline__ void load_queries(const Params& p, const __half* src,
+__device__ __forceinline__ void load_queries(const Params& p, const Walk& w, int r0,
                                              unsigned char* tile, int row) {
-  (void)p;
-  const uint4* q = reinterpret_cast<const uint4*>(src);
+  const int lane = threadIdx.x & 31, m = lane & 15, rows = p.c.n_q * p.d.gq;
 #pragma unroll 1
-  for (int h = 0; h < 16; h += 8) {
+  for (int h = 0; h < 32; h += 16) {
     uint4 v[8];
 #pragma unroll
-    for (int m = 0; m < 8; ++m) v[m] = src ? q[h + m] : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < 8; ++i) {
+      const int r = h + 2 * i + (lane >> 4);
+      v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (r0 + r < rows)
+        v[i] = __ldg(reinterpret_cast<const uint4*>(
+                         p.q + row_offset(p, p.c.q_stride, w.bl, w.head, r0 + r)) + m);
+    }
 #pragma unroll
-    for (int m = 0; m < 8; ++m) put_key_row<BK>(tile, row, h + m, v[m]);
+    for (int i = 0; i < 8; ++i) put_key_row<BK>(tile, row + h + 2 * i + (lane >> 4), m, v[i]);
   }
 }
 
@@ -755,39 +770,37 @@ __device__ __forceinline__ void load_queries(const Params& p, const __half* src,
 // tensor memory by a short loop to keep the code of the others small.
 __device__ __forceinline__ void mask_row(uint32_t ts, int hi, int lo, int sink) {
 #pragma unroll 1
-  for (int c = 0; c < 128; c += 8) {
-    uint32_t r[8];
-    tm_load8(ts + c, r);
+  for (int c = 0; c < 128; c += 32) {
+    uint32_t r[32];
+    tm_load32(ts + c, r);
     tm_load_wait();
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const int t = c + run_token(n);
+    for (int n = 0; n < 32; ++n) {
+      const int t = c + (n & ~7) + run_token(n & 7);
       if (t > hi || (t <= lo && t >= sink)) r[n] = 0xff800000u;
     }
-    tm_store8(ts + c, r);
+    tm_store32(ts + c, r);
   }
   tm_store_wait();
 }
 
 // One step of a stream's softmax for a row (a thread); `first`: no accumulator
-// yet.  The scores are read twice, 32 at a time (holding all 128 would take
-// the registers that the loading warps need more); the next 32 are on their
-// way while 32 are worked on.
+// yet.  All 128 scores are read at once and stay in registers (a read takes
+// several hundred cycles beside the products).
 __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sl2, bool first,
                                              Row& row) {
-  uint32_t r[2][32];
+  uint32_t r[4][32];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) tm_load32(ts + 32 * c, r[c]);
+  tm_load_wait();
   float mc[4];
-  tm_load32(ts, r[0]);
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const uint32_t(&x)[32] = r[c & 1];
-    tm_load_wait();
-    tm_load32(ts + 32 * ((c + 1) & 3), r[(c + 1) & 1]);  // at the end: the first again
-    mc[c] = __uint_as_float(x[0]);
+    mc[c] = __uint_as_float(r[c][0]);
 #pragma unroll
     for (int n = 1; n < 31; n += 2)
-      mc[c] = fmaxf(fmaxf(mc[c], __uint_as_float(x[n])), __uint_as_float(x[n + 1]));
-    mc[c] = fmaxf(mc[c], __uint_as_float(x[31]));
+      mc[c] = fmaxf(fmaxf(mc[c], __uint_as_float(r[c][n])), __uint_as_float(r[c][n + 1]));
+    mc[c] = fmaxf(mc[c], __uint_as_float(r[c][31]));
   }
   const float mx = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])) * sl2;
   if (first) {
@@ -815,20 +828,18 @@ __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sl2
   uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const uint32_t(&x)[32] = r[c & 1];
     uint32_t w[16];
-    tm_load_wait();
-    if (c < 3) tm_load32(ts + 32 * (c + 1), r[(c + 1) & 1]);
 #pragma unroll
     for (int n = 0; n < 16; ++n) {
       float a, b;
-      unpair(fma2(pair(__uint_as_float(x[2 * n]), __uint_as_float(x[2 * n + 1])), sl, of), a, b);
+      unpair(fma2(pair(__uint_as_float(r[c][2 * n]), __uint_as_float(r[c][2 * n + 1])), sl, of), a,
+             b);
       a = exp2_fast(a);
       b = exp2_fast(b);
       sum[n & 1] = add2(sum[n & 1], pair(a, b));
       w[n] = pack_half2(a, b);
     }
-    tm_store16(ts + 16 * c, w);  // columns that have been read
+    tm_store16(ts + 16 * c, w);
   }
   float a, b;
   unpair(add2(sum[0], sum[1]), a, b);
@@ -836,27 +847,31 @@ __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sl2
   tm_store_wait();
 }
 
-// Write 32 accumulator columns times f: fp16 results or fp32 partials, in
-// channel order.
-__device__ __forceinline__ void put_half(__half* dst, int c, const float (&o)[32]) {
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      // channels 2i and 2i + 1 of the run
-      const int a = 2 * i < 4 ? 4 * i : 4 * i - 7;
-      w[i] = pack_half2(o[8 * g + a], o[8 * g + a + 2]);
-    }
-    *reinterpret_cast<uint4*>(dst + 32 * c + 8 * g) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+// Results leave through shared memory (the queries' tile, no longer read): each
+// lane writes 256 bytes of its own row to the warp's 32 x 256 byte area, then 16
+// lanes copy a row to memory.  Chunk m of a row is at m ^ (row mod 8).
+__device__ __forceinline__ uint32_t stage_at(int row, int m) {
+  return row * 256 + ((m ^ (row & 7)) << 4);
 }
-__device__ __forceinline__ void put_float(float* dst, int c, const float (&o)[32]) {
+// 32 accumulator columns (run order) in channel order: fp16 or fp32.
+__device__ __forceinline__ void stage_half(unsigned char* area, int c, const float (&o)[32]) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const float* x = o + 8 * g;
-    *reinterpret_cast<float4*>(dst + 32 * c + 8 * g) = make_float4(x[0], x[2], x[4], x[6]);
-    *reinterpret_cast<float4*>(dst + 32 * c + 8 * g + 4) = make_float4(x[1], x[3], x[5], x[7]);
+    st16(area, stage_at(lane, 4 * c + g),
+         make_uint4(pack_half2(x[0], x[2]), pack_half2(x[4], x[6]), pack_half2(x[1], x[3]),
+                    pack_half2(x[5], x[7])));
+  }
+}
+__device__ __forceinline__ void stage_float(unsigned char* area, int c, const float (&o)[32]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const uint32_t* x = reinterpret_cast<const uint32_t*>(o + 8 * g);
+    const int m = 8 * (c & 1) + 2 * g;
+    st16(area, stage_at(lane, m), make_uint4(x[0], x[2], x[4], x[6]));
+    st16(area, stage_at(lane, m + 1), make_uint4(x[1], x[3], x[5], x[7]));
   }
 }
 
@@ -867,8 +882,8 @@ __device__ __forceinline__ void put_float(float* dst, int c, const float (&o)[32
 // every other CTA's share begins here (slot 0).
 __device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk& w, int c0, int c1,
                                            bool inside, uint32_t& met) {
-  const int tr = kTile << p.streams_rows, gq = p.d.gq, tid = threadIdx.x, tile = w.row_tile;
-  const int n_rows = min(tr, p.c.n_q * gq - tile * tr);
+  const int tr = kTile << p.streams_rows, tid = threadIdx.x, tile = w.row_tile;
+  const int n_rows = min(tr, p.c.n_q * p.d.gq - tile * tr);
   const auto slot_of = [&](int c) {
     return (long long)(2 * c + (inside && c == c0 ? 1 : 0)) * tr;
   };
@@ -900,7 +915,7 @@ __device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk&
     }
   }
   if (!meet_softmax(s, met)) return false;
-  const int ch = 4 * (tid & 31), bl = w.bl;
+  const int ch = 4 * (tid & 31);
 #pragma unroll 2
   for (int r = tid >> 5; r < n_rows; r += kSoftmaxWarps) {
     const float m = s.row_m[r], f = s.row_f[r];
@@ -918,58 +933,83 @@ __device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk&
         o.w = fmaf(v.w, x, o.w);
       }
     }
-    const int g = tile * tr + r, t = token_of_row(p, g), head = w.head * gq + g - t * gq;
-    __half* dst = p.out + bl * p.c.out_stride[0] + t * p.c.out_stride[1] +
-                  head * p.c.out_stride[2] + ch;
+    __half* dst = p.out + row_offset(p, p.c.out_stride, w.bl, w.head, tile * tr + r) + ch;
     *reinterpret_cast<uint2*>(dst) =
         make_uint2(pack_half2(o.x * f, o.y * f), pack_half2(o.z * f, o.w * f));
   }
   return true;
 }
 
-template <int BK>
+template <int BK, int BV>
 __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, int u1,
                                              const Shares& shares) {
   const int warp = threadIdx.x >> 5, x = warp >> 2, lane_row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes a warp, in bits 16 up
-  const uint32_t ts = s.tmem + lanes + kColS + 128 * x, to = s.tmem + lanes + kColO + 128 * x;
-  const int two = p.streams_rows, tr = kTile << two, rows = p.c.n_q * p.d.gq, gq = p.d.gq;
-  uint32_t ns = 0, no[2] = {0, 0}, met = 0;
+  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0) + 128 * x;
+  const uint32_t ts = tm + lanes + kColS, to = tm + lanes + kColO;
+  const bool issuer = (warp & 3) == 0;  // of its stream's products
+  const uint32_t leader = elect_lane();
+  const int two = p.streams_rows, tr = kTile << two, rows = p.c.n_q * p.d.gq;
+  uint32_t ns = 0, np = 0, no[2] = {0, 0}, met = 0, items = 0, nt = 0;  // nt: tiles of the items before
   Walk w;
   w.begin(s, u0, u1);
   for (; w.next(p); w.advance(p)) {
-    const int bl = w.bl, tile = w.row_tile;
+    const int tile = w.row_tile;
     const int tr_row = (two ? kTile * x : 0) + lane_row;  // row in the item
-    const int g = tile * tr + tr_row;
+    const int g = tile * tr + tr_row, g_warp = g - (threadIdx.x & 31);
     const bool valid = g < rows;
-    const int t = token_of_row(p, g), head = w.head * gq + g - t * gq;
-    const int pos = w.s.L - p.c.n_q + t;
+    const int pos = w.s.L - p.c.n_q + token_of_row(p, g);
     if (two || x == 0) {
-      const long long off = bl * p.c.q_stride[0] + t * p.c.q_stride[1] + head * p.c.q_stride[2];
-      load_queries<BK>(p, valid ? p.q + off : nullptr, s.q[x], lane_row);
+      load_queries<BK>(p, w, g_warp, s.q[x], lane_row & ~31);
       fence_async();
-      bar_arrive(&s.q_full);
+      warp_arrive(&s.q_full);
     }
     const bool live = __any_sync(0xffffffffu, valid);
     Row row{-INFINITY, 0.0f};
     const int n = w.i1 - w.i0;
-    bool first = true;
-    for (int i = two ? 0 : x; i < n; i += two ? 1 : 2, ++ns, first = false) {
-      if (!warp_wait(s, &s.s_full[x], ns & 1)) return;
-      tc_after();
-      if (live) {
-        const int t0 = w.s.tile(w.i0 + i) * kTile;
-        // every token of the tile is seen by every row of the item
-        const bool whole = w.s.p0 >= t0 + kTile - 1 &&
-                           (!p.c.window || t0 > w.s.p1 - p.c.window || t0 + kTile <= p.c.sinks);
-        if (!whole)
-          mask_row(ts, (valid ? pos : -1) - t0, p.c.window ? pos - p.c.window - t0 : -1 - t0,
-                   p.c.sinks - t0);
-        softmax_step(ts, to, p.c.scale_log2, first, row);
+    const int steps = two ? n : (n - x + 1) >> 1;
+    if (issuer && !warp_wait(s, &s.q_full, items & 1)) return;
+    ++items;
+    // step -1 only issues the first scores
+#pragma unroll 1
+    for (int st = -1; st < steps; ++st) {
+      const int i = two ? st : 2 * st + x;  // tile of the share
+      if (st >= 0) {
+        if (!warp_wait(s, &s.s_full[x], ns++ & 1)) return;
+        tc_after();
+        if (live) {
+          const int t0 = w.s.tile(w.i0 + i) * kTile;
+          // every token of the tile is seen by every row of the item
+          const bool whole = w.s.p0 >= t0 + kTile - 1 &&
+                             (!p.c.window || t0 > w.s.p1 - p.c.window || t0 + kTile <= p.c.sinks);
+          if (!whole)
+            mask_row(ts, (valid ? pos : -1) - t0, p.c.window ? pos - p.c.window - t0 : -1 - t0,
+                     p.c.sinks - t0);
+          softmax_step(ts, to, p.c.scale_log2, st == 0, row);
+        }
+        tc_before();
+        warp_arrive(&s.p_ready[x]);
       }
-      tc_before();
-      bar_arrive(&s.p_ready[x]);
+      if (!issuer) continue;
+      if (st >= 0) {
+        const uint32_t t = nt + i, buf = t & 1;
+        if (!warp_wait(s, &s.p_ready[x], np++ & 1)) return;
+        if (!warp_wait(s, &s.v_full[buf], (t >> 1) & 1)) return;
+        tc_after();
+        issue_values<BV>(leader, tm + kColO, tm + kColS, s.v[buf], st > 0);
+        tc_commit(leader, &s.v_empty[buf]);
+        if (st + 1 == steps) tc_commit(leader, &s.o_full[x]);
+      }
+      if (st + 1 < steps) {
+        const uint32_t t = nt + (two ? st + 1 : 2 * st + 2 + x), buf = t & 1;
+        if (!warp_wait(s, &s.k_full[buf], (t >> 1) & 1)) return;
+        tc_after();
+        issue_scores<BK>(leader, tm + kColS, s.q[two ? x : 0], s.k[buf]);
+        tc_commit(leader, &s.s_full[x]);
+        tc_commit(leader, &s.k_empty[buf]);
+      }
     }
+    nt += n;
     // both accumulators complete (a stream without a step has none)
     const bool has1 = two || n > 1;
     if (x == 0 || two) {
@@ -1003,14 +1043,12 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
       const float scale = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
       f0 *= scale;
       f1 *= scale;
-      const long long off =
-          bl * p.c.out_stride[0] + t * p.c.out_stride[1] + head * p.c.out_stride[2];
       const long long pr = (long long)slot * tr + tr_row;
+      unsigned char* area = s.q[x] + (lane_row & ~31) * 256;
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         uint32_t r[32];
         float o[32];
-        __syncwarp();
         tm_load32(to + 32 * c, r);
         tm_load_wait();
 #pragma unroll
@@ -1021,9 +1059,25 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
 #pragma unroll
           for (int k = 0; k < 32; ++k) o[k] = fmaf(__uint_as_float(r[k]), f1, o[k]);
         }
-        if (valid) {
-          if (direct) put_half(p.out + off, c, o);
-          else put_float(p.part_o + pr * kHeadDim, c, o);
+        if (direct) stage_half(area, c, o);
+        else stage_float(area, c, o);
+        if (c == 3 || (!direct && c == 1)) {  // 256 bytes of every row
+          __syncwarp();
+          const int lane = threadIdx.x & 31, m = lane & 15;
+#pragma unroll 4
+          for (int k = 0; k < 32; k += 2) {
+            const int rr = k + (lane >> 4);
+            if (g_warp + rr < rows) {
+              const uint4 v = *reinterpret_cast<const uint4*>(area + stage_at(rr, m));
+              if (direct)
+                *reinterpret_cast<uint4*>(
+                    p.out + row_offset(p, p.c.out_stride, w.bl, w.head, g_warp + rr) + 8 * m) = v;
+              else
+                *reinterpret_cast<uint4*>(p.part_o + (pr - lane + rr) * kHeadDim + 64 * (c >> 1) +
+                                          4 * m) = v;
+            }
+          }
+          __syncwarp();
         }
       }
       if (valid && !direct) p.part_ml[pr] = make_float2(m, l);
@@ -1082,25 +1136,28 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     for (int i = 0; i < 2; ++i) {
       bar_init(&s.k_full[i], 4);
       bar_init(&s.v_full[i], 4);
-      bar_init(&s.k_empty[i], 1);
-      bar_init(&s.v_empty[i], 1);
+      bar_init(&s.k_empty[i], 1 << p.streams_rows);  // a commit of every stream that reads it
+      bar_init(&s.v_empty[i], 1 << p.streams_rows);
+      bar_init(&s.drained[i], 1);
       bar_init(&s.s_full[i], 1);
-      bar_init(&s.p_ready[i], kTile);
+      bar_init(&s.p_ready[i], 4);
       bar_init(&s.o_full[i], 1);
     }
-    bar_init(&s.q_full, kTile << p.streams_rows);
-    bar_init(&s.meet, 32 * kSoftmaxWarps);
-    bar_init(&s.drained, 1);
+    bar_init(&s.q_full, 4 << p.streams_rows);
+    bar_init(&s.meet, kSoftmaxWarps);
     s.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  int before = 0, total = 0;
-#pragma unroll 1
-  for (int i = 0; i < kThreads / 32; ++i) {
-    if (i < warp) before += s.scan[i];
-    total += s.scan[i];
+  int warps = lane < kThreads / 32 ? s.scan[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, warps, o);
+    if (lane >= o) warps += y;
   }
+  const int total = __shfl_sync(0xffffffffu, warps, 31);
+  int before = __shfl_sync(0xffffffffu, warps, warp > 0 ? warp - 1 : 0);
+  if (warp == 0) before = 0;
   before += inc - mine;
   Shares shares;
   shares.n = min((int)gridDim.x, total);
@@ -1123,7 +1180,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       if (++tl == p.tiles) tl = 0, ++sq;
     }
   }
-  if (warp == kSoftmaxWarps + kLoadWarps) {
+  if (warp == kSoftmaxWarps) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
                      sptr(&s.tmem))
                  : "memory");
@@ -1135,34 +1192,30 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(&s.tmem);
 
   if (warp < kSoftmaxWarps) {
-    regs_up<kRegsSoftmax>();
-    softmax_role<BK>(p, s, u0, u1, shares);
-  } else if (warp < kSoftmaxWarps + kLoadWarps) {
-    regs_up<kRegsLoad>();
+    regs_up<regs_softmax<BK, BV>()>();
+    softmax_role<BK, BV>(p, s, u0, u1, shares);
+    if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort)) && (warp & 3) == 0) {
+      // products in flight end before the tile memory is given back
+      uint64_t* drained = &s.drained[warp >> 2];
+      tc_commit(elect_lane(), drained);
+      const uint32_t t0 = (uint32_t)clock();
+      while (!bar_try(drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
+      }
+      if (lane == 0)
+        atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
+    }
+    __syncwarp();
+  } else {
+    regs_down<regs_load<BK, BV>()>();
     const bool key = warp < kSoftmaxWarps + 4;
     if constexpr (BK == BV) load_role<BK>(p, s, u0, u1, warp & 3, key);
     else if (key) load_role<BK>(p, s, u0, u1, warp & 3, true);
     else load_role<BV>(p, s, u0, u1, warp & 3, false);
-  } else {
-    regs_down<kRegsIssue>();
-    if (warp == kSoftmaxWarps + kLoadWarps) {
-      mma_role<BK, BV>(p, s, u0, u1);
-      if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort))) {
-        // products in flight end before the tile memory is given back
-        tc_commit(elect_lane(), &s.drained);
-        const uint32_t t0 = (uint32_t)clock();
-        while (!bar_try(&s.drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
-        }
-        if (lane == 0)
-          atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
-      }
-    }
-    __syncwarp();
   }
   tc_before();
   __syncthreads();
   tc_after();
-  if (warp == kSoftmaxWarps + kLoadWarps)
+  if (warp == kSoftmaxWarps)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
