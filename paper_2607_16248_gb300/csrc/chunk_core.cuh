@@ -13,17 +13,19 @@
 // row, maximum, sum) in the workspace; the CTA that finishes last merges them
 // in the order of the tokens, so results repeat bit for bit.
 //
-// A CTA.  Per step: S = Q K^T (M 128 rows x N 128 tokens, fp16 operands in
-// shared memory, fp32 in tensor memory), softmax by the four warps that own
-// the 128 lanes of S (a thread per row), P as fp16 over the same tensor memory
-// columns, O += P V with P read from tensor memory.  Two such streams
-// alternate, so that one's softmax runs under the other's products: two row
-// tiles on the same key tiles, or (items of at most 128 rows) the same row
-// tile on alternate key tiles, joined at the end.
-//   warps 0-3, 4-7  softmax of streams 0 and 1, queries in, results out; the
-//                   first warp of each issues its stream's products
+// A CTA.  Per step (128 rows, half a key tile of 64 tokens): S = Q K^T (fp16
+// operands in shared memory, fp32 in tensor memory), softmax by the four warps
+// that own the 128 lanes of S (a thread per row), P as fp16 over the same
+// tensor memory columns, O += P V with P read from tensor memory.  Two such
+// streams of steps alternate: two row tiles on the same key tiles, or (items of
+// at most 128 rows) the two halves of the key tiles, joined at the end.  Each
+// stream has two buffers of scores, so a softmax does not wait for the products
+// around it: with steps of 128 tokens and one buffer, a step's chain of score
+// product, softmax and value product (about 5000 cycles) set the pace.
+//   warps 0-3, 4-7  softmax of streams 0 and 1, queries in, results out
 //   warps 8-11      keys: one 32-token block each, codes -> fp16 tile
 //   warps 12-15     values, the same
+//   warp 16         issues the products (17-19 idle)
 // The running maximum of a row moves only when a score is more than 8 (in log2)
 // above it, so the accumulator is rescaled rarely; weights stay below 2^8.
 //
@@ -44,23 +46,17 @@ namespace kvq {
 namespace chunk {
 
 constexpr int kTile = 128;                  // tokens of a key / value tile, rows of a product
+constexpr int kStep = 64;                   // tokens of a step
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;  // 64 elements of the contiguous axis
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 8;
-constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps);
-// Registers a thread: at launch, then by role: softmax holds a row's 128
-// scores, a loading warp four parts of a block (those of 1 and 8 bits are the
-// largest).  Together the roles have what the launch got.
-constexpr int kRegsLaunch = 128;
-template <int BK, int BV>
-constexpr int regs_load() {
-  return BK == 1 || BV == 1 || BK == 8 || BV == 8 ? 112 : 96;
-}
-template <int BK, int BV>
-constexpr int regs_softmax() {
-  return 2 * kRegsLaunch - regs_load<BK, BV>();
-}
-static_assert(kSoftmaxWarps == kLoadWarps, "the two shares are of equal size");
+constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps + 4);
+// Registers a thread: at launch, then by role.  The shares must not exceed what
+// the launch got.
+constexpr int kRegsLaunch = 96, kRegsSoftmax = 104, kRegsLoad = 112, kRegsIssue = 48;
+static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kLoadWarps * kRegsLoad + 4 * kRegsIssue) <=
+                  kThreads * kRegsLaunch,
+              "register shares exceed the launch's");
 constexpr uint32_t kWaitLimit = 2000000000u;  // cycles of a bounded wait (~1 s)
 constexpr int kAhead = 2;  // blocks behind the next whose table entry (and L2 copy) is on its way
 constexpr float kRescaleLog2 = 8.0f;
@@ -69,8 +65,9 @@ struct Smem {
   unsigned char q[2][kTileBytes];
   unsigned char k[2][kTileBytes];
   unsigned char v[2][kTileBytes];
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_full[2], q_full;
-  uint64_t meet, drained[2];
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t s_full[2][2], p_ready[2][2], o_done[2][2], o_full[2];  // [stream][buffer], [stream]
+  uint64_t q_full, meet, drained;
   int scan[32];
   int start_seq, start_tile, start_head, start_step;
   uint32_t tmem;
@@ -166,7 +163,7 @@ __device__ __forceinline__ void tc_commit(uint32_t leader, uint64_t* b) {
       : "memory");
 }
 
-// D[128 x 128] (+)= A B, fp16 in, fp32 out, K = 16, by the warp's elected lane
+// D[128 x N] (+)= A B, fp16 in, fp32 out, K = 16, by the warp's elected lane
 // (`leader`); all lanes run it, so that the descriptors stay uniform.
 // A in shared memory.
 __device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b,
@@ -297,9 +294,9 @@ __device__ __forceinline__ uint32_t step_major_k(int ks) {
 }
 __device__ __forceinline__ uint32_t step_major_mn(int ks) { return (ks * 2048) >> 4; }
 
-// fp32 accumulator, fp16 operands, M = N = 128; b_mn: B's contiguous axis is N.
-__host__ __device__ constexpr uint32_t instr_desc(bool b_mn) {
-  return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+// fp32 accumulator, fp16 operands, M = 128; b_mn: B's contiguous axis is N.
+__host__ __device__ constexpr uint32_t instr_desc(bool b_mn, int n) {
+  return (1u << 4) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
 // ---------------------------------------------------------------------------
@@ -703,25 +700,73 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
 
 constexpr uint32_t kColS = 0, kColO = 256;  // tensor memory columns: S0 S1 O0 O1, 128 each
 
-// Scores of a row tile: S = Q K^T.
-template <int BK>
-__device__ __forceinline__ void issue_scores(uint32_t leader, uint32_t ts, const unsigned char* q,
-                                             const unsigned char* k) {
-  const uint64_t a = tile_desc(sptr(q), false), b = tile_desc(sptr(k), BK != 1);
+template <int BK, int BV>
+__device__ __forceinline__ void issue_role(const Params& p, Smem& s, int u0, int u1) {
+  constexpr uint32_t kIdS = instr_desc(BK != 1, kStep), kIdO = instr_desc(BV != 1, kHeadDim);
+  // where the second half of a tile's tokens begins
+  constexpr int kHalfK = BK == 1 ? kStep * 128 : kHalfBytes;
+  constexpr int kHalfV = BV == 1 ? kHalfBytes : kStep * 128;
+  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0), leader = elect_lane();
+  const int two = p.streams_rows;  // a half serves a step of either stream
+  uint32_t nk = 0, nv = 0, ns = 0, items = 0;  // tiles, steps (of a stream) and items done
+  Walk w;
+  w.begin(s, u0, u1);
+#pragma unroll 1
+  for (; w.next(p); w.advance(p), ++items) {
+    const int steps = (w.i1 - w.i0) << (1 + two);  // of both streams
+    if (!warp_wait(s, &s.q_full, items & 1)) return;
+    tc_after();
+    // step st: stream st mod 2; scores run four steps (two a stream) ahead
+#pragma unroll 1
+    for (int st = -4; st < steps; ++st) {
+      // stream, its step (counted over all items), its buffer (four steps on: the same)
+      const int x = st & 1;
+      const uint32_t k = ns + (st >> 1), b = k & 1;
+      const int half = two ? b : x;  // with two row tiles an item has an even number
+      const bool begins = x == 0 && (!two || b == 0), ends = x == 1 && (!two || b == 1);
+      const uint32_t ts = tm + kColS + 128 * x + kStep * b;
+      if (st >= 0) {
+        const int buf = nv & 1;
+        if (!warp_wait(s, &s.p_ready[x][b], (k >> 1) & 1)) return;
+        if (begins && !warp_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
+        tc_after();
+        const uint64_t v = tile_desc(sptr(s.v[buf]) + half * kHalfV, BV != 1);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks)
-    mma_ss(leader, ts, a + step_major_k(ks), b + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)),
-           instr_desc(BK != 1), ks > 0);
-}
-// Weights times values: O (+)= P V, P in the columns of S.
-template <int BV>
-__device__ __forceinline__ void issue_values(uint32_t leader, uint32_t to, uint32_t ts,
-                                             const unsigned char* v, bool add) {
-  const uint64_t b = tile_desc(sptr(v), BV != 1);
+        for (int ks = 0; ks < kStep / 16; ++ks)
+          mma_ts(leader, tm + kColO + 128 * x, ts + 8 * ks,
+                 v + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 1 || ks > 0);
+        // o_done has a phase for every second step, like p_ready: who rescales at
+        // step k knows that the product of step k - 3 is in and that of k + 1 has
+        // not begun, so a parity tells whether that of k - 1 is.  At an item's end
+        // a stream may be two products behind; o_full has a phase an item.
+        tc_commit(leader, &s.o_done[x][b]);
+        if (st + 2 >= steps) tc_commit(leader, &s.o_full[x]);
+        if (ends) {
+          tc_commit(leader, &s.v_empty[buf]);
+          ++nv;
+        }
+      }
+      if (st + 4 < steps) {
+        const int buf = nk & 1;
+        if (begins) {
+          if (!warp_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return;
+          tc_after();
+        }
+        const uint64_t q = tile_desc(sptr(s.q[two ? x : 0]), false),
+                       kd = tile_desc(sptr(s.k[buf]) + half * kHalfK, BK != 1);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks)
-    mma_ts(leader, to, ts + 8 * ks, b + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)),
-           instr_desc(BV != 1), add || ks > 0);
+        for (int ks = 0; ks < kHeadDim / 16; ++ks)
+          mma_ss(leader, ts, q + step_major_k(ks),
+                 kd + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdS, ks > 0);
+        tc_commit(leader, &s.s_full[x][b]);
+        if (ends) {
+          tc_commit(leader, &s.k_empty[buf]);
+          ++nk;
+        }
+      }
+    }
+    ns += steps >> 1;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -770,7 +815,7 @@ __device__ __forceinline__ void load_queries(const Params& p, const Walk& w, int
 // tensor memory by a short loop to keep the code of the others small.
 __device__ __forceinline__ void mask_row(uint32_t ts, int hi, int lo, int sink) {
 #pragma unroll 1
-  for (int c = 0; c < 128; c += 32) {
+  for (int c = 0; c < kStep; c += 32) {
     uint32_t r[32];
     tm_load32(ts + c, r);
     tm_load_wait();
@@ -784,67 +829,17 @@ __device__ __forceinline__ void mask_row(uint32_t ts, int hi, int lo, int sink) 
   tm_store_wait();
 }
 
-// One step of a stream's softmax for a row (a thread); `first`: no accumulator
-// yet.  All 128 scores are read at once and stay in registers (a read takes
-// several hundred cycles beside the products).
-__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sl2, bool first,
-                                             Row& row) {
-  uint32_t r[4][32];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) tm_load32(ts + 32 * c, r[c]);
-  tm_load_wait();
-  float mc[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    mc[c] = __uint_as_float(r[c][0]);
-#pragma unroll
-    for (int n = 1; n < 31; n += 2)
-      mc[c] = fmaxf(fmaxf(mc[c], __uint_as_float(r[c][n])), __uint_as_float(r[c][n + 1]));
-    mc[c] = fmaxf(mc[c], __uint_as_float(r[c][31]));
-  }
-  const float mx = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])) * sl2;
-  if (first) {
-    row.m = mx;
-    row.l = 0.0f;
-  } else {
-    const bool up = mx > row.m + kRescaleLog2;
-    if (__any_sync(0xffffffffu, up)) {
-      const float f = up ? exp2_fast(row.m - mx) : 1.0f;
-      if (up) row.m = mx;
-      row.l *= f;
+// Multiply the thread's row of the accumulator by f.
+__device__ __forceinline__ void rescale_row(uint32_t to, float f) {
 #pragma unroll 1
-      for (int c = 0; c < 16; ++c) {
-        uint32_t o[8];
-        tm_load8(to + 8 * c, o);
-        tm_load_wait();
+  for (int c = 0; c < kHeadDim; c += 8) {
+    uint32_t o[8];
+    tm_load8(to + c, o);
+    tm_load_wait();
 #pragma unroll
-        for (int n = 0; n < 8; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
-        tm_store8(to + 8 * c, o);
-      }
-    }
+    for (int n = 0; n < 8; ++n) o[n] = __float_as_uint(__uint_as_float(o[n]) * f);
+    tm_store8(to + c, o);
   }
-  const float off = row.m == -INFINITY ? 0.0f : -row.m;
-  const uint64_t sl = pair(sl2, sl2), of = pair(off, off);
-  uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    uint32_t w[16];
-#pragma unroll
-    for (int n = 0; n < 16; ++n) {
-      float a, b;
-      unpair(fma2(pair(__uint_as_float(r[c][2 * n]), __uint_as_float(r[c][2 * n + 1])), sl, of), a,
-             b);
-      a = exp2_fast(a);
-      b = exp2_fast(b);
-      sum[n & 1] = add2(sum[n & 1], pair(a, b));
-      w[n] = pack_half2(a, b);
-    }
-    tm_store16(ts + 16 * c, w);
-  }
-  float a, b;
-  unpair(add2(sum[0], sum[1]), a, b);
-  row.l += a + b;
-  tm_store_wait();
 }
 
 // Results leave through shared memory (the queries' tile, no longer read): each
@@ -940,17 +935,16 @@ __device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk&
   return true;
 }
 
-template <int BK, int BV>
+template <int BK>
 __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, int u1,
                                              const Shares& shares) {
   const int warp = threadIdx.x >> 5, x = warp >> 2, lane_row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // 32 lanes a warp, in bits 16 up
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0) + 128 * x;
   const uint32_t ts = tm + lanes + kColS, to = tm + lanes + kColO;
-  const bool issuer = (warp & 3) == 0;  // of its stream's products
-  const uint32_t leader = elect_lane();
   const int two = p.streams_rows, tr = kTile << two, rows = p.c.n_q * p.d.gq;
-  uint32_t ns = 0, np = 0, no[2] = {0, 0}, met = 0, items = 0, nt = 0;  // nt: tiles of the items before
+  uint32_t ns = 0, met = 0, items = 0;  // steps of the stream, meetings, items so far
+  const float sl2 = p.c.scale_log2;
   Walk w;
   w.begin(s, u0, u1);
   for (; w.next(p); w.advance(p)) {
@@ -966,61 +960,80 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
     }
     const bool live = __any_sync(0xffffffffu, valid);
     Row row{-INFINITY, 0.0f};
-    const int n = w.i1 - w.i0;
-    const int steps = two ? n : (n - x + 1) >> 1;
-    if (issuer && !warp_wait(s, &s.q_full, items & 1)) return;
-    ++items;
-    // step -1 only issues the first scores
+    const int steps = (w.i1 - w.i0) << two;
 #pragma unroll 1
-    for (int st = -1; st < steps; ++st) {
-      const int i = two ? st : 2 * st + x;  // tile of the share
-      if (st >= 0) {
-        if (!warp_wait(s, &s.s_full[x], ns++ & 1)) return;
-        tc_after();
-        if (live) {
-          const int t0 = w.s.tile(w.i0 + i) * kTile;
-          // every token of the tile is seen by every row of the item
-          const bool whole = w.s.p0 >= t0 + kTile - 1 &&
-                             (!p.c.window || t0 > w.s.p1 - p.c.window || t0 + kTile <= p.c.sinks);
-          if (!whole)
-            mask_row(ts, (valid ? pos : -1) - t0, p.c.window ? pos - p.c.window - t0 : -1 - t0,
-                     p.c.sinks - t0);
-          softmax_step(ts, to, p.c.scale_log2, st == 0, row);
+    for (int st = 0; st < steps; ++st, ++ns) {
+      const int b = ns & 1;
+      const uint32_t sb = ts + kStep * b;
+      if (!warp_wait(s, &s.s_full[x][b], (ns >> 1) & 1)) return;
+      tc_after();
+      if (live) {
+        const int t0 = w.s.tile(w.i0 + (st >> two)) * kTile + kStep * (two ? st & 1 : x);
+        // every token of the step is seen by every row of the item
+        const bool whole = w.s.p0 >= t0 + kStep - 1 &&
+                           (!p.c.window || t0 > w.s.p1 - p.c.window || t0 + kStep <= p.c.sinks);
+        if (!whole)
+          mask_row(sb, (valid ? pos : -1) - t0, p.c.window ? pos - p.c.window - t0 : -1 - t0,
+                   p.c.sinks - t0);
+        uint32_t r[2][32];
+        tm_load32(sb, r[0]);
+        tm_load32(sb + 32, r[1]);
+        tm_load_wait();
+        float mc[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t* y = &r[c >> 1][16 * (c & 1)];
+          mc[c] = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+#pragma unroll
+          for (int n = 2; n < 16; n += 2)
+            mc[c] = fmaxf(fmaxf(mc[c], __uint_as_float(y[n])), __uint_as_float(y[n + 1]));
         }
-        tc_before();
-        warp_arrive(&s.p_ready[x]);
+        const float mx = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])) * sl2;
+        if (st == 0) {
+          row.m = mx;
+        } else {
+          const bool up = mx > row.m + kRescaleLog2;
+          if (__any_sync(0xffffffffu, up)) {
+            const float f = up ? exp2_fast(row.m - mx) : 1.0f;
+            if (up) row.m = mx;
+            row.l *= f;
+            // the product before this step's has to be in
+            if (!warp_wait(s, &s.o_done[x][b ^ 1], ((ns - 1) >> 1) & 1)) return;
+            tc_after();
+            rescale_row(to, f);
+          }
+        }
+        const float off = row.m == -INFINITY ? 0.0f : -row.m;
+        const uint64_t sl = pair(sl2, sl2), of = pair(off, off);
+        uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t h[16];
+#pragma unroll
+          for (int n = 0; n < 16; ++n) {
+            float y0, y1;
+            unpair(fma2(pair(__uint_as_float(r[c][2 * n]), __uint_as_float(r[c][2 * n + 1])), sl,
+                        of),
+                   y0, y1);
+            y0 = exp2_fast(y0);
+            y1 = exp2_fast(y1);
+            sum[n & 1] = add2(sum[n & 1], pair(y0, y1));
+            h[n] = pack_half2(y0, y1);
+          }
+          tm_store16(sb + 16 * c, h);
+        }
+        float y0, y1;
+        unpair(add2(sum[0], sum[1]), y0, y1);
+        row.l += y0 + y1;
+        tm_store_wait();
       }
-      if (!issuer) continue;
-      if (st >= 0) {
-        const uint32_t t = nt + i, buf = t & 1;
-        if (!warp_wait(s, &s.p_ready[x], np++ & 1)) return;
-        if (!warp_wait(s, &s.v_full[buf], (t >> 1) & 1)) return;
-        tc_after();
-        issue_values<BV>(leader, tm + kColO, tm + kColS, s.v[buf], st > 0);
-        tc_commit(leader, &s.v_empty[buf]);
-        if (st + 1 == steps) tc_commit(leader, &s.o_full[x]);
-      }
-      if (st + 1 < steps) {
-        const uint32_t t = nt + (two ? st + 1 : 2 * st + 2 + x), buf = t & 1;
-        if (!warp_wait(s, &s.k_full[buf], (t >> 1) & 1)) return;
-        tc_after();
-        issue_scores<BK>(leader, tm + kColS, s.q[two ? x : 0], s.k[buf]);
-        tc_commit(leader, &s.s_full[x]);
-        tc_commit(leader, &s.k_empty[buf]);
-      }
+      tc_before();
+      warp_arrive(&s.p_ready[x][b]);
     }
-    nt += n;
-    // both accumulators complete (a stream without a step has none)
-    const bool has1 = two || n > 1;
-    if (x == 0 || two) {
-      if (!warp_wait(s, &s.o_full[x], no[x] & 1)) return;
-    }
-    if (!two && x == 0 && has1 && !warp_wait(s, &s.o_full[1], no[1] & 1)) return;
-    if (two) ++no[x];
-    else {
-      ++no[0];
-      if (has1) ++no[1];
-    }
+    // the accumulator is complete; items of one row tile need both streams'
+    if (!warp_wait(s, &s.o_full[x], items & 1)) return;
+    if (!two && x == 0 && !warp_wait(s, &s.o_full[1], items & 1)) return;
+    ++items;
     tc_after();
     if (!two && x == 1) {
       s.m[lane_row] = row.m;
@@ -1031,7 +1044,7 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
     const int slot = 2 * blockIdx.x + (w.u == u0 ? 0 : 1);
     if ((two || x == 0) && live) {
       float f0 = 1.0f, f1 = 0.0f, m = row.m, l = row.l;
-      if (!two && has1) {
+      if (!two) {
         const float m1 = s.m[lane_row], l1 = s.l[lane_row];
         m = fmaxf(row.m, m1);
         if (m > -INFINITY) {
@@ -1053,7 +1066,7 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
         tm_load_wait();
 #pragma unroll
         for (int k = 0; k < 32; ++k) o[k] = __uint_as_float(r[k]) * f0;
-        if (!two && has1) {
+        if (!two) {
           tm_load32(to + 128 + 32 * c, r);
           tm_load_wait();
 #pragma unroll
@@ -1136,13 +1149,16 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     for (int i = 0; i < 2; ++i) {
       bar_init(&s.k_full[i], 4);
       bar_init(&s.v_full[i], 4);
-      bar_init(&s.k_empty[i], 1 << p.streams_rows);  // a commit of every stream that reads it
-      bar_init(&s.v_empty[i], 1 << p.streams_rows);
-      bar_init(&s.drained[i], 1);
-      bar_init(&s.s_full[i], 1);
-      bar_init(&s.p_ready[i], 4);
+      bar_init(&s.k_empty[i], 1);
+      bar_init(&s.v_empty[i], 1);
       bar_init(&s.o_full[i], 1);
+      for (int b = 0; b < 2; ++b) {
+        bar_init(&s.s_full[i][b], 1);
+        bar_init(&s.p_ready[i][b], 4);
+        bar_init(&s.o_done[i][b], 1);
+      }
     }
+    bar_init(&s.drained, 1);
     bar_init(&s.q_full, 4 << p.streams_rows);
     bar_init(&s.meet, kSoftmaxWarps);
     s.abort = 0;
@@ -1180,7 +1196,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       if (++tl == p.tiles) tl = 0, ++sq;
     }
   }
-  if (warp == kSoftmaxWarps) {
+  constexpr int kIssueWarp = kSoftmaxWarps + kLoadWarps;
+  if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
                      sptr(&s.tmem))
                  : "memory");
@@ -1192,30 +1209,36 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(&s.tmem);
 
   if (warp < kSoftmaxWarps) {
-    regs_up<regs_softmax<BK, BV>()>();
-    softmax_role<BK, BV>(p, s, u0, u1, shares);
-    if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort)) && (warp & 3) == 0) {
-      // products in flight end before the tile memory is given back
-      uint64_t* drained = &s.drained[warp >> 2];
-      tc_commit(elect_lane(), drained);
-      const uint32_t t0 = (uint32_t)clock();
-      while (!bar_try(drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
-      }
-      if (lane == 0)
-        atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
-    }
+    regs_up<kRegsSoftmax>();
+    softmax_role<BK>(p, s, u0, u1, shares);
     __syncwarp();
-  } else {
-    regs_down<regs_load<BK, BV>()>();
+  } else if (warp < kIssueWarp) {
+    regs_up<kRegsLoad>();
     const bool key = warp < kSoftmaxWarps + 4;
     if constexpr (BK == BV) load_role<BK>(p, s, u0, u1, warp & 3, key);
     else if (key) load_role<BK>(p, s, u0, u1, warp & 3, true);
     else load_role<BV>(p, s, u0, u1, warp & 3, false);
+    __syncwarp();
+  } else {
+    regs_down<kRegsIssue>();
+    if (warp == kIssueWarp) {
+      issue_role<BK, BV>(p, s, u0, u1);
+      if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort))) {
+        // products in flight end before the tile memory is given back
+        tc_commit(elect_lane(), &s.drained);
+        const uint32_t t0 = (uint32_t)clock();
+        while (!bar_try(&s.drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
+        }
+        if (lane == 0)
+          atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
+      }
+      __syncwarp();
+    }
   }
   tc_before();
   __syncthreads();
   tc_after();
-  if (warp == kSoftmaxWarps)
+  if (warp == kIssueWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
