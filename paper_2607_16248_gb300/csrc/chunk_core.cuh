@@ -51,12 +51,20 @@ constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kHalfBytes = kTileBytes / 2;  // 64 elements of the contiguous axis
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 8;
 constexpr int kThreads = 32 * (kSoftmaxWarps + kLoadWarps + 4);
-// Registers a thread: at launch, then by role.  The shares must not exceed what
-// the launch got.
-constexpr int kRegsLaunch = 96, kRegsSoftmax = 104, kRegsLoad = 112, kRegsIssue = 48;
-static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kLoadWarps * kRegsLoad + 4 * kRegsIssue) <=
-                  kThreads * kRegsLaunch,
-              "register shares exceed the launch's");
+// Registers a thread: at launch, then by role.  The loading warps' parts of 1 and
+// 8 bits are the largest.  The shares must not exceed what the launch got.
+constexpr int kRegsLaunch = 96, kRegsIssue = 48;
+template <int BK, int BV>
+struct Regs {
+  static constexpr int kLoad = BK == 1 || BV == 1 || BK == 8 || BV == 8 ? 112 : 96;
+  static constexpr int kSoftmax = 216 - kLoad;
+  static_assert(32 * (kSoftmaxWarps * kSoftmax + kLoadWarps * kLoad + 4 * kRegsIssue) <=
+                    kThreads * kRegsLaunch,
+                "register shares exceed the launch's");
+};
+// Fixed cost of an item in units (a unit is a 128-token tile): queries in, results
+// out, the first tile's way through the pipeline.
+constexpr int kItemCost = 3;
 constexpr uint32_t kWaitLimit = 2000000000u;  // cycles of a bounded wait (~1 s)
 constexpr int kAhead = 2;  // blocks behind the next whose table entry (and L2 copy) is on its way
 constexpr float kRescaleLog2 = 8.0f;
@@ -65,10 +73,12 @@ struct Smem {
   unsigned char q[2][kTileBytes];
   unsigned char k[2][kTileBytes];
   unsigned char v[2][kTileBytes];
+  unsigned char stage[kSoftmaxWarps][32 * 64];  // results on their way out
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t s_full[2][2], p_ready[2][2], o_done[2][2], o_full[2];  // [stream][buffer], [stream]
   uint64_t q_full, meet, drained;
   int scan[32];
+  int walk[kSoftmaxWarps][2][16];      // a softmax warp's item and the next one (Walk)
   int start_seq, start_tile, start_head, start_step;
   uint32_t tmem;
   int abort, last;
@@ -223,6 +233,15 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16
       "r"(addr)
       : "memory");
 }
+__device__ __forceinline__ void tm_load16(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
 __device__ __forceinline__ void tm_load8(uint32_t addr, uint32_t (&r)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
@@ -347,29 +366,31 @@ struct Shares {
 // kv-head); every role walks them.
 struct Walk {
   int u, end, base;        // next unit, end of the share, first unit of the item
-  int bl, row_tile, head, step;
+  int bl, row_tile, head;
   Span s;
-  int i0, i1;              // the item's units in this share
+  int i0, i1;              // the item's tiles in this share
   __device__ __forceinline__ void begin(const Smem& sm, int u0, int u1) {
     u = u0;
     end = u1;
     bl = sm.start_seq;
     row_tile = sm.start_tile;
     head = sm.start_head;
-    step = sm.start_step;
-    base = u0 - step;
+    base = u0 - sm.start_step;
   }
   __device__ __forceinline__ bool next(const Params& p) {
-    if (u >= end) return false;
-    s = span_of(p, bl, row_tile);
-    i0 = step;
-    i1 = min(s.n, step + (end - u));
-    return true;
+    while (u < end) {
+      s = span_of(p, bl, row_tile);
+      const int local = u - base, stop = min(s.n + kItemCost, local + end - u);
+      i0 = max(local - kItemCost, 0);
+      i1 = stop - kItemCost;
+      if (i1 > i0) return true;
+      advance(p);  // nothing but a piece of the item's fixed cost
+    }
+    return false;
   }
   __device__ __forceinline__ void advance(const Params& p) {
-    u += i1 - i0;
-    base += s.n;
-    step = 0;
+    base += s.n + kItemCost;
+    u = min(base, end);
     if (++head == p.d.hkv) {
       head = 0;
       if (++row_tile == p.tiles) {
@@ -379,6 +400,8 @@ struct Walk {
     }
   }
 };
+
+static_assert(sizeof(Walk) <= sizeof(Smem::walk[0][0]), "an item's walk fits its place");
 
 // ---------------------------------------------------------------------------
 // Codes to fp16 tiles
@@ -842,32 +865,31 @@ __device__ __forceinline__ void rescale_row(uint32_t to, float f) {
   }
 }
 
-// Results leave through shared memory (the queries' tile, no longer read): each
-// lane writes 256 bytes of its own row to the warp's 32 x 256 byte area, then 16
-// lanes copy a row to memory.  Chunk m of a row is at m ^ (row mod 8).
-__device__ __forceinline__ uint32_t stage_at(int row, int m) {
-  return row * 256 + ((m ^ (row & 7)) << 4);
-}
-// 32 accumulator columns (run order) in channel order: fp16 or fp32.
-__device__ __forceinline__ void stage_half(unsigned char* area, int c, const float (&o)[32]) {
+// Results leave through shared memory, 64 bytes a row at a time: each lane
+// writes its own row, then four lanes copy a row to memory.  Chunk m of row r is
+// at m ^ (r / 2 mod 4), so neither side meets a bank twice.
+struct Rows {
+  char* at[4];  // rows lane / 4 + 8 k, this lane's 16 bytes; nullptr past the end
+};
+template <int N>
+__device__ __forceinline__ void stage_row(unsigned char* stage, int first, const uint4 (&v)[N]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const float* x = o + 8 * g;
-    st16(area, stage_at(lane, 4 * c + g),
-         make_uint4(pack_half2(x[0], x[2]), pack_half2(x[4], x[6]), pack_half2(x[1], x[3]),
-                    pack_half2(x[5], x[7])));
-  }
+  for (int m = 0; m < N; ++m)
+    st16(stage, lane * 64 + (((first + m) ^ ((lane >> 1) & 3)) << 4), v[m]);
 }
-__device__ __forceinline__ void stage_float(unsigned char* area, int c, const float (&o)[32]) {
+__device__ __forceinline__ void put_rows(const unsigned char* stage, const Rows& rows,
+                                         int offset) {
   const int lane = threadIdx.x & 31;
+  __syncwarp();
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const uint32_t* x = reinterpret_cast<const uint32_t*>(o + 8 * g);
-    const int m = 8 * (c & 1) + 2 * g;
-    st16(area, stage_at(lane, m), make_uint4(x[0], x[2], x[4], x[6]));
-    st16(area, stage_at(lane, m + 1), make_uint4(x[1], x[3], x[5], x[7]));
+  for (int k = 0; k < 4; ++k) {
+    const int r = (lane >> 2) + 8 * k;
+    const uint4 x = *reinterpret_cast<const uint4*>(
+        stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+    if (rows.at[k]) *reinterpret_cast<uint4*>(rows.at[k] + offset) = x;
   }
+  __syncwarp();
 }
 
 // The partials of CTAs c0 .. c1 to results, by all softmax threads: first each
@@ -945,20 +967,34 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
   const int two = p.streams_rows, tr = kTile << two, rows = p.c.n_q * p.d.gq;
   uint32_t ns = 0, met = 0, items = 0;  // steps of the stream, meetings, items so far
   const float sl2 = p.c.scale_log2;
-  Walk w;
-  w.begin(s, u0, u1);
-  for (; w.next(p); w.advance(p)) {
-    const int tile = w.row_tile;
+  const auto queries = [&](const Walk& w) {
+    const int r0 = w.row_tile * tr + (two ? kTile * x : 0) + (lane_row & ~31);
+    load_queries<BK>(p, w, r0, s.q[x], lane_row & ~31);
+    fence_async();
+    warp_arrive(&s.q_full);
+  };
+  // The item and the next one are kept in shared memory: their fields would take
+  // registers from the scores.
+  const auto walk = [&](uint32_t i) -> Walk& {
+    return *reinterpret_cast<Walk*>(s.walk[warp][i & 1]);
+  };
+  bool more;
+  {
+    Walk first;
+    first.begin(s, u0, u1);
+    more = first.next(p);
+    walk(0) = first;
+    __syncwarp();
+    if (more && (two || x == 0)) queries(first);
+  }
+#pragma unroll 1
+  while (more) {
+    const Walk& w = walk(items);
     const int tr_row = (two ? kTile * x : 0) + lane_row;  // row in the item
-    const int g = tile * tr + tr_row, g_warp = g - (threadIdx.x & 31);
+    const int g = w.row_tile * tr + tr_row, g_warp = g - (threadIdx.x & 31);
     const bool valid = g < rows;
+    const bool live = g_warp < rows;  // the warp has a row
     const int pos = w.s.L - p.c.n_q + token_of_row(p, g);
-    if (two || x == 0) {
-      load_queries<BK>(p, w, g_warp, s.q[x], lane_row & ~31);
-      fence_async();
-      warp_arrive(&s.q_full);
-    }
-    const bool live = __any_sync(0xffffffffu, valid);
     Row row{-INFINITY, 0.0f};
     const int steps = (w.i1 - w.i0) << two;
 #pragma unroll 1
@@ -1005,7 +1041,7 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
         }
         const float off = row.m == -INFINITY ? 0.0f : -row.m;
         const uint64_t sl = pair(sl2, sl2), of = pair(off, off);
-        uint64_t sum[2] = {0ull, 0ull};
+        uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           uint32_t h[16];
@@ -1017,23 +1053,35 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
                    y0, y1);
             y0 = exp2_fast(y0);
             y1 = exp2_fast(y1);
-            sum[n & 1] = add2(sum[n & 1], pair(y0, y1));
+            acc[n & 1] = add2(acc[n & 1], pair(y0, y1));
             h[n] = pack_half2(y0, y1);
           }
           tm_store16(sb + 16 * c, h);
         }
         float y0, y1;
-        unpair(add2(sum[0], sum[1]), y0, y1);
+        unpair(add2(acc[0], acc[1]), y0, y1);
         row.l += y0 + y1;
         tm_store_wait();
       }
       tc_before();
       warp_arrive(&s.p_ready[x][b]);
     }
+    // The next item's queries: all scores of this one are done (an item of one
+    // row tile has the other stream's too).
+    {
+      Walk next = w;
+      next.advance(p);
+      more = next.next(p);
+      walk(items + 1) = next;
+      __syncwarp();
+      if (more && (two || x == 0)) {
+        if (!two && !warp_wait(s, &s.s_full[1][(ns - 1) & 1], ((ns - 1) >> 1) & 1)) return;
+        queries(next);
+      }
+    }
     // the accumulator is complete; items of one row tile need both streams'
     if (!warp_wait(s, &s.o_full[x], items & 1)) return;
     if (!two && x == 0 && !warp_wait(s, &s.o_full[1], items & 1)) return;
-    ++items;
     tc_after();
     if (!two && x == 1) {
       s.m[lane_row] = row.m;
@@ -1041,7 +1089,6 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
     }
     if (!two && !meet_softmax(s, met)) return;
     const bool direct = w.i0 == 0 && w.i1 == w.s.n;
-    const int slot = 2 * blockIdx.x + (w.u == u0 ? 0 : 1);
     if ((two || x == 0) && live) {
       float f0 = 1.0f, f1 = 0.0f, m = row.m, l = row.l;
       if (!two) {
@@ -1056,41 +1103,54 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
       const float scale = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
       f0 *= scale;
       f1 *= scale;
-      const long long pr = (long long)slot * tr + tr_row;
-      unsigned char* area = s.q[x] + (lane_row & ~31) * 256;
+      // slot 0 of a CTA: the item its share begins in
+      const int pr = (2 * blockIdx.x + (u0 < w.base ? 1 : 0)) * tr + tr_row;
+      const int lane = threadIdx.x & 31;
+      Rows at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = (lane >> 2) + 8 * k;
+        char* row_at =
+            direct ? reinterpret_cast<char*>(
+                         p.out + row_offset(p, p.c.out_stride, w.bl, w.head, g_warp + r))
+                   : reinterpret_cast<char*>(p.part_o + (long long)(pr - lane + r) * kHeadDim);
+        at.at[k] = g_warp + r < rows ? row_at + 16 * (lane & 3) : nullptr;
+      }
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        uint32_t r[32];
-        float o[32];
-        tm_load32(to + 32 * c, r);
+      for (int c = 0; c < kHeadDim; c += 16) {
+        uint32_t r[16];
+        float o[16];
+        tm_load16(to + c, r);
         tm_load_wait();
 #pragma unroll
-        for (int k = 0; k < 32; ++k) o[k] = __uint_as_float(r[k]) * f0;
+        for (int k = 0; k < 16; ++k) o[k] = __uint_as_float(r[k]) * f0;
         if (!two) {
-          tm_load32(to + 128 + 32 * c, r);
+          tm_load16(to + 128 + c, r);
           tm_load_wait();
 #pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] = fmaf(__uint_as_float(r[k]), f1, o[k]);
+          for (int k = 0; k < 16; ++k) o[k] = fmaf(__uint_as_float(r[k]), f1, o[k]);
         }
-        if (direct) stage_half(area, c, o);
-        else stage_float(area, c, o);
-        if (c == 3 || (!direct && c == 1)) {  // 256 bytes of every row
-          __syncwarp();
-          const int lane = threadIdx.x & 31, m = lane & 15;
-#pragma unroll 4
-          for (int k = 0; k < 32; k += 2) {
-            const int rr = k + (lane >> 4);
-            if (g_warp + rr < rows) {
-              const uint4 v = *reinterpret_cast<const uint4*>(area + stage_at(rr, m));
-              if (direct)
-                *reinterpret_cast<uint4*>(
-                    p.out + row_offset(p, p.c.out_stride, w.bl, w.head, g_warp + rr) + 8 * m) = v;
-              else
-                *reinterpret_cast<uint4*>(p.part_o + (pr - lane + rr) * kHeadDim + 64 * (c >> 1) +
-                                          4 * m) = v;
-            }
+        // accumulator columns stand in the run order
+        if (direct) {
+          uint4 v[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float* y = o + 8 * k;
+            v[k] = make_uint4(pack_half2(y[0], y[2]), pack_half2(y[4], y[6]),
+                              pack_half2(y[1], y[3]), pack_half2(y[5], y[7]));
           }
-          __syncwarp();
+          stage_row<2>(s.stage[warp], (c >> 4) & 1 ? 2 : 0, v);
+          if ((c >> 4) & 1) put_rows(s.stage[warp], at, 2 * (c & ~31));
+        } else {
+          uint4 v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float* y = o + 8 * (k >> 1) + (k & 1);
+            v[k] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[2]), __float_as_uint(y[4]),
+                              __float_as_uint(y[6]));
+          }
+          stage_row<4>(s.stage[warp], 0, v);
+          put_rows(s.stage[warp], at, 4 * c);
         }
       }
       if (valid && !direct) p.part_ml[pr] = make_float2(m, l);
@@ -1099,7 +1159,8 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
     if (!direct) {
       // the last of the item's CTAs merges its partials, in the order of the
       // tokens
-      const int c0 = shares.owner(w.base), c1 = shares.owner(w.base + w.s.n - 1);
+      const int first = w.base + kItemCost;
+      const int c0 = shares.owner(first), c1 = shares.owner(first + w.s.n - 1);
       const int item = (w.bl * p.tiles + w.row_tile) * p.d.hkv + w.head;
       __threadfence();
       if (!meet_softmax(s, met)) return;
@@ -1114,6 +1175,7 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
       }
     }
     if (!meet_softmax(s, met)) return;  // s.m, s.last and both accumulators may be written again
+    ++items;
   }
 }
 
@@ -1135,7 +1197,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   int mine = 0;
 #pragma unroll 1
   for (int g = g0, sq = seq0, tl = tile0; g < g1; ++g) {
-    mine += span_of(p, sq, tl).n * p.d.hkv;
+    mine += (span_of(p, sq, tl).n + kItemCost) * p.d.hkv;
     if (++tl == p.tiles) tl = 0, ++sq;
   }
   int inc = mine;
@@ -1184,7 +1246,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   if (before <= u0 && u0 < before + mine) {
 #pragma unroll 1
     for (int at = before, sq = seq0, tl = tile0;;) {
-      const int n = span_of(p, sq, tl).n;
+      const int n = span_of(p, sq, tl).n + kItemCost;
       if (u0 < at + n * p.d.hkv) {
         s.start_seq = sq;
         s.start_tile = tl;
@@ -1209,11 +1271,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   const uint32_t tm = *reinterpret_cast<volatile uint32_t*>(&s.tmem);
 
   if (warp < kSoftmaxWarps) {
-    regs_up<kRegsSoftmax>();
+    regs_up<Regs<BK, BV>::kSoftmax>();
     softmax_role<BK>(p, s, u0, u1, shares);
     __syncwarp();
   } else if (warp < kIssueWarp) {
-    regs_up<kRegsLoad>();
+    regs_up<Regs<BK, BV>::kLoad>();
     const bool key = warp < kSoftmaxWarps + 4;
     if constexpr (BK == BV) load_role<BK>(p, s, u0, u1, warp & 3, key);
     else if (key) load_role<BK>(p, s, u0, u1, warp & 3, true);
