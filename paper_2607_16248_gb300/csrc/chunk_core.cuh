@@ -25,7 +25,7 @@
 //   warps 0-3, 4-7  softmax of streams 0 and 1, queries in, results out
 //   warps 8-11      keys: one 32-token block each, codes -> fp16 tile
 //   warps 12-15     values, the same
-//   warp 16         issues the products (17-19 idle)
+//   warps 16, 17    issue the products of streams 0 and 1 (18, 19 idle)
 // The running maximum of a row moves only when a score is more than 8 (in log2)
 // above it, so the accumulator is rescaled rarely; weights stay below 2^8.
 //
@@ -75,8 +75,8 @@ struct Smem {
   unsigned char v[2][kTileBytes];
   unsigned char stage[kSoftmaxWarps][32 * 64];  // results on their way out
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t s_full[2][2], p_ready[2][2], o_done[2][2], o_full[2];  // [stream][buffer], [stream]
-  uint64_t q_full, meet, drained;
+  uint64_t s_full[2][2], p_ready[2][2], o_last[2], o_full[2];  // [stream][buffer], [stream]
+  uint64_t q_full, meet, drained[2];
   int scan[32];
   int walk[kSoftmaxWarps][2][16];      // a softmax warp's item and the next one (Walk)
   int start_seq, start_tile, start_head, start_step;
@@ -232,15 +232,6 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t (&r)[16
       "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
       "r"(addr)
       : "memory");
-}
-__device__ __forceinline__ void tm_load16(uint32_t addr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
-      "%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
-      : "r"(addr));
 }
 __device__ __forceinline__ void tm_load8(uint32_t addr, uint32_t (&r)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -723,72 +714,64 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
 
 constexpr uint32_t kColS = 0, kColO = 256;  // tensor memory columns: S0 S1 O0 O1, 128 each
 
+// The products of stream x, by one warp (one for both streams took as long to
+// issue them as they take).
 template <int BK, int BV>
-__device__ __forceinline__ void issue_role(const Params& p, Smem& s, int u0, int u1) {
+__device__ __forceinline__ void issue_role(const Params& p, Smem& s, int u0, int u1, int x) {
   constexpr uint32_t kIdS = instr_desc(BK != 1, kStep), kIdO = instr_desc(BV != 1, kHeadDim);
   // where the second half of a tile's tokens begins
   constexpr int kHalfK = BK == 1 ? kStep * 128 : kHalfBytes;
   constexpr int kHalfV = BV == 1 ? kHalfBytes : kStep * 128;
-  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0), leader = elect_lane();
-  const int two = p.streams_rows;  // a half serves a step of either stream
-  uint32_t nk = 0, nv = 0, ns = 0, items = 0;  // tiles, steps (of a stream) and items done
+  const int two = p.streams_rows;  // two steps a tile (the stream takes both halves)
+  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0) + 128 * x, leader = elect_lane();
+  const uint64_t q = tile_desc(sptr(s.q[two ? x : 0]), false);
+  uint32_t nt = 0, ns = 0, items = 0;  // tiles, steps and items done
   Walk w;
   w.begin(s, u0, u1);
 #pragma unroll 1
   for (; w.next(p); w.advance(p), ++items) {
-    const int steps = (w.i1 - w.i0) << (1 + two);  // of both streams
+    const int steps = (w.i1 - w.i0) << two;
     if (!warp_wait(s, &s.q_full, items & 1)) return;
     tc_after();
-    // step st: stream st mod 2; scores run four steps (two a stream) ahead
+    // scores run two steps ahead
 #pragma unroll 1
-    for (int st = -4; st < steps; ++st) {
-      // stream, its step (counted over all items), its buffer (four steps on: the same)
-      const int x = st & 1;
-      const uint32_t k = ns + (st >> 1), b = k & 1;
-      const int half = two ? b : x;  // with two row tiles an item has an even number
-      const bool begins = x == 0 && (!two || b == 0), ends = x == 1 && (!two || b == 1);
-      const uint32_t ts = tm + kColS + 128 * x + kStep * b;
+    for (int st = -2; st < steps; ++st) {
+      const uint32_t k = ns + st, b = k & 1;  // the step counted over all items, its buffer
+      const uint32_t ts = tm + kColS + kStep * b;
       if (st >= 0) {
-        const int buf = nv & 1;
+        const uint32_t t = nt + (st >> two), buf = t & 1;
+        const int half = two ? st & 1 : x;
         if (!warp_wait(s, &s.p_ready[x][b], (k >> 1) & 1)) return;
-        if (begins && !warp_wait(s, &s.v_full[buf], (nv >> 1) & 1)) return;
+        if ((!two || half == 0) && !warp_wait(s, &s.v_full[buf], (t >> 1) & 1)) return;
         tc_after();
         const uint64_t v = tile_desc(sptr(s.v[buf]) + half * kHalfV, BV != 1);
 #pragma unroll
         for (int ks = 0; ks < kStep / 16; ++ks)
-          mma_ts(leader, tm + kColO + 128 * x, ts + 8 * ks,
-                 v + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 1 || ks > 0);
-        // o_done has a phase for every second step, like p_ready: who rescales at
-        // step k knows that the product of step k - 3 is in and that of k + 1 has
-        // not begun, so a parity tells whether that of k - 1 is.  At an item's end
-        // a stream may be two products behind; o_full has a phase an item.
-        tc_commit(leader, &s.o_done[x][b]);
-        if (st + 2 >= steps) tc_commit(leader, &s.o_full[x]);
-        if (ends) {
-          tc_commit(leader, &s.v_empty[buf]);
-          ++nv;
-        }
+          mma_ts(leader, tm + kColO, ts + 8 * ks,
+                 v + (BV == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdO, st > 0 || ks > 0);
+        if (!two || half == 1) tc_commit(leader, &s.v_empty[buf]);
+        // the last two products of an item tell that they are in; the others
+        // are when the scores issued behind them are
+        if (st + 2 >= steps) tc_commit(leader, st + 1 == steps ? &s.o_full[x] : &s.o_last[x]);
       }
-      if (st + 4 < steps) {
-        const int buf = nk & 1;
-        if (begins) {
-          if (!warp_wait(s, &s.k_full[buf], (nk >> 1) & 1)) return;
+      if (st + 2 < steps) {
+        const uint32_t t = nt + ((st + 2) >> two), buf = t & 1;
+        const int half = two ? st & 1 : x;
+        if (!two || half == 0) {
+          if (!warp_wait(s, &s.k_full[buf], (t >> 1) & 1)) return;
           tc_after();
         }
-        const uint64_t q = tile_desc(sptr(s.q[two ? x : 0]), false),
-                       kd = tile_desc(sptr(s.k[buf]) + half * kHalfK, BK != 1);
+        const uint64_t kd = tile_desc(sptr(s.k[buf]) + half * kHalfK, BK != 1);
 #pragma unroll
         for (int ks = 0; ks < kHeadDim / 16; ++ks)
           mma_ss(leader, ts, q + step_major_k(ks),
                  kd + (BK == 1 ? step_major_k(ks) : step_major_mn(ks)), kIdS, ks > 0);
         tc_commit(leader, &s.s_full[x][b]);
-        if (ends) {
-          tc_commit(leader, &s.k_empty[buf]);
-          ++nk;
-        }
+        if (!two || half == 1) tc_commit(leader, &s.k_empty[buf]);
       }
     }
-    ns += steps >> 1;
+    nt += w.i1 - w.i0;
+    ns += steps;
   }
 }
 
@@ -871,12 +854,10 @@ __device__ __forceinline__ void rescale_row(uint32_t to, float f) {
 struct Rows {
   char* at[4];  // rows lane / 4 + 8 k, this lane's 16 bytes; nullptr past the end
 };
-template <int N>
-__device__ __forceinline__ void stage_row(unsigned char* stage, int first, const uint4 (&v)[N]) {
+__device__ __forceinline__ void stage_row(unsigned char* stage, const uint4 (&v)[4]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int m = 0; m < N; ++m)
-    st16(stage, lane * 64 + (((first + m) ^ ((lane >> 1) & 3)) << 4), v[m]);
+  for (int m = 0; m < 4; ++m) st16(stage, lane * 64 + ((m ^ ((lane >> 1) & 3)) << 4), v[m]);
 }
 __device__ __forceinline__ void put_rows(const unsigned char* stage, const Rows& rows,
                                          int offset) {
@@ -932,27 +913,44 @@ __device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk&
     }
   }
   if (!meet_softmax(s, met)) return false;
+  // eight rows a warp, so that many loads are on their way
+  constexpr int kRows = 8;
   const int ch = 4 * (tid & 31);
-#pragma unroll 2
-  for (int r = tid >> 5; r < n_rows; r += kSoftmaxWarps) {
-    const float m = s.row_m[r], f = s.row_f[r];
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 1
+  for (int r0 = kRows * (tid >> 5); r0 < n_rows; r0 += kRows * kSoftmaxWarps) {
+    float4 o[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
     for (int c = c0; c <= c1; ++c) {
-      const long long pr = slot_of(c) + r;
-      const float2 ml = __ldcg(&p.part_ml[pr]);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + pr * kHeadDim + ch));
-      const float x = exp2_fast(ml.x - m);
-      if (ml.y > 0.0f) {
-        o.x = fmaf(v.x, x, o.x);
-        o.y = fmaf(v.y, x, o.y);
-        o.z = fmaf(v.z, x, o.z);
-        o.w = fmaf(v.w, x, o.w);
+      const long long first = slot_of(c);
+      float2 ml[kRows];
+      float4 v[kRows];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const long long pr = first + min(r0 + i, n_rows - 1);
+        ml[i] = __ldcg(&p.part_ml[pr]);
+        v[i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + pr * kHeadDim + ch));
+      }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        // a partial without a seen token counts nothing
+        const float x =
+            ml[i].y > 0.0f ? exp2_fast(ml[i].x - s.row_m[min(r0 + i, n_rows - 1)]) : 0.0f;
+        o[i].x = fmaf(v[i].x, x, o[i].x);
+        o[i].y = fmaf(v[i].y, x, o[i].y);
+        o[i].z = fmaf(v[i].z, x, o[i].z);
+        o[i].w = fmaf(v[i].w, x, o[i].w);
       }
     }
-    __half* dst = p.out + row_offset(p, p.c.out_stride, w.bl, w.head, tile * tr + r) + ch;
-    *reinterpret_cast<uint2*>(dst) =
-        make_uint2(pack_half2(o.x * f, o.y * f), pack_half2(o.z * f, o.w * f));
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      if (r0 + i >= n_rows) break;
+      const float f = s.row_f[r0 + i];
+      __half* dst = p.out + row_offset(p, p.c.out_stride, w.bl, w.head, tile * tr + r0 + i) + ch;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_half2(o[i].x * f, o[i].y * f),
+                                                  pack_half2(o[i].z * f, o[i].w * f));
+    }
   }
   return true;
 }
@@ -965,7 +963,8 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0) + 128 * x;
   const uint32_t ts = tm + lanes + kColS, to = tm + lanes + kColO;
   const int two = p.streams_rows, tr = kTile << two, rows = p.c.n_q * p.d.gq;
-  uint32_t ns = 0, met = 0, items = 0;  // steps of the stream, meetings, items so far
+  // steps of the stream, meetings, items and phases of o_last so far
+  uint32_t ns = 0, met = 0, items = 0, lasts = 0;
   const float sl2 = p.c.scale_log2;
   const auto queries = [&](const Walk& w) {
     const int r0 = w.row_tile * tr + (two ? kTile * x : 0) + (lane_row & ~31);
@@ -1033,8 +1032,11 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
             const float f = up ? exp2_fast(row.m - mx) : 1.0f;
             if (up) row.m = mx;
             row.l *= f;
-            // the product before this step's has to be in
-            if (!warp_wait(s, &s.o_done[x][b ^ 1], ((ns - 1) >> 1) & 1)) return;
+            // The product before this step's has to be in: the next scores are
+            // issued behind it; an item's last step has none behind.
+            if (st + 1 < steps ? !warp_wait(s, &s.s_full[x][b ^ 1], ((ns + 1) >> 1) & 1)
+                               : !warp_wait(s, &s.o_last[x], lasts & 1))
+              return;
             tc_after();
             rescale_row(to, f);
           }
@@ -1066,6 +1068,7 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
       tc_before();
       warp_arrive(&s.p_ready[x][b]);
     }
+    lasts += steps > 1;
     // The next item's queries: all scores of this one are done (an item of one
     // row tile has the other stream's too).
     {
@@ -1117,40 +1120,42 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
         at.at[k] = g_warp + r < rows ? row_at + 16 * (lane & 3) : nullptr;
       }
 #pragma unroll 1
-      for (int c = 0; c < kHeadDim; c += 16) {
-        uint32_t r[16];
-        float o[16];
-        tm_load16(to + c, r);
+      for (int c = 0; c < kHeadDim; c += 32) {
+        uint32_t r[32];
+        float o[32];
+        tm_load32(to + c, r);
         tm_load_wait();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) o[k] = __uint_as_float(r[k]) * f0;
+        for (int k = 0; k < 32; ++k) o[k] = __uint_as_float(r[k]) * f0;
         if (!two) {
-          tm_load16(to + 128 + c, r);
+          tm_load32(to + 128 + c, r);
           tm_load_wait();
 #pragma unroll
-          for (int k = 0; k < 16; ++k) o[k] = fmaf(__uint_as_float(r[k]), f1, o[k]);
+          for (int k = 0; k < 32; ++k) o[k] = fmaf(__uint_as_float(r[k]), f1, o[k]);
         }
         // accumulator columns stand in the run order
+        uint4 v[4];
         if (direct) {
-          uint4 v[2];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
+          for (int k = 0; k < 4; ++k) {
             const float* y = o + 8 * k;
             v[k] = make_uint4(pack_half2(y[0], y[2]), pack_half2(y[4], y[6]),
                               pack_half2(y[1], y[3]), pack_half2(y[5], y[7]));
           }
-          stage_row<2>(s.stage[warp], (c >> 4) & 1 ? 2 : 0, v);
-          if ((c >> 4) & 1) put_rows(s.stage[warp], at, 2 * (c & ~31));
+          stage_row(s.stage[warp], v);
+          put_rows(s.stage[warp], at, 2 * c);
         } else {
-          uint4 v[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float* y = o + 8 * (k >> 1) + (k & 1);
-            v[k] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[2]), __float_as_uint(y[4]),
-                              __float_as_uint(y[6]));
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float* y = o + 16 * h + 8 * (k >> 1) + (k & 1);
+              v[k] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[2]),
+                                __float_as_uint(y[4]), __float_as_uint(y[6]));
+            }
+            stage_row(s.stage[warp], v);
+            put_rows(s.stage[warp], at, 4 * (c + 16 * h));
           }
-          stage_row<4>(s.stage[warp], 0, v);
-          put_rows(s.stage[warp], at, 4 * c);
         }
       }
       if (valid && !direct) p.part_ml[pr] = make_float2(m, l);
@@ -1211,16 +1216,16 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     for (int i = 0; i < 2; ++i) {
       bar_init(&s.k_full[i], 4);
       bar_init(&s.v_full[i], 4);
-      bar_init(&s.k_empty[i], 1);
-      bar_init(&s.v_empty[i], 1);
+      bar_init(&s.k_empty[i], 2);  // a commit of either stream
+      bar_init(&s.v_empty[i], 2);
       bar_init(&s.o_full[i], 1);
+      bar_init(&s.o_last[i], 1);
+      bar_init(&s.drained[i], 1);
       for (int b = 0; b < 2; ++b) {
         bar_init(&s.s_full[i][b], 1);
         bar_init(&s.p_ready[i][b], 4);
-        bar_init(&s.o_done[i][b], 1);
       }
     }
-    bar_init(&s.drained, 1);
     bar_init(&s.q_full, 4 << p.streams_rows);
     bar_init(&s.meet, kSoftmaxWarps);
     s.abort = 0;
@@ -1283,13 +1288,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     __syncwarp();
   } else {
     regs_down<kRegsIssue>();
-    if (warp == kIssueWarp) {
-      issue_role<BK, BV>(p, s, u0, u1);
+    if (warp < kIssueWarp + 2) {
+      issue_role<BK, BV>(p, s, u0, u1, warp - kIssueWarp);
       if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort))) {
         // products in flight end before the tile memory is given back
-        tc_commit(elect_lane(), &s.drained);
+        uint64_t* drained = &s.drained[warp - kIssueWarp];
+        tc_commit(elect_lane(), drained);
         const uint32_t t0 = (uint32_t)clock();
-        while (!bar_try(&s.drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
+        while (!bar_try(drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
         }
         if (lane == 0)
           atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
