@@ -564,7 +564,8 @@ kvq_status kvq_sample(const float* logits, int64_t logits_stride, const float* n
   c.token = token;
   c.logprob = logprob;
   trace("kvq_sample batch %d vocab %d", batch, vocab);
-  return cuda_status(launch_sample(c, static_cast<cudaStream_t>(stream)), "kvq_sample launch");
+  return cuda_status(launch_sample(c, sm_count(), static_cast<cudaStream_t>(stream)),
+                     "kvq_sample launch");
 }
 
 static kvq_status check_dgap(const dgap_params* p, int32_t batch, int32_t vocab) {

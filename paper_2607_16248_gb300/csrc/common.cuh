@@ -521,7 +521,7 @@ struct SampleCall {
   float* logprob;
 };
 int sample_max_vocab();
-cudaError_t launch_sample(const SampleCall& call, cudaStream_t stream);
+cudaError_t launch_sample(const SampleCall& call, int sm_count, cudaStream_t stream);
 
 struct DgapDims {
   int batch, vocab, K, hidden, n_chunks;

@@ -1,9 +1,27 @@
-// The next token of each row of logits (kvq_sample): one CTA per row.
+// The next token of each row of logits (kvq_sample).
 //
 // The order of the tokens (value descending, lowest index first) is the order
-// of the 64-bit number (ordered bits of z) << 32 | ~index, descending.  A limit
-// keeps the tokens at or above the largest threshold whose count (top-k) or
-// mass (top-p) reaches its goal; the threshold is found bit by bit.
+// of the 64-bit number (ordered bits of z) << 32 | ~index, descending: a limit
+// keeps the tokens at or above a threshold of that number.  What a row's limits
+// keep is usually a small part of it, so a row is read once:
+//   sample   8192 logits spread over the row give a bound tau below which the
+//            limits will hardly reach (counts of a coarse histogram);
+//   stream   tokens at or above tau go to a list in shared memory, the weights
+//            of the others to a sum;
+//   select   on the list: a histogram over 2048 value ranges finds the range in
+//            which a limit falls, the few tokens of that range are ranked exactly;
+//   draw     the kept token with the largest d - ln(-ln u).
+// Up to eight CTAs (a cluster) stream a row when rows are few; their lists are
+// joined in the first.  When the list does not hold what the limits need (a flat
+// row, a limit near 1, ties beyond the list) the row itself takes its place in
+// the last two steps: the result is the same, later.
+//
+// Bound: the stream, 4 bytes a logit.  One pass over memory and a list of a few
+// thousand tokens; reading the row again for every step took 2.4 to 2.8 ms with
+// thresholds found bit by bit.
+//
+// Sums that decide what is kept are of integers (weights in units of 2^-40) or,
+// for the weights left out of the list, of fp32 numbers in a fixed order.
 
 #include "common.cuh"
 
@@ -12,7 +30,29 @@ namespace kvq {
 namespace {
 
 using u64 = unsigned long long;
-constexpr int kThreads = 1024, kMaxVocab = 262144;
+constexpr int kThreads = 1024, kWarps = kThreads / 32, kMaxVocab = 262144;
+constexpr int kCap = 20480;      // list entries of a CTA
+constexpr int kBins = 2048;      // value ranges of the selection
+constexpr int kEdge = 1024;      // tokens of one range ranked directly
+constexpr int kSample = 8 * kThreads, kCoarse = 512;  // sampled logits, ranges of 1/16 nat
+constexpr float kPerNat = 16.0f;
+
+struct Entry {
+  float z;
+  int i;
+};
+struct Sm {
+  Entry list[kCap];
+  uint32_t count[kBins], mass[3][kBins];  // 14-bit pieces of the weights
+  u64 edge_key[kEdge], edge_mass[kEdge];
+  u64 part[kWarps];
+  float fpart[kWarps];
+  u64 pick[4];
+  float tau, tail;
+  int n, n_edge, range;
+  u64 best;
+  float best_z;
+};
 
 // Bits of a float32 whose unsigned order is the numbers' (-0 as +0).
 __device__ __forceinline__ uint32_t ordered(float z) {
@@ -22,14 +62,15 @@ __device__ __forceinline__ uint32_t ordered(float z) {
 __device__ __forceinline__ u64 rank_key(float z, int i) {
   return ((u64)ordered(z) << 32) | (uint32_t)~i;
 }
+__device__ __forceinline__ float key_value(u64 k) {
+  const uint32_t u = (uint32_t)(k >> 32);
+  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int key_index(u64 k) { return (int)~(uint32_t)k; }
 
-struct Sm {
-  u64 part[32];
-  u64 result;
-};
-
+// A reduction over the CTA; every thread gets the result.
 template <typename F>
-__device__ u64 reduce(Sm& s, u64 v, F f) {
+__device__ __forceinline__ u64 reduce(Sm& s, u64 v, F f) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
   __syncthreads();
@@ -46,79 +87,512 @@ __device__ __forceinline__ u64 most(u64 a, u64 b) { return a > b ? a : b; }
 // e in [0, 1] as a multiple of 2^-40.
 __device__ __forceinline__ u64 mass_of(float e) { return (u64)__float2ull_rn(e * 0x1p40f); }
 
-__global__ void __launch_bounds__(kThreads) sample_kernel(SampleCall p) {
-  __shared__ Sm s;
-  const int b = blockIdx.x, tid = threadIdx.x, V = p.vocab;
-  const float* z = p.logits + b * p.logits_stride;
-  const float* u = p.noise ? p.noise + b * p.noise_stride : nullptr;
-  float T = p.temperature ? p.temperature[b] : 1.0f;
-  const bool greedy = !(T > 0.0f) || !u;
-  if (!(T > 0.0f)) T = 1.0f;
-  u64 top = 0;
-  for (int i = tid; i < V; i += kThreads) top = most(top, rank_key(z[i], i));
-  top = reduce(s, top, most);
-  const int best = (int)~(uint32_t)top;
-  const float zmax = z[best];
-  if (zmax == -INFINITY) {
-    if (tid == 0) {
-      p.token[b] = -1;
-      if (p.logprob) p.logprob[b] = -INFINITY;
+struct Row {
+  const float *z, *u;
+  int V;
+  float T;                 // > 0
+  bool greedy;
+  int k;                   // 0: no limit
+  float p, m;              // >= 1, <= 0: no limit
+};
+
+// Where the tokens of a selection are: the list, or the whole row.
+struct ListSource {
+  const Entry* list;
+  int n;
+  __device__ __forceinline__ int size() const { return n; }
+  __device__ __forceinline__ Entry at(int j) const { return list[j]; }
+};
+struct RowSource {
+  const float* z;
+  int V;
+  __device__ __forceinline__ int size() const { return V; }
+  __device__ __forceinline__ Entry at(int j) const { return Entry{z[j], j}; }
+};
+
+// Prefix of the ranges: the first range at which `goal` tokens (or weights) are
+// reached, and the count and weight before it; -1 if it is not reached.  By warp
+// 0 (64 ranges a lane); results in s.range, s.pick[0..1].
+__device__ void find_range(Sm& s, u64 goal, bool by_mass) {
+  const int lane = threadIdx.x;
+  if (threadIdx.x < 32) {
+    u64 c = 0, m = 0;
+#pragma unroll 4
+    for (int j = 0; j < kBins / 32; ++j) {
+      const int b = lane * (kBins / 32) + ((j + lane) & (kBins / 32 - 1));
+      c += s.count[b];
+      m += s.mass[0][b] + ((u64)s.mass[1][b] << 14) + ((u64)s.mass[2][b] << 28);
     }
-    return;
-  }
-  const auto dist = [&](int i) { return __fdiv_rn(z[i] - zmax, T); };
-  u64 total = 0;
-  for (int i = tid; i < V; i += kThreads) total += mass_of(expf(dist(i)));
-  total = reduce(s, total, add);
-  int token = best;
-  if (!greedy) {
-    // the largest threshold at or above which there are `goal` tokens (or mass)
-    const auto search = [&](u64 goal, bool mass) {
-      u64 t = 0;
-      for (int bit = 63; bit >= 0; --bit) {
-        const u64 c = t | (1ull << bit);
-        u64 n = 0;
-        for (int i = tid; i < V; i += kThreads)
-          if (rank_key(z[i], i) >= c) n += mass ? mass_of(expf(dist(i))) : 1ull;
-        if (reduce(s, n, add) >= goal) t = c;
+    u64 ci = c, mi = m;
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 a = __shfl_up_sync(0xffffffffu, ci, o), b = __shfl_up_sync(0xffffffffu, mi, o);
+      if (lane >= o) ci += a, mi += b;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, (by_mass ? mi : ci) >= goal);
+    if (!hit) {
+      if (lane == 0) s.range = -1;
+    } else if (lane == __ffs(hit) - 1) {
+      u64 cb = ci - c, mb = mi - m;
+      int b = lane * (kBins / 32);
+      for (;; ++b) {
+        const u64 bm = s.mass[0][b] + ((u64)s.mass[1][b] << 14) + ((u64)s.mass[2][b] << 28);
+        if ((by_mass ? mb + bm : cb + s.count[b]) >= goal) break;
+        cb += s.count[b];
+        mb += bm;
       }
-      return t;
-    };
-    const int k = p.top_k ? p.top_k[b] : 0;
-    const float tp = p.top_p ? p.top_p[b] : 1.0f, mp = p.min_p ? p.min_p[b] : 0.0f;
-    u64 cut = k > 0 && k < V ? search((u64)k, false) : 0ull;
-    if (tp < 1.0f) {
-      u64 n = 0;
-      for (int i = tid; i < V; i += kThreads)
-        if (rank_key(z[i], i) >= cut) n += mass_of(expf(dist(i)));
-      n = reduce(s, n, add);
-      const u64 goal = tp > 0.0f ? (u64)ceil((double)tp * (double)n) : 0ull;
-      cut = goal ? search(goal, true) : top;
+      s.range = b;
+      s.pick[0] = cb;
+      s.pick[1] = mb;
     }
-    u64 win = 0;
-    for (int i = tid; i < V; i += kThreads) {
-      const u64 r = rank_key(z[i], i);
-      const float d = dist(i);
-      if (r < cut || (expf(d) < mp && r != top) || z[i] == -INFINITY) continue;
-      const float key = d - logf(-logf(u[i]));
-      win = most(win, rank_key(key, i));
-    }
-    win = reduce(s, win, most);
-    token = (int)~(uint32_t)win;
   }
+  __syncthreads();
+}
+
+// The threshold of a limit: the largest rank key at or above which there are
+// `goal` tokens (or weights), 0 if the source has fewer.  *weight: the weights
+// at or above it.
+template <typename S, typename BinOf, typename MassOf>
+__device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u64 goal,
+                         bool by_mass, u64* weight) {
+  const int tid = threadIdx.x;
+  find_range(s, goal, by_mass);
+  const int range = s.range;
+  const u64 before_c = s.pick[0], before_m = s.pick[1];
+  if (range < 0) return 0;
+  if (tid == 0) s.n_edge = 0, s.pick[2] = 0, s.pick[3] = 0;
+  __syncthreads();
+  for (int j = tid; j < src.size(); j += kThreads) {
+    const Entry e = src.at(j);
+    if (e.z > -INFINITY && bin_of(e.z) == range) {
+      const int at = atomicAdd(&s.n_edge, 1);
+      if (at < kEdge) {
+        s.edge_key[at] = rank_key(e.z, e.i);
+        s.edge_mass[at] = weight_of(e.z);
+      }
+    }
+  }
+  __syncthreads();
+  const int n = s.n_edge;
+  if (n <= kEdge) {
+    if (tid < n) {
+      const u64 mine = s.edge_key[tid];
+      u64 c = before_c, m = before_m;
+      for (int j = 0; j < n; ++j)
+        if (s.edge_key[j] > mine) {
+          ++c;
+          m += s.edge_mass[j];
+        }
+      // the token with which the goal is reached
+      if ((by_mass ? m : c) < goal && (by_mass ? m + s.edge_mass[tid] : c + 1) >= goal) {
+        s.pick[2] = mine;
+        s.pick[3] = m + s.edge_mass[tid];
+      }
+    }
+    __syncthreads();
+    *weight = s.pick[3];
+    return s.pick[2];
+  }
+  // more tokens than can be ranked at once (ties): bit by bit
+  u64 t = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const u64 c = t | (1ull << bit);
+    u64 sum = 0;
+    for (int j = tid; j < src.size(); j += kThreads) {
+      const Entry e = src.at(j);
+      if (e.z > -INFINITY && rank_key(e.z, e.i) >= c) sum += by_mass ? weight_of(e.z) : 1ull;
+    }
+    if (reduce(s, sum, add) >= goal) t = c;
+  }
+  u64 sum = 0;
+  for (int j = tid; j < src.size(); j += kThreads) {
+    const Entry e = src.at(j);
+    if (e.z > -INFINITY && rank_key(e.z, e.i) >= t) sum += weight_of(e.z);
+  }
+  *weight = reduce(s, sum, add);
+  return t;
+}
+
+// Selection and draw on a source.  tau: the source holds every token at or
+// above it; tail: the weights (relative to the largest logit) of the others.
+// *weight: all tokens' weights.  False: the source does not hold what the limits
+// need.
+template <typename S>
+__device__ bool choose(Sm& s, const Row& r, const S& src, float tau, double tail, u64 given,
+                       int* token, double* weight) {
+  const int tid = threadIdx.x, n = src.size();
+  u64 top = 0, low = 0;  // largest key, complement of the least
+  for (int j = tid; j < n; j += kThreads) {
+    const Entry e = src.at(j);
+    if (e.z > -INFINITY) {
+      const u64 key = rank_key(e.z, e.i);
+      top = most(top, key);
+      low = most(low, ~key);
+    }
+  }
+  top = reduce(s, top, most);
+  if (top == 0) return false;
+  const float zmax = key_value(top);
+  const auto dist = [&](float z) { return __fdiv_rn(z - zmax, r.T); };
+  const auto weight_of = [&](float z) { return mass_of(expf(dist(z))); };
+  const bool limits = !r.greedy && !given && (r.k > 0 || r.p < 1.0f);
+  // ranges of equal width from the largest value to the least of the source
+  const float width = zmax - key_value(~reduce(s, low, most));
+  const float scale = width > 0.0f && width < INFINITY ? (kBins - 1) / width : 0.0f;
+  const auto bin_of = [&](float z) {
+    return min((int)__fmul_rn(__fsub_rn(zmax, z), scale), kBins - 1);
+  };
+  if (limits) {
+    for (int j = tid; j < kBins; j += kThreads) {
+      s.count[j] = 0;
+      s.mass[0][j] = s.mass[1][j] = s.mass[2][j] = 0;
+    }
+    __syncthreads();
+  }
+  u64 sum = 0;
+  for (int j = tid; j < n; j += kThreads) {
+    const float z = src.at(j).z;
+    if (z == -INFINITY) continue;
+    const u64 q = weight_of(z);
+    sum += q;
+    if (limits) {
+      const int b = bin_of(z);
+      atomicAdd(&s.count[b], 1u);
+      if (q) {
+        atomicAdd(&s.mass[0][b], (uint32_t)(q & 0x3fffu));
+        if (q >> 14) atomicAdd(&s.mass[1][b], (uint32_t)(q >> 14) & 0x3fffu);
+        if (q >> 28) atomicAdd(&s.mass[2][b], (uint32_t)(q >> 28));
+      }
+    }
+  }
+  sum = reduce(s, sum, add);
+  const double total = (double)sum * 0x1p-40 + tail;
+  u64 win = top;
+  if (given) {
+    win = given;
+  } else if (!r.greedy) {
+    // a limit that the source ends before is as good as none where min-p ends
+    // earlier still
+    const bool enough = r.m > 0.0f && expf(dist(tau)) < r.m;
+    u64 cut = 0, kept = (u64)(total * 0x1p40);
+    if (r.k > 0) {
+      u64 w = 0;
+      cut = threshold(s, src, bin_of, weight_of, (u64)r.k, false, &w);
+      if (cut) kept = w;
+      else if (tau > -INFINITY && (!enough || r.p < 1.0f)) return false;
+    }
+    if (r.p < 1.0f) {
+      const u64 goal = r.p > 0.0f ? (u64)ceil((double)r.p * (double)kept) : 0ull;
+      u64 w;
+      const u64 c = goal ? threshold(s, src, bin_of, weight_of, goal, true, &w) : top;
+      if (c) cut = most(cut, c);
+      else if (tau > -INFINITY && !enough) return false;
+    }
+    if (r.k <= 0 && r.p >= 1.0f && tau > -INFINITY && !enough) return false;
+    u64 best = 0;
+    for (int j = tid; j < n; j += kThreads) {
+      const Entry e = src.at(j);
+      const u64 key = rank_key(e.z, e.i);
+      if (e.z == -INFINITY || key < cut) continue;
+      const float d = dist(e.z);
+      if (expf(d) < r.m && key != top) continue;
+      best = most(best, rank_key(d - logf(-logf(r.u[e.i])), e.i));
+    }
+    win = reduce(s, best, most);
+  }
+  *token = key_index(win);
+  *weight = total;
+  if (tid == 0) s.best_z = zmax;
+  return true;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+          : "memory");
+}
+__device__ __forceinline__ uint32_t peer(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+               : "=r"(a)
+               : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ uint32_t peer_u32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ u64 peer_u64(uint32_t a) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// kCl CTAs a row.
+template <int kCl>
+__global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  Sm& s = *reinterpret_cast<Sm*>(raw);
+  const int tid = threadIdx.x, lane = tid & 31, b = blockIdx.x / kCl;
+  const int rank = kCl > 1 ? (int)cluster_rank() : 0;
+  Row r;
+  r.z = p.logits + b * p.logits_stride;
+  r.u = p.noise ? p.noise + b * p.noise_stride : nullptr;
+  r.V = p.vocab;
+  r.T = p.temperature ? p.temperature[b] : 1.0f;
+  r.greedy = !(r.T > 0.0f) || !r.u;
+  if (!(r.T > 0.0f)) r.T = 1.0f;
+  r.k = p.top_k ? p.top_k[b] : 0;
+  if (r.k < 0 || r.k >= r.V) r.k = 0;
+  r.p = p.top_p ? p.top_p[b] : 1.0f;
+  r.m = p.min_p ? p.min_p[b] : 0.0f;
+  const bool all = !r.greedy && r.k <= 0 && !(r.p < 1.0f) && !(r.m > 0.0f);
+  const float per_t = 1.0f / r.T;
+
+  // Sample: every CTA of the row takes the same logits and finds the same tau.
+  float x[8];
+  float m0 = -INFINITY;
+  const int taken = min(r.V, kSample);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int at = r.V <= kSample ? j * kThreads + tid
+                                  : (int)((long long)j * (r.V - kThreads) / 7) + tid;
+    x[j] = at < r.V ? r.z[at] : -INFINITY;
+    m0 = fmaxf(m0, x[j]);
+  }
+  for (int j = tid; j < kCoarse; j += kThreads) s.count[j] = 0;
+  if (tid == 0) s.n = 0;
+  m0 = key_value(reduce(s, rank_key(m0, 0), most));
+  const bool seen = m0 > -INFINITY;  // else the sample says nothing: the row itself
+  if (seen) {
+    const float scale = kPerNat * per_t;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (x[j] > -INFINITY) atomicAdd(&s.count[min((int)((m0 - x[j]) * scale), kCoarse - 1)], 1u);
+    __syncthreads();
+    if (tid < 32) {
+      // counts and weights up to each range, 16 ranges a lane
+      constexpr int kPer = kCoarse / 32;
+      float c[kPer], w[kPer], cs = 0.0f, ws = 0.0f;
+      for (int j = 0; j < kPer; ++j) {
+        c[j] = (float)s.count[lane * kPer + j];
+        w[j] = c[j] * __expf(-(lane * kPer + j + 0.5f) / kPerNat);
+        cs += c[j];
+        ws += w[j];
+      }
+      float ci = cs, wi = ws;
+      for (int o = 1; o < 32; o <<= 1) {
+        const float a = __shfl_up_sync(0xffffffffu, ci, o), d = __shfl_up_sync(0xffffffffu, wi, o);
+        if (lane >= o) ci += a, wi += d;
+      }
+      const float all_w = __shfl_sync(0xffffffffu, wi, 31);
+      const float rate = (float)taken / (float)r.V;
+      // how many sampled tokens and which weight the list should reach down to
+      const float most_c = 0.6f * kCap * rate;
+      float want_c = 0.0f, want_w = 0.0f;
+      if (r.k > 0) {
+        want_c = 1.5f * r.k * rate + 8.0f;
+      } else if (r.p < 1.0f) {
+        want_c = 2048.0f * rate;
+        want_w = all_w * (1.0f - 0.125f * (1.0f - r.p));
+      }
+      int mine = kCoarse;  // first range that reaches both
+      int last = -1;       // last range within the list's room
+      float cc = ci - cs, ww = wi - ws;
+      for (int j = 0; j < kPer; ++j) {
+        cc += c[j];
+        ww += w[j];
+        if (mine == kCoarse && cc >= want_c && ww >= want_w) mine = lane * kPer + j;
+        if (cc <= most_c) last = lane * kPer + j;
+      }
+      for (int o = 16; o; o >>= 1) {
+        mine = min(mine, __shfl_xor_sync(0xffffffffu, mine, o));
+        last = max(last, __shfl_xor_sync(0xffffffffu, last, o));
+      }
+      int range = min(mine, max(last, 0));
+      if (r.m > 0.0f) {
+        // nothing is kept below min-p of the sample's maximum, nor of the row's
+        const int floor_range = max(0, (int)fminf(-logf(r.m) * kPerNat + 1.0f, (float)kCoarse));
+        if (r.k <= 0 && !(r.p < 1.0f)) range = floor_range;
+        else range = min(range, floor_range);
+      }
+      if (lane == 0)
+        s.tau = r.greedy || all ? m0
+                : range >= kCoarse - 1 && mine < kCoarse
+                    ? -INFINITY
+                    : m0 - (range + 1) / kPerNat * r.T;
+    }
+  }
+  __syncthreads();
+  const float tau = seen ? s.tau : 0.0f;
+
+  // Stream: this CTA's part of the row.
+  if (seen) {
+    const int per = (r.V + kCl - 1) / kCl, lo = min(r.V, rank * per), hi = min(r.V, lo + per);
+    const float c2 = per_t * 1.4426950408889634f, o2 = -m0 * c2;
+    float tail[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    u64 best = 0;
+    const auto put = [&](float z, int i) {  // the warp's tokens at or above tau
+      const bool in = z >= tau && z > -INFINITY;
+      const unsigned ball = __ballot_sync(0xffffffffu, in);
+      if (in) {
+        const unsigned act = ball;
+        const int leader = __ffs(act) - 1;
+        int at = 0;
+        if (lane == leader) at = atomicAdd(&s.n, __popc(ball));
+        at = __shfl_sync(ball, at, leader) + __popc(ball & ((1u << lane) - 1u));
+        if (at < kCap) s.list[at] = Entry{z, i};
+      }
+    };
+    const auto one = [&](float z, int i, float& sum) {
+      if (z < tau) {
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(z, c2, o2)));
+        sum += e;
+      }
+      if (all && z > -INFINITY)
+        best = most(best, rank_key(__fdiv_rn(z - m0, r.T) - logf(-logf(r.u[i])), i));
+    };
+    // up to three logits before the first 16-byte boundary, then four at a time
+    const int head = min(hi - lo, (int)((4 - ((reinterpret_cast<uintptr_t>(r.z + lo) >> 2) & 3)) & 3));
+    const int quads = (hi - lo - head) / 4, body = lo + head, end = body + 4 * quads;
+    const float4* z4 = reinterpret_cast<const float4*>(r.z + body);
+    constexpr int kUnroll = 4;
+#pragma unroll 1
+    for (int q0 = 0; q0 < quads; q0 += kUnroll * kThreads) {
+      float4 v[kUnroll];
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int q = q0 + k * kThreads + tid;
+        v[k] = q < quads ? __ldg(z4 + q)
+                         : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      }
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int i = body + 4 * (q0 + k * kThreads + tid);
+        const float y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        const float hi4 = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) one(y[c], i + c, tail[c]);
+        if (__any_sync(0xffffffffu, hi4 >= tau)) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) put(y[c], i + c);
+        }
+      }
+    }
+    {  // the ragged ends, by the first warp
+      const int i = lane < head ? lo + lane : end + lane - head;
+      if (tid < 32) {
+        const float z = i < hi && (lane < head || i >= end) ? r.z[i] : -INFINITY;
+        one(z, i, tail[0]);
+        put(z, i);
+      }
+    }
+    float t = (tail[0] + tail[1]) + (tail[2] + tail[3]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (lane == 0) s.fpart[tid >> 5] = t;
+    best = all ? reduce(s, best, most) : 0;
+    __syncthreads();
+    if (tid == 0) {
+      float sum = 0.0f;
+      for (int w = 0; w < kWarps; ++w) sum += s.fpart[w];
+      s.tail = sum;
+      s.best = best;
+    }
+  }
+  __syncthreads();
+
+  // The first CTA joins the lists.
+  bool fits = seen && s.n <= kCap;
+  u64 given = 0;
+  double tail = 0.0;
+  int n = 0;
+  if (kCl > 1) {
+    cluster_sync();
+    if (rank == 0 && seen) {
+      n = s.n;
+      tail = s.tail;
+      given = s.best;
+      for (int c = 1; c < kCl; ++c) {
+        const int m = (int)peer_u32(peer(&s.n, c));
+        tail += __uint_as_float(peer_u32(peer(&s.tail, c)));
+        given = most(given, peer_u64(peer(&s.best, c)));
+        fits = fits && m <= kCap && n + m <= kCap;
+        if (fits) {
+          const uint32_t src = peer(s.list, c);
+          for (int j = tid; j < m; j += kThreads)
+            *reinterpret_cast<u64*>(&s.list[n + j]) = peer_u64(src + 8 * j);
+          n += m;
+        }
+      }
+    }
+    cluster_sync();
+    if (rank) return;
+  } else if (seen) {
+    n = s.n;
+    tail = s.tail;
+    given = s.best;
+  }
+  __syncthreads();
+
+  int token = -1;
+  double weight = 0.0;
+  bool done = false;
+  if (fits) {
+    // the tail's weights are relative to the sample's maximum so far
+    u64 top = 0;
+    for (int j = tid; j < n; j += kThreads) top = most(top, rank_key(s.list[j].z, s.list[j].i));
+    top = reduce(s, top, most);
+    const double rel = tail * expf(__fdiv_rn(m0 - key_value(top), r.T));
+    done = choose(s, r, ListSource{s.list, n}, tau, rel, given, &token, &weight);
+    __syncthreads();
+  }
+  if (!done) choose(s, r, RowSource{r.z, r.V}, -INFINITY, 0.0, 0ull, &token, &weight);
   if (tid == 0) {
     p.token[b] = token;
-    if (p.logprob) p.logprob[b] = dist(token) - logf((float)((double)total * 0x1p-40));
+    if (p.logprob)
+      p.logprob[b] =
+          token < 0 ? -INFINITY : __fdiv_rn(r.z[token] - s.best_z, r.T) - (float)log(weight);
   }
+}
+
+template <int kCl>
+cudaError_t launch_cluster(const SampleCall& call, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(sample_kernel<kCl>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sm));
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(call.batch * kCl);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Sm);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kCl;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = kCl > 1 ? 1 : 0;
+  e = cudaLaunchKernelEx(&cfg, sample_kernel<kCl>, call);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
 int sample_max_vocab() { return kMaxVocab; }
 
-cudaError_t launch_sample(const SampleCall& call, cudaStream_t stream) {
-  sample_kernel<<<call.batch, kThreads, 0, stream>>>(call);
-  return cudaGetLastError();
+// CTAs per row: as many as keep the launch within one wave (one CTA per SM).
+cudaError_t launch_sample(const SampleCall& call, int sm_count, cudaStream_t stream) {
+  if (call.batch * 8 <= sm_count) return launch_cluster<8>(call, stream);
+  if (call.batch * 4 <= sm_count) return launch_cluster<4>(call, stream);
+  if (call.batch * 2 <= sm_count) return launch_cluster<2>(call, stream);
+  return launch_cluster<1>(call, stream);
 }
 
 }  // namespace kvq
