@@ -45,9 +45,9 @@ struct Sm {
   Entry list[kCap];
   uint32_t count[kBins], mass[3][kBins];  // 14-bit pieces of the weights
   u64 edge_key[kEdge], edge_mass[kEdge];
-  u64 part[kWarps];
+  u64 part[kWarps], part2[kWarps];
   float fpart[kWarps];
-  u64 pick[4];
+  u64 before_c, before_m, cut_key, cut_mass;
   float tau, tail;
   int n, n_edge, range;
   u64 best;
@@ -81,6 +81,26 @@ __device__ __forceinline__ u64 reduce(Sm& s, u64 v, F f) {
   for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
+// The larger of a and of b over the CTA, in one go.
+__device__ __forceinline__ void most2(Sm& s, u64& a, u64& b) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const u64 x = __shfl_xor_sync(0xffffffffu, a, o), y = __shfl_xor_sync(0xffffffffu, b, o);
+    a = a > x ? a : x;
+    b = b > y ? b : y;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) s.part[threadIdx.x >> 5] = a, s.part2[threadIdx.x >> 5] = b;
+  __syncthreads();
+  a = s.part[threadIdx.x & 31];
+  b = s.part2[threadIdx.x & 31];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const u64 x = __shfl_xor_sync(0xffffffffu, a, o), y = __shfl_xor_sync(0xffffffffu, b, o);
+    a = a > x ? a : x;
+    b = b > y ? b : y;
+  }
+}
 __device__ __forceinline__ u64 add(u64 a, u64 b) { return a + b; }
 __device__ __forceinline__ u64 most(u64 a, u64 b) { return a > b ? a : b; }
 
@@ -112,37 +132,49 @@ struct RowSource {
 
 // Prefix of the ranges: the first range at which `goal` tokens (or weights) are
 // reached, and the count and weight before it; -1 if it is not reached.  By warp
-// 0 (64 ranges a lane); results in s.range, s.pick[0..1].
+// 0: 64 ranges a lane, then the 64 of the lane where it happens, two a lane.
+// Results in s.range, s.before_c, s.before_m.
+__device__ __forceinline__ u64 range_mass(const Sm& s, int b) {
+  return s.mass[0][b] + ((u64)s.mass[1][b] << 14) + ((u64)s.mass[2][b] << 28);
+}
 __device__ void find_range(Sm& s, u64 goal, bool by_mass) {
+  constexpr int kPer = kBins / 32;
   const int lane = threadIdx.x;
   if (threadIdx.x < 32) {
     u64 c = 0, m = 0;
 #pragma unroll 4
-    for (int j = 0; j < kBins / 32; ++j) {
-      const int b = lane * (kBins / 32) + ((j + lane) & (kBins / 32 - 1));
+    for (int j = 0; j < kPer; ++j) {
+      const int b = lane * kPer + ((j + lane) & (kPer - 1));
       c += s.count[b];
-      m += s.mass[0][b] + ((u64)s.mass[1][b] << 14) + ((u64)s.mass[2][b] << 28);
+      m += range_mass(s, b);
     }
     u64 ci = c, mi = m;
     for (int o = 1; o < 32; o <<= 1) {
-      const u64 a = __shfl_up_sync(0xffffffffu, ci, o), b = __shfl_up_sync(0xffffffffu, mi, o);
-      if (lane >= o) ci += a, mi += b;
+      const u64 x = __shfl_up_sync(0xffffffffu, ci, o), y = __shfl_up_sync(0xffffffffu, mi, o);
+      if (lane >= o) ci += x, mi += y;
     }
     const unsigned hit = __ballot_sync(0xffffffffu, (by_mass ? mi : ci) >= goal);
     if (!hit) {
       if (lane == 0) s.range = -1;
-    } else if (lane == __ffs(hit) - 1) {
-      u64 cb = ci - c, mb = mi - m;
-      int b = lane * (kBins / 32);
-      for (;; ++b) {
-        const u64 bm = s.mass[0][b] + ((u64)s.mass[1][b] << 14) + ((u64)s.mass[2][b] << 28);
-        if ((by_mass ? mb + bm : cb + s.count[b]) >= goal) break;
-        cb += s.count[b];
-        mb += bm;
+    } else {
+      const int at = __ffs(hit) - 1, b = at * kPer + 2 * lane;
+      const u64 c0 = __shfl_sync(0xffffffffu, ci - c, at);
+      const u64 m0 = __shfl_sync(0xffffffffu, mi - m, at);
+      const u64 ca = s.count[b], cb = s.count[b + 1], ma = range_mass(s, b),
+                mb = range_mass(s, b + 1);
+      u64 cs = ca + cb, ms = ma + mb;
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 x = __shfl_up_sync(0xffffffffu, cs, o), y = __shfl_up_sync(0xffffffffu, ms, o);
+        if (lane >= o) cs += x, ms += y;
       }
-      s.range = b;
-      s.pick[0] = cb;
-      s.pick[1] = mb;
+      const unsigned inner = __ballot_sync(0xffffffffu, (by_mass ? m0 + ms : c0 + cs) >= goal);
+      if (lane == __ffs(inner) - 1) {
+        const u64 before_c = c0 + cs - ca - cb, before_m = m0 + ms - ma - mb;
+        const bool second = (by_mass ? before_m + ma : before_c + ca) < goal;
+        s.range = b + (second ? 1 : 0);
+        s.before_c = before_c + (second ? ca : 0ull);
+        s.before_m = before_m + (second ? ma : 0ull);
+      }
     }
   }
   __syncthreads();
@@ -157,9 +189,9 @@ __device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u6
   const int tid = threadIdx.x;
   find_range(s, goal, by_mass);
   const int range = s.range;
-  const u64 before_c = s.pick[0], before_m = s.pick[1];
+  const u64 before_c = s.before_c, before_m = s.before_m;
   if (range < 0) return 0;
-  if (tid == 0) s.n_edge = 0, s.pick[2] = 0, s.pick[3] = 0;
+  if (tid == 0) s.n_edge = 0, s.cut_key = 0, s.cut_mass = 0;
   __syncthreads();
   for (int j = tid; j < src.size(); j += kThreads) {
     const Entry e = src.at(j);
@@ -184,13 +216,13 @@ __device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u6
         }
       // the token with which the goal is reached
       if ((by_mass ? m : c) < goal && (by_mass ? m + s.edge_mass[tid] : c + 1) >= goal) {
-        s.pick[2] = mine;
-        s.pick[3] = m + s.edge_mass[tid];
+        s.cut_key = mine;
+        s.cut_mass = m + s.edge_mass[tid];
       }
     }
     __syncthreads();
-    *weight = s.pick[3];
-    return s.pick[2];
+    *weight = s.cut_mass;
+    return s.cut_key;
   }
   // more tokens than can be ranked at once (ties): bit by bit
   u64 t = 0;
@@ -212,14 +244,14 @@ __device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u6
   return t;
 }
 
-// Selection and draw on a source.  tau: the source holds every token at or
-// above it; tail: the weights (relative to the largest logit) of the others.
-// *weight: all tokens' weights.  False: the source does not hold what the limits
-// need.
+// Selection and draw on a source.  tau: the source holds every token at or above
+// it; tail: the weights of the others, relative to a logit of m0.  *weight: all
+// tokens' weights.  False: the source does not hold what the limits need.
 template <typename S>
-__device__ bool choose(Sm& s, const Row& r, const S& src, float tau, double tail, u64 given,
-                       int* token, double* weight) {
+__device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, double tail,
+                       u64 given, int* token, double* weight) {
   const int tid = threadIdx.x, n = src.size();
+  const bool limits = !r.greedy && !given && (r.k > 0 || r.p < 1.0f);
   u64 top = 0, low = 0;  // largest key, complement of the least
   for (int j = tid; j < n; j += kThreads) {
     const Entry e = src.at(j);
@@ -229,25 +261,23 @@ __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, double tail
       low = most(low, ~key);
     }
   }
-  top = reduce(s, top, most);
-  if (top == 0) return false;
-  const float zmax = key_value(top);
-  const auto dist = [&](float z) { return __fdiv_rn(z - zmax, r.T); };
-  const auto weight_of = [&](float z) { return mass_of(expf(dist(z))); };
-  const bool limits = !r.greedy && !given && (r.k > 0 || r.p < 1.0f);
-  // ranges of equal width from the largest value to the least of the source
-  const float width = zmax - key_value(~reduce(s, low, most));
-  const float scale = width > 0.0f && width < INFINITY ? (kBins - 1) / width : 0.0f;
-  const auto bin_of = [&](float z) {
-    return min((int)__fmul_rn(__fsub_rn(zmax, z), scale), kBins - 1);
-  };
   if (limits) {
     for (int j = tid; j < kBins; j += kThreads) {
       s.count[j] = 0;
       s.mass[0][j] = s.mass[1][j] = s.mass[2][j] = 0;
     }
-    __syncthreads();
   }
+  most2(s, top, low);
+  if (top == 0) return false;
+  const float zmax = key_value(top);
+  const auto dist = [&](float z) { return __fdiv_rn(z - zmax, r.T); };
+  const auto weight_of = [&](float z) { return mass_of(expf(dist(z))); };
+  // ranges of equal width from the largest value to the least of the source
+  const float width = zmax - key_value(~low);
+  const float scale = width > 0.0f && width < INFINITY ? (kBins - 1) / width : 0.0f;
+  const auto bin_of = [&](float z) {
+    return min((int)__fmul_rn(__fsub_rn(zmax, z), scale), kBins - 1);
+  };
   u64 sum = 0;
   for (int j = tid; j < n; j += kThreads) {
     const float z = src.at(j).z;
@@ -265,7 +295,7 @@ __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, double tail
     }
   }
   sum = reduce(s, sum, add);
-  const double total = (double)sum * 0x1p-40 + tail;
+  const double total = (double)sum * 0x1p-40 + (tail > 0.0 ? tail * expf(dist(m0)) : 0.0);
   u64 win = top;
   if (given) {
     win = given;
@@ -436,27 +466,30 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
     const int per = (r.V + kCl - 1) / kCl, lo = min(r.V, rank * per), hi = min(r.V, lo + per);
     const float c2 = per_t * 1.4426950408889634f, o2 = -m0 * c2;
     float tail[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    u64 best = 0;
-    const auto put = [&](float z, int i) {  // the warp's tokens at or above tau
-      const bool in = z >= tau && z > -INFINITY;
-      const unsigned ball = __ballot_sync(0xffffffffu, in);
-      if (in) {
-        const unsigned act = ball;
-        const int leader = __ffs(act) - 1;
-        int at = 0;
-        if (lane == leader) at = atomicAdd(&s.n, __popc(ball));
-        at = __shfl_sync(ball, at, leader) + __popc(ball & ((1u << lane) - 1u));
-        if (at < kCap) s.list[at] = Entry{z, i};
+    float best_key = -INFINITY;
+    int best_i = -1;  // of an unlimited draw
+    // places in the list for the warp's `mine` tokens a lane
+    const auto reserve = [&](int mine) {
+      int sum = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
       }
+      int at = 0;
+      if (lane == 31 && sum) at = atomicAdd(&s.n, sum);
+      return __shfl_sync(0xffffffffu, at, 31) + sum - mine;
     };
+    const auto wanted = [&](float z) { return z >= tau && z > -INFINITY; };
     const auto one = [&](float z, int i, float& sum) {
-      if (z < tau) {
-        float e;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(z, c2, o2)));
-        sum += e;
+      float e;
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(z, c2, o2)));
+      sum += z < tau ? e : 0.0f;
+      if (all && z > -INFINITY) {
+        const float key = __fdiv_rn(z - m0, r.T) - logf(-logf(r.u[i]));
+        if (best_i < 0 || key > best_key || (key == best_key && i < best_i))
+          best_key = key, best_i = i;
       }
-      if (all && z > -INFINITY)
-        best = most(best, rank_key(__fdiv_rn(z - m0, r.T) - logf(-logf(r.u[i])), i));
     };
     // up to three logits before the first 16-byte boundary, then four at a time
     const int head = min(hi - lo, (int)((4 - ((reinterpret_cast<uintptr_t>(r.z + lo) >> 2) & 3)) & 3));
@@ -466,6 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
 #pragma unroll 1
     for (int q0 = 0; q0 < quads; q0 += kUnroll * kThreads) {
       float4 v[kUnroll];
+      int mine = 0;
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) {
         const int q = q0 + k * kThreads + tid;
@@ -476,28 +510,39 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
       for (int k = 0; k < kUnroll; ++k) {
         const int i = body + 4 * (q0 + k * kThreads + tid);
         const float y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-        const float hi4 = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) one(y[c], i + c, tail[c]);
-        if (__any_sync(0xffffffffu, hi4 >= tau)) {
+        for (int c = 0; c < 4; ++c) {
+          one(y[c], i + c, tail[c]);
+          mine += wanted(y[c]);
+        }
+      }
+      if (__any_sync(0xffffffffu, mine)) {
+        int at = reserve(mine);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) put(y[c], i + c);
+        for (int k = 0; k < kUnroll; ++k) {
+          const int i = body + 4 * (q0 + k * kThreads + tid);
+          const float y[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (wanted(y[c])) {
+              if (at < kCap) s.list[at] = Entry{y[c], i + c};
+              ++at;
+            }
         }
       }
     }
-    {  // the ragged ends, by the first warp
+    if (tid < 32) {  // the ragged ends
       const int i = lane < head ? lo + lane : end + lane - head;
-      if (tid < 32) {
-        const float z = i < hi && (lane < head || i >= end) ? r.z[i] : -INFINITY;
-        one(z, i, tail[0]);
-        put(z, i);
-      }
+      const float z = i < hi && (lane < head || i >= end) ? r.z[i] : -INFINITY;
+      one(z, i, tail[0]);
+      const int at = reserve(wanted(z));
+      if (wanted(z) && at < kCap) s.list[at] = Entry{z, i};
     }
     float t = (tail[0] + tail[1]) + (tail[2] + tail[3]);
 #pragma unroll
     for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     if (lane == 0) s.fpart[tid >> 5] = t;
-    best = all ? reduce(s, best, most) : 0;
+    const u64 best = all ? reduce(s, best_i < 0 ? 0ull : rank_key(best_key, best_i), most) : 0ull;
     __syncthreads();
     if (tid == 0) {
       float sum = 0.0f;
@@ -545,15 +590,10 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
   double weight = 0.0;
   bool done = false;
   if (fits) {
-    // the tail's weights are relative to the sample's maximum so far
-    u64 top = 0;
-    for (int j = tid; j < n; j += kThreads) top = most(top, rank_key(s.list[j].z, s.list[j].i));
-    top = reduce(s, top, most);
-    const double rel = tail * expf(__fdiv_rn(m0 - key_value(top), r.T));
-    done = choose(s, r, ListSource{s.list, n}, tau, rel, given, &token, &weight);
+    done = choose(s, r, ListSource{s.list, n}, tau, m0, tail, given, &token, &weight);
     __syncthreads();
   }
-  if (!done) choose(s, r, RowSource{r.z, r.V}, -INFINITY, 0.0, 0ull, &token, &weight);
+  if (!done) choose(s, r, RowSource{r.z, r.V}, -INFINITY, 0.0f, 0.0, 0ull, &token, &weight);
   if (tid == 0) {
     p.token[b] = token;
     if (p.logprob)
