@@ -49,7 +49,7 @@ struct Sm {
   float fpart[kWarps];
   u64 before_c, before_m, cut_key, cut_mass;
   float tau, tail;
-  int n, n_edge, range;
+  int n, n_edge, range, peer_n[8];
   u64 best;
   float best_z;
 };
@@ -248,8 +248,8 @@ __device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u6
 // it; tail: the weights of the others, relative to a logit of m0.  *weight: all
 // tokens' weights.  False: the source does not hold what the limits need.
 template <typename S>
-__device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, double tail,
-                       u64 given, int* token, double* weight) {
+__device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, float tail,
+                       u64 given, int* token, u64* weight) {
   const int tid = threadIdx.x, n = src.size();
   const bool limits = !r.greedy && !given && (r.k > 0 || r.p < 1.0f);
   u64 top = 0, low = 0;  // largest key, complement of the least
@@ -295,7 +295,7 @@ __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, d
     }
   }
   sum = reduce(s, sum, add);
-  const double total = (double)sum * 0x1p-40 + (tail > 0.0 ? tail * expf(dist(m0)) : 0.0);
+  const u64 total = sum + (tail > 0.0f ? mass_of(tail * expf(dist(m0))) : 0ull);
   u64 win = top;
   if (given) {
     win = given;
@@ -303,7 +303,7 @@ __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, d
     // a limit that the source ends before is as good as none where min-p ends
     // earlier still
     const bool enough = r.m > 0.0f && expf(dist(tau)) < r.m;
-    u64 cut = 0, kept = (u64)(total * 0x1p40);
+    u64 cut = 0, kept = total;
     if (r.k > 0) {
       u64 w = 0;
       cut = threshold(s, src, bin_of, weight_of, (u64)r.k, false, &w);
@@ -311,7 +311,11 @@ __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, d
       else if (tau > -INFINITY && (!enough || r.p < 1.0f)) return false;
     }
     if (r.p < 1.0f) {
-      const u64 goal = r.p > 0.0f ? (u64)ceil((double)r.p * (double)kept) : 0ull;
+      // the least whole number >= p * kept, p in units of 2^-32 (64-bit floating
+      // point would take longer than the rest)
+      const u64 p32 = (u64)__float2ull_rn(fmaxf(r.p, 0.0f) * 0x1p32f);
+      const u64 frac = kept * p32, whole = __umul64hi(kept, p32);
+      const u64 goal = (whole << 32 | frac >> 32) + ((uint32_t)frac ? 1 : 0);
       u64 w;
       const u64 c = goal ? threshold(s, src, bin_of, weight_of, goal, true, &w) : top;
       if (c) cut = most(cut, c);
@@ -399,7 +403,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
   if (tid == 0) s.n = 0;
   m0 = key_value(reduce(s, rank_key(m0, 0), most));
   const bool seen = m0 > -INFINITY;  // else the sample says nothing: the row itself
-  if (seen) {
+  if (seen && (r.greedy || all)) {
+    if (tid == 0) s.tau = m0;
+  } else if (seen) {
     const float scale = kPerNat * per_t;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -449,13 +455,11 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
         // nothing is kept below min-p of the sample's maximum, nor of the row's
         const int floor_range = max(0, (int)fminf(-logf(r.m) * kPerNat + 1.0f, (float)kCoarse));
         if (r.k <= 0 && !(r.p < 1.0f)) range = floor_range;
-        else range = min(range, floor_range);
+        else if (r.k <= 0 || !(r.p < 1.0f)) range = min(range, floor_range);  // p needs all of k
       }
       if (lane == 0)
-        s.tau = r.greedy || all ? m0
-                : range >= kCoarse - 1 && mine < kCoarse
-                    ? -INFINITY
-                    : m0 - (range + 1) / kPerNat * r.T;
+        s.tau = range >= kCoarse - 1 && mine < kCoarse ? -INFINITY
+                                                       : m0 - (range + 1) / kPerNat * r.T;
     }
   }
   __syncthreads();
@@ -556,24 +560,36 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
   // The first CTA joins the lists.
   bool fits = seen && s.n <= kCap;
   u64 given = 0;
-  double tail = 0.0;
+  float tail = 0.0f;
   int n = 0;
   if (kCl > 1) {
     cluster_sync();
     if (rank == 0 && seen) {
-      n = s.n;
-      tail = s.tail;
-      given = s.best;
-      for (int c = 1; c < kCl; ++c) {
-        const int m = (int)peer_u32(peer(&s.n, c));
-        tail += __uint_as_float(peer_u32(peer(&s.tail, c)));
-        given = most(given, peer_u64(peer(&s.best, c)));
-        fits = fits && m <= kCap && n + m <= kCap;
-        if (fits) {
+      if (tid < kCl) {  // all peers at once: a remote read takes about a microsecond
+        s.peer_n[tid] = (int)peer_u32(peer(&s.n, tid));
+        s.fpart[tid] = __uint_as_float(peer_u32(peer(&s.tail, tid)));
+        s.part[tid] = peer_u64(peer(&s.best, tid));
+      }
+      __syncthreads();
+      int first[kCl];
+#pragma unroll
+      for (int c = 0; c < kCl; ++c) {
+        first[c] = n;
+        n += min(s.peer_n[c], kCap);
+        fits = fits && s.peer_n[c] <= kCap;
+        tail += s.fpart[c];
+        given = most(given, s.part[c]);
+      }
+      fits = fits && n <= kCap;
+      if (fits) {
+#pragma unroll
+        for (int c = 1; c < kCl; ++c) {
           const uint32_t src = peer(s.list, c);
-          for (int j = tid; j < m; j += kThreads)
-            *reinterpret_cast<u64*>(&s.list[n + j]) = peer_u64(src + 8 * j);
-          n += m;
+          const int m = s.peer_n[c];
+          for (int j = tid; j < m; j += kThreads) {
+            const u64 v = peer_u64(src + 8 * j);
+            s.list[first[c] + j] = Entry{__uint_as_float((uint32_t)v), (int)(v >> 32)};
+          }
         }
       }
     }
@@ -587,18 +603,19 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
   __syncthreads();
 
   int token = -1;
-  double weight = 0.0;
+  u64 weight = 0;
   bool done = false;
   if (fits) {
     done = choose(s, r, ListSource{s.list, n}, tau, m0, tail, given, &token, &weight);
     __syncthreads();
   }
-  if (!done) choose(s, r, RowSource{r.z, r.V}, -INFINITY, 0.0f, 0.0, 0ull, &token, &weight);
+  if (!done) choose(s, r, RowSource{r.z, r.V}, -INFINITY, 0.0f, 0.0f, 0ull, &token, &weight);
   if (tid == 0) {
     p.token[b] = token;
     if (p.logprob)
       p.logprob[b] =
-          token < 0 ? -INFINITY : __fdiv_rn(r.z[token] - s.best_z, r.T) - (float)log(weight);
+          token < 0 ? -INFINITY : __fdiv_rn(r.z[token] - s.best_z, r.T) -
+                                          logf(__ull2float_rn(weight) * 0x1p-40f);
   }
 }
 
@@ -627,10 +644,12 @@ cudaError_t launch_cluster(const SampleCall& call, cudaStream_t stream) {
 
 int sample_max_vocab() { return kMaxVocab; }
 
-// CTAs per row: as many as keep the launch within one wave (one CTA per SM).
+// CTAs per row: as many as run in one wave.  The CTAs of a cluster share a
+// neighbourhood of the GPU, so larger ones do not fill it: 16 rows of 32768 took
+// 28 us with eight each (the last clusters waited) and 19 with four.
 cudaError_t launch_sample(const SampleCall& call, int sm_count, cudaStream_t stream) {
-  if (call.batch * 8 <= sm_count) return launch_cluster<8>(call, stream);
-  if (call.batch * 4 <= sm_count) return launch_cluster<4>(call, stream);
+  if (call.batch * 12 <= sm_count) return launch_cluster<8>(call, stream);
+  if (call.batch * 5 <= sm_count) return launch_cluster<4>(call, stream);
   if (call.batch * 2 <= sm_count) return launch_cluster<2>(call, stream);
   return launch_cluster<1>(call, stream);
 }
