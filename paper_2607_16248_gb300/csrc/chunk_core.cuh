@@ -253,6 +253,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ unsigned ticket(unsigned* p) {
+  unsigned n;
+  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(n) : "l"(p) : "memory");
+  return n;
+}
 // Two fp32 numbers in one 64-bit register, for the packed instructions.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t v;
@@ -1124,14 +1129,17 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
         uint32_t r[32];
         float o[32];
         tm_load32(to + c, r);
-        tm_load_wait();
-#pragma unroll
-        for (int k = 0; k < 32; ++k) o[k] = __uint_as_float(r[k]) * f0;
-        if (!two) {
-          tm_load32(to + 128 + c, r);
+        if (two) {
           tm_load_wait();
 #pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] = fmaf(__uint_as_float(r[k]), f1, o[k]);
+          for (int k = 0; k < 32; ++k) o[k] = __uint_as_float(r[k]) * f0;
+        } else {
+          uint32_t r1[32];
+          tm_load32(to + 128 + c, r1);
+          tm_load_wait();
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            o[k] = fmaf(__uint_as_float(r1[k]), f1, __uint_as_float(r[k]) * f0);
         }
         // accumulator columns stand in the run order
         uint4 v[4];
@@ -1167,12 +1175,10 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
       const int first = w.base + kItemCost;
       const int c0 = shares.owner(first), c1 = shares.owner(first + w.s.n - 1);
       const int item = (w.bl * p.tiles + w.row_tile) * p.d.hkv + w.head;
-      __threadfence();
       if (!meet_softmax(s, met)) return;
-      if (threadIdx.x == 0) {
-        s.last = atomicAdd(&p.tickets[item], 1u) == (unsigned)(c1 - c0);
-        __threadfence();
-      }
+      // what the CTA wrote and thread 0 saw at the meeting is released with the
+      // ticket, and acquired with the last one
+      if (threadIdx.x == 0) s.last = ticket(&p.tickets[item]) == (unsigned)(c1 - c0);
       if (!meet_softmax(s, met)) return;
       if (s.last) {
         if (threadIdx.x == 0) p.tickets[item] = 0u;
