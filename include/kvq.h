@@ -372,10 +372,12 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  *   out[b, t, i] = softmax_j(q[b, t, i] . K_hat[b, g(i), j] * softmax_scale)
  *                  V_hat[b, g(i), j]
  * A query that stands before the first token (L < n_q) gets a zero output.
+ * Blocks that no query of the call can see are not read and need not be mapped.
  * Dequantized keys and values are rounded once to fp16 (zero + scale * code in
- * one fused multiply-add), the softmax weights too; scores, the running
- * maximum and sum, and the output accumulate in fp32, and the result is
- * rounded once to fp16.
+ * one fused multiply-add; magnitudes up to 32752 stay finite), the softmax
+ * weights too; scores, the running maximum and sum, and the output accumulate in
+ * fp32, and the result is rounded once to fp16: 5e-4 to 9e-4 of the results' rms
+ * from the exact result, where a single rounding gives 2e-4.
  *   q, out       device fp16, element (b, t, i, d) at b * stride[0] + t *
  *                stride[1] + i * stride[2] + d for sequence batch_begin + b;
  *                16-byte aligned; they must not overlap.
@@ -384,6 +386,9 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  *                zeroed once by kvq_workspace_init; calls sharing it must not
  *                overlap on the GPU.
  * Lengths are read on the device; the call can be captured in a CUDA graph.
+ * After KVQ_FLAG_WAIT_TIMEOUT the workspace has to be zeroed again.
+ * Limits: batch_count * n_q * n_q_heads <= 2^28, and the 128-token tiles that all
+ * its row tiles could see must number below 2^31 (KVQ_ERR_SHAPE; split the call).
  */
 typedef struct kvq_chunk_params {
   int32_t n_q;           /* queries per sequence, 1 .. max_len */
@@ -494,8 +499,9 @@ int32_t kvq_sample_max_vocab(void);
  *   logprob      device fp32 [batch] or NULL: d_token - ln(sum of all e_i), the
  *                token's log-probability at temperature T (1 where T <= 0)
  *                before any limit; -inf for a row of -inf alone.
- * The e_i are summed as multiples of 2^-40 in integers, so the kept set does
- * not depend on any order of summation and repeats bit for bit.
+ * The e_i are summed as multiples of 2^-40 in integers where they decide what is
+ * kept (those far below the limits as fp32 numbers in a fixed order), so results
+ * repeat bit for bit.
  * No workspace; calls on different outputs may overlap.
  */
 kvq_status kvq_sample(const float* logits, int64_t logits_stride,

@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include "common.cuh"
+#include "serve.cuh"
 
 namespace kvq {
 

@@ -40,7 +40,7 @@
 // (q1_offset; the queries alike).
 #pragma once
 
-#include "common.cuh"
+#include "serve.cuh"
 
 namespace kvq {
 namespace chunk {

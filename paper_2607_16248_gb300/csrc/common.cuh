@@ -497,32 +497,6 @@ cudaError_t launch_decode_attn_static(const Dims& d, const kvq_cache& cache, con
                                       float* out, float scale_log2, int n_splits,
                                       cudaStream_t stream);
 
-// Chunk attention (chunk.cu): kvq_chunk_params with the scale in the log2
-// domain and the range of sequences.
-struct ChunkCall {
-  int n_q, window, sinks, batch_begin, batch_count;
-  float scale_log2;
-  long long q_stride[3], out_stride[3];
-};
-size_t chunk_workspace_bytes(const Dims& d, int n_q, int batch_count, int sm_count);
-cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __half* q, __half* out,
-                              const ChunkCall& call, int sm_count, void* workspace,
-                              cudaStream_t stream);
-
-// Sampling (sample.cu).
-struct SampleCall {
-  const float *logits, *noise;
-  long long logits_stride, noise_stride;
-  int batch, vocab;
-  const float* temperature;
-  const int32_t* top_k;
-  const float *top_p, *min_p;
-  int32_t* token;
-  float* logprob;
-};
-int sample_max_vocab();
-cudaError_t launch_sample(const SampleCall& call, int sm_count, cudaStream_t stream);
-
 struct DgapDims {
   int batch, vocab, K, hidden, n_chunks;
   float logit_tau;  // gate when f > logit_tau

@@ -23,7 +23,7 @@
 // Sums that decide what is kept are of integers (weights in units of 2^-40) or,
 // for the weights left out of the list, of fp32 numbers in a fixed order.
 
-#include "common.cuh"
+#include "serve.cuh"
 
 namespace kvq {
 
