@@ -1,5 +1,8 @@
 // Host side of the chunk attention: sizes of the work plan, workspace and the
-// kernel of the cache's code widths.
+// kernel of the cache's code widths; the kernel that joins the partials of items
+// that several CTAs shared.
+
+#include <algorithm>
 
 #include "chunk_core.cuh"
 
@@ -7,15 +10,123 @@ namespace kvq {
 
 namespace {
 
+constexpr int kJoinWarps = 8, kFewParts = 4;
+
+// The partials of a split item to results: the CTAs (c, y) share the rows of the
+// item that CTA c left.  In the attention kernel itself the CTA that came last took
+// up to 14 us for this behind all others, and its registers.
+//   up to four partials: eight rows a warp, four lanes a row, so that eight loads
+//   a lane are on their way (y = 0, 8, ...: 64 rows a CTA);
+//   more: a row a warp; each lane finds the weights of one of every 32 partials,
+//   then the weighted rows are summed in the order of the tokens.
+// A partial without a seen token weighs nothing, whatever it holds.
+__global__ void __launch_bounds__(32 * kJoinWarps, 2)
+join_kernel(const __grid_constant__ chunk::Params p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const chunk::Split sp = p.splits[blockIdx.x];
+  if (!sp.valid) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int tr = chunk::kTile << p.streams_rows, n = sp.last - (int)blockIdx.x + 1;
+  const int n_rows = min(tr, p.c.n_q * p.d.gq - sp.row_tile * tr);
+  const auto slot = [&](int i) {  // first row of the i-th partial
+    return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? sp.inside : 0)) * tr;
+  };
+  const auto result = [&](int r) {
+    return p.out + chunk::row_offset(p, p.c.out_stride, sp.bl, sp.head, sp.row_tile * tr + r);
+  };
+  if (n <= kFewParts) {
+    if (blockIdx.y & 7) return;
+    const int r = kJoinWarps * ((int)blockIdx.y + warp) + (lane >> 2);
+    if (r >= n_rows) return;
+    float2 ml[kFewParts];
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kFewParts; ++i) {
+      ml[i] = i < n ? __ldcg(&p.part_ml[slot(i) + r]) : make_float2(0.0f, 0.0f);
+      if (ml[i].y > 0.0f) m = fmaxf(m, ml[i].x);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewParts; ++i) {
+      ml[i].x = ml[i].y > 0.0f ? chunk::exp2_fast(ml[i].x - m) : 0.0f;
+      l += ml[i].y * ml[i].x;
+    }
+    const float f = l > 0.0f ? 1.0f / l : 0.0f;
+    float4 out[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) out[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kFewParts; ++i) {
+      const float x = ml[i].x * f;
+      if (!(x > 0.0f)) continue;
+      const float4* src =
+          reinterpret_cast<const float4*>(p.part_o + (slot(i) + r) * kHeadDim) + (lane & 3);
+      float4 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __ldcg(src + 4 * j);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        out[j].x = fmaf(v[j].x, x, out[j].x);
+        out[j].y = fmaf(v[j].y, x, out[j].y);
+        out[j].z = fmaf(v[j].z, x, out[j].z);
+        out[j].w = fmaf(v[j].w, x, out[j].w);
+      }
+    }
+    uint2* dst = reinterpret_cast<uint2*>(result(r)) + (lane & 3);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      dst[4 * j] = make_uint2(chunk::pack_half2(out[j].x, out[j].y),
+                              chunk::pack_half2(out[j].z, out[j].w));
+    return;
+  }
+  constexpr int kMost = (kMaxSplits + 31) / 32;  // partials a lane
+  const int r = kJoinWarps * blockIdx.y + warp;
+  if (r >= n_rows) return;
+  float2 ml[kMost];
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = 32 * k + lane;
+    ml[k] = i < n ? __ldcg(&p.part_ml[slot(i) + r]) : make_float2(0.0f, 0.0f);
+    if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    ml[k].x = ml[k].y > 0.0f ? chunk::exp2_fast(ml[k].x - m) : 0.0f;
+    l += ml[k].y * ml[k].x;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const float f = l > 0.0f ? 1.0f / l : 0.0f;
+  float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+#pragma unroll 8
+    for (int i = 32 * k; i < min(n, 32 * k + 32); ++i) {
+      const float x = __shfl_sync(0xffffffffu, ml[k].x, i & 31) * f;
+      const float4 v =
+          __ldcg(reinterpret_cast<const float4*>(p.part_o + (slot(i) + r) * kHeadDim) + lane);
+      if (x > 0.0f) {
+        out.x = fmaf(v.x, x, out.x);
+        out.y = fmaf(v.y, x, out.y);
+        out.z = fmaf(v.z, x, out.z);
+        out.w = fmaf(v.w, x, out.w);
+      }
+    }
+  }
+  reinterpret_cast<uint2*>(result(r))[lane] =
+      make_uint2(chunk::pack_half2(out.x, out.y), chunk::pack_half2(out.z, out.w));
+}
+
 // Rows of a (sequence, kv-head) up to this many make one row tile of 128.
 constexpr int kOneTileRows = chunk::kTile;
 
 struct Plan {
   int tiles, streams_rows, rows;  // row tiles per pair, see Params; rows of an item
-  size_t items, o_bytes, ml_bytes, total;
+  size_t o_bytes, ml_bytes, total;
 };
-
-size_t up16(size_t x) { return (x + 15) / 16 * 16; }
 
 Plan plan_of(const Dims& d, int n_q, int batch_count, int ctas) {
   Plan p;
@@ -23,10 +134,10 @@ Plan plan_of(const Dims& d, int n_q, int batch_count, int ctas) {
   p.streams_rows = rows > kOneTileRows ? 1 : 0;
   p.rows = chunk::kTile << p.streams_rows;
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
-  p.items = (size_t)p.tiles * d.hkv * batch_count;
+  (void)batch_count;
   p.o_bytes = (size_t)2 * ctas * p.rows * kHeadDim * sizeof(float);
   p.ml_bytes = (size_t)2 * ctas * p.rows * sizeof(float2);
-  p.total = p.o_bytes + p.ml_bytes + up16(p.items * sizeof(unsigned));
+  p.total = p.o_bytes + p.ml_bytes + (size_t)ctas * sizeof(chunk::Split);
   return p;
 }
 
@@ -52,13 +163,27 @@ cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __hal
   char* w = static_cast<char*>(workspace);
   p.part_o = reinterpret_cast<float*>(w);
   p.part_ml = reinterpret_cast<float2*>(w + plan.o_bytes);
-  p.tickets = reinterpret_cast<unsigned*>(w + plan.o_bytes + plan.ml_bytes);
+  p.splits = reinterpret_cast<chunk::Split*>(w + plan.o_bytes + plan.ml_bytes);
+  cudaError_t e;
   switch (d.bits_k) {
-    case 1: return chunk::launch_k1(p, sm_count, stream);
-    case 2: return chunk::launch_k2(p, sm_count, stream);
-    case 4: return chunk::launch_k4(p, sm_count, stream);
-    default: return chunk::launch_k8(p, sm_count, stream);
+    case 1: e = chunk::launch_k1(p, sm_count, stream); break;
+    case 2: e = chunk::launch_k2(p, sm_count, stream); break;
+    case 4: e = chunk::launch_k4(p, sm_count, stream); break;
+    default: e = chunk::launch_k8(p, sm_count, stream); break;
   }
+  if (e != cudaSuccess) return e;
+  const int rows = (int)std::min<long long>(plan.rows, (long long)call.n_q * d.gq);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sm_count, (rows + kJoinWarps - 1) / kJoinWarps);
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, join_kernel, p);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace kvq

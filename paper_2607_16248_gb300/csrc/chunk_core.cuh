@@ -10,8 +10,8 @@
 // end and every CTA (one per SM) takes an equal contiguous share: a long cache
 // with few rows is split over many CTAs and a whole prompt leaves no tail of
 // half-empty waves.  An item that is shared leaves partials (unnormalised
-// row, maximum, sum) in the workspace; the CTA that finishes last merges them
-// in the order of the tokens, so results repeat bit for bit.
+// row, maximum, sum) in the workspace; a second, small kernel (chunk.cu) joins
+// them in the order of the tokens, so results repeat bit for bit.
 //
 // A CTA.  Per step (128 rows, half a key tile of 64 tokens): S = Q K^T (fp16
 // operands in shared memory, fp32 in tensor memory), softmax by the four warps
@@ -81,9 +81,14 @@ struct Smem {
   int walk[kSoftmaxWarps][2][16];      // a softmax warp's item and the next one (Walk)
   int start_seq, start_tile, start_head, start_step;
   uint32_t tmem;
-  int abort, last;
+  int abort;
   float m[kTile], l[kTile];            // stream 1's statistics of a shared row tile
-  float row_m[2 * kTile], row_f[2 * kTile];
+};
+
+// An item that the shares of CTAs c .. last divide, left by CTA c for the kernel
+// that joins the partials.
+struct Split {
+  int valid, inside, last, bl, row_tile, head;
 };
 
 struct Params {
@@ -97,7 +102,7 @@ struct Params {
   int streams_rows;  // 1: items of 256 rows (a row tile per stream), 0: of 128
   float* part_o;     // [2 * CTAs][rows of an item][128]
   float2* part_ml;   // [2 * CTAs][rows of an item]
-  unsigned* tickets; // [items]
+  Split* splits;     // [CTAs]
 };
 
 // ---------------------------------------------------------------------------
@@ -252,11 +257,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-__device__ __forceinline__ unsigned ticket(unsigned* p) {
-  unsigned n;
-  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(n) : "l"(p) : "memory");
-  return n;
 }
 // Two fp32 numbers in one 64-bit register, for the packed instructions.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
@@ -878,88 +878,6 @@ __device__ __forceinline__ void put_rows(const unsigned char* stage, const Rows&
   __syncwarp();
 }
 
-// The partials of CTAs c0 .. c1 to results, by all softmax threads: first each
-// row's maximum and sum (256 / rows threads a row share the CTAs), then a warp
-// per row, four channels a lane.
-// `inside`: c0's share begins in an earlier item, so this one is in its slot 1;
-// every other CTA's share begins here (slot 0).
-__device__ __forceinline__ bool merge_item(const Params& p, Smem& s, const Walk& w, int c0, int c1,
-                                           bool inside, uint32_t& met) {
-  const int tr = kTile << p.streams_rows, tid = threadIdx.x, tile = w.row_tile;
-  const int n_rows = min(tr, p.c.n_q * p.d.gq - tile * tr);
-  const auto slot_of = [&](int c) {
-    return (long long)(2 * c + (inside && c == c0 ? 1 : 0)) * tr;
-  };
-  int parts = 1;
-  while (parts < 32 && 2 * parts * n_rows <= 32 * kSoftmaxWarps) parts *= 2;
-  for (int r0 = 0; r0 < n_rows; r0 += 32 * kSoftmaxWarps / parts) {
-    const int r = r0 + tid / parts, q = tid % parts;
-    float m = -INFINITY, l = 0.0f;
-    if (r < n_rows) {
-#pragma unroll 4
-      for (int c = c0 + q; c <= c1; c += parts) {
-        const float2 ml = __ldcg(&p.part_ml[slot_of(c) + r]);
-        if (ml.y > 0.0f) {
-          const float mm = fmaxf(m, ml.x);
-          l = l * exp2_fast(m - mm) + ml.y * exp2_fast(ml.x - mm);
-          m = mm;
-        }
-      }
-    }
-    for (int o = 1; o < parts; o *= 2) {
-      const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o);
-      const float mm = fmaxf(m, m1);
-      if (mm > -INFINITY) l = l * exp2_fast(m - mm) + l1 * exp2_fast(m1 - mm);
-      m = mm;
-    }
-    if (r < n_rows && q == 0) {
-      s.row_m[r] = m > -INFINITY ? m : 0.0f;
-      s.row_f[r] = l > 0.0f ? 1.0f / l : 0.0f;
-    }
-  }
-  if (!meet_softmax(s, met)) return false;
-  // eight rows a warp, so that many loads are on their way
-  constexpr int kRows = 8;
-  const int ch = 4 * (tid & 31);
-#pragma unroll 1
-  for (int r0 = kRows * (tid >> 5); r0 < n_rows; r0 += kRows * kSoftmaxWarps) {
-    float4 o[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 1
-    for (int c = c0; c <= c1; ++c) {
-      const long long first = slot_of(c);
-      float2 ml[kRows];
-      float4 v[kRows];
-#pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const long long pr = first + min(r0 + i, n_rows - 1);
-        ml[i] = __ldcg(&p.part_ml[pr]);
-        v[i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + pr * kHeadDim + ch));
-      }
-#pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        // a partial without a seen token counts nothing
-        const float x =
-            ml[i].y > 0.0f ? exp2_fast(ml[i].x - s.row_m[min(r0 + i, n_rows - 1)]) : 0.0f;
-        o[i].x = fmaf(v[i].x, x, o[i].x);
-        o[i].y = fmaf(v[i].y, x, o[i].y);
-        o[i].z = fmaf(v[i].z, x, o[i].z);
-        o[i].w = fmaf(v[i].w, x, o[i].w);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      if (r0 + i >= n_rows) break;
-      const float f = s.row_f[r0 + i];
-      __half* dst = p.out + row_offset(p, p.c.out_stride, w.bl, w.head, tile * tr + r0 + i) + ch;
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_half2(o[i].x * f, o[i].y * f),
-                                                  pack_half2(o[i].z * f, o[i].w * f));
-    }
-  }
-  return true;
-}
-
 template <int BK>
 __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, int u1,
                                              const Shares& shares) {
@@ -1169,23 +1087,12 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
       if (valid && !direct) p.part_ml[pr] = make_float2(m, l);
       tc_before();
     }
-    if (!direct) {
-      // the last of the item's CTAs merges its partials, in the order of the
-      // tokens
+    if (!direct && w.i0 == 0 && threadIdx.x == 0) {
       const int first = w.base + kItemCost;
-      const int c0 = shares.owner(first), c1 = shares.owner(first + w.s.n - 1);
-      const int item = (w.bl * p.tiles + w.row_tile) * p.d.hkv + w.head;
-      if (!meet_softmax(s, met)) return;
-      // what the CTA wrote and thread 0 saw at the meeting is released with the
-      // ticket, and acquired with the last one
-      if (threadIdx.x == 0) s.last = ticket(&p.tickets[item]) == (unsigned)(c1 - c0);
-      if (!meet_softmax(s, met)) return;
-      if (s.last) {
-        if (threadIdx.x == 0) p.tickets[item] = 0u;
-        if (!merge_item(p, s, w, c0, c1, shares.begin(c0) < w.base, met)) return;
-      }
+      p.splits[blockIdx.x] = Split{1, u0 < w.base ? 1 : 0, shares.owner(first + w.s.n - 1), w.bl,
+                                   w.row_tile, w.head};
     }
-    if (!meet_softmax(s, met)) return;  // s.m, s.last and both accumulators may be written again
+    if (!meet_softmax(s, met)) return;  // s.m, s.l and both accumulators may be written again
     ++items;
   }
 }
@@ -1200,6 +1107,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   Smem& s = *reinterpret_cast<Smem*>(raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
+  if (tid == 0) p.splits[blockIdx.x].valid = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // Units of every (sequence, row tile), summed over the threads in order.
   const int groups = p.c.batch_count * p.tiles;
   const int per = (int)((uint32_t)(groups + kThreads - 1) / kThreads);
