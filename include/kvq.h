@@ -382,11 +382,10 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  *                stride[1] + i * stride[2] + d for sequence batch_begin + b;
  *                16-byte aligned; they must not overlap.
  *   params       below.
- *   workspace    device, >= kvq_chunk_workspace_bytes(cfg, n_q, batch_count),
- *                zeroed once by kvq_workspace_init; calls sharing it must not
- *                overlap on the GPU.
+ *   workspace    device, >= kvq_chunk_workspace_bytes(cfg, n_q, batch_count);
+ *                needs no initialisation; calls sharing it must not overlap on
+ *                the GPU.
  * Lengths are read on the device; the call can be captured in a CUDA graph.
- * After KVQ_FLAG_WAIT_TIMEOUT the workspace has to be zeroed again.
  * Limits: batch_count * n_q * n_q_heads <= 2^28, and the 128-token tiles that all
  * its row tiles could see must number below 2^31 (KVQ_ERR_SHAPE; split the call).
  */
@@ -489,7 +488,8 @@ int32_t kvq_sample_max_vocab(void);
  *   token the kept i with the largest d_i - ln(-ln u_i), lowest index on ties:
  *         with u uniform in [0, 1) an exact draw from the kept tokens'
  *         renormalised probabilities.
- * T <= 0 (or NaN) takes the first token of the order.
+ * T <= 0 (or NaN) takes the first token of the order; a T beyond 1e-30 .. 1e30
+ * counts as that bound.
  *   logits       device fp32, row b at b * logits_stride, read only.
  *   noise        device fp32 u, row b at b * noise_stride; only kept tokens'
  *                numbers are read.  NULL: every row takes its first token.

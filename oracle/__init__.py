@@ -18,6 +18,8 @@ quant      asymmetric b-bit group quantizer, bit packing, residual window
 attention  GQA decode attention softmax(q K^T / sqrt(d)) V over the cache
 dgap       top-K window, risk features, detector, gate, corrector, merge
 drift      offline drift metrics (C(alpha), c_t, d_loc, y_t) and the K_b rule
+chunk      causal attention of a chunk of new tokens, sliding window and sinks
+sample     the next token by temperature, top-k, top-p, min-p from given numbers
 """
 
-from . import quant, attention, dgap, drift  # noqa: F401
+from . import quant, attention, dgap, drift, chunk, sample  # noqa: F401

@@ -1227,15 +1227,19 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
 
 template <int BK, int BV>
 cudaError_t launch_widths(const Params& p, int ctas, cudaStream_t stream) {
-  const cudaError_t e =
-      cudaFuncSetAttribute(chunk_attn_kernel<BK, BV>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)sizeof(Smem));
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = once_per_device(done, [] {
+    const cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<BK, BV>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)sizeof(Smem));
+    if (e != cudaSuccess) return e;
+    // the register shares wait for registers that a smaller launch would lack
+    cudaFuncAttributes attr;
+    const cudaError_t ea = cudaFuncGetAttributes(&attr, chunk_attn_kernel<BK, BV>);
+    if (ea != cudaSuccess) return ea;
+    return attr.numRegs < kRegsLaunch ? cudaErrorInvalidConfiguration : cudaSuccess;
+  });
   if (e != cudaSuccess) return e;
-  // the register shares below wait for registers that a smaller launch lacks
-  cudaFuncAttributes attr;
-  const cudaError_t ea = cudaFuncGetAttributes(&attr, chunk_attn_kernel<BK, BV>);
-  if (ea != cudaSuccess) return ea;
-  if (attr.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
   chunk_attn_kernel<BK, BV><<<ctas, kThreads, sizeof(Smem), stream>>>(p);
   return cudaGetLastError();
 }

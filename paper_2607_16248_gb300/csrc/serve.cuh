@@ -4,7 +4,23 @@
 
 #include "common.cuh"
 
+#include <atomic>
+
 namespace kvq {
+
+// Runs `prepare` (function attributes) at a kernel's first launch on each device;
+// `done` is the kernel's own.
+template <typename F>
+cudaError_t once_per_device(std::atomic<unsigned long long>& done, F prepare) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  const cudaError_t p = prepare();
+  if (p == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return p;
+}
 
 // Chunk attention (chunk.cu): kvq_chunk_params with the scale in the log2
 // domain and the range of sequences.

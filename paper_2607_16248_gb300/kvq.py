@@ -218,6 +218,7 @@ class QuantKVCache:
         self.cfg = cfg
         self.n_pages = n_pages
         c = cfg.c()
+        self._cfg_ref = ctypes.byref(c)
         if n_pages is None:
             total, self.offsets = cfg.layout()
         else:
@@ -246,6 +247,7 @@ class QuantKVCache:
                 ctypes.byref(c), ctypes.c_void_p(self.buffer.data_ptr()),
                 ctypes.c_void_p(self.pool.data_ptr()), int(n_pages),
                 ctypes.c_void_p(self.block_table.data_ptr()), ctypes.byref(self._c)))
+        self._c_ref = ctypes.byref(self._c)
         self.reset()
 
     @property
@@ -433,25 +435,30 @@ def kvq_decode_attn_noalloc(cache: QuantKVCache, q, out, softmax_scale=0.0, n_sp
 
 
 def chunk_workspace(cfg: CacheConfig, n_q, batch_count=None, device="cuda"):
-    """A zeroed workspace for kvq_chunk_attn of n_q queries per sequence."""
+    """A workspace for kvq_chunk_attn of n_q queries per sequence."""
     c = cfg.c()
     n = lib().kvq_chunk_workspace_bytes(ctypes.byref(c), n_q,
                                         cfg.batch if batch_count is None else batch_count)
     if n == 0:
         raise KvqError(1, last_error())
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _rows(t, name):
-    """The pointer of an fp16 CUDA tensor [..., 128] whose last dimension is
+def _address(t, dtype, name):
+    """Data pointer of a CUDA tensor of ``dtype`` whose last dimension is
     contiguous (the others may have any strides)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype != torch.float16:
-        raise TypeError(f"{name} must be torch.float16, got {t.dtype}")
-    if t.stride(-1) != 1:
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+def _strides(t):
+    # the stride of a dimension of size 1 says nothing
+    return tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape))
 
 
 def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_scale=0.0,
@@ -462,25 +469,23 @@ def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_
     shape.  window > 0: each query sees the ``window`` newest tokens up to its
     own and the first ``sinks`` tokens.  n_q = 1 is the windowed form of a
     decode step."""
-    cfg = cache.cfg
-    if q.dim() != 4 or q.shape[2] != cfg.n_q_heads or q.shape[3] != cfg.head_dim:
+    cfg, shape = cache.cfg, q.shape
+    if len(shape) != 4 or shape[2] != cfg.n_q_heads or shape[3] != cfg.head_dim:
         raise ValueError(f"q must be [batch_count, n_q, {cfg.n_q_heads}, {cfg.head_dim}]")
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
-    if out.shape != q.shape:
+        out = torch.empty(shape, dtype=torch.float16, device=q.device)
+    elif out.shape != shape:
         raise ValueError("out must have the shape of q")
-    batch_count, n_q = q.shape[:2]
+    batch_count, n_q = shape[0], shape[1]
     if workspace is None:
         workspace = chunk_workspace(cfg, n_q, batch_count, q.device)
-    # the stride of a dimension of size 1 says nothing
-    strides = [[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)] for t in (q, out)]
-    p = _ChunkParams(n_q, int(window), int(sinks), float(softmax_scale),
-                     (ctypes.c_int64 * 3)(*strides[0]), (ctypes.c_int64 * 3)(*strides[1]))
-    c = cfg.c()
-    _check(lib().kvq_chunk_attn(ctypes.byref(c), ctypes.byref(cache._c), _rows(q, "q"),
-                                _rows(out, "out"), ctypes.byref(p), batch_begin, batch_count,
-                                _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
-                                _stream(stream)))
+    p = _ChunkParams(n_q, int(window), int(sinks), float(softmax_scale), _strides(q),
+                     _strides(out))
+    _check(lib().kvq_chunk_attn(cache._cfg_ref, cache._c_ref, _address(q, torch.float16, "q"),
+                                _address(out, torch.float16, "out"), ctypes.byref(p),
+                                batch_begin, batch_count,
+                                _address(workspace, torch.uint8, "workspace"),
+                                workspace.numel(), _stream(stream)))
     return out
 
 
@@ -495,17 +500,12 @@ def sample_outputs(batch, device="cuda"):
                 logprob=torch.empty(batch, dtype=torch.float32, device=device))
 
 
-def _logit_rows(t, shape, name):
-    """Pointer and row stride of an fp32 CUDA tensor [batch, vocab]."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype != torch.float32:
-        raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
+def _per_row(t, shape, dtype, name):
+    if t is None:
+        return None
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0)
+    return _address(t, dtype, name)
 
 
 def kvq_sample(logits, noise=None, temperature=None, top_k=None, top_p=None, min_p=None,
@@ -515,25 +515,21 @@ def kvq_sample(logits, noise=None, temperature=None, top_k=None, top_p=None, min
     temperature, top_p, min_p (fp32) and top_k (int32) are device tensors
     [batch] or None; noise None is greedy.  Returns a dict of device tensors:
     token (int32) and logprob (fp32, may be None in ``outputs``)."""
-    if logits.dim() != 2:
+    shape = logits.shape
+    if len(shape) != 2:
         raise ValueError("logits must be [batch, vocab]")
-    B, V = logits.shape
-    o = sample_outputs(B, logits.device) if outputs is None else outputs
-
-    def row(t, dt, name):
-        if t is None:
-            return ctypes.c_void_p(None)
-        if t.shape != (B,):
-            raise ValueError(f"{name} must be [{B}]")
-        return _dev(t, dt, name)
-
-    z, zs = _logit_rows(logits, (B, V), "logits")
-    u, us = (ctypes.c_void_p(None), 0) if noise is None else _logit_rows(noise, (B, V), "noise")
+    B, V = shape
     f32 = torch.float32
-    _check(lib().kvq_sample(z, zs, u, us, B, V, row(temperature, f32, "temperature"),
-                            row(top_k, torch.int32, "top_k"), row(top_p, f32, "top_p"),
-                            row(min_p, f32, "min_p"), row(o["token"], torch.int32, "token"),
-                            row(o.get("logprob"), f32, "logprob"), _stream(stream)))
+    z = _address(logits, f32, "logits")
+    u = _per_row(noise, shape, f32, "noise")
+    o = sample_outputs(B, logits.device) if outputs is None else outputs
+    row = shape[:1]
+    _check(lib().kvq_sample(
+        z, logits.stride(0), u, 0 if noise is None else noise.stride(0), B, V,
+        _per_row(temperature, row, f32, "temperature"), _per_row(top_k, row, torch.int32, "top_k"),
+        _per_row(top_p, row, f32, "top_p"), _per_row(min_p, row, f32, "min_p"),
+        _per_row(o["token"], row, torch.int32, "token"),
+        _per_row(o.get("logprob"), row, f32, "logprob"), _stream(stream)))
     return o
 
 
