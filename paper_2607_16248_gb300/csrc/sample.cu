@@ -440,15 +440,31 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(SampleCall p) {
         if (lane >= o) ci += a, wi += d;
       }
       const float all_w = __shfl_sync(0xffffffffu, wi, 31);
+      // The weights of the first tokens of the sample say little about the row (one
+      // far above the rest stands for V / 8192 others): those up to the range that
+      // reaches eight tokens do not count.
+      float head = 0.0f;
+      {
+        float cc = ci - cs, ww = wi - ws;
+        bool there = false;
+        for (int j = 0; j < kPer; ++j) {
+          cc += c[j];
+          ww += w[j];
+          if (!there && cc >= 8.0f) there = true, head = ww;
+        }
+        const unsigned reached = __ballot_sync(0xffffffffu, there);
+        head = __shfl_sync(0xffffffffu, head, reached ? __ffs(reached) - 1 : 31);
+      }
       const float rate = (float)taken / (float)r.V;
       // how many sampled tokens and which weight the list should reach down to
       const float most_c = 0.6f * kCap * rate;
       float want_c = 0.0f, want_w = 0.0f;
       if (r.k > 0) {
-        want_c = 1.5f * r.k * rate + 8.0f;
+        // the first k hold about k * rate sampled tokens, six deviations more at most
+        want_c = 1.5f * r.k * rate + 6.0f * sqrtf(r.k * rate) + 8.0f;
       } else if (r.p < 1.0f) {
         want_c = 2048.0f * rate;
-        want_w = all_w * (1.0f - 0.125f * (1.0f - r.p));
+        want_w = all_w - 0.125f * (1.0f - r.p) * (all_w - head);
       }
       int mine = kCoarse;  // first range that reaches both
       int last = -1;       // last range within the list's room
