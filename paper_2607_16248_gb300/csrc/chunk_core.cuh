@@ -29,6 +29,21 @@
 // The running maximum of a row moves only when a score is more than 8 (in log2)
 // above it, so the accumulator is rescaled rarely; weights stay below 2^8.
 //
+// What bounds it.  A prompt chunk: the tensor cores by count (4 * 128 flops a
+// query, visible key and head), measured the chain around them: 1.23 PFLOP/s of a
+// cuBLAS product's 1.92 for a chunk of 2048 tokens over 64k (K1V1, groups of 5,
+// 2.21 ms); with the softmax, or the restoring of codes, left out of a working copy
+// it is 1.84, or 1.97 ms, and the products alone take 1.7.  Few rows over a long
+// cache: the restoring of codes, about 1900 cycles a 32-token block and warp (four
+// drafts in 16 sequences of 8k to 32k, K2V2: 212 us, 1.6 us a tile and SM), where the
+// bytes take 39.  The smallest calls: the chain of launch, lengths, first tile,
+// partials and their join, about 19 us.
+// Tried and dropped: products issued by a lane of a diverged warp (2 to 4 times the
+// issue time), one warp for both streams' products, steps of 128 tokens with one
+// score buffer a stream, all 128 scores of a row in registers, a block's loads held
+// in a second set of registers, the weights' sum in place of the row maximum as
+// the sign for a new maximum.
+//
 // Tile layouts (128-byte swizzle, [half][row][128 bytes]).  Tokens of an
 // 8-token run stand in the order 0 4 1 5 2 6 3 7 and so do the channels of the
 // accumulator: two elements four apart come out of a code word in one
