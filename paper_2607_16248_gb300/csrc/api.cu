@@ -519,8 +519,10 @@ kvq_status kvq_chunk_attn(const kvq_config* cfg, const kvq_cache* cache, const u
       p->softmax_scale == 0.0f ? 1.0f / sqrtf((float)kHeadDim) : p->softmax_scale;
   call.scale_log2 = scale * 1.4426950408889634f;
   call.n_q = p->n_q;
-  call.window = p->window;
-  call.sinks = p->window ? p->sinks : 0;
+  // no token stands at max_len or beyond: larger numbers say the same, and sums with
+  // positions stay within 32 bits
+  call.window = p->window < cfg->max_len ? p->window : cfg->max_len;
+  call.sinks = !p->window ? 0 : p->sinks < cfg->max_len ? p->sinks : cfg->max_len;
   call.batch_begin = batch_begin;
   call.batch_count = batch_count;
   trace("kvq_chunk_attn batch [%d, %d) n_q %d window %d sinks %d heads %d/%d bits K%dV%d",

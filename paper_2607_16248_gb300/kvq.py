@@ -472,6 +472,8 @@ def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_
     cfg, shape = cache.cfg, q.shape
     if len(shape) != 4 or shape[2] != cfg.n_q_heads or shape[3] != cfg.head_dim:
         raise ValueError(f"q must be [batch_count, n_q, {cfg.n_q_heads}, {cfg.head_dim}]")
+    if max(window, sinks) >= 2 ** 31:
+        raise ValueError("window and sinks must be less than 2^31")
     if out is None:
         out = torch.empty(shape, dtype=torch.float16, device=q.device)
     elif out.shape != shape:
