@@ -444,6 +444,16 @@ def chunk_workspace(cfg: CacheConfig, n_q, batch_count=None, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
+def _made_on(stream, make, *args):
+    """make(*args) with ``stream`` (None: the current one) as the current stream:
+    what a call allocates for itself belongs to the stream that it launches on, so
+    the allocator hands its memory to no other stream while the call still runs."""
+    if stream is None:
+        return make(*args)
+    with torch.cuda.stream(stream):
+        return make(*args)
+
+
 def _address(t, dtype, name):
     """Data pointer of a CUDA tensor of ``dtype`` whose last dimension is
     contiguous (the others may have any strides)."""
@@ -475,12 +485,12 @@ def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_
     if max(window, sinks) >= 2 ** 31:
         raise ValueError("window and sinks must be less than 2^31")
     if out is None:
-        out = torch.empty(shape, dtype=torch.float16, device=q.device)
+        out = _made_on(stream, lambda: torch.empty(shape, dtype=torch.float16, device=q.device))
     elif out.shape != shape:
         raise ValueError("out must have the shape of q")
     batch_count, n_q = shape[0], shape[1]
     if workspace is None:
-        workspace = chunk_workspace(cfg, n_q, batch_count, q.device)
+        workspace = _made_on(stream, chunk_workspace, cfg, n_q, batch_count, q.device)
     p = _ChunkParams(n_q, int(window), int(sinks), float(softmax_scale), _strides(q),
                      _strides(out))
     _check(lib().kvq_chunk_attn(cache._cfg_ref, cache._c_ref, _address(q, torch.float16, "q"),
@@ -524,7 +534,7 @@ def kvq_sample(logits, noise=None, temperature=None, top_k=None, top_p=None, min
     f32 = torch.float32
     z = _address(logits, f32, "logits")
     u = _per_row(noise, shape, f32, "noise")
-    o = sample_outputs(B, logits.device) if outputs is None else outputs
+    o = _made_on(stream, sample_outputs, B, logits.device) if outputs is None else outputs
     row = shape[:1]
     _check(lib().kvq_sample(
         z, logits.stride(0), u, 0 if noise is None else noise.stride(0), B, V,
