@@ -38,6 +38,11 @@ constexpr int kBins = 2048;      // value ranges of the selection
 constexpr int kEdge = 1024;      // tokens of one range ranked directly
 constexpr int kSample = 8 * kThreads, kCoarse = 512;  // sampled logits, ranges of 1/16 nat
 constexpr float kPerNat = 16.0f;
+// An unlimited draw is made in the stream with keys relative to the sampled maximum.
+// They are taken when the row's maximum is at most this many units of T above it: the
+// three roundings of a key that can win then add up to less than 1e-5.  Further up the
+// noise would be lost in the rounding of (z - m0) / T.
+constexpr float kDrawReach = 32.0f;
 
 struct Entry {
   float z;
@@ -267,7 +272,8 @@ __device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u6
 
 // Selection and draw on a source.  tau: the source holds every token at or above
 // it; tail: the weights of the others, relative to a logit of m0.  *weight: all
-// tokens' weights.  False: the source does not hold what the limits need.
+// tokens' weights.  given: the winner of an unlimited draw made relative to m0, or 0.
+// False: the source does not hold what the limits need, or m0 was too low for the draw.
 template <typename S>
 __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, float tail,
                        u64 given, int* token, u64* weight) {
@@ -289,6 +295,7 @@ __device__ bool choose(Sm& s, const Row& r, const S& src, float tau, float m0, f
   if (top == 0) return false;
   const float zmax = key_value(top);
   const auto dist = [&](float z) { return __fdiv_rn(z - zmax, r.T); };
+  if (given && !(dist(m0) >= -kDrawReach)) return false;
   const auto weight_of = [&](float z) { return mass_of(expf(dist(z))); };
   // ranges of equal width from the largest value to the least of the source
   const float width = zmax - key_value(~low);
