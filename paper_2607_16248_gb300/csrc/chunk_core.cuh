@@ -364,7 +364,8 @@ __device__ __forceinline__ Span span_of(const Params& p, int bl, int tile) {
   s.p1 = s.L - p.c.n_q + token_of_row(p, r1);
   s.lo = p.c.window ? max(0, max(s.p0, 0) - p.c.window + 1) : 0;
   s.first = s.lo >> 7;
-  s.n_sink = min((p.c.sinks + kTile - 1) >> 7, s.first);  // sinks is 0 without a window
+  // sinks is 0 without a window; the sum passes 2^31 in the largest caches
+  s.n_sink = min((int)(((uint32_t)p.c.sinks + (kTile - 1)) >> 7), s.first);
   s.n = s.n_sink + (max(s.p1, 0) >> 7) - s.first + 1;
   return s;
 }
@@ -674,8 +675,9 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
     // index of unit i's block; kNone where there is nothing to restore
     constexpr int kNone = -0x7fffffff - 1;
     const auto index = [&](int i) {
+      if (i >= w.i1) return kNone;
       const int t0 = token(i);
-      if (i >= w.i1 || t0 >= lq || !seen(t0)) return kNone;
+      if (t0 >= lq || !seen(t0)) return kNone;
       return table ? __ldg(table + (t0 >> 5)) : t0 >> 5;
     };
     const auto address = [&](int e) -> const char* {
@@ -951,10 +953,11 @@ __device__ __forceinline__ void softmax_role(const Params& p, Smem& s, int u0, i
         const int t0 = w.s.tile(w.i0 + (st >> two)) * kTile + kStep * (two ? st & 1 : x);
         // every token of the step is seen by every row of the item
         const bool whole = w.s.p0 >= t0 + kStep - 1 &&
-                           (!p.c.window || t0 > w.s.p1 - p.c.window || t0 + kStep <= p.c.sinks);
-        if (!whole)
-          mask_row(sb, (valid ? pos : -1) - t0, p.c.window ? pos - p.c.window - t0 : -1 - t0,
-                   p.c.sinks - t0);
+                           (!p.c.window || t0 > w.s.p1 - p.c.window || t0 <= p.c.sinks - kStep);
+        // the last token behind the window, -1 if there is none (positions and
+        // windows each reach 2^31)
+        const int behind = p.c.window ? max(max(pos, 0) - p.c.window, -1) : -1;
+        if (!whole) mask_row(sb, (valid ? pos : -1) - t0, behind - t0, p.c.sinks - t0);
         uint32_t r[2][32];
         tm_load32(sb, r[0]);
         tm_load32(sb + 32, r[1]);
