@@ -219,9 +219,9 @@ __device__ u64 threshold(Sm& s, const S& src, BinOf bin_of, MassOf weight_of, u6
   find_range(s, goal, by_mass);
   const int range = s.range;
   const u64 before_c = s.before_c, before_m = s.before_m;
-  if (range < 0) return 0;
   if (tid == 0) s.n_edge = 0, s.cut_key = 0, s.cut_mass = 0;
-  __syncthreads();
+  __syncthreads();  // ahead of any return: the next limit's find_range writes s.range again
+  if (range < 0) return 0;
   for_each(src, [&](const Entry& e) {
     if (bin_of(e.z) == range) {
       const int at = atomicAdd(&s.n_edge, 1);
