@@ -496,7 +496,7 @@ def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_
     _check(lib().kvq_chunk_attn(cache._cfg_ref, cache._c_ref, _address(q, torch.float16, "q"),
                                 _address(out, torch.float16, "out"), ctypes.byref(p),
                                 batch_begin, batch_count,
-                                _address(workspace, torch.uint8, "workspace"),
+                                _dev(workspace, torch.uint8, "workspace"),
                                 workspace.numel(), _stream(stream)))
     return out
 
