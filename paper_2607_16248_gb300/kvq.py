@@ -434,11 +434,19 @@ def kvq_decode_attn_noalloc(cache: QuantKVCache, q, out, softmax_scale=0.0, n_sp
     return out
 
 
+def _in_32_bits(names, *numbers):
+    """ctypes cuts an int to its argument's 32 bits without a word."""
+    for x in numbers:
+        if not -2147483648 <= x <= 2147483647:
+            raise ValueError(f"{names} must fit 32 bits (got {x})")
+
+
 def chunk_workspace(cfg: CacheConfig, n_q, batch_count=None, device="cuda"):
     """A workspace for kvq_chunk_attn of n_q queries per sequence."""
     c = cfg.c()
-    n = lib().kvq_chunk_workspace_bytes(ctypes.byref(c), n_q,
-                                        cfg.batch if batch_count is None else batch_count)
+    batch_count = cfg.batch if batch_count is None else batch_count
+    _in_32_bits("n_q and batch_count", n_q, batch_count)
+    n = lib().kvq_chunk_workspace_bytes(ctypes.byref(c), n_q, batch_count)
     if n == 0:
         raise KvqError(1, last_error())
     return torch.empty(n, dtype=torch.uint8, device=device)
@@ -482,8 +490,8 @@ def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_
     cfg, shape = cache.cfg, q.shape
     if len(shape) != 4 or shape[2] != cfg.n_q_heads or shape[3] != cfg.head_dim:
         raise ValueError(f"q must be [batch_count, n_q, {cfg.n_q_heads}, {cfg.head_dim}]")
-    if max(window, sinks) >= 2 ** 31:
-        raise ValueError("window and sinks must be less than 2^31")
+    _in_32_bits("window and sinks", window, sinks)
+    _in_32_bits("batch_begin, batch_count and n_q", batch_begin, shape[0], shape[1])
     if out is None:
         out = _made_on(stream, lambda: torch.empty(shape, dtype=torch.float16, device=q.device))
     elif out.shape != shape:
@@ -531,6 +539,7 @@ def kvq_sample(logits, noise=None, temperature=None, top_k=None, top_p=None, min
     if len(shape) != 2:
         raise ValueError("logits must be [batch, vocab]")
     B, V = shape
+    _in_32_bits("batch and vocab", B, V)
     f32 = torch.float32
     z = _address(logits, f32, "logits")
     u = _per_row(noise, shape, f32, "noise")
