@@ -391,7 +391,9 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  *                the GPU.
  * Lengths are read on the device; the call can be captured in a CUDA graph.
  * Limits: batch_count * n_q * n_q_heads <= 2^28, and the 128-token tiles that all
- * its row tiles could see must number below 2^31 (KVQ_ERR_SHAPE; split the call).
+ * its row tiles (of 256 query rows of a kv-head, or of 128 where there are no more)
+ * could see at max_len, with three for each row tile, must number below 2^31
+ * (KVQ_ERR_SHAPE; split the call).
  */
 typedef struct kvq_chunk_params {
   int32_t n_q;           /* queries per sequence, 1 .. max_len */

@@ -467,9 +467,8 @@ static kvq_status check_chunk_sizes(const kvq_config* cfg, int32_t n_q, int32_t 
     return fail(KVQ_ERR_SHAPE, "batch_count must be in [1, %d] (got %d)", cfg->batch, batch_count);
   if ((long long)n_q * cfg->n_q_heads * batch_count > (1LL << 28))
     return fail(KVQ_ERR_SHAPE, "batch_count * n_q * n_q_heads must be <= 2^28");
-  // key tiles over all row tiles, counted in 32 bits
-  const long long row_tiles = ((long long)n_q * (cfg->n_q_heads / cfg->n_kv_heads) + 127) / 128;
-  if (row_tiles * cfg->n_kv_heads * batch_count * (cfg->max_len / 128 + 2) >= (1LL << 31))
+  // the kernel counts its units of work in 32 bits
+  if (chunk_most_units(make_dims(*cfg), n_q, batch_count) >= (1LL << 31))
     return fail(KVQ_ERR_SHAPE, "too many tiles in one call: split the chunk or the batch");
   return KVQ_OK;
 }

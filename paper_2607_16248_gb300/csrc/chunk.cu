@@ -143,6 +143,11 @@ Plan plan_of(const Dims& d, int n_q, int batch_count, int ctas) {
 
 }  // namespace
 
+long long chunk_most_units(const Dims& d, int n_q, int batch_count) {
+  const long long items = (long long)plan_of(d, n_q, batch_count, 1).tiles * d.hkv * batch_count;
+  return items * ((d.max_len + chunk::kTile - 1LL) / chunk::kTile + chunk::kItemCost);
+}
+
 size_t chunk_workspace_bytes(const Dims& d, int n_q, int batch_count, int sm_count) {
   return plan_of(d, n_q, batch_count, sm_count).total;
 }

@@ -29,6 +29,8 @@ struct ChunkCall {
   float scale_log2;
   long long q_stride[3], out_stride[3];
 };
+// The most units of work that the kernel can count for a call (full sequences).
+long long chunk_most_units(const Dims& d, int n_q, int batch_count);
 size_t chunk_workspace_bytes(const Dims& d, int n_q, int batch_count, int sm_count);
 cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __half* q, __half* out,
                               const ChunkCall& call, int sm_count, void* workspace,
