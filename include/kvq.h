@@ -407,7 +407,9 @@ typedef struct kvq_chunk_params {
 } kvq_chunk_params;
 
 /* Workspace bytes of kvq_chunk_attn (0 on an invalid config, n_q outside
- * [1, max_len] or batch_count outside [1, batch]). */
+ * [1, max_len], batch_count outside [1, batch] or a call beyond the limits).  Two
+ * partial row tiles per SM: one size while a kv-head's n_q * n_q_heads / n_kv_heads
+ * rows are at most 128, about twice that above, whatever batch_count and max_len. */
 size_t kvq_chunk_workspace_bytes(const kvq_config* cfg, int32_t n_q, int32_t batch_count);
 
 kvq_status kvq_chunk_attn(const kvq_config* cfg, const kvq_cache* cache,

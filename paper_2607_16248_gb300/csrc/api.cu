@@ -475,7 +475,7 @@ static kvq_status check_chunk_sizes(const kvq_config* cfg, int32_t n_q, int32_t 
 
 size_t kvq_chunk_workspace_bytes(const kvq_config* cfg, int32_t n_q, int32_t batch_count) {
   if (check_chunk_sizes(cfg, n_q, batch_count) != KVQ_OK) return 0;
-  return chunk_workspace_bytes(make_dims(*cfg), n_q, batch_count, sm_count());
+  return chunk_workspace_bytes(make_dims(*cfg), n_q, sm_count());
 }
 
 kvq_status kvq_chunk_attn(const kvq_config* cfg, const kvq_cache* cache, const uint16_t* q,
@@ -509,7 +509,7 @@ kvq_status kvq_chunk_attn(const kvq_config* cfg, const kvq_cache* cache, const u
     call.out_stride[i] = p->out_stride[i];
   }
   const Dims d = make_dims(*cfg);
-  const size_t need = chunk_workspace_bytes(d, p->n_q, batch_count, sm_count());
+  const size_t need = chunk_workspace_bytes(d, p->n_q, sm_count());
   if (!workspace) return fail(KVQ_ERR_ARG, "workspace is NULL");
   if (!aligned16(workspace)) return fail(KVQ_ERR_ALIGN, "workspace must be 16-byte aligned");
   if (ws_bytes < need)

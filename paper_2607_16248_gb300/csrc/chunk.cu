@@ -128,13 +128,12 @@ struct Plan {
   size_t o_bytes, ml_bytes, total;
 };
 
-Plan plan_of(const Dims& d, int n_q, int batch_count, int ctas) {
+Plan plan_of(const Dims& d, int n_q, int ctas) {
   Plan p;
   const long long rows = (long long)n_q * d.gq;
   p.streams_rows = rows > kOneTileRows ? 1 : 0;
   p.rows = chunk::kTile << p.streams_rows;
   p.tiles = (int)((rows + p.rows - 1) / p.rows);
-  (void)batch_count;
   p.o_bytes = (size_t)2 * ctas * p.rows * kHeadDim * sizeof(float);
   p.ml_bytes = (size_t)2 * ctas * p.rows * sizeof(float2);
   p.total = p.o_bytes + p.ml_bytes + (size_t)ctas * sizeof(chunk::Split);
@@ -144,18 +143,18 @@ Plan plan_of(const Dims& d, int n_q, int batch_count, int ctas) {
 }  // namespace
 
 long long chunk_most_units(const Dims& d, int n_q, int batch_count) {
-  const long long items = (long long)plan_of(d, n_q, batch_count, 1).tiles * d.hkv * batch_count;
+  const long long items = (long long)plan_of(d, n_q, 1).tiles * d.hkv * batch_count;
   return items * ((d.max_len + chunk::kTile - 1LL) / chunk::kTile + chunk::kItemCost);
 }
 
-size_t chunk_workspace_bytes(const Dims& d, int n_q, int batch_count, int sm_count) {
-  return plan_of(d, n_q, batch_count, sm_count).total;
+size_t chunk_workspace_bytes(const Dims& d, int n_q, int sm_count) {
+  return plan_of(d, n_q, sm_count).total;
 }
 
 cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __half* q, __half* out,
                               const ChunkCall& call, int sm_count, void* workspace,
                               cudaStream_t stream) {
-  const Plan plan = plan_of(d, call.n_q, call.batch_count, sm_count);
+  const Plan plan = plan_of(d, call.n_q, sm_count);
   chunk::Params p;
   p.d = d;
   p.cache = cache;

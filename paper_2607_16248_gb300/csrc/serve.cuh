@@ -31,7 +31,7 @@ struct ChunkCall {
 };
 // The most units of work that the kernel can count for a call (full sequences).
 long long chunk_most_units(const Dims& d, int n_q, int batch_count);
-size_t chunk_workspace_bytes(const Dims& d, int n_q, int batch_count, int sm_count);
+size_t chunk_workspace_bytes(const Dims& d, int n_q, int sm_count);
 cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __half* q, __half* out,
                               const ChunkCall& call, int sm_count, void* workspace,
                               cudaStream_t stream);

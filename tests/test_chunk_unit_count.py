@@ -28,3 +28,18 @@ def test_units(batch, hq, hkv, n_q, max_len, fits):
                           max_len=max_len)
     n = kvq.lib().kvq_chunk_workspace_bytes(ctypes.byref(cfg.c()), n_q, batch)
     assert (n > 0) == fits, kvq.last_error()
+
+
+def test_workspace_takes_one_of_two_sizes():
+    build.build()
+
+    def size(n_q, batch, count, max_len=4096):
+        cfg = kvq.CacheConfig(batch=batch, n_q_heads=32, n_kv_heads=8, bits_k=2, bits_v=2,
+                              max_len=max_len)
+        return kvq.lib().kvq_chunk_workspace_bytes(ctypes.byref(cfg.c()), n_q, count)
+
+    small = {size(n_q, b, c, m) for n_q in (1, 32) for b, c in ((1, 1), (64, 3), (64, 64))
+             for m in (64, 65536)}
+    large = {size(n_q, b, c) for n_q in (33, 4096) for b, c in ((1, 1), (64, 3), (64, 64))}
+    assert len(small) == len(large) == 1
+    assert 0 < small.pop() < large.pop()
