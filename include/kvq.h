@@ -531,6 +531,15 @@ kvq_status kvq_sample(const float* logits, int64_t logits_stride,
 kvq_status kvq_selftest_wait_timeout(uint32_t* flag, void* stream);
 
 /*
+ * kvq_selftest_chunk_wait_timeout — the same for the waits between the roles of
+ * kvq_chunk_attn's kernel (limit ~1 s there, ~10 ms here): the warps of `role` (0
+ * softmax, 1 loading, 2 issuing) wait where nothing arrives, the other softmax and
+ * loading warps with the kernel's own limit.  All leave once the first give up, and
+ * the way out that the kernel takes sets KVQ_FLAG_WAIT_TIMEOUT in *flag.
+ */
+kvq_status kvq_selftest_chunk_wait_timeout(int32_t role, uint32_t* flag, void* stream);
+
+/*
  * Offline drift metrics (Sec. 4.1 "Adaptive recovery-window selection",
  * Sec. 4.2 "Offline supervision and calibration").  Tooling for paired
  * traces: each row holds one decode step's FP16-cache logits z_fp and

@@ -635,6 +635,16 @@ kvq_status kvq_selftest_wait_timeout(uint32_t* flag, void* stream) {
                      "kvq_selftest_wait_timeout launch");
 }
 
+kvq_status kvq_selftest_chunk_wait_timeout(int32_t role, uint32_t* flag, void* stream) {
+  if (role < 0 || role > 2) return fail(KVQ_ERR_ARG, "role must be 0, 1 or 2 (got %d)", role);
+  if (!flag) return fail(KVQ_ERR_ARG, "flag is NULL");
+  if (reinterpret_cast<uintptr_t>(flag) & 3u)
+    return fail(KVQ_ERR_ALIGN, "flag must be 4-byte aligned");
+  return cuda_status(launch_chunk_wait_selftest(role, reinterpret_cast<int32_t*>(flag), 20000000u,
+                                                static_cast<cudaStream_t>(stream)),
+                     "kvq_selftest_chunk_wait_timeout launch");
+}
+
 int32_t kvq_drift_max_vocab(void) { return drift_max_vocab(); }
 
 kvq_status kvq_drift_metrics(const float* z_fp, const float* z_q, int32_t rows, int32_t vocab,

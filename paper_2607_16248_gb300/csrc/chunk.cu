@@ -120,6 +120,31 @@ join_kernel(const __grid_constant__ chunk::Params p) {
       make_uint2(chunk::pack_half2(out.x, out.y), chunk::pack_half2(out.z, out.w));
 }
 
+// The waits of the attention kernel's roles: the warps of `role` (0 softmax, 1
+// loading, 2 issuing) wait with a short limit on a barrier at which nothing arrives,
+// the softmax and loading warps otherwise with the usual one, the issuing warps have
+// finished.  All leave when the first ones give up.
+__global__ void __launch_bounds__(chunk::kThreads, 1)
+wait_selftest_kernel(int role, int32_t* flag, uint32_t limit) {
+  extern __shared__ __align__(1024) unsigned char raw[];
+  chunk::Smem& s = *reinterpret_cast<chunk::Smem*>(raw);
+  const int warp = threadIdx.x >> 5;
+  const int mine = warp < chunk::kSoftmaxWarps ? 0 : warp < chunk::kIssueWarp ? 1 : 2;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      chunk::bar_init(&s.k_full[i], 1);
+      chunk::bar_init(&s.drained[i], 1);
+    }
+    s.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (mine == role) chunk::warp_wait(s, &s.k_full[0], 0, limit);
+  else if (mine < 2) chunk::warp_wait(s, &s.k_full[1], 0);
+  __syncwarp();
+  chunk::leave(s, flag);
+}
+
 // Rows of a (sequence, kv-head) up to this many make one row tile of 128.
 constexpr int kOneTileRows = chunk::kTile;
 
@@ -149,6 +174,19 @@ long long chunk_most_units(const Dims& d, int n_q, int batch_count) {
 
 size_t chunk_workspace_bytes(const Dims& d, int n_q, int sm_count) {
   return plan_of(d, n_q, sm_count).total;
+}
+
+cudaError_t launch_chunk_wait_selftest(int role, int32_t* flag, uint32_t limit_cycles,
+                                       cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = once_per_device(done, [] {
+    return cudaFuncSetAttribute(wait_selftest_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)sizeof(chunk::Smem));
+  });
+  if (e != cudaSuccess) return e;
+  wait_selftest_kernel<<<1, chunk::kThreads, sizeof(chunk::Smem), stream>>>(role, flag,
+                                                                            limit_cycles);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __half* q, __half* out,

@@ -155,12 +155,13 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
 }
 // Bounded: after the limit, or once another role has given up, it returns
 // false; every role then leaves its loop.
-__device__ __forceinline__ bool bar_wait(Smem& s, uint64_t* b, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(Smem& s, uint64_t* b, uint32_t parity,
+                                         uint32_t limit = kWaitLimit) {
   if (bar_try(b, parity)) return true;
   const uint32_t t0 = (uint32_t)clock();
 #pragma unroll 1
   while (!bar_try(b, parity)) {
-    if (*reinterpret_cast<volatile int*>(&s.abort) || (uint32_t)clock() - t0 > kWaitLimit) {
+    if (*reinterpret_cast<volatile int*>(&s.abort) || (uint32_t)clock() - t0 > limit) {
       *reinterpret_cast<volatile int*>(&s.abort) = 1;
       return false;
     }
@@ -168,8 +169,9 @@ __device__ __forceinline__ bool bar_wait(Smem& s, uint64_t* b, uint32_t parity) 
   return true;
 }
 // The same for a whole warp (all lanes leave together).
-__device__ __forceinline__ bool warp_wait(Smem& s, uint64_t* b, uint32_t parity) {
-  return __all_sync(0xffffffffu, bar_wait(s, b, parity));
+__device__ __forceinline__ bool warp_wait(Smem& s, uint64_t* b, uint32_t parity,
+                                          uint32_t limit = kWaitLimit) {
+  return __all_sync(0xffffffffu, bar_wait(s, b, parity, limit));
 }
 // One arrival for a warp, behind what all its lanes did (32 arrivals on one
 // barrier are served one by one).
@@ -200,6 +202,33 @@ __device__ __forceinline__ void tc_commit(uint32_t leader, uint64_t* b) {
       : "memory");
 }
 
+// One of the warp's lanes, the same each time.
+__device__ __forceinline__ uint32_t elect_lane() {
+  uint32_t e;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(e));
+  return e;
+}
+constexpr int kIssueWarp = kSoftmaxWarps + kLoadWarps;
+// All threads, once every role has left its loop.  If one gave up, whichever it was,
+// the products in flight end (bounded) before tensor and shared memory are given back,
+// and the flag word says so.
+__device__ __forceinline__ void leave(Smem& s, int32_t* flag) {
+  tc_before();
+  __syncthreads();
+  tc_after();
+  if (!*reinterpret_cast<volatile int*>(&s.abort)) return;  // nobody writes it any more
+  const int x = (int)(threadIdx.x >> 5) - kIssueWarp;
+  if (x == 0 || x == 1) {
+    tc_commit(elect_lane(), &s.drained[x]);
+    const uint32_t t0 = (uint32_t)clock();
+    while (!bar_try(&s.drained[x], 0) && (uint32_t)clock() - t0 < kWaitLimit) {
+    }
+  }
+  if (threadIdx.x == 0) atomicOr(reinterpret_cast<unsigned*>(flag), KVQ_FLAG_WAIT_TIMEOUT);
+  __syncthreads();
+}
+
 // D[128 x N] (+)= A B, fp16 in, fp32 out, K = 16, by the warp's elected lane
 // (`leader`); all lanes run it, so that the descriptors stay uniform.
 // A in shared memory.
@@ -219,12 +248,6 @@ __device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, 
       " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
       : "memory");
-}
-__device__ __forceinline__ uint32_t elect_lane() {
-  uint32_t e;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}"
-               : "=r"(e));
-  return e;
 }
 __device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
@@ -1203,7 +1226,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       if (++tl == p.tiles) tl = 0, ++sq;
     }
   }
-  constexpr int kIssueWarp = kSoftmaxWarps + kLoadWarps;
   if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
                      sptr(&s.tmem))
@@ -1228,24 +1250,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     __syncwarp();
   } else {
     regs_down<kRegsIssue>();
-    if (warp < kIssueWarp + 2) {
-      issue_role<BK, BV>(p, s, u0, u1, warp - kIssueWarp);
-      if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s.abort))) {
-        // products in flight end before the tile memory is given back
-        uint64_t* drained = &s.drained[warp - kIssueWarp];
-        tc_commit(elect_lane(), drained);
-        const uint32_t t0 = (uint32_t)clock();
-        while (!bar_try(drained, 0) && (uint32_t)clock() - t0 < kWaitLimit) {
-        }
-        if (lane == 0)
-          atomicOr(reinterpret_cast<unsigned*>(p.cache.seq_len + p.d.batch), KVQ_FLAG_WAIT_TIMEOUT);
-      }
-      __syncwarp();
-    }
+    if (warp < kIssueWarp + 2) issue_role<BK, BV>(p, s, u0, u1, warp - kIssueWarp);
+    __syncwarp();
   }
-  tc_before();
-  __syncthreads();
-  tc_after();
+  leave(s, p.cache.seq_len + p.d.batch);
   if (warp == kIssueWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }

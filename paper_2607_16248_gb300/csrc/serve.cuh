@@ -35,6 +35,8 @@ size_t chunk_workspace_bytes(const Dims& d, int n_q, int sm_count);
 cudaError_t launch_chunk_attn(const Dims& d, const kvq_cache& cache, const __half* q, __half* out,
                               const ChunkCall& call, int sm_count, void* workspace,
                               cudaStream_t stream);
+cudaError_t launch_chunk_wait_selftest(int role, int32_t* flag, uint32_t limit_cycles,
+                                       cudaStream_t stream);
 
 // Sampling (sample.cu).
 struct SampleCall {

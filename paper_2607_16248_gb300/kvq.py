@@ -33,7 +33,7 @@ EXPORTS = (
     "kvq_decode_attn_noalloc", "kvq_chunk_workspace_bytes", "kvq_chunk_attn",
     "kvq_sample_max_vocab", "kvq_sample", "dgap_workspace_bytes",
     "dgap_restore", "kvq_drift_max_vocab", "kvq_drift_metrics", "kvq_drift_window",
-    "kvq_selftest_wait_timeout",
+    "kvq_selftest_wait_timeout", "kvq_selftest_chunk_wait_timeout",
 )
 NOALLOC_SCRATCH_BYTES = 4 << 20
 
@@ -117,6 +117,7 @@ def lib():
             "dgap_restore": (I32, [par_p, P, I32, I32, P, P, P, P, P, P, P, SZ, P]),
             "kvq_drift_max_vocab": (I32, []),
             "kvq_selftest_wait_timeout": (I32, [P, P]),
+            "kvq_selftest_chunk_wait_timeout": (I32, [I32, P, P]),
             "kvq_drift_metrics": (I32, [P, P, I32, I32, ctypes.POINTER(_DriftParams),
                                         P, P, P, P, P, P]),
             "kvq_drift_window": (I32, [P, I32, I32, F32, P, P, P]),
@@ -684,4 +685,13 @@ def selftest_wait_timeout(stream=None):
     a copy that never arrives ran out (KVQ_FLAG_WAIT_TIMEOUT expected)."""
     flag = torch.zeros(1, dtype=torch.int32, device="cuda")
     _check(lib().kvq_selftest_wait_timeout(_dev(flag, torch.int32, "flag"), _stream(stream)))
+    return flag
+
+
+def selftest_chunk_wait_timeout(role, stream=None):
+    """kvq_selftest_chunk_wait_timeout: the flag word after the waits of a role
+    (0 softmax, 1 loading, 2 issuing) of the chunk attention ran out."""
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    _check(lib().kvq_selftest_chunk_wait_timeout(role, _dev(flag, torch.int32, "flag"),
+                                                 _stream(stream)))
     return flag
