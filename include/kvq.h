@@ -368,10 +368,22 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  * of sequence b stands at position p = L - n_q + t and sees token j when
  *   0 <= j <= p  and  (window == 0  or  j > p - window  or  j < sinks),
  * packed tokens in quantized form and the residual window in fp16, as
- * kvq_decode_attn does (n_q = 1 without a window is the same operator).
+ * kvq_decode_attn does (n_q = 1 without a window is the same operator, with the
+ * roundings below).
  *   out[b, t, i] = softmax_j(q[b, t, i] . K_hat[b, g(i), j] * softmax_scale)
  *                  V_hat[b, g(i), j]
  * A query that stands before the first token (L < n_q) gets a zero output.
+ * Every query sees the cache as it is at length L: tokens that the chunk's own append
+ * pushed out of the residual window are seen as codes, also by its first queries, for
+ * which a decode step would have found them in fp16.
+ * Drafts.  A call on the next token and drafts behind it (n_q in all, from length L0)
+ * may be followed by lowering seq_len[b] to L' >= L0 + 1, ordered on the stream, as
+ * long as no group left the window behind the first of them: Lq(L0 + n_q) = Lq(L0 + 1),
+ * i.e. the append wrote no block in [Lq(L0 + 1) / 32, Lq(L0 + n_q) / 32).  The tokens
+ * up to L' are then untouched, and every query has seen just what a decode step would
+ * have.  Otherwise lowering the length is an error that nothing detects: the window's
+ * slot of a token that became codes may hold a draft.  Near a group's end, take fewer
+ * drafts.
  * Blocks that no query of the call can see are not read and need not be mapped.
  * Dequantized keys and values are rounded once to fp16 (zero + scale * code in
  * one fused multiply-add; magnitudes up to 32752 stay finite), the softmax
