@@ -384,9 +384,12 @@ kvq_status kvq_decode_attn_noalloc(const kvq_config* cfg, const kvq_cache* cache
  * have.  Otherwise lowering the length is an error that nothing detects: the window's
  * slot of a token that became codes may hold a draft.  Near a group's end, take fewer
  * drafts.
- * Blocks that no query of the call can see are not read and need not be mapped.
+ * Blocks that no query of the call can see are not read and need not be mapped.  In
+ * the others a key may be anything where a query does not see it, but values have to
+ * be finite for all of them: a value that a query does not see counts with weight zero.
  * Dequantized keys and values are rounded once to fp16 (zero + scale * code in
- * one fused multiply-add; magnitudes up to 32752 stay finite), the softmax
+ * one fused multiply-add, to which a 1-bit code's scale goes halved: below 2^-13 that
+ * is up to 2^-24 off; magnitudes up to 32752 stay finite), the softmax
  * weights too; scores, the running maximum and sum, and the output accumulate in
  * fp32, and the result is rounded once to fp16: 5e-4 to 9e-4 of the results' rms
  * from the exact result, where a single rounding gives 2e-4.  A weight keeps its 11
@@ -506,8 +509,9 @@ int32_t kvq_sample_max_vocab(void);
  *   M     the tokens with e_i >= m (m <= 0: all);
  *   kept  P and M, and the first token of the order in any case; never -inf;
  *   token the kept i with the largest d_i - ln(-ln u_i), lowest index on ties:
- *         with u uniform in [0, 1) an exact draw from the kept tokens'
- *         renormalised probabilities.
+ *         with u uniform in [0, 1) a draw from the kept tokens' renormalised
+ *         probabilities, as exact as u is fine: with 24-bit numbers -ln(-ln u) ends
+ *         at 16.6, and one row of 150000 kept tokens in a hundred holds the top one.
  * T <= 0 (or NaN) takes the first token of the order; a T beyond 1e-30 .. 1e30
  * counts as that bound.
  *   logits       device fp32, row b at b * logits_stride, read only.

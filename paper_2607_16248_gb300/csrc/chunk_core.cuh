@@ -585,6 +585,8 @@ __device__ __forceinline__ void restore_part(const Part<B>& c, int k, unsigned c
     const int row = 32 * (key ? j : k) + 8 * (gid >> 1) + (gid & 1);
     unsigned char* base = tile + half * kHalfBytes + row * 128;
     const uint32_t x0 = (uint32_t)(chunk ^ (gid & 1)) << 4;
+    // Halves of the scales, to meet codes that read 2.0: exact down to 2^-13; below, the
+    // last bit of a scale (the spacing of the inputs there, 2^-24) may be lost.
     __half2 s[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) s[r] = __hmul2(as_half2(c.s[r]), __float2half2_rn(0.5f));
