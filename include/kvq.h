@@ -53,8 +53,9 @@ typedef enum kvq_status {
 
 /* Device-side flag bits (cache flag word). */
 #define KVQ_FLAG_OVERFLOW 1u /* an append would have passed max_len */
-#define KVQ_FLAG_WAIT_TIMEOUT 2u /* an attention kernel's copy wait gave up (~2 s);
-                                    its output for that call is not valid */
+#define KVQ_FLAG_WAIT_TIMEOUT 2u /* a wait inside an attention kernel gave up (~2 s,
+                                    ~1 s in kvq_chunk_attn's); its output for that
+                                    call is not valid */
 #define KVQ_FLAG_BAD_PAGE 4u /* a paged cache's block table mapped a block that a
                                 call had to read or write outside [0, n_pages):
                                 the write was skipped, and an output that needed

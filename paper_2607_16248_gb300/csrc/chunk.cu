@@ -13,8 +13,8 @@ namespace {
 constexpr int kJoinWarps = 8, kFewParts = 4;
 
 // The partials of a split item to results: the CTAs (c, y) share the rows of the
-// item that CTA c left.  In the attention kernel itself the CTA that came last took
-// up to 14 us for this behind all others, and its registers.
+// item that CTA c left.  (In the attention kernel itself it would fall to the CTA that
+// comes last, behind all others, and take registers from the scores.)
 //   up to four partials: eight rows a warp, four lanes a row, so that eight loads
 //   a lane are on their way (y = 0, 8, ...: 64 rows a CTA);
 //   more: a row a warp; each lane finds the weights of one of every 32 partials,

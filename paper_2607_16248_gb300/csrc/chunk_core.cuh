@@ -21,7 +21,7 @@
 // at most 128 rows) the two halves of the key tiles, joined at the end.  Each
 // stream has two buffers of scores, so a softmax does not wait for the products
 // around it: with steps of 128 tokens and one buffer, a step's chain of score
-// product, softmax and value product (about 5000 cycles) set the pace.
+// product, softmax and value product set the pace.
 //   warps 0-3, 4-7  softmax of streams 0 and 1, queries in, results out
 //   warps 8-11      keys: one 32-token block each, codes -> fp16 tile
 //   warps 12-15     values, the same
@@ -33,17 +33,24 @@
 // What bounds it.  A prompt chunk: the tensor cores by count (4 * 128 flops a
 // query, visible key and head), measured the chain around them: 1.23 PFLOP/s of a
 // cuBLAS product's 1.92 for a chunk of 2048 tokens over 64k (K1V1, groups of 5,
-// 2.21 ms); with the softmax, or the restoring of codes, left out of a working copy
-// it is 1.84, or 1.97 ms, and the products alone take 1.7.  Few rows over a long
-// cache: the restoring of codes, about 1900 cycles a 32-token block and warp (four
-// drafts in 16 sequences of 8k to 32k, K2V2: 212 us, 1.6 us a tile and SM), where the
-// bytes take 39.  The smallest calls: the chain of launch, lengths, first tile,
-// partials and their join, about 19 us.
-// Tried and dropped: products issued by a lane of a diverged warp (2 to 4 times the
-// issue time), one warp for both streams' products, steps of 128 tokens with one
-// score buffer a stream, all 128 scores of a row in registers, a block's loads held
-// in a second set of registers, the weights' sum in place of the row maximum as
-// the sign for a new maximum.
+// 2.2 ms).  Counters of chunks over 4k at 1, 2 and 4 bits: the tensor pipe 34 to 41%
+// of the active cycles, issue slots 52 to 60, no unit full; warps wait for loads and
+// for one another.  Few rows over a long cache: the restoring of every code into a
+// whole tile, whatever the rows that use it (four drafts in 16 sequences of 8k to 32k,
+// K2V2: 212 us, 1.6 us a tile and SM), where the bytes take 39.  The smallest calls:
+// the chain of launch, lengths, first tile, partials and their join, 18 to 22 us.
+// Tried and dropped: products issued by a lane of a diverged warp, one warp for both
+// streams' products, steps of 128 tokens with one score buffer a stream, all 128
+// scores of a row in registers, a block's loads held in a second set of registers,
+// the weights' sum in place of the row maximum as the sign for a new maximum.
+//
+// Roundings.  Operands are fp16: keys, values and weights are rounded once each, which
+// leaves 3e-4 to 9e-4 of the results' rms where the rounding of exact results leaves
+// 2e-4; most of it comes from keys with channels far above the others.  The scales
+// cannot move to the queries, as the decode kernel has it: every 32-token block has its
+// own, and one tile of queries meets them all.  The keys' low parts in a second product
+// would add half to the products and 64 KB of tiles to the 215 KB in use.  Sums, maxima
+// and accumulators are fp32.
 //
 // Tile layouts (128-byte swizzle, [half][row][128 bytes]).  Tokens of an
 // 8-token run stand in the order 0 4 1 5 2 6 3 7 and so do the channels of the
@@ -768,8 +775,7 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
 
 constexpr uint32_t kColS = 0, kColO = 256;  // tensor memory columns: S0 S1 O0 O1, 128 each
 
-// The products of stream x, by one warp (one for both streams took as long to
-// issue them as they take).
+// The products of stream x, by one warp.
 template <int BK, int BV>
 __device__ __forceinline__ void issue_role(const Params& p, Smem& s, int u0, int u1, int x) {
   constexpr uint32_t kIdS = instr_desc(BK != 1, kStep), kIdO = instr_desc(BV != 1, kHeadDim);

@@ -16,11 +16,11 @@
 // row, a limit near 1, ties beyond the list) the row itself takes its place in
 // the last two steps: the result is the same, later.
 //
-// Bound: the stream, 4 bytes a logit, for many rows (128 rows of 152063 by top-p 0.9:
-// 68 us, where the bytes take 11 and reading them once more from L2 takes 8; the
-// list of 12000 tokens a row takes the rest); for one row the chain of a dozen
-// barriers and two cluster exchanges (128256: 12 us greedy, 21 with top-k and top-p).
-// Thresholds found bit by bit, one CTA a row, took 2.4 to 2.8 ms.
+// Bound: many rows, the stream, 4 bytes a logit, and what follows it on the lists
+// (128 rows of 152063 by top-p 0.9, about 12000 tokens a list: 67 us, where the bytes
+// take 11); one row, the chain of a dozen barriers and two cluster exchanges (128256:
+// 13 us greedy, 22 with top-k and top-p).  The row in place of its list costs 60 us
+// (128256, 20 free tokens, k 50) to 250 (128 rows of 152064 by top-p 0.99).
 //
 // Sums that decide what is kept are of integers (weights in units of 2^-40) or,
 // for the weights left out of the list, of fp32 numbers in a fixed order.
@@ -140,7 +140,7 @@ struct RowSource {
 };
 
 // f on every token of a source that is not -inf; eight loads at a time from memory
-// (one by one, a pass over a row of 152064 by one CTA took 50 us).
+// (one by one, a row of 152064 by top-p 0.99 took 284 us and takes 221).
 template <typename S, typename F>
 __device__ __forceinline__ void for_each(const S& src, F f) {
   constexpr int kAtOnce = S::kAtOnce;
@@ -686,8 +686,11 @@ cudaError_t launch_cluster(const SampleCall& call, cudaStream_t stream) {
 int sample_max_vocab() { return kMaxVocab; }
 
 // CTAs per row: as many as run in one wave.  The CTAs of a cluster share a
-// neighbourhood of the GPU, so larger ones do not fill it: 16 rows of 32768 took
-// 28 us with eight each (the last clusters waited) and 19 with four.
+// neighbourhood of the GPU, so larger ones do not fill it, and those left over wait for
+// a second wave.  Rows of 152064 by top-p 0.9, one, two, four and eight CTAs a row:
+// 12 rows 63, 51, 46 and 43 us; 16 rows 63, 51, 47 and 57; 32 rows 64, 52, 47 and 73;
+// 64 rows 64, 52, 87 and 113; 80 rows 64, 98, 97 and 138.  (From 31 rows on four CTAs
+// would need more clusters than 152 SMs are sure to hold, so two are taken there.)
 cudaError_t launch_sample(const SampleCall& call, int sm_count, cudaStream_t stream) {
   if (call.batch * 12 <= sm_count) return launch_cluster<8>(call, stream);
   if (call.batch * 5 <= sm_count) return launch_cluster<4>(call, stream);
