@@ -315,7 +315,7 @@ def prepare(case, seed):
         st["cache"] = kvq.Block8Cache(cfg, tensors={n: st[n] for n in (
             "k_codes", "v_codes", "scales", "k_ring", "v_ring")}, block_table=st["table"])
         if c["kind"] == "attend":
-            st["workspace"] = kvq.kvq8_workspace(cfg, st["max_new"])
+            st["workspace"] = kvq.block8_workspace(cfg, st["max_new"])
     return st
 
 
@@ -472,11 +472,11 @@ def run(state):
             bias_ids=st["bias_ids"], bias_values=st["bias_values"],
             bias_starts=st["bias_starts"], mask=st["mask"])
     if c["kind"] == "attend":
-        return kvq.kvq8_attn(st["cache"], st["q"], st["lengths"], starts=st["starts"],
+        return kvq.kvq_block8_attn(st["cache"], st["q"], st["lengths"], starts=st["starts"],
                              max_new=st["max_new"], window=c["window"], sinks=c["sinks"],
                              out=st["out"], workspace=st["workspace"])
     q, k, v = st["qkv"].split([c["hq"], c["hkv"], c["hkv"]], 1)
-    kvq.kvq8_append(st["cache"], k, v, st["lengths"], starts=st["starts"], q=q,
+    kvq.kvq_block8_append(st["cache"], k, v, st["lengths"], starts=st["starts"], q=q,
                     q_out=st["q_out"], cos=st["cos"], sin=st["sin"], paired=bool(c["paired"]))
     return [st[x] for x in ("q_out", "k_codes", "v_codes", "scales", "k_ring", "v_ring")]
 
