@@ -11,8 +11,13 @@
  *                    chunks, draft tokens), with a sliding window and sinks
  *   dgap_restore     features, detector, gate, top-K corrector, sparse merge
  *                    on the step's logits (Sec. 4.1-4.3, Eqs. 2, 6, 11-13)
+ *   kvq_adjust_logits  penalties for repeated tokens, biases and a grammar's mask
+ *                    on rows of logits
  *   kvq_sample       the next token of each row of logits by temperature,
  *                    top-k, top-p and min-p from given random numbers
+ *   kvq_block8_*     append with position rotation and attention of ragged
+ *                    batches on a paged cache of 8-bit blocks, for layers or
+ *                    runs that stay wider than KbVb
  *   kvq_drift_*      offline drift metrics on paired FP16 / low-bit logits and
  *                    the recovery-window rule (Sec. 4.1, Sec. 4.2)
  *
@@ -60,6 +65,10 @@ typedef enum kvq_status {
                                 call had to read or write outside [0, n_pages):
                                 the write was skipped, and an output that needed
                                 the block is not valid */
+#define KVQ_FLAG_BAD_BATCH 8u /* kvq_block8_*: starts out of order or outside
+                                 [0, n_tokens], more new tokens than max_new or than
+                                 the sequence's length, or a position outside the
+                                 tables: see kvq_block8_batch */
 
 /*
  * Cache configuration.  KbVb with b_k = bits_k and b_v = bits_v (Sec. 3.1
@@ -535,6 +544,203 @@ kvq_status kvq_sample(const float* logits, int64_t logits_stride,
                       const int32_t* top_k, const float* top_p,
                       const float* min_p, int32_t* token, float* logprob,
                       void* stream);
+
+/*
+ * Block-8 cache: keys and values in e4m3 (OCP 8-bit floating point, 4 exponent and 3
+ * mantissa bits, largest value 448), with one fp32 scale for each block of 32
+ * tokens and kv-head, on pages; the tokens behind the last whole block in the
+ * inputs' 16-bit type.  All tensors belong to the caller, who may also fill them.
+ *   block   tokens [32 j, 32 j + 32) of a sequence.  A block gets its codes by the
+ *           append that completes it, from the 16-bit values x of its 32 x 128
+ *           elements (keys after rotation):
+ *             scale = clamp(RN32(max |x| / 448), 2^-60, 2^60), 1 if all are zero
+ *             code  = RN_e4m3(RN32(x / scale)), at most 448 in magnitude
+ *           and stands for scale * code.
+ *   ring    the token at position p also sits in slot p mod 64 of the ring while it
+ *           is among the last two blocks, so a block's codes do not depend on how
+ *           many calls appended it, and up to 32 of the newest tokens may be
+ *           dropped again: lower the lengths given to the next call by at most 32
+ *           in all below the largest so far, and the next append takes the kept
+ *           part of a broken block from the ring.
+ */
+#define KVQ_F16 0  /* IEEE binary16 */
+#define KVQ_BF16 1 /* bfloat16 */
+#define KVQ_F32 2  /* IEEE binary32 (logits only) */
+#define KVQ_BLOCK8_RING 64
+typedef struct kvq_block8_config {
+  int32_t batch;      /* 1 .. 8192 */
+  int32_t n_q_heads;  /* query head i reads kv-head i / (n_q_heads / n_kv_heads): */
+  int32_t n_kv_heads; /* an integer in [1, 32] */
+  int32_t head_dim;   /* 128 */
+  int32_t block;      /* 32 */
+  int32_t max_len;    /* a positive multiple of 32 */
+  int32_t dtype;      /* KVQ_F16 or KVQ_BF16: q, k, v, out and the rings */
+} kvq_block8_config;
+
+/* Device pointers, 16-byte aligned (flags: 4). */
+typedef struct kvq_block8_cache {
+  uint8_t* k_codes;           /* [n_pages][n_kv_heads][32][128] e4m3 */
+  uint8_t* v_codes;           /* the same */
+  float* scales;              /* [n_pages][n_kv_heads][2]: keys', values'; > 0 */
+  uint16_t* k_ring;           /* [batch][n_kv_heads][64][128] */
+  uint16_t* v_ring;           /* the same */
+  const int32_t* block_table; /* [batch][max_len / 32]: a block's page; entries of
+                                 blocks that no call reads or writes may be anything */
+  uint32_t* flags;            /* one word, KVQ_FLAG_* are OR-ed in */
+  int32_t n_pages;            /* 1 .. 2^31 - 1; pages * n_kv_heads <= 2^26 */
+} kvq_block8_cache;
+
+/*
+ * The new tokens of a call, the same for the append and the attention of all layers:
+ * rows [starts[b], starts[b + 1]) of q, k, v and the outputs are the newest tokens of
+ * sequence b, oldest first, the last of them at position lengths[b] - 1.  Rows
+ * outside all ranges are left alone, and so is a sequence without new tokens.
+ * Ranges that are out of order, reach outside [0, n_tokens] or hold more than max_new
+ * tokens set KVQ_FLAG_BAD_BATCH, a length above max_len sets KVQ_FLAG_OVERFLOW; the
+ * calls leave such a sequence's rows and cache alone.
+ */
+typedef struct kvq_block8_batch {
+  const int32_t* lengths; /* device [batch]: tokens of each sequence, new ones included */
+  const int32_t* starts;  /* device [batch + 1]; NULL: n_tokens / batch rows each */
+  int32_t n_tokens;       /* rows, 1 .. 2^28 / n_q_heads */
+  int32_t max_new;        /* at least the new tokens of any sequence, 1 .. max_len */
+} kvq_block8_batch;
+
+/* Host-only: KVQ_OK when `cfg` is supported. */
+kvq_status kvq_block8_validate_config(const kvq_block8_config* cfg);
+
+/*
+ * kvq_block8_append — rotate queries and keys by their positions, and append keys and
+ * values.
+ *   k, v       device [n_tokens][n_kv_heads][128] with the strides below; may be
+ *              slices of one projection.
+ *   q, q_out   device [n_tokens][n_q_heads][128], or both NULL.  q_out may be q.
+ *   cos, sin   device fp32 [n_positions][rot_dim / 2]: of the angle by which a
+ *              position rotates each pair of channels (x1, x2) of a head:
+ *                y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
+ *              in fp32, rounded once to the type (keys: as if computed without
+ *              rounding before).  Pair i is channels (i, i + rot_dim / 2), or with
+ *              `paired` (2 i, 2 i + 1); channels from rot_dim on stay as they are.
+ *   positions  device int32 [n_tokens]: rows of the tables; NULL: a token's place in
+ *              its sequence.  One outside the tables takes the nearest row and sets
+ *              KVQ_FLAG_BAD_BATCH.
+ *   rot_dim    0 (no rotation) .. 128, a multiple of 8.
+ *   strides    elements between tokens and between heads: multiples of 8, >= 0; q_out's
+ *              >= 128 where the size is over 1, and no two rows may overlap.
+ * A sequence with fewer tokens than new ones sets KVQ_FLAG_BAD_BATCH and is left alone.
+ * A completed block whose page lies outside [0, n_pages) sets KVQ_FLAG_BAD_PAGE and
+ * writes no codes.  Pages must be distinct.  Values are expected to be finite.
+ */
+typedef struct kvq_block8_append_params {
+  const uint16_t* k;
+  const uint16_t* v;
+  const uint16_t* q;
+  uint16_t* q_out;
+  const float* cos;
+  const float* sin;
+  const int32_t* positions;
+  int32_t n_positions;
+  int32_t rot_dim;
+  int32_t paired;
+  int64_t k_stride[2];
+  int64_t v_stride[2];
+  int64_t q_stride[2];
+  int64_t q_out_stride[2];
+} kvq_block8_append_params;
+kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
+                             const kvq_block8_batch* batch,
+                             const kvq_block8_append_params* params, void* stream);
+
+/*
+ * kvq_block8_attn — causal attention of each sequence's new tokens over its cache, which
+ * holds them already.  The token at position p sees token j when
+ *   0 <= j <= p  and  (window == 0  or  j > p - window  or  j < sinks),
+ * tokens of whole blocks as codes, the others from the ring:
+ *   out[t, i] = softmax_j(q[t, i] . K[g(i), j] * softmax_scale) V[g(i), j]
+ * A query ahead of its sequence's first token gets a zero output.  Blocks that no query
+ * of the call sees are not read and need not be mapped.  In the others a key may be
+ * anything where a query does not see it; values have to be finite for all of them.
+ * A block mapped outside [0, n_pages) counts as unseen and sets KVQ_FLAG_BAD_PAGE.
+ * Codes are exact in the fp16 operands, scales meet fp32 numbers, and bf16 queries and
+ * ring rows go to fp16 times a power of two; the softmax weights (times their block's
+ * value scale) are rounded once to fp16.  Sums, maxima and outputs are fp32, rounded once
+ * to the type.
+ *   q, out      device [n_tokens][n_q_heads][128] with the strides below (as in
+ *               kvq_block8_append); they must not overlap.
+ *   workspace   device, >= kvq_block8_workspace_bytes(cfg, max_new); needs no
+ *               initialisation; calls sharing it must not overlap on the GPU.
+ * Lengths and starts are read on the device; the call can be captured in a CUDA graph.
+ * batch * n_kv_heads * (max_len / 32 + 8) times the row tiles of max_new must be below
+ * 2^31 (KVQ_ERR_SHAPE).
+ */
+typedef struct kvq_block8_attn_params {
+  int32_t window;      /* newest tokens seen, the query's own included; 0: all */
+  int32_t sinks;       /* with a window: first tokens that stay visible, >= 0 */
+  float softmax_scale; /* 0 selects 1/sqrt(128) */
+  int64_t q_stride[2];
+  int64_t out_stride[2];
+} kvq_block8_attn_params;
+/* 0 on an invalid config or max_new outside [1, max_len]. */
+size_t kvq_block8_workspace_bytes(const kvq_block8_config* cfg, int32_t max_new);
+kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
+                           const kvq_block8_batch* batch, const uint16_t* q, uint16_t* out,
+                           const kvq_block8_attn_params* params, void* workspace,
+                           size_t ws_bytes, void* stream);
+
+/*
+ * kvq_adjust_logits — what a request asks of its logits ahead of dgap_restore or
+ * kvq_sample.  For each row z, in fp32 and this order (each part only where given):
+ *   repetition  z_i > 0 ? z_i / r : z_i * r   for every token i of the row's history
+ *               (r <= 0 or NaN counts as 1);
+ *   frequency, presence
+ *               z_i - f * (times i was answered) - p   for every i that was: in the
+ *               history behind its first prompt_lengths tokens;
+ *   bias        z_i + value   for the ids of the row's list; of an id that is there
+ *               more than once the last counts;
+ *   mask        -inf where the token's bit is 0.
+ * A row that nothing is left of is -inf throughout (kvq_sample answers -1).
+ *   logits        device KVQ_F16, KVQ_BF16 or KVQ_F32, row b at b * logits_stride.
+ *   out           device fp32, row b at b * out_stride; may be the logits themselves
+ *                 (fp32, the same stride), otherwise they must not overlap.
+ *   history       device int32 ids of all rows, those of row b at [history_starts[b],
+ *                 history_starts[b + 1]); ids outside the vocabulary are passed over.
+ *                 n_history of them.  NULL, with n_history 0: no history.
+ *   prompt_lengths  device int32 [rows]; NULL: 0 (all of a history was answered).
+ *   repetition, frequency, presence
+ *                 device fp32 [rows], each NULL for "none".
+ *   bias_ids, bias_values, bias_starts
+ *                 device lists as the history's, n_bias entries in all.
+ *   mask          device int32 [n_masks][mask_stride], token i at bit i mod 32 of word
+ *                 i / 32; row b takes mask row mask_rows[b], or b where mask_rows is
+ *                 NULL (n_masks >= rows).  A number outside [0, n_masks) sets no limit.
+ * Parts of a list that starts out of order or outside are passed over.
+ * No workspace; calls on different outputs may overlap.
+ */
+typedef struct kvq_adjust_params {
+  const void* logits;
+  float* out;
+  const int32_t* history;
+  const int32_t* history_starts;
+  const int32_t* prompt_lengths;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  const int32_t* bias_starts;
+  const int32_t* mask;
+  const int32_t* mask_rows;
+  int64_t logits_stride;
+  int64_t out_stride;
+  int64_t mask_stride; /* words */
+  int32_t dtype;
+  int32_t rows;        /* 1 .. 65535 */
+  int32_t vocab;       /* 1 .. 2^30 */
+  int32_t n_history;
+  int32_t n_bias;
+  int32_t n_masks;
+} kvq_adjust_params;
+kvq_status kvq_adjust_logits(const kvq_adjust_params* params, void* stream);
 
 /*
  * kvq_selftest_wait_timeout — checks on the device that a bounded wait gives

@@ -8,6 +8,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include "block8.cuh"
 #include "common.cuh"
 #include "serve.cuh"
 
@@ -691,6 +692,251 @@ kvq_status kvq_drift_window(const float* cov, int32_t rows, int32_t k_max, float
   return cuda_status(launch_drift_window(cov, rows, k_max, rho_k, mean_cov, k_b,
                                          static_cast<cudaStream_t>(stream)),
                      "kvq_drift_window launch");
+}
+
+static kvq_status check_block8_config(const kvq_block8_config* c) {
+  if (!c) return fail(KVQ_ERR_ARG, "config is NULL");
+  if (c->batch < 1 || c->batch > 8192)
+    return fail(KVQ_ERR_SHAPE, "batch must be in [1, 8192] (got %d)", c->batch);
+  if (c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_kv_heads > 65535)
+    return fail(KVQ_ERR_SHAPE, "head counts must be >= 1 and n_kv_heads <= 65535");
+  if (c->n_q_heads % c->n_kv_heads)
+    return fail(KVQ_ERR_SHAPE, "n_q_heads (%d) must be a multiple of n_kv_heads (%d)",
+                c->n_q_heads, c->n_kv_heads);
+  if (c->n_q_heads / c->n_kv_heads > 32)
+    return fail(KVQ_ERR_UNSUPPORTED, "n_q_heads / n_kv_heads must be <= 32");
+  if (c->head_dim != kHeadDim)
+    return fail(KVQ_ERR_UNSUPPORTED, "head_dim must be 128 (got %d)", c->head_dim);
+  if (c->block != kGroup) return fail(KVQ_ERR_UNSUPPORTED, "block must be 32 (got %d)", c->block);
+  if (c->max_len < kGroup || c->max_len % kGroup)
+    return fail(KVQ_ERR_SHAPE, "max_len must be a positive multiple of 32 (got %d)", c->max_len);
+  if (c->dtype != KVQ_F16 && c->dtype != KVQ_BF16)
+    return fail(KVQ_ERR_UNSUPPORTED, "dtype must be KVQ_F16 or KVQ_BF16 (got %d)", c->dtype);
+  g_err[0] = 0;
+  return KVQ_OK;
+}
+
+static kvq_status check_block8_cache(const kvq_block8_config& c, const kvq_block8_cache* cache) {
+  if (!cache) return fail(KVQ_ERR_ARG, "cache is NULL");
+  for (const void* p : {(const void*)cache->k_codes, (const void*)cache->v_codes,
+                        (const void*)cache->scales, (const void*)cache->k_ring,
+                        (const void*)cache->v_ring}) {
+    if (!p) return fail(KVQ_ERR_ARG, "cache has a NULL pointer");
+    if (!aligned16(p)) return fail(KVQ_ERR_ALIGN, "cache pointers must be 16-byte aligned");
+  }
+  if (!cache->block_table || !cache->flags)
+    return fail(KVQ_ERR_ARG, "block_table or flags is NULL");
+  if ((reinterpret_cast<uintptr_t>(cache->block_table) |
+       reinterpret_cast<uintptr_t>(cache->flags)) & 3u)
+    return fail(KVQ_ERR_ALIGN, "block_table and flags must be 4-byte aligned");
+  if (cache->n_pages < 1) return fail(KVQ_ERR_ARG, "n_pages must be >= 1 (got %d)", cache->n_pages);
+  if ((long long)cache->n_pages * c.n_kv_heads > (1LL << 26))
+    return fail(KVQ_ERR_SHAPE, "n_pages * n_kv_heads must be <= 2^26");
+  return KVQ_OK;
+}
+
+static kvq_status check_block8_batch(const kvq_block8_config& c, const kvq_block8_batch* b) {
+  if (!b) return fail(KVQ_ERR_ARG, "batch is NULL");
+  if (!b->lengths) return fail(KVQ_ERR_ARG, "lengths is NULL");
+  if ((reinterpret_cast<uintptr_t>(b->lengths) | reinterpret_cast<uintptr_t>(b->starts)) & 3u)
+    return fail(KVQ_ERR_ALIGN, "lengths and starts must be 4-byte aligned");
+  if (b->n_tokens < 1 || (long long)b->n_tokens * c.n_q_heads > (1LL << 28))
+    return fail(KVQ_ERR_SHAPE, "n_tokens must be in [1, 2^28 / n_q_heads] (got %d)", b->n_tokens);
+  if (b->max_new < 1 || b->max_new > c.max_len)
+    return fail(KVQ_ERR_ARG, "max_new must be in [1, max_len] (got %d)", b->max_new);
+  if (!b->starts && (long long)b->max_new * c.batch != b->n_tokens)
+    return fail(KVQ_ERR_SHAPE, "without starts, n_tokens (%d) must be batch * max_new", b->n_tokens);
+  return KVQ_OK;
+}
+
+// Strides between tokens and heads of an array of n_tokens x heads rows.
+static kvq_status check_block8_rows(const char* name, const void* p, const int64_t (&stride)[2],
+                                    int n_tokens, int heads, bool written) {
+  if (!aligned16(p)) return fail(KVQ_ERR_ALIGN, "%s must be 16-byte aligned", name);
+  const int sizes[2] = {n_tokens, heads};
+  for (int i = 0; i < 2; ++i) {
+    if (stride[i] < 0) return fail(KVQ_ERR_ARG, "strides of %s must be >= 0", name);
+    if (stride[i] & 7)
+      return fail(KVQ_ERR_ALIGN, "strides of %s must be multiples of 8 elements", name);
+    if (written && sizes[i] > 1 && stride[i] < kHeadDim)
+      return fail(KVQ_ERR_ARG, "strides of %s must be >= 128", name);
+  }
+  return KVQ_OK;
+}
+
+static block8::Dims8 block8_dims(const kvq_block8_config& c) {
+  block8::Dims8 d;
+  d.batch = c.batch;
+  d.hq = c.n_q_heads;
+  d.hkv = c.n_kv_heads;
+  d.gq = c.n_q_heads / c.n_kv_heads;
+  d.max_len = c.max_len;
+  d.max_blocks = c.max_len / kGroup;
+  d.bf16 = c.dtype == KVQ_BF16;
+  return d;
+}
+
+kvq_status kvq_block8_validate_config(const kvq_block8_config* cfg) {
+  return check_block8_config(cfg);
+}
+
+kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
+                             const kvq_block8_batch* batch, const kvq_block8_append_params* p,
+                             void* stream) {
+  kvq_status s = check_block8_config(cfg);
+  if (s != KVQ_OK) return s;
+  if ((s = check_block8_cache(*cfg, cache)) != KVQ_OK) return s;
+  if ((s = check_block8_batch(*cfg, batch)) != KVQ_OK) return s;
+  if (!p) return fail(KVQ_ERR_ARG, "params is NULL");
+  if (!p->k || !p->v) return fail(KVQ_ERR_ARG, "k / v is NULL");
+  if (!p->q != !p->q_out) return fail(KVQ_ERR_ARG, "q and q_out come together");
+  const int n = batch->n_tokens;
+  if ((s = check_block8_rows("k", p->k, p->k_stride, n, cfg->n_kv_heads, false)) != KVQ_OK ||
+      (s = check_block8_rows("v", p->v, p->v_stride, n, cfg->n_kv_heads, false)) != KVQ_OK)
+    return s;
+  if (p->q &&
+      ((s = check_block8_rows("q", p->q, p->q_stride, n, cfg->n_q_heads, false)) != KVQ_OK ||
+       (s = check_block8_rows("q_out", p->q_out, p->q_out_stride, n, cfg->n_q_heads, true)) !=
+           KVQ_OK))
+    return s;
+  if (p->q && p->q == p->q_out &&
+      ((n > 1 && p->q_stride[0] != p->q_out_stride[0]) ||
+       (cfg->n_q_heads > 1 && p->q_stride[1] != p->q_out_stride[1])))
+    return fail(KVQ_ERR_ARG, "in place, q and q_out must have the same strides");
+  if (p->rot_dim < 0 || p->rot_dim > kHeadDim || p->rot_dim % 8)
+    return fail(KVQ_ERR_UNSUPPORTED, "rot_dim must be a multiple of 8 in [0, 128] (got %d)",
+                p->rot_dim);
+  if (p->rot_dim) {
+    if (!p->cos || !p->sin) return fail(KVQ_ERR_ARG, "cos / sin is NULL");
+    if (!aligned16(p->cos) || !aligned16(p->sin))
+      return fail(KVQ_ERR_ALIGN, "cos and sin must be 16-byte aligned");
+    if (p->n_positions < 1)
+      return fail(KVQ_ERR_ARG, "n_positions must be >= 1 (got %d)", p->n_positions);
+    if (reinterpret_cast<uintptr_t>(p->positions) & 3u)
+      return fail(KVQ_ERR_ALIGN, "positions must be 4-byte aligned");
+  }
+  block8::AppendCall call;
+  call.d = block8_dims(*cfg);
+  call.cache = *cache;
+  call.batch = *batch;
+  call.p = *p;
+  trace("kvq_block8_append batch %d tokens %d heads %d/%d rot %d%s %s", cfg->batch, n,
+        cfg->n_q_heads, cfg->n_kv_heads, p->rot_dim, p->paired ? " paired" : "",
+        call.d.bf16 ? "bf16" : "fp16");
+  return cuda_status(block8::launch_append(call, static_cast<cudaStream_t>(stream)),
+                     "kvq_block8_append launch");
+}
+
+size_t kvq_block8_workspace_bytes(const kvq_block8_config* cfg, int32_t max_new) {
+  if (check_block8_config(cfg) != KVQ_OK) return 0;
+  if (max_new < 1 || max_new > cfg->max_len) {
+    set_error("max_new must be in [1, max_len] (got %d)", max_new);
+    return 0;
+  }
+  return block8::attn_workspace_bytes(block8_dims(*cfg), max_new, sm_count());
+}
+
+kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
+                           const kvq_block8_batch* batch, const uint16_t* q, uint16_t* out,
+                           const kvq_block8_attn_params* p, void* workspace, size_t ws_bytes,
+                           void* stream) {
+  kvq_status s = check_block8_config(cfg);
+  if (s != KVQ_OK) return s;
+  if ((s = check_block8_cache(*cfg, cache)) != KVQ_OK) return s;
+  if ((s = check_block8_batch(*cfg, batch)) != KVQ_OK) return s;
+  if (!p) return fail(KVQ_ERR_ARG, "params is NULL");
+  if (!q || !out) return fail(KVQ_ERR_ARG, "q / out is NULL");
+  const int n = batch->n_tokens;
+  if ((s = check_block8_rows("q", q, p->q_stride, n, cfg->n_q_heads, false)) != KVQ_OK ||
+      (s = check_block8_rows("out", out, p->out_stride, n, cfg->n_q_heads, true)) != KVQ_OK)
+    return s;
+  if (p->window < 0 || p->sinks < 0)
+    return fail(KVQ_ERR_ARG, "window and sinks must be >= 0 (got %d, %d)", p->window, p->sinks);
+  if (!(p->softmax_scale >= 0.0f) || isinf(p->softmax_scale))
+    return fail(KVQ_ERR_ARG, "softmax_scale must be finite and >= 0");
+  const block8::Dims8 d = block8_dims(*cfg);
+  if (block8::attn_most_units(d, batch->max_new) >= (1LL << 31))
+    return fail(KVQ_ERR_SHAPE, "batch * n_kv_heads * max_len and max_new give too many tiles");
+  const size_t need = block8::attn_workspace_bytes(d, batch->max_new, sm_count());
+  if (!workspace) return fail(KVQ_ERR_ARG, "workspace is NULL");
+  if (!aligned16(workspace)) return fail(KVQ_ERR_ALIGN, "workspace must be 16-byte aligned");
+  if (ws_bytes < need)
+    return fail(KVQ_ERR_CAPACITY, "workspace too small: %zu < %zu bytes", ws_bytes, need);
+  block8::AttnCall call;
+  call.d = d;
+  call.cache = *cache;
+  call.batch = *batch;
+  call.q = q;
+  call.out = out;
+  // no token stands at max_len or beyond: larger numbers say the same, and sums with
+  // positions stay within 32 bits
+  call.window = p->window < cfg->max_len ? p->window : cfg->max_len;
+  call.sinks = !p->window ? 0 : p->sinks < cfg->max_len ? p->sinks : cfg->max_len;
+  const float scale =
+      p->softmax_scale == 0.0f ? 1.0f / sqrtf((float)kHeadDim) : p->softmax_scale;
+  call.scale_log2 = scale * 1.4426950408889634f;
+  for (int i = 0; i < 2; ++i) {
+    call.q_stride[i] = p->q_stride[i];
+    call.out_stride[i] = p->out_stride[i];
+  }
+  trace("kvq_block8_attn batch %d tokens %d max_new %d window %d sinks %d heads %d/%d %s",
+        cfg->batch, n, batch->max_new, call.window, call.sinks, d.hq, d.hkv,
+        d.bf16 ? "bf16" : "fp16");
+  return cuda_status(
+      block8::launch_attn(call, sm_count(), workspace, static_cast<cudaStream_t>(stream)),
+      "kvq_block8_attn launch");
+}
+
+kvq_status kvq_adjust_logits(const kvq_adjust_params* p, void* stream) {
+  if (!p) return fail(KVQ_ERR_ARG, "params is NULL");
+  if (!p->logits || !p->out) return fail(KVQ_ERR_ARG, "logits or out is NULL");
+  if (p->dtype != KVQ_F16 && p->dtype != KVQ_BF16 && p->dtype != KVQ_F32)
+    return fail(KVQ_ERR_UNSUPPORTED, "dtype must be KVQ_F16, KVQ_BF16 or KVQ_F32 (got %d)",
+                p->dtype);
+  if (p->rows < 1 || p->rows > 65535)
+    return fail(KVQ_ERR_SHAPE, "rows must be in [1, 65535] (got %d)", p->rows);
+  if (p->vocab < 1 || p->vocab > (1 << 30))
+    return fail(KVQ_ERR_SHAPE, "vocab must be in [1, 2^30] (got %d)", p->vocab);
+  if (p->rows > 1 && (p->logits_stride < 0 || p->out_stride < p->vocab))
+    return fail(KVQ_ERR_ARG, "logits_stride must be >= 0 and out_stride >= vocab");
+  if ((const void*)p->out == p->logits &&
+      (p->dtype != KVQ_F32 || (p->rows > 1 && p->logits_stride != p->out_stride)))
+    return fail(KVQ_ERR_ARG, "in place, logits must be fp32 with the stride of out");
+  if (p->n_history < 0 || p->n_bias < 0)
+    return fail(KVQ_ERR_SHAPE, "n_history and n_bias must be >= 0");
+  if ((p->history && !p->history_starts) || (p->n_history && !p->history))
+    return fail(KVQ_ERR_ARG, "history and history_starts come together");
+  if (((p->bias_ids || p->bias_values) && !p->bias_starts) ||
+      (p->n_bias && (!p->bias_ids || !p->bias_values)))
+    return fail(KVQ_ERR_ARG, "bias_ids, bias_values and bias_starts come together");
+  if (!p->history_starts && (p->prompt_lengths || p->repetition || p->frequency || p->presence))
+    return fail(KVQ_ERR_ARG, "penalties need a history");
+  if (p->mask_rows && !p->mask) return fail(KVQ_ERR_ARG, "mask_rows needs a mask");
+  if (p->mask) {
+    if (p->n_masks < 1 || (!p->mask_rows && p->n_masks < p->rows))
+      return fail(KVQ_ERR_SHAPE, "n_masks must be >= 1, and >= rows without mask_rows (got %d)",
+                  p->n_masks);
+    if (p->n_masks > 1 && p->mask_stride < (p->vocab + 31) / 32)
+      return fail(KVQ_ERR_ARG, "mask_stride must be >= vocab / 32 words");
+  }
+  if (reinterpret_cast<uintptr_t>(p->logits) & (p->dtype == KVQ_F32 ? 3u : 1u))
+    return fail(KVQ_ERR_ALIGN, "logits must be aligned to their type");
+  for (const void* x : {(const void*)p->out, (const void*)p->history,
+                        (const void*)p->history_starts, (const void*)p->prompt_lengths,
+                        (const void*)p->repetition, (const void*)p->frequency,
+                        (const void*)p->presence, (const void*)p->bias_ids,
+                        (const void*)p->bias_values, (const void*)p->bias_starts,
+                        (const void*)p->mask, (const void*)p->mask_rows})
+    if (reinterpret_cast<uintptr_t>(x) & 3u)
+      return fail(KVQ_ERR_ALIGN, "pointers must be 4-byte aligned");
+  kvq_adjust_params c = *p;
+  if (p->rows == 1) c.logits_stride = c.out_stride = 0;
+  if (!p->n_history) c.history_starts = nullptr;
+  if (!p->n_bias) c.bias_starts = nullptr;
+  trace("kvq_adjust_logits rows %d vocab %d%s%s%s", p->rows, p->vocab,
+        p->n_history ? " history" : "", p->n_bias ? " bias" : "", p->mask ? " mask" : "");
+  return cuda_status(launch_adjust(c, static_cast<cudaStream_t>(stream)),
+                     "kvq_adjust_logits launch");
 }
 
 }  // extern "C"

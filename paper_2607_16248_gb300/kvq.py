@@ -21,6 +21,7 @@ STATUS_NAMES = {0: "KVQ_OK", 1: "KVQ_ERR_ARG", 2: "KVQ_ERR_SHAPE", 3: "KVQ_ERR_U
 FLAG_OVERFLOW = 1
 FLAG_WAIT_TIMEOUT = 2
 FLAG_BAD_PAGE = 4
+FLAG_BAD_BATCH = 8
 
 # Every symbol include/kvq.h declares.
 EXPORTS = (
@@ -31,6 +32,8 @@ EXPORTS = (
     "kvq_workspace_init",
     "kvq_decode_attn", "kvq_decode_attn_f32", "kvq_decode_step", "kvq_decode_step_f32",
     "kvq_decode_attn_noalloc", "kvq_chunk_workspace_bytes", "kvq_chunk_attn",
+    "kvq_block8_validate_config", "kvq_block8_append", "kvq_block8_workspace_bytes",
+    "kvq_block8_attn", "kvq_adjust_logits",
     "kvq_sample_max_vocab", "kvq_sample", "dgap_workspace_bytes",
     "dgap_restore", "kvq_drift_max_vocab", "kvq_drift_metrics", "kvq_drift_window",
     "kvq_selftest_wait_timeout", "kvq_selftest_chunk_wait_timeout",
@@ -65,6 +68,46 @@ class _ChunkParams(ctypes.Structure):
     _fields_ = [("n_q", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 3),
                 ("out_stride", ctypes.c_int64 * 3)]
+
+
+class _Block8Config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "n_q_heads", "n_kv_heads", "head_dim", "block", "max_len", "dtype")]
+
+
+class _Block8Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "k_codes", "v_codes", "scales", "k_ring", "v_ring", "block_table", "flags")] + [
+        ("n_pages", ctypes.c_int32)]
+
+
+class _Block8Batch(ctypes.Structure):
+    _fields_ = [("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("n_tokens", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+
+
+_Pair = ctypes.c_int64 * 2
+
+
+class _Block8Append(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "k", "v", "q", "q_out", "cos", "sin", "positions")] + [
+        (n, ctypes.c_int32) for n in ("n_positions", "rot_dim", "paired")] + [
+        (n, _Pair) for n in ("k_stride", "v_stride", "q_stride", "q_out_stride")]
+
+
+class _Block8Attn(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("q_stride", _Pair), ("out_stride", _Pair)]
+
+
+class _AdjustParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "logits", "out", "history", "history_starts", "prompt_lengths", "repetition",
+        "frequency", "presence", "bias_ids", "bias_values", "bias_starts", "mask",
+        "mask_rows")] + [(n, ctypes.c_int64) for n in (
+            "logits_stride", "out_stride", "mask_stride")] + [(n, ctypes.c_int32) for n in (
+                "dtype", "rows", "vocab", "n_history", "n_bias", "n_masks")]
 
 
 class _DgapParams(ctypes.Structure):
@@ -111,6 +154,11 @@ def lib():
             "kvq_chunk_workspace_bytes": (SZ, [cfg_p, I32, I32]),
             "kvq_chunk_attn": (I32, [cfg_p, cache_p, P, P, ctypes.POINTER(_ChunkParams), I32,
                                      I32, P, SZ, P]),
+            "kvq_block8_validate_config": (I32, [P]),
+            "kvq_block8_append": (I32, [P, P, P, P, P]),
+            "kvq_block8_workspace_bytes": (SZ, [P, I32]),
+            "kvq_block8_attn": (I32, [P, P, P, P, P, P, P, SZ, P]),
+            "kvq_adjust_logits": (I32, [P, P]),
             "kvq_sample_max_vocab": (I32, []),
             "kvq_sample": (I32, [P, I64, P, I64, I32, I32, P, P, P, P, P, P, P]),
             "dgap_workspace_bytes": (SZ, [I32, I32, par_p]),
@@ -507,6 +555,318 @@ def kvq_chunk_attn(cache: QuantKVCache, q, out=None, window=0, sinks=0, softmax_
                                 batch_begin, batch_count,
                                 _dev(workspace, torch.uint8, "workspace"),
                                 workspace.numel(), _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Block-8 cache
+# ---------------------------------------------------------------------------
+
+_BLOCK8_TYPES = {torch.float16: 0, torch.bfloat16: 1}
+_LOGIT_TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+BLOCK8_RING = 64
+
+
+@dataclass(frozen=True)
+class Block8Config:
+    """Shape of a block-8 cache (see kvq_block8_config in include/kvq.h)."""
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    max_len: int
+    dtype: torch.dtype = torch.float16
+    head_dim: int = 128
+    block: int = 32
+
+    def c(self):
+        _in_32_bits("sizes", self.batch, self.n_q_heads, self.n_kv_heads, self.max_len)
+        return _Block8Config(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim,
+                             self.block, self.max_len, _BLOCK8_TYPES.get(self.dtype, -1))
+
+    @property
+    def max_blocks(self):
+        return self.max_len // self.block
+
+    def validate(self):
+        c = self.c()
+        _check(lib().kvq_block8_validate_config(ctypes.byref(c)))
+
+
+def block8_written(length, n_new):
+    """Blocks that appending n_new tokens to ``length`` completes."""
+    return range(length // 32, (length + n_new) // 32)
+
+
+class Block8Cache:
+    """A paged cache of e4m3 blocks, one scale per 32 tokens and kv-head.
+
+    ``n_pages`` makes its tensors (all blocks unmapped); ``tensors`` takes the
+    caller's own: a dict of k_codes, v_codes (float8_e4m3fn [n_pages, n_kv_heads,
+    32, 128]), scales (fp32 [n_pages, n_kv_heads, 2]), k_ring, v_ring (cfg.dtype
+    [batch, n_kv_heads, 64, 128]).  ``block_table`` (int32 [batch, max_len / 32])
+    may be shared by the caches of several layers.  Lengths are the caller's too:
+    each call gets them."""
+
+    def __init__(self, cfg: Block8Config, n_pages=None, device="cuda", tensors=None,
+                 block_table=None):
+        cfg.validate()
+        self.cfg = cfg
+        if (n_pages is None) == (tensors is None):
+            raise ValueError("give either n_pages or tensors")
+        h, d = cfg.n_kv_heads, cfg.head_dim
+        if tensors is None:
+            _in_32_bits("n_pages", n_pages)
+            if n_pages < 1:
+                raise ValueError(f"n_pages must be >= 1 (got {n_pages})")
+            tensors = {n: torch.zeros(n_pages, h, 32, d, dtype=torch.uint8, device=device)
+                       .view(torch.float8_e4m3fn) for n in ("k_codes", "v_codes")}
+            tensors["scales"] = torch.ones(n_pages, h, 2, dtype=torch.float32, device=device)
+            for n in ("k_ring", "v_ring"):
+                tensors[n] = torch.zeros(cfg.batch, h, BLOCK8_RING, d, dtype=cfg.dtype,
+                                         device=device)
+        self.n_pages = tensors["scales"].shape[0]
+        code, ring = (self.n_pages, h, 32, d), (cfg.batch, h, BLOCK8_RING, d)
+        want = {"k_codes": (torch.float8_e4m3fn, code), "v_codes": (torch.float8_e4m3fn, code),
+                "scales": (torch.float32, (self.n_pages, h, 2)), "k_ring": (cfg.dtype, ring),
+                "v_ring": (cfg.dtype, ring)}
+        for n, (dtype, shape) in want.items():
+            if tuple(tensors[n].shape) != shape:
+                raise ValueError(f"{n} must be {list(shape)}")
+            _dev(tensors[n], dtype, n)
+            setattr(self, n, tensors[n])
+        self.device = self.scales.device
+        if block_table is None:
+            block_table = torch.full((cfg.batch, cfg.max_blocks), -1, dtype=torch.int32,
+                                     device=self.device)
+        elif tuple(block_table.shape) != (cfg.batch, cfg.max_blocks):
+            raise ValueError(f"block_table must be [{cfg.batch}, {cfg.max_blocks}]")
+        _dev(block_table, torch.int32, "block_table")
+        self.block_table = block_table
+        self._flags = torch.zeros(1, dtype=torch.int32, device=self.device)
+        for t in (self.k_codes, self.v_codes, self.k_ring, self.v_ring, block_table):
+            if t.device != self.device:
+                raise ValueError("a cache's tensors must be on one device")
+        self._cfg = cfg.c()
+        self._c = _Block8Cache(*(t.data_ptr() for t in (
+            self.k_codes, self.v_codes, self.scales, self.k_ring, self.v_ring, block_table,
+            self._flags)), self.n_pages)
+        self._cfg_ref, self._c_ref = ctypes.byref(self._cfg), ctypes.byref(self._c)
+
+    def map_blocks(self, b, blocks, pages):
+        """block_table[b, blocks[i]] = pages[i] (a copy on the current stream)."""
+        idx = torch.as_tensor(list(blocks), dtype=torch.long)
+        val = torch.as_tensor(list(pages), dtype=torch.int32)
+        self.block_table[b, idx.to(self.device)] = val.to(self.device)
+
+    def flags(self):
+        return int(self._flags.item())
+
+    def clear_flags(self):
+        self._flags.zero_()
+
+
+def _rows(t, shape, dtype, name, device):
+    """Address and strides (tokens, heads) of a [tokens, heads, 128] tensor."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    s = t.stride()
+    return _address(t, dtype, name), _Pair(s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0)
+
+
+def _list32(t, n, name, device, dtype=torch.int32):
+    """Address of a contiguous 1-d tensor on the device (n elements, or any number)."""
+    if t is None:
+        return None
+    if t.dim() != 1 or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be [{'n' if n is None else n}]")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    return _address(t, dtype, name)
+
+
+def _block8_batch(cache, n_tokens, lengths, starts, max_new):
+    batch = cache.cfg.batch
+    if starts is None:
+        if n_tokens % batch:
+            raise ValueError("without starts, every sequence has as many new tokens")
+        if max_new not in (None, n_tokens // batch):
+            raise ValueError("without starts, max_new is the tokens of each sequence")
+        max_new = n_tokens // batch
+    elif max_new is None:
+        max_new = min(n_tokens, cache.cfg.max_len)
+    _in_32_bits("n_tokens and max_new", n_tokens, max_new)
+    return _Block8Batch(_list32(lengths, batch, "lengths", cache.device),
+                        _list32(starts, batch + 1, "starts", cache.device), n_tokens, max_new)
+
+
+def _stream_on(device, stream):
+    """The stream's handle; the device's own current stream where none is given."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"stream must be on {device}")
+    return stream.cuda_stream
+
+
+class _on:
+    """The device as the current one, if it is not."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.was != self.device.index:
+            torch.cuda.set_device(self.device)
+
+    def __exit__(self, *exc):
+        if self.was != self.device.index:
+            torch.cuda.set_device(self.was)
+
+
+def kvq_block8_append(cache: Block8Cache, k, v, lengths, starts=None, q=None, q_out=None,
+                      cos=None, sin=None, paired=False, positions=None, max_new=None,
+                      stream=None):
+    """Append the newest tokens of each sequence, keys (and queries) rotated on the way.
+
+    k, v [tokens, n_kv_heads, 128] and q [tokens, n_q_heads, 128] in cfg.dtype, strided
+    views of one projection too; rows starts[b] .. starts[b + 1] - 1 are sequence b's
+    (starts int32 [batch + 1] on the device; None: as many for each), the last of them
+    at position lengths[b] - 1 (int32 [batch], new tokens included).  cos, sin fp32
+    [n_positions, rot_dim / 2] (None: no rotation); ``paired`` rotates channels (2i,
+    2i + 1) instead of (i, i + rot_dim / 2); ``positions`` int32 [tokens] are rows of
+    the tables in place of the tokens' places.  Returns q_out (made if None; may be
+    q), or None without q."""
+    cfg, dev = cache.cfg, cache.device
+    n = k.shape[0]
+    kv = (n, cfg.n_kv_heads, cfg.head_dim)
+    p = _Block8Append()
+    batch = _block8_batch(cache, n, lengths, starts, max_new)
+    p.k, p.k_stride = _rows(k, kv, cfg.dtype, "k", dev)
+    p.v, p.v_stride = _rows(v, kv, cfg.dtype, "v", dev)
+    if q is not None:
+        shape = (n, cfg.n_q_heads, cfg.head_dim)
+        p.q, p.q_stride = _rows(q, shape, cfg.dtype, "q", dev)
+        if q_out is None:
+            q_out = _made_on(stream, lambda: torch.empty(shape, dtype=cfg.dtype, device=dev))
+        p.q_out, p.q_out_stride = _rows(q_out, shape, cfg.dtype, "q_out", dev)
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    if cos is not None:
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must both be [n_positions, rot_dim / 2]")
+        if cos.device != dev or sin.device != dev:
+            raise ValueError(f"cos and sin must be on {dev}")
+        p.n_positions, p.rot_dim = cos.shape[0], 2 * cos.shape[1]
+        if p.rot_dim:
+            p.cos = _dev(cos, torch.float32, "cos").value
+            p.sin = _dev(sin, torch.float32, "sin").value
+            p.positions = _list32(positions, n, "positions", dev)
+        p.paired = int(bool(paired))
+    with _on(dev):
+        _check(lib().kvq_block8_append(cache._cfg_ref, cache._c_ref, ctypes.byref(batch),
+                                       ctypes.byref(p), _stream_on(dev, stream)))
+    return q_out
+
+
+def block8_workspace(cfg: Block8Config, max_new, device="cuda"):
+    """A workspace for kvq_block8_attn of up to max_new new tokens a sequence."""
+    c = cfg.c()
+    _in_32_bits("max_new", max_new)
+    n = lib().kvq_block8_workspace_bytes(ctypes.byref(c), max_new)
+    if n == 0:
+        raise KvqError(1, last_error())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def kvq_block8_attn(cache: Block8Cache, q, lengths, starts=None, max_new=None, window=0, sinks=0,
+                    softmax_scale=0.0, out=None, workspace=None, stream=None):
+    """Causal attention of the newest tokens of each sequence, which kvq_block8_append
+    has appended: q [tokens, n_q_heads, 128] (rotated; strided views too) -> out of that
+    shape.  lengths, starts as there; ``max_new`` is the most new tokens of any sequence
+    (a smaller number serves single tokens and drafts faster).  window, sinks as in
+    kvq_chunk_attn."""
+    cfg, dev = cache.cfg, cache.device
+    n = q.shape[0]
+    shape = (n, cfg.n_q_heads, cfg.head_dim)
+    batch = _block8_batch(cache, n, lengths, starts, max_new)
+    _in_32_bits("window and sinks", window, sinks)
+    qa, qs = _rows(q, shape, cfg.dtype, "q", dev)
+    if out is None:
+        out = _made_on(stream, lambda: torch.empty(shape, dtype=cfg.dtype, device=dev))
+    oa, os = _rows(out, shape, cfg.dtype, "out", dev)
+    if workspace is None:
+        workspace = _made_on(stream, block8_workspace, cfg, batch.max_new, dev)
+    elif workspace.device != dev:
+        raise ValueError(f"workspace must be on {dev}")
+    p = _Block8Attn(window, sinks, softmax_scale, qs, os)
+    with _on(dev):
+        _check(lib().kvq_block8_attn(cache._cfg_ref, cache._c_ref, ctypes.byref(batch), qa, oa,
+                                     ctypes.byref(p), _dev(workspace, torch.uint8, "workspace"),
+                                     workspace.numel(), _stream_on(dev, stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Adjusted logits
+# ---------------------------------------------------------------------------
+
+
+def kvq_adjust_logits(logits, out=None, history=None, history_starts=None, prompt_lengths=None,
+                      repetition=None, frequency=None, presence=None, bias_ids=None,
+                      bias_values=None, bias_starts=None, mask=None, mask_rows=None,
+                      stream=None):
+    """Penalties for repeated tokens, biases and a grammar's mask on logits [rows, vocab]
+    (fp32, fp16 or bf16; rows may be strided) -> fp32 ``out``, which may be the logits.
+
+    history, bias_ids (int32) and bias_values (fp32) hold all rows' lists one behind the
+    other, row b's at starts[b] .. starts[b + 1] - 1 (int32 [rows + 1]); the first
+    prompt_lengths[b] tokens of a history were asked, the others answered.  repetition,
+    frequency, presence are fp32 [rows]; mask int32 [n, ceil(vocab / 32)] of bits, row b's
+    at mask_rows[b] (None: b).  All on the device."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    rows, V = logits.shape
+    dev = logits.device
+    _in_32_bits("rows and vocab", rows, V)
+    if logits.dtype not in _LOGIT_TYPES:
+        raise TypeError(f"logits must be float32, float16 or bfloat16, got {logits.dtype}")
+    p = _AdjustParams()
+    p.logits = _address(logits, logits.dtype, "logits")
+    p.dtype = _LOGIT_TYPES[logits.dtype]
+    if out is None:
+        out = _made_on(stream, lambda: torch.empty(rows, V, dtype=torch.float32, device=dev))
+    elif out.shape != logits.shape or out.device != dev:
+        raise ValueError("out must have the logits' shape and device")
+    p.out = _address(out, torch.float32, "out")
+    p.logits_stride, p.out_stride, p.rows, p.vocab = logits.stride(0), out.stride(0), rows, V
+    f32 = torch.float32
+    if history is not None:
+        p.history, p.n_history = _list32(history, None, "history", dev), history.shape[0]
+    p.history_starts = _list32(history_starts, rows + 1, "history_starts", dev)
+    p.prompt_lengths = _list32(prompt_lengths, rows, "prompt_lengths", dev)
+    p.repetition = _list32(repetition, rows, "repetition", dev, f32)
+    p.frequency = _list32(frequency, rows, "frequency", dev, f32)
+    p.presence = _list32(presence, rows, "presence", dev, f32)
+    if bias_ids is not None:
+        p.bias_ids, p.n_bias = _list32(bias_ids, None, "bias_ids", dev), bias_ids.shape[0]
+        if bias_values is None or bias_values.shape != bias_ids.shape:
+            raise ValueError("bias_values must have the shape of bias_ids")
+    p.bias_values = _list32(bias_values, None, "bias_values", dev, f32)
+    p.bias_starts = _list32(bias_starts, rows + 1, "bias_starts", dev)
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[1] < (V + 31) // 32 or mask.device != dev:
+            raise ValueError("mask must be [n, ceil(vocab / 32)] on the logits' device")
+        p.mask, p.n_masks = _address(mask, torch.int32, "mask"), mask.shape[0]
+        p.mask_stride = mask.stride(0)
+    p.mask_rows = _list32(mask_rows, rows, "mask_rows", dev)
+    _in_32_bits("lists", p.n_history, p.n_bias)
+    with _on(dev):
+        _check(lib().kvq_adjust_logits(ctypes.byref(p), _stream_on(dev, stream)))
     return out
 
 
