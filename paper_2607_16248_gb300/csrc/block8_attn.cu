@@ -1,5 +1,8 @@
-// kvq_block8_attn, the simple form: a warp per query row, a token at a time.
-#include "block8.cuh"
+// Host side of kvq_block8_attn: which kernel takes which sequences, the workspace, and the
+// kernel that joins the partials of shared items.
+#include <algorithm>
+
+#include "block8_plan.cuh"
 
 #include <cuda_fp8.h>
 
@@ -23,7 +26,8 @@ __device__ __forceinline__ float4 code4(uint32_t v) {
   return make_float4(x.x, x.y, y.x, y.y);
 }
 
-__global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ AttnCall call) {
+__global__ void __launch_bounds__(256) simple_kernel(const __grid_constant__ AttnCall call,
+                                                     int min_rows) {
   const int lane = threadIdx.x & 31;
   const long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int row = (int)(task / call.d.hq), head = (int)(task - (long long)row * call.d.hq);
@@ -35,7 +39,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ AttnC
     if (s.bad && lane == 0 && row == 0 && head == 0) set_flag(call.cache, s.bad);
     if (row >= s.row && row < s.row + s.n) break;
   }
-  if (b == call.d.batch) return;
+  if (b == call.d.batch || s.n * call.d.gq < min_rows) return;
   const int h = head / call.d.gq, pos = s.L - s.n + row - s.row;
   const float4 q = half4(*reinterpret_cast<const uint2*>(
                              call.q + row * call.q_stride[0] + head * call.q_stride[1] + 4 * lane),
@@ -93,16 +97,138 @@ __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ AttnC
                             4 * lane) = r;
 }
 
-}  // namespace
+// The partials of a split item to results: the CTAs (c, y) share the rows of the item that
+// CTA c left, a row a warp.  Each lane finds the weights of one of every 32 partials, then
+// the weighted rows are summed in the order of the tokens.  A partial without a seen token
+// weighs nothing, whatever it holds.
+constexpr int kJoinWarps = 8;
 
-size_t attn_workspace_bytes(const Dims8&, int, int) { return 16; }
-long long attn_most_units(const Dims8& d, int max_new) {
-  return (long long)d.batch * d.hkv * (d.max_blocks + 8) * ((max_new * d.gq + 255) / 256);
+template <bool BF16>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+join_kernel(const __grid_constant__ AttnParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Split sp = p.splits[blockIdx.x];
+  if (!sp.valid) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = sp.last - (int)blockIdx.x + 1;
+  const Seq q = seq_of(p.c.d, p.c.batch, sp.b);
+  const int r = kJoinWarps * blockIdx.y + warp;
+  const int row = sp.row_tile * p.item_rows + r;
+  if (r >= p.item_rows || row >= q.n * p.c.d.gq) return;
+  const auto slot = [&](int i) {  // row r of the i-th partial
+    return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? sp.inside : 0)) * p.item_rows + r;
+  };
+  constexpr int kMost = (kMaxSplits + 31) / 32;  // partials a lane
+  float2 ml[kMost];
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = 32 * k + lane;
+    ml[k] = i < n ? __ldcg(&p.part_ml[slot(i)]) : make_float2(0.0f, 0.0f);
+    if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    ml[k].x = ml[k].y > 0.0f ? exp2_fast(ml[k].x - m) : 0.0f;
+    l += ml[k].y * ml[k].x;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const float f = l > 0.0f ? 1.0f / l : 0.0f;
+  float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+#pragma unroll 8
+    for (int i = 32 * k; i < min(n, 32 * k + 32); ++i) {
+      const float x = __shfl_sync(0xffffffffu, ml[k].x, i & 31) * f;
+      const float4 v =
+          __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
+      if (x > 0.0f) {
+        out.x = fmaf(v.x, x, out.x);
+        out.y = fmaf(v.y, x, out.y);
+        out.z = fmaf(v.z, x, out.z);
+        out.w = fmaf(v.w, x, out.w);
+      }
+    }
+  }
+  reinterpret_cast<uint2*>(p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row))[lane] =
+      make_uint2(pack16<BF16>(out.x, out.y), pack16<BF16>(out.z, out.w));
 }
 
-cudaError_t launch_attn(const AttnCall& call, int, void*, cudaStream_t stream) {
+cudaError_t launch_join(const AttnParams& p, int ctas, int rows, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas, (rows + kJoinWarps - 1) / kJoinWarps);
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = p.c.d.bf16 ? cudaLaunchKernelEx(&cfg, join_kernel<true>, p)
+                                   : cudaLaunchKernelEx(&cfg, join_kernel<false>, p);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// Which kernels a call runs: `few`, rows of the items of the kernel for few rows.
+struct Plan {
+  int few;
+  bool many;  // sequences of more rows may be there
+  size_t total;
+};
+size_t parts_bytes(int ctas, int rows) {
+  return (size_t)2 * ctas * rows * (kHeadDim * sizeof(float) + sizeof(float2)) +
+         (size_t)ctas * sizeof(Split) + 256;
+}
+Plan plan_of(const Dims8& d, int max_new, int ctas) {
+  Plan p;
+  const long long rows = (long long)max_new * d.gq;
+  p.many = rows > kFewRows;
+  // beside longer ones, single tokens alone are short: more columns would cost them products
+  const int most = p.many ? d.gq : (int)rows;
+  p.few = most <= 8 ? 8 : most <= 16 ? 16 : 32;
+  p.total = parts_bytes(ctas, p.few);
+  return p;
+}
+
+AttnParams params_of(const AttnCall& call, int ctas, int item_rows, void* workspace) {
+  AttnParams p;
+  p.c = call;
+  p.gq_inverse = (uint32_t)((1ull << 32) / call.d.gq + 1);
+  p.item_rows = item_rows;
+  char* w = static_cast<char*>(workspace);
+  p.part_o = reinterpret_cast<float*>(w);
+  w += (size_t)2 * ctas * item_rows * kHeadDim * sizeof(float);
+  p.part_ml = reinterpret_cast<float2*>(w);
+  w += (size_t)2 * ctas * item_rows * sizeof(float2);
+  p.splits = reinterpret_cast<Split*>(w);
+  return p;
+}
+
+}  // namespace
+
+size_t attn_workspace_bytes(const Dims8& d, int max_new, int sm_count) {
+  return plan_of(d, max_new, sm_count).total;
+}
+long long attn_most_units(const Dims8& d, int max_new) {
+  const Plan plan = plan_of(d, max_new, 1);
+  const long long tiles = plan.many ? ((long long)max_new * d.gq + 255) / 256 : 1;
+  return (long long)d.batch * d.hkv * (d.max_blocks + 8) * tiles;
+}
+
+cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream) {
+  const Plan plan = plan_of(call.d, call.batch.max_new, sm_count);
+  AttnParams p = params_of(call, sm_count, plan.few, workspace);
+  p.min_rows = 1;
+  p.max_rows = plan.few;
+  cudaError_t e = launch_rows(p, sm_count, stream);
+  if (e != cudaSuccess) return e;
+  if ((e = launch_join(p, sm_count, plan.few, stream)) != cudaSuccess || !plan.many) return e;
   const long long tasks = (long long)call.batch.n_tokens * call.d.hq;
-  rows_kernel<<<(unsigned)((tasks + 7) / 8), 256, 0, stream>>>(call);
+  simple_kernel<<<(unsigned)((tasks + 7) / 8), 256, 0, stream>>>(call, plan.few + 1);
   return cudaGetLastError();
 }
 

@@ -1,0 +1,242 @@
+// Work of kvq_block8_attn's kernels: who does what, and how shared items meet again.
+//
+// An item is one row tile of one (sequence, kv-head): rows t * gq + head of the sequence's
+// new tokens t and the gq heads that share the kv-head.  Its units are the tiles of
+// 2^TOK tokens that any of its rows sees, after a fixed cost in units.  All items' units
+// lie end to end (sequence, row tile, kv-head) and every CTA takes an equal contiguous
+// share.  An item that several CTAs share leaves partials (unnormalised rows, maximum,
+// sum) that a second kernel joins in the order of the tokens.
+#pragma once
+
+#include "block8.cuh"
+
+namespace kvq {
+namespace block8 {
+
+// An item that the shares of CTAs c .. last divide, left by CTA c for the join.
+struct Split {
+  int valid, inside, last, b, row_tile, head;
+};
+
+struct AttnParams {
+  AttnCall c;
+  uint32_t gq_inverse;      // floor(2^32 / gq) + 1
+  int min_rows, max_rows;   // the sequences this kernel takes, by their rows n * gq
+  int item_rows;            // rows of an item and of a partial
+  float* part_o;            // [2 * CTAs][item_rows][128]
+  float2* part_ml;          // [2 * CTAs][item_rows]
+  Split* splits;            // [CTAs]
+};
+
+#ifdef __CUDACC__
+// Row r of a sequence: its token.  Rows stay below 2^28 (checked on the host), where the
+// product with gq_inverse gives the exact quotient.
+__device__ __forceinline__ int token_of_row(const AttnParams& p, int r) {
+  return p.c.d.gq == 1 ? r : (int)__umulhi((uint32_t)r, p.gq_inverse);
+}
+// Offset of row r of (sequence with first row `row`, kv-head) in an array of queries.
+__device__ __forceinline__ long long row_offset(const AttnParams& p,
+                                                const long long (&stride)[2], int row,
+                                                int kv_head, int r) {
+  const int t = token_of_row(p, r);
+  return (row + t) * stride[0] + (kv_head * p.c.d.gq + r - t * p.c.d.gq) * stride[1];
+}
+
+// A sequence as this kernel takes it: n is 0 where it is another kernel's.
+__device__ __forceinline__ Seq attn_seq(const AttnParams& p, int b) {
+  Seq s = seq_of(p.c.d, p.c.batch, b);
+  const long long rows = (long long)s.n * p.c.d.gq;
+  if (rows < p.min_rows || rows > p.max_rows) s.n = 0;
+  return s;
+}
+
+// What one row tile of a sequence sees: token tiles 0 .. n_sink - 1, then from first on;
+// n of them in all.
+struct Span {
+  int p0, p1;  // positions of the first and last row (may be < 0)
+  int lo;      // first token of the window of the first row
+  int n_sink, first, n;
+  __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : first + i - n_sink; }
+};
+template <int TOK>
+__device__ __forceinline__ Span span_of(const AttnParams& p, const Seq& q, int row_tile) {
+  Span s;
+  const int r0 = row_tile * p.item_rows;
+  const int r1 = min(r0 + p.item_rows, q.n * p.c.d.gq) - 1;
+  s.p0 = q.L - q.n + token_of_row(p, r0);
+  s.p1 = q.L - q.n + token_of_row(p, r1);
+  s.lo = p.c.window ? max(0, max(s.p0, 0) - p.c.window + 1) : 0;
+  s.first = s.lo >> TOK;
+  // sinks is 0 without a window; the sum passes 2^31 in the largest caches
+  s.n_sink = min((int)(((uint32_t)p.c.sinks + ((1u << TOK) - 1)) >> TOK), s.first);
+  s.n = s.n_sink + (max(s.p1, 0) >> TOK) - s.first + 1;
+  return s;
+}
+__device__ __forceinline__ int row_tiles(const AttnParams& p, const Seq& q) {
+  return q.n > 0 ? (int)((uint32_t)(q.n * p.c.d.gq + p.item_rows - 1) / (uint32_t)p.item_rows)
+                 : 0;
+}
+
+// CTA c's share of the units: [begin(c), begin(c + 1)), equal to within one.
+struct Shares {
+  int q, r, n;  // units = n q + r over n CTAs
+  __device__ __forceinline__ int begin(int c) const { return c * q + min(c, r); }
+  __device__ __forceinline__ int owner(int u) const {
+    const int wide = (q + 1) * r;  // units of the CTAs that have q + 1
+    return u < wide ? (int)((uint32_t)u / (uint32_t)(q + 1))
+                    : r + (int)((uint32_t)(u - wide) / (uint32_t)q);
+  }
+};
+
+// Where a CTA's share begins.
+struct Start {
+  int b, row_tile, head, step;
+};
+
+// Units of all sequences, this CTA's share and where it begins, by all threads of the CTA
+// (at most 32 warps).  At least `least` units a CTA.  Ends behind a barrier; false where
+// the CTA has no share.
+template <int TOK, int COST>
+__device__ __forceinline__ bool plan_share(const AttnParams& p, int* scan, Start* start,
+                                           int least, Shares& shares, int& u0, int& u1) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+  const int per = (p.c.d.batch + threads - 1) / threads;
+  const int b0 = min(p.c.d.batch, tid * per), b1 = min(p.c.d.batch, b0 + per);
+  const auto units = [&](const Seq& q) {
+    int n = 0;
+    const int tiles = row_tiles(p, q);
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) n += (span_of<TOK>(p, q, t).n + COST) * p.c.d.hkv;
+    return n;
+  };
+  int mine = 0;
+#pragma unroll 1
+  for (int b = b0; b < b1; ++b) {
+    const Seq q = attn_seq(p, b);
+    if (q.bad && blockIdx.x == 0) set_flag(p.c.cache, q.bad);
+    mine += units(q);
+  }
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == 31) scan[warp] = inc;
+  __syncthreads();
+  int warps = lane < threads / 32 ? scan[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, warps, o);
+    if (lane >= o) warps += y;
+  }
+  const int total = __shfl_sync(0xffffffffu, warps, 31);
+  int before = __shfl_sync(0xffffffffu, warps, warp > 0 ? warp - 1 : 0);
+  if (warp == 0) before = 0;
+  before += inc - mine;
+  shares.n = min((int)gridDim.x, (int)(((uint32_t)total + least - 1) / (uint32_t)least));
+  if ((int)blockIdx.x >= shares.n) return false;
+  shares.q = (int)((uint32_t)total / (uint32_t)shares.n);
+  shares.r = total - shares.q * shares.n;
+  u0 = shares.begin(blockIdx.x);
+  u1 = shares.begin(blockIdx.x + 1);
+  if (before <= u0 && u0 < before + mine) {
+    int at = before;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+      const Seq q = attn_seq(p, b);
+      const int tiles = row_tiles(p, q);
+#pragma unroll 1
+      for (int t = 0; t < tiles; ++t) {
+        const int n = span_of<TOK>(p, q, t).n + COST;
+        if (u0 >= at && u0 < at + n * p.c.d.hkv) {
+          start->b = b;
+          start->row_tile = t;
+          start->head = (int)((uint32_t)(u0 - at) / (uint32_t)n);
+          start->step = u0 - at - start->head * n;
+        }
+        at += n * p.c.d.hkv;
+      }
+    }
+  }
+  __syncthreads();
+  return true;
+}
+
+// The items of a share, in order; every role walks them.
+template <int TOK, int COST>
+struct Walk {
+  int u, end, base;       // next unit, end of the share, first unit of the item
+  int b, row_tile, head;
+  Seq q;                  // the item's sequence
+  Span s;
+  int i0, i1;             // the item's tiles in this share
+  __device__ __forceinline__ void begin(const AttnParams& p, const Start& st, int u0, int u1) {
+    u = u0;
+    end = u1;
+    b = st.b;
+    row_tile = st.row_tile;
+    head = st.head;
+    base = u0 - st.step;
+    if (u < end) {
+      q = attn_seq(p, b);
+      s = span_of<TOK>(p, q, row_tile);
+    }
+  }
+  // The current item's part of the share; false at the end.
+  __device__ __forceinline__ bool next(const AttnParams& p) {
+    while (u < end) {
+      const int local = u - base, stop = min(s.n + COST, local + end - u);
+      i0 = max(local - COST, 0);
+      i1 = stop - COST;
+      if (i1 > i0) return true;
+      advance(p);  // nothing but a piece of the item's fixed cost
+    }
+    return false;
+  }
+  __device__ __forceinline__ void advance(const AttnParams& p) {
+    base += s.n + COST;
+    u = min(base, end);
+    if (++head < p.c.d.hkv || u >= end) return;
+    head = 0;
+    if (++row_tile == row_tiles(p, q)) {
+      row_tile = 0;
+      do {
+        q = attn_seq(p, ++b);
+      } while (q.n == 0);  // the share ends behind another item
+    }
+    s = span_of<TOK>(p, q, row_tile);
+  }
+  __device__ __forceinline__ bool whole() const { return i0 == 0 && i1 == s.n; }
+  // Slot of the CTA's partial: 0 for the item that its share begins in.
+  __device__ __forceinline__ int slot(int u0) const { return 2 * blockIdx.x + (u0 < base ? 1 : 0); }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float log2_fast(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+  if constexpr (BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+#endif
+
+// Launchers of the kernels: few rows (block8_rows.cu).
+constexpr int kFewRows = 32;
+cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream);
+
+}  // namespace block8
+}  // namespace kvq

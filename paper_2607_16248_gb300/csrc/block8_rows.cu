@@ -1,0 +1,677 @@
+// kvq_block8_attn for few rows a kv-head (single tokens, drafts): the cache is read once
+// at memory speed, the arithmetic stays out of its way.
+//
+// A warp takes whole blocks of 32 tokens.  TMA brings a block's keys and values (2 x 4 KB,
+// 128-byte swizzle) into the warp's own ring of slots; the block's scales follow by a small
+// asynchronous copy on the same barrier.  Scores S^T = K Q^T by m16n8k16 products with the
+// codes as A (tokens x channels) and eight query rows as B; O^T += V^T W^T with the codes
+// as A again (channels x tokens).  Codes become fp16 exactly, two at a time.  The sum over
+// a product's index may run in any order, so a lane takes 32 neighbouring channels of a
+// key (and of its query row), and 16 neighbouring channels of eight values; with the
+// swizzle no load of 16 bytes meets a bank twice.  Tokens of a value pair come together by
+// a byte permutation, weights get from the scores' layout to B's by an 8 x 8 transposition
+// in registers.
+//
+// Scales.  A score is (codes . q) * s_k: s_k joins the factor of the exponent.  A weight
+// times s_v is 2^(x + log2 s_v): the running maximum is taken of x + log2 s_v, fp16 weights
+// are w = 2^(x + log2 s_v - m + kLift), and the sum of the softmax is that of w / s_v, in
+// fp32.  So neither scale rounds a code, and weights stay within fp16 whatever the scales.
+//
+// The tokens behind the last whole block are a block of 16-bit elements that one warp loads
+// from the ring; bf16 ones go to fp16 times a power of two, which acts as their scale.
+#include <cuda.h>
+
+#include "block8_plan.cuh"
+
+namespace kvq {
+namespace block8 {
+
+namespace {
+
+constexpr int kTok = 5;            // 32 tokens a unit
+constexpr int kItemCost = 4;       // of an item in units: queries, merge, results
+constexpr int kWarps = 8;
+constexpr int kHalfPage = kGroup * kHeadDim;  // bytes of a block's keys (or values)
+constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
+constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
+constexpr float kNone = -1e30f;    // the maximum before any token
+constexpr long long kWaitCycles = 4000000000LL;  // bound of a wait (~2 s)
+
+template <int NT>
+struct Smem {
+  static constexpr int kSlots = NT == 4 ? 2 : 3;
+  unsigned char page[kWarps][kSlots][2 * kHalfPage];
+  float4 merge[kWarps / 2][NT * 8][32];
+  float m[kWarps][8 * NT], l[kWarps][8 * NT];
+  float2 scale[kWarps][kSlots];
+  uint64_t full[kWarps][kSlots];
+  int scan[32];
+  Start start;
+};
+
+__device__ __forceinline__ uint32_t sptr(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                    uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Codes 2 i, 2 i + 1 of a word as fp16.
+__device__ __forceinline__ uint32_t wide_lo(uint32_t v) {
+  uint32_t r;
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %1;\n cvt.rn.f16x2.e4m3x2 %0, a;\n}"
+      : "=r"(r)
+      : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t wide_hi(uint32_t v) {
+  uint32_t r;
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %1;\n cvt.rn.f16x2.e4m3x2 %0, b;\n}"
+      : "=r"(r)
+      : "r"(v));
+  return r;
+}
+
+template <int NT>
+struct State {
+  float m[NT][2], l[NT][2];  // of rows 8 nt + 2 tig, + 1; l of this lane's tokens alone
+  float o[NT][8][4];         // channels 16 gid + 2 i (0, 1) and + 1 (2, 3), the same rows
+  uint32_t q[NT][8][2];      // queries of row 8 nt + gid, channels 32 tig ..
+  float f[NT][2];            // factor of a score in the exponent
+};
+
+// What masks a block's tokens: the rows' positions.
+template <int NT>
+struct Rows {
+  int pos[NT][2];
+};
+
+// The softmax of a block's scores s[half of 16 tokens][nt][4], and its weights as B.
+// t0: the block's first token; edge: some row may not see some token.
+template <int NT>
+__device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
+                                        float (&s)[2][NT][4], int t0, bool edge, float sk,
+                                        float sv, uint32_t (&w)[2][NT][2]) {
+  const int gid = (threadIdx.x & 31) >> 2;
+  if (edge) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = t0 + 16 * h + 8 * (i >> 1) + gid, pos = rows.pos[n][i & 1];
+          if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks))
+            s[h][n][i] = -INFINITY;
+        }
+  }
+  const float lsv = log2_fast(sv), inv = 1.0f / sv;
+  bool up = false;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
+      up |= fmaf(mx, sk * st.f[n][j], lsv - st.m[n][j]) > kLag;
+    }
+  if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float m = fmaxf(st.m[n][j], fmaf(mx, sk * st.f[n][j], lsv));
+        const float f = exp2_fast(st.m[n][j] - m);
+        st.m[n][j] = m;
+        st.l[n][j] *= f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          st.o[n][i][j] *= f;
+          st.o[n][i][j + 2] *= f;
+        }
+      }
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float y[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float f = sk * st.f[n][j], c = lsv + kLift - st.m[n][j];
+      float sum = 0.0f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float x = exp2_fast(fmaf(s[h][n][j + 2 * i], f, c));
+          y[h][j + 2 * i] = x;
+          sum += x;
+        }
+      st.l[n][j] = fmaf(sum, inv, st.l[n][j]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        w[h][n][i] = transpose(pack16<false>(y[h][2 * i], y[h][2 * i + 1]));
+  }
+}
+
+// One block of codes in shared memory.
+template <int NT>
+__device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
+                                      const unsigned char* page, float2 scale, int t0, bool edge) {
+  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  float s[2][NT][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[h][n][i] = 0.0f;
+  const unsigned char* kr = page + gid * kHeadDim;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const unsigned char* at = kr + (((2 * tig + c) ^ gid) << 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4 x = *reinterpret_cast<const uint4*>(at + h * 16 * kHeadDim);
+      const uint4 y = *reinterpret_cast<const uint4*>(at + (h * 16 + 8) * kHeadDim);
+      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t a0 = wide_lo(xw[k]), a1 = wide_lo(yw[k]);
+        const uint32_t a2 = wide_hi(xw[k]), a3 = wide_hi(yw[k]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          mma(s[h][n], a0, a1, a2, a3, st.q[n][4 * c + k][0], st.q[n][4 * c + k][1]);
+      }
+    }
+  }
+  uint32_t w[2][NT][2];
+  weights<NT>(p, st, rows, s, t0, edge, scale.x, scale.y, w);
+  const unsigned char* vb = page + kHalfPage;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint4 x[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 16 * h + 8 * i + 2 * tig + e;
+        x[i][e] = *reinterpret_cast<const uint4*>(vb + r * kHeadDim + ((gid ^ (r & 7)) << 4));
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const auto word = [&](int i, int e) {
+        return k == 0 ? x[i][e].x : k == 1 ? x[i][e].y : k == 2 ? x[i][e].z : x[i][e].w;
+      };
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const uint32_t u = __byte_perm(word(0, 0), word(0, 1), z ? 0x7362 : 0x5140);
+        const uint32_t v = __byte_perm(word(1, 0), word(1, 1), z ? 0x7362 : 0x5140);
+        const uint32_t a0 = wide_lo(u), a1 = wide_hi(u), a2 = wide_lo(v), a3 = wide_hi(v);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          mma(st.o[n][2 * k + z], a0, a1, a2, a3, w[h][n][0], w[h][n][1]);
+      }
+    }
+  }
+}
+
+// 16-bit elements of a word as fp16, times f.
+template <bool BF16>
+__device__ __forceinline__ uint32_t to_half2(uint32_t u, float f) {
+  if constexpr (!BF16) return u;
+  return pack16<false>(__uint_as_float(u << 16) * f, __uint_as_float(u & 0xffff0000u) * f);
+}
+// The power of two that takes a magnitude (bf16 bits) to [2^14, 2^15).
+__device__ __forceinline__ float lift_of(uint32_t bits) {
+  const int e = max((int)(bits >> 7), 27) - 127;  // at least 2^-100
+  return bits ? __uint_as_float((uint32_t)(14 - e + 127) << 23) : 1.0f;
+}
+__device__ __forceinline__ uint32_t largest(uint32_t m, const uint4& v) {
+  m = __vmaxu2(m, v.x & 0x7fff7fffu);
+  m = __vmaxu2(m, v.y & 0x7fff7fffu);
+  m = __vmaxu2(m, v.z & 0x7fff7fffu);
+  return __vmaxu2(m, v.w & 0x7fff7fffu);
+}
+
+// The block of 16-bit tokens t0 .. L - 1 (fewer than 32), from the ring's rows.
+template <int NT, bool BF16>
+__device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
+                                        const uint16_t* k, const uint16_t* v, int t0, int L) {
+  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3, valid = L - t0;
+  float fk = 1.0f, fv = 1.0f;
+  if constexpr (BF16) {
+    uint32_t mk = 0u, mv = 0u;
+#pragma unroll 1
+    for (int r = lane >> 4; r < valid; r += 2) {
+      mk = largest(mk, *reinterpret_cast<const uint4*>(k + r * kHeadDim + 8 * (lane & 15)));
+      mv = largest(mv, *reinterpret_cast<const uint4*>(v + r * kHeadDim + 8 * (lane & 15)));
+    }
+    mk = max(mk & 0xffffu, mk >> 16);
+    mv = max(mv & 0xffffu, mv >> 16);
+    fk = lift_of(__reduce_max_sync(0xffffffffu, mk));
+    fv = lift_of(__reduce_max_sync(0xffffffffu, mv));
+  }
+  const auto load = [&](const uint16_t* base, int r, int part) {
+    return r < valid ? *reinterpret_cast<const uint4*>(base + r * kHeadDim + part)
+                     : make_uint4(0u, 0u, 0u, 0u);
+  };
+  float s[2][NT][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[h][n][i] = 0.0f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {  // 8 channels: two steps of the product
+      const uint4 x = load(k, 16 * h + gid, 32 * tig + 8 * c);
+      const uint4 y = load(k, 16 * h + 8 + gid, 32 * tig + 8 * c);
+      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t a0 = to_half2<BF16>(xw[2 * i], fk), a1 = to_half2<BF16>(yw[2 * i], fk);
+        const uint32_t a2 = to_half2<BF16>(xw[2 * i + 1], fk),
+                       a3 = to_half2<BF16>(yw[2 * i + 1], fk);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          mma(s[h][n], a0, a1, a2, a3, st.q[n][2 * c + i][0], st.q[n][2 * c + i][1]);
+      }
+    }
+  }
+  uint32_t w[2][NT][2];
+  weights<NT>(p, st, rows, s, t0, true, 1.0f / fk, 1.0f / fv, w);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {  // 8 channels each
+      uint4 x[2][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          x[i][e] = load(v, 16 * h + 8 * i + 2 * tig + e, 16 * gid + 8 * c);
+#pragma unroll
+      for (int k2 = 0; k2 < 4; ++k2) {
+        const auto word = [&](int i, int e) {
+          return to_half2<BF16>(k2 == 0   ? x[i][e].x
+                                : k2 == 1 ? x[i][e].y
+                                : k2 == 2 ? x[i][e].z
+                                          : x[i][e].w,
+                                fv);
+        };
+        const uint32_t a0 = __byte_perm(word(0, 0), word(0, 1), 0x5410);
+        const uint32_t a1 = __byte_perm(word(0, 0), word(0, 1), 0x7632);
+        const uint32_t a2 = __byte_perm(word(1, 0), word(1, 1), 0x5410);
+        const uint32_t a3 = __byte_perm(word(1, 0), word(1, 1), 0x7632);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          mma(st.o[n][4 * c + k2], a0, a1, a2, a3, w[h][n][0], w[h][n][1]);
+      }
+    }
+}
+
+// Queries of an item: row 8 n + gid's channels 32 tig .. 32 tig + 31, bf16 ones times a power
+// of two; the rows' factors and positions.
+template <int NT, bool BF16>
+__device__ __forceinline__ void load_queries(const AttnParams& p, const Seq& q, int head,
+                                             State<NT>& st, Rows<NT>& rows) {
+  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const int n_rows = q.n * p.c.d.gq;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = 8 * n + gid;
+    uint4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (r < n_rows) {
+      const uint4* src = reinterpret_cast<const uint4*>(
+          p.c.q + row_offset(p, p.c.q_stride, q.row, head, r) + 32 * tig);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __ldg(src + i);
+    }
+    float f = 1.0f;
+    if constexpr (BF16) {
+      uint32_t m = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = largest(m, x[i]);
+      m = max(m & 0xffffu, m >> 16);
+      m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      f = lift_of(m);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      st.q[n][2 * i][0] = to_half2<BF16>(x[i].x, f);
+      st.q[n][2 * i][1] = to_half2<BF16>(x[i].y, f);
+      st.q[n][2 * i + 1][0] = to_half2<BF16>(x[i].z, f);
+      st.q[n][2 * i + 1][1] = to_half2<BF16>(x[i].w, f);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      st.f[n][j] = p.c.scale_log2 / (BF16 ? __shfl_sync(0xffffffffu, f, 8 * tig + 4 * j) : 1.0f);
+      rows.pos[n][j] = q.L - q.n + token_of_row(p, 8 * n + 2 * tig + j);
+      st.m[n][j] = kNone;
+      st.l[n][j] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) st.o[n][i][j] = 0.0f;
+  }
+}
+
+// A warp's blocks over all items of the share, in order, ahead of their use.
+struct Feed {
+  Walk<kTok, kItemCost> w;
+  bool more;
+  int i, entry;        // next unit of the item; this lane's table entry of 32 units
+  int i_entry;         // the unit of lane 0's entry
+};
+
+template <int NT, bool BF16>
+__global__ void __launch_bounds__(32 * kWarps, 1)
+rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map,
+            const __grid_constant__ CUtensorMap v_map) {
+  extern __shared__ __align__(1024) unsigned char raw[];
+  Smem<NT>& sm = *reinterpret_cast<Smem<NT>*>(raw);
+  constexpr int kSlots = Smem<NT>::kSlots;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  if (tid == 0) p.splits[blockIdx.x].valid = 0;
+  if (lane == 0) {
+    for (int i = 0; i < kSlots; ++i)
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(sptr(&sm.full[warp][i]))
+                   : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  Shares shares;
+  int u0, u1;
+  if (!plan_share<kTok, kItemCost>(p, sm.scan, &sm.start, kWarps, shares, u0, u1)) return;
+
+  // Units of an item before the 16-bit ones are whole blocks; warp w takes every eighth.
+  const auto whole_units = [](const Walk<kTok, kItemCost>& w) {
+    return w.s.tile(w.s.n - 1) * kGroup + kGroup > w.q.L ? min(w.i1, w.s.n - 1) : w.i1;
+  };
+  Feed f;
+  f.w.begin(p, sm.start, u0, u1);
+  f.more = f.w.next(p);
+  f.i = f.w.i0 + warp;
+  f.i_entry = -1;
+  // The next block of this warp into slot `slot`.
+  const auto feed = [&](int slot) {
+    while (f.more && f.i >= whole_units(f.w)) {
+      f.w.advance(p);
+      f.more = f.w.next(p);
+      f.i = f.w.i0 + warp;
+      f.i_entry = -1;
+    }
+    if (!f.more) return;
+    if (f.i_entry < 0 || f.i >= f.i_entry + 32 * kWarps) {
+      f.i_entry = f.i;
+      const int i = f.i + kWarps * lane;
+      f.entry = i < whole_units(f.w)
+                    ? __ldg(p.c.cache.block_table + (long long)f.w.b * p.c.d.max_blocks +
+                            f.w.s.tile(i))
+                    : 0;
+    }
+    const int page = __shfl_sync(0xffffffffu, f.entry, (f.i - f.i_entry) / kWarps);
+    f.i += kWarps;
+    if (lane == 0) {
+      const uint32_t bar = sptr(&sm.full[warp][slot]);
+      if ((unsigned)page < (unsigned)p.c.cache.n_pages) {
+        const int at = page * p.c.d.hkv + f.w.head;
+        const uint32_t dst = sptr(sm.page[warp][slot]);
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                     "r"(2 * kHalfPage)
+                     : "memory");
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], "
+            "[%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(&k_map), "r"(0), "r"(at * kGroup), "r"(bar)
+            : "memory");
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], "
+            "[%1, {%2, %3}], [%4];" ::"r"(dst + kHalfPage),
+            "l"(&v_map), "r"(0), "r"(at * kGroup), "r"(bar)
+            : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(
+                         sptr(&sm.scale[warp][slot])),
+                     "l"(p.c.cache.scales + 2ll * at)
+                     : "memory");
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+      } else {
+        set_flag(p.c.cache, KVQ_FLAG_BAD_PAGE);
+        sm.scale[warp][slot] = make_float2(-1.0f, -1.0f);
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 2;" ::"r"(bar) : "memory");
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) feed(i);
+
+  int slot = 0;
+  uint32_t phase = 0;
+  const auto arrived = [&](int i, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 10000;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(sptr(&sm.full[warp][i])), "r"(parity)
+        : "memory");
+    return ok != 0;
+  };
+  // Bounded; for a whole warp.
+  const auto wait = [&](int i, uint32_t parity) {
+    bool ok = arrived(i, parity);
+    if (!ok) {
+      const long long begun = clock64();
+      while (!(ok = arrived(i, parity)) && clock64() - begun < kWaitCycles) {
+      }
+    }
+    return __all_sync(0xffffffffu, ok) != 0;
+  };
+  bool lost = false;  // a wait ran out: the warp only keeps the others company
+  Walk<kTok, kItemCost> w;
+  w.begin(p, sm.start, u0, u1);
+#pragma unroll 1
+  for (; w.next(p); w.advance(p)) {
+    State<NT> st;
+    Rows<NT> rows;
+    load_queries<NT, BF16>(p, w.q, w.head, st, rows);
+    const int whole = whole_units(w);
+    if (warp == kWarps - 1 && whole < w.i1) {
+      const int t0 = w.s.tile(whole) * kGroup;
+      const long long at =
+          (((long long)w.b * p.c.d.hkv + w.head) * kRing + (t0 & (kRing - 1))) * kHeadDim;
+      tail_block<NT, BF16>(p, st, rows, p.c.cache.k_ring + at, p.c.cache.v_ring + at, t0, w.q.L);
+    }
+#pragma unroll 1
+    for (int i = w.i0 + warp; i < whole; i += kWarps) {
+      const int t0 = w.s.tile(i) * kGroup;
+      if (lost || !wait(slot, phase)) {
+        if (!lost && lane == 0) set_flag(p.c.cache, KVQ_FLAG_WAIT_TIMEOUT);
+        lost = true;
+        break;
+      }
+      const float2 scale = sm.scale[warp][slot];
+      if (scale.x > 0.0f) {
+        const bool edge = t0 + kGroup - 1 > w.s.p0 ||
+                          (p.c.window && t0 <= w.s.p1 - p.c.window &&
+                           t0 + kGroup > p.c.sinks);
+        block<NT>(p, st, rows, sm.page[warp][slot], scale, t0, edge);
+      }
+      __syncwarp();
+      feed(slot);
+      if (++slot == kSlots) slot = 0, phase ^= 1;
+    }
+    // The warps' parts of the item meet in shared memory, always in the same order.
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float l = st.l[n][j];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (gid == 0) {
+          sm.m[warp][8 * n + 2 * tig + j] = st.m[n][j];
+          sm.l[warp][8 * n + 2 * tig + j] = l;
+        }
+      }
+    __syncthreads();
+    float mm[NT][2], ll[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = 8 * n + 2 * tig + j;
+        float m = kNone, l = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) m = fmaxf(m, sm.m[k][r]);
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) l = fmaf(sm.l[k][r], exp2_fast(sm.m[k][r] - m), l);
+        mm[n][j] = m;
+        ll[n][j] = l;
+        const float g = exp2_fast(st.m[n][j] - m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          st.o[n][i][j] *= g;
+          st.o[n][i][j + 2] *= g;
+        }
+      }
+#pragma unroll
+    for (int k = kWarps / 2; k; k >>= 1) {
+      if (warp >= k && warp < 2 * k) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            sm.merge[warp - k][8 * n + i][lane] =
+                make_float4(st.o[n][i][0], st.o[n][i][1], st.o[n][i][2], st.o[n][i][3]);
+      }
+      __syncthreads();
+      if (warp < k) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 x = sm.merge[warp][8 * n + i][lane];
+            st.o[n][i][0] += x.x, st.o[n][i][1] += x.y;
+            st.o[n][i][2] += x.z, st.o[n][i][3] += x.w;
+          }
+      }
+    }
+    if (warp == 0) {
+      const int n_rows = w.q.n * p.c.d.gq;
+      const bool direct = w.whole();
+      const int slot_row = w.slot(u0) * p.item_rows;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = 8 * n + 2 * tig + j;
+          if (r >= n_rows) continue;
+          if (direct) {
+            const float f = ll[n][j] > 0.0f ? 1.0f / ll[n][j] : 0.0f;
+            uint32_t x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = pack16<BF16>(st.o[n][i][j] * f, st.o[n][i][j + 2] * f);
+            uint4* dst = reinterpret_cast<uint4*>(
+                p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r) + 16 * gid);
+            dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
+            dst[1] = make_uint4(x[4], x[5], x[6], x[7]);
+          } else {
+            float4* dst = reinterpret_cast<float4*>(
+                p.part_o + (long long)(slot_row + r) * kHeadDim + 16 * gid);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              dst[i] = make_float4(st.o[n][2 * i][j], st.o[n][2 * i][j + 2],
+                                   st.o[n][2 * i + 1][j], st.o[n][2 * i + 1][j + 2]);
+            if (gid == 0) p.part_ml[slot_row + r] = make_float2(mm[n][j], ll[n][j]);
+          }
+        }
+      if (!direct && w.i0 == 0 && lane == 0)
+        p.splits[blockIdx.x] = Split{1, u0 < w.base ? 1 : 0,
+                                     shares.owner(w.base + kItemCost + w.s.n - 1), w.b, 0, w.head};
+    }
+  }
+  // copies that are still on their way get their time before the memory goes
+  if (lost)
+    for (int i = 0; i < kSlots; ++i)
+      wait((slot + i) % kSlots, slot + i < kSlots ? phase : phase ^ 1);
+}
+
+// The tensor map of codes [rows][128], 32 rows a copy.
+cudaError_t make_map(CUtensorMap* map, const void* base, long long rows) {
+  using Encode = decltype(&cuTensorMapEncodeTiled);
+  static std::atomic<Encode> found{nullptr};
+  Encode encode = found.load(std::memory_order_acquire);
+  if (!encode) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    const cudaError_t e =
+        cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &r);
+    if (e != cudaSuccess) return e;
+    if (r != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+    encode = reinterpret_cast<Encode>(fn);
+    found.store(encode, std::memory_order_release);
+  }
+  const cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)kHeadDim};
+  const cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)kGroup}, one[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims,
+                            strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int NT, bool BF16>
+cudaError_t launch(const AttnParams& p, int ctas, cudaStream_t stream) {
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = once_per_device(done, [] {
+    return cudaFuncSetAttribute(rows_kernel<NT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)sizeof(Smem<NT>));
+  });
+  if (e != cudaSuccess) return e;
+  CUtensorMap k, v;
+  const long long rows = (long long)p.c.cache.n_pages * p.c.d.hkv * kGroup;
+  if ((e = make_map(&k, p.c.cache.k_codes, rows)) != cudaSuccess) return e;
+  if ((e = make_map(&v, p.c.cache.v_codes, rows)) != cudaSuccess) return e;
+  rows_kernel<NT, BF16><<<ctas, 32 * kWarps, sizeof(Smem<NT>), stream>>>(p, k, v);
+  return cudaGetLastError();
+}
+
+template <int NT>
+cudaError_t launch_type(const AttnParams& p, int ctas, cudaStream_t stream) {
+  return p.c.d.bf16 ? launch<NT, true>(p, ctas, stream) : launch<NT, false>(p, ctas, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream) {
+  switch (p.item_rows) {
+    case 8: return launch_type<1>(p, ctas, stream);
+    case 16: return launch_type<2>(p, ctas, stream);
+    default: return launch_type<4>(p, ctas, stream);
+  }
+}
+
+}  // namespace block8
+}  // namespace kvq
