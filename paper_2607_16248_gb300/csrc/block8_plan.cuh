@@ -234,9 +234,10 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
 }
 #endif
 
-// Launchers of the kernels: few rows (block8_rows.cu).
+// Launchers of the kernels: few rows (block8_rows.cu), many (block8_chunk.cu).
 constexpr int kFewRows = 32;
 cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream);
+cudaError_t launch_chunk(const AttnParams& p, int ctas, cudaStream_t stream);
 
 }  // namespace block8
 }  // namespace kvq
