@@ -570,7 +570,7 @@ kvq_status kvq_sample(const float* logits, int64_t logits_stride,
 typedef struct kvq_block8_config {
   int32_t batch;      /* 1 .. 8192 */
   int32_t n_q_heads;  /* query head i reads kv-head i / (n_q_heads / n_kv_heads): */
-  int32_t n_kv_heads; /* an integer in [1, 32] */
+  int32_t n_kv_heads; /* an integer in [1, 32]; n_kv_heads 1 .. 1024 */
   int32_t head_dim;   /* 128 */
   int32_t block;      /* 32 */
   int32_t max_len;    /* a positive multiple of 32 */

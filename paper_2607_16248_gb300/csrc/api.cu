@@ -698,8 +698,8 @@ static kvq_status check_block8_config(const kvq_block8_config* c) {
   if (!c) return fail(KVQ_ERR_ARG, "config is NULL");
   if (c->batch < 1 || c->batch > 8192)
     return fail(KVQ_ERR_SHAPE, "batch must be in [1, 8192] (got %d)", c->batch);
-  if (c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_kv_heads > 65535)
-    return fail(KVQ_ERR_SHAPE, "head counts must be >= 1 and n_kv_heads <= 65535");
+  if (c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_kv_heads > 1024)
+    return fail(KVQ_ERR_SHAPE, "head counts must be >= 1 and n_kv_heads <= 1024");
   if (c->n_q_heads % c->n_kv_heads)
     return fail(KVQ_ERR_SHAPE, "n_q_heads (%d) must be a multiple of n_kv_heads (%d)",
                 c->n_q_heads, c->n_kv_heads);

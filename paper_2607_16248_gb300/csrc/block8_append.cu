@@ -1,12 +1,11 @@
 // kvq_block8_append: rotation of queries and keys, the rings, and the codes of the
 // blocks that the new tokens complete, in one launch.
 //
-// A warp's task is either one block's keys or values of one kv-head (32 x 128 elements,
-// two rows at a time, all in its registers: the block's largest magnitude is known before
-// the first code) or one token's queries of eight heads.  In both, 16 lanes share a row
-// of 128 channels; a lane holds two groups of four channels such that it has both
-// channels of its four rotated pairs (`Lane`), so a rotation needs no exchange and each
-// cosine is read once.
+// A CTA of four warps takes one block's keys or values of one kv-head (32 x 128 elements in
+// its registers: the block's largest magnitude is known before the first code), or a warp
+// each takes one token's queries of eight heads.  16 lanes share a row of 128 channels; a
+// lane holds two groups of four channels such that it has both channels of its four rotated
+// pairs (`Lane`), so a rotation needs no exchange and each cosine is read once.
 //
 // The codes need the keys' exact roundings: a key next to a border of its type changes
 // its block's scale, and a quotient next to a border its code.  Products and sums
@@ -15,7 +14,7 @@
 //
 // A block that was begun by an earlier call has its first rows in the ring, in slots that
 // this call's newest tokens may take.  Of the two blocks whose tokens go to the ring, the
-// one with the same slots (an even number of blocks behind) is done by the same warp,
+// one with the same slots (an even number of blocks behind) is done by the same CTA,
 // after the begun block's rows are in its registers.
 #include "block8.cuh"
 
@@ -26,7 +25,7 @@ namespace block8 {
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 constexpr int kQueryHeads = 8;  // heads of a query task
 
 __device__ __forceinline__ uint2 ld8(const uint16_t* p) {
@@ -120,36 +119,37 @@ __device__ __forceinline__ int table_row(const AppendCall& call, int row, int po
   return at;
 }
 
+// Two neighbouring results of a type's word, y = x1 c - x2 s each.  Keys: rounded as if
+// nothing had been rounded before.  The quick sum is within 2^-23 (|x1 c| + |x2 s|) of the
+// exact one, so where both ends of that range round alike, so does the exact sum; the
+// others (one fp16 number in 20) take the long way.
+template <bool BF16, bool KEY>
+__device__ __forceinline__ uint32_t rotate2(float x1, float c1, float x2, float s1, float w1,
+                                            float c2, float w2, float s2) {
+  const float p = x1 * c1, q = x2 * s1, u = w1 * c2, v = w2 * s2;
+  const float y = p - q, z = u - v;
+  if constexpr (!KEY) return narrow<BF16>(y, z);
+  constexpr float kRange = 1.25f * 0x1p-23f;
+  const float dy = (fabsf(p) + fabsf(q)) * kRange, dz = (fabsf(u) + fabsf(v)) * kRange;
+  const uint32_t lo = narrow<BF16>(y - dy, z - dz), hi = narrow<BF16>(y + dy, z + dz);
+  if (lo == hi) return lo;
+  return narrow<BF16>(rotate_odd(x1, c1, x2, s1), rotate_odd(w1, c2, w2, s2));
+}
+
 template <bool BF16, bool KEY>
 __device__ __forceinline__ void rotate(uint2& a, uint2& b, const Lane& l, const Angles& t) {
   const float2 a0 = widen<BF16>(a.x), a1 = widen<BF16>(a.y);
   const float2 b0 = widen<BF16>(b.x), b1 = widen<BF16>(b.y);
-  float x1[4], x2[4];
   if (l.paired) {
-    x1[0] = a0.x, x2[0] = a0.y, x1[1] = a1.x, x2[1] = a1.y;
-    x1[2] = b0.x, x2[2] = b0.y, x1[3] = b1.x, x2[3] = b1.y;
+    a.x = rotate2<BF16, KEY>(a0.x, t.c.x, a0.y, t.s.x, a0.y, t.c.x, a0.x, -t.s.x);
+    a.y = rotate2<BF16, KEY>(a1.x, t.c.y, a1.y, t.s.y, a1.y, t.c.y, a1.x, -t.s.y);
+    b.x = rotate2<BF16, KEY>(b0.x, t.c.z, b0.y, t.s.z, b0.y, t.c.z, b0.x, -t.s.z);
+    b.y = rotate2<BF16, KEY>(b1.x, t.c.w, b1.y, t.s.w, b1.y, t.c.w, b1.x, -t.s.w);
   } else {
-    x1[0] = a0.x, x1[1] = a0.y, x1[2] = a1.x, x1[3] = a1.y;
-    x2[0] = b0.x, x2[1] = b0.y, x2[2] = b1.x, x2[3] = b1.y;
-  }
-  const float c[4] = {t.c.x, t.c.y, t.c.z, t.c.w}, s[4] = {t.s.x, t.s.y, t.s.z, t.s.w};
-  float y1[4], y2[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (KEY) {
-      y1[i] = rotate_odd(x1[i], c[i], x2[i], s[i]);
-      y2[i] = rotate_odd(x2[i], c[i], x1[i], -s[i]);
-    } else {
-      y1[i] = x1[i] * c[i] - x2[i] * s[i];
-      y2[i] = x2[i] * c[i] + x1[i] * s[i];
-    }
-  }
-  if (l.paired) {
-    a = make_uint2(narrow<BF16>(y1[0], y2[0]), narrow<BF16>(y1[1], y2[1]));
-    b = make_uint2(narrow<BF16>(y1[2], y2[2]), narrow<BF16>(y1[3], y2[3]));
-  } else {
-    a = make_uint2(narrow<BF16>(y1[0], y1[1]), narrow<BF16>(y1[2], y1[3]));
-    b = make_uint2(narrow<BF16>(y2[0], y2[1]), narrow<BF16>(y2[2], y2[3]));
+    a.x = rotate2<BF16, KEY>(a0.x, t.c.x, b0.x, t.s.x, a0.y, t.c.y, b0.y, t.s.y);
+    a.y = rotate2<BF16, KEY>(a1.x, t.c.z, b1.x, t.s.z, a1.y, t.c.w, b1.y, t.s.w);
+    b.x = rotate2<BF16, KEY>(b0.x, t.c.x, a0.x, -t.s.x, b0.y, t.c.y, a0.y, -t.s.y);
+    b.y = rotate2<BF16, KEY>(b1.x, t.c.z, a1.x, -t.s.z, b1.y, t.c.w, a1.y, -t.s.w);
   }
 }
 
@@ -158,96 +158,144 @@ __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
   return __vmaxu2(a, b & 0x7fff7fffu);
 }
 
-template <bool BF16>
-__device__ __forceinline__ uint32_t codes_of(uint2 v, float scale) {
-  const float2 x = widen<BF16>(v.x), y = widen<BF16>(v.y);
-  const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(
-      make_float2(__fdiv_rn(x.x, scale), __fdiv_rn(x.y, scale)), __NV_SATFINITE, __NV_E4M3);
-  const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(
-      make_float2(__fdiv_rn(y.x, scale), __fdiv_rn(y.y, scale)), __NV_SATFINITE, __NV_E4M3);
+// Four codes.  A product with 1 / scale is within 2^-22 of the quotient; where it is not
+// that near to a border of the codes (bits 0 .. 19 of the fp32 number at their middle, as
+// long as the code is a normal number), it rounds as the quotient does.
+__device__ __forceinline__ bool near_border(float q) {
+  const uint32_t u = __float_as_uint(q);
+  return ((u & 0xfffffu) - 0x7fff8u) <= 16u || (q != 0.0f && fabsf(q) < 0x1p-6f);
+}
+__device__ __forceinline__ uint32_t to_codes(float x, float y, float z, float w) {
+  const __nv_fp8x2_storage_t a =
+      __nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3);
+  const __nv_fp8x2_storage_t b =
+      __nv_cvt_float2_to_fp8x2(make_float2(z, w), __NV_SATFINITE, __NV_E4M3);
   return (uint32_t)a | ((uint32_t)b << 16);
 }
-
-// Block `blk` of a sequence: keys (KEY) or values of kv-head h.
-template <bool BF16, bool KEY>
-__device__ __forceinline__ void block_task(const AppendCall& call, const Seq& s, int b, int blk,
-                                           int h) {
-  const int lane = threadIdx.x & 31, c = lane & 15, half = lane >> 4;
-  const Lane l = lane_of(c, KEY ? call.p.rot_dim >> 1 : 0, KEY && call.p.paired);
-  const int before = s.L - s.n, t0 = blk * kGroup;
-  const bool whole = t0 + kGroup <= s.L;
-  const uint16_t* src = KEY ? call.p.k : call.p.v;
-  const int64_t* stride = KEY ? call.p.k_stride : call.p.v_stride;
-  uint16_t* ring = (KEY ? call.cache.k_ring : call.cache.v_ring) +
-                   ((long long)b * call.d.hkv + h) * (kRing * kHeadDim);
-  const bool keep = blk >= s.L / kGroup - 1;  // the block's new tokens go to the ring
-  src += h * stride[1];
-  uint2 x[16][2];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int pos = t0 + 2 * i + half;
-    x[i][0] = x[i][1] = make_uint2(0u, 0u);
-    if (pos < before) {
-      if (whole) {
-        const uint16_t* r = ring + (pos & (kRing - 1)) * kHeadDim;
-        x[i][0] = ld8_ring(r + l.g0);
-        x[i][1] = ld8_ring(r + l.g1);
-      }
-    } else if (pos < s.L) {
-      const uint16_t* r = src + (long long)(s.row + pos - before) * stride[0];
-      x[i][0] = ld8(r + l.g0);
-      x[i][1] = ld8(r + l.g1);
-    }
-  }
-  if constexpr (KEY) {
-    if (l.rotate) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int pos = t0 + 2 * i + half;
-        if (pos >= before && pos < s.L)
-          rotate<BF16, true>(x[i][0], x[i][1], l,
-                             angles_of(call.p, l, table_row(call, s.row + pos - before, pos)));
-      }
-    }
-  }
-  if (keep) {
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int pos = t0 + 2 * i + half;
-      if (pos >= before && pos < s.L) {
-        uint16_t* r = ring + (pos & (kRing - 1)) * kHeadDim;
-        st8(r + l.g0, x[i][0]);
-        st8(r + l.g1, x[i][1]);
-      }
-    }
-  }
-  if (!whole) return;
-  const int page = __ldg(call.cache.block_table + (long long)b * call.d.max_blocks + blk);
-  if ((unsigned)page >= (unsigned)call.cache.n_pages) {
-    if (lane == 0) set_flag(call.cache, KVQ_FLAG_BAD_PAGE);
-    return;
-  }
-  uint32_t m = 0u;
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    m = larger(larger(m, x[i][0].x), larger(larger(x[i][0].y & 0x7fff7fffu, x[i][1].x), x[i][1].y));
-  m = max(m & 0xffffu, m >> 16);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-  const float amax = widen<BF16>(m).x;
-  const float scale =
-      m ? fminf(fmaxf(__fdiv_rn(amax, kMaxCode), 0x1p-60f), 0x1p60f) : 1.0f;
-  const long long at = (long long)page * call.d.hkv + h;
-  if (lane == 0) call.cache.scales[2 * at + (KEY ? 0 : 1)] = scale;
-  uint8_t* codes = (KEY ? call.cache.k_codes : call.cache.v_codes) + at * (kGroup * kHeadDim);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    uint8_t* r = codes + (2 * i + half) * kHeadDim;
-    *reinterpret_cast<uint32_t*>(r + l.g0) = codes_of<BF16>(x[i][0], scale);
-    *reinterpret_cast<uint32_t*>(r + l.g1) = codes_of<BF16>(x[i][1], scale);
-  }
+template <bool BF16>
+__device__ __forceinline__ uint32_t codes_of(uint2 v, float scale, float inv) {
+  const float2 x = widen<BF16>(v.x), y = widen<BF16>(v.y);
+  const float a = x.x * inv, b = x.y * inv, c = y.x * inv, d = y.y * inv;
+  if (near_border(a) || near_border(b) || near_border(c) || near_border(d))
+    return to_codes(__fdiv_rn(x.x, scale), __fdiv_rn(x.y, scale), __fdiv_rn(y.x, scale),
+                    __fdiv_rn(y.y, scale));
+  return to_codes(a, b, c, d);
 }
+
+// Keys (KEY) or values of kv-head h of a sequence.
+template <bool BF16, bool KEY>
+struct Task {
+  const AppendCall& call;
+  const Seq& s;
+  int b, h, before;
+  Lane l;
+  const uint16_t* src;
+  uint16_t* ring;
+  __device__ __forceinline__ Task(const AppendCall& call, const Seq& s, int b, int h)
+      : call(call), s(s), b(b), h(h), before(s.L - s.n) {
+    l = lane_of(threadIdx.x & 15, KEY ? call.p.rot_dim >> 1 : 0, KEY && call.p.paired);
+    src = (KEY ? call.p.k : call.p.v) + h * (KEY ? call.p.k_stride : call.p.v_stride)[1];
+    ring = (KEY ? call.cache.k_ring : call.cache.v_ring) +
+           ((long long)b * call.d.hkv + h) * (kRing * kHeadDim);
+  }
+  __device__ __forceinline__ const uint16_t* new_row(int pos) const {
+    return src + (long long)(s.row + pos - before) * (KEY ? call.p.k_stride : call.p.v_stride)[0];
+  }
+  __device__ __forceinline__ uint16_t* ring_row(int pos) const {
+    return ring + (pos & (kRing - 1)) * kHeadDim;
+  }
+  // N rows from pos on, every second one: rotated if they are new.
+  template <int N>
+  __device__ __forceinline__ void turn(uint2 (&x)[N][2], int pos) const {
+    if constexpr (KEY) {
+      if (!l.rotate) return;
+      Angles t[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int at = pos + 2 * i;
+        const bool fresh = at >= before && at < s.L;
+        t[i] = angles_of(call.p, l, fresh ? table_row(call, s.row + at - before, at) : 0);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int at = pos + 2 * i;
+        if (at >= before && at < s.L) rotate<BF16, true>(x[i][0], x[i][1], l, t[i]);
+      }
+    }
+  }
+
+  // New tokens of a block that stays open: to the ring.
+  __device__ __forceinline__ void open_block(int blk) const {
+#pragma unroll 1
+    for (int pos = max(blk * kGroup, before) + (threadIdx.x >> 4); pos < s.L;
+         pos += 2 * kWarps) {
+      uint2 x[1][2];
+      x[0][0] = ld8(new_row(pos) + l.g0);
+      x[0][1] = ld8(new_row(pos) + l.g1);
+      turn<1>(x, pos);
+      st8(ring_row(pos) + l.g0, x[0][0]);
+      st8(ring_row(pos) + l.g1, x[0][1]);
+    }
+  }
+
+  // A block that is whole now: codes, and the ring if it is among the last two.
+  __device__ __forceinline__ void whole_block(int blk, uint32_t* share) const {
+    constexpr int N = kGroup / (2 * kWarps);  // rows of a lane
+    const int warp = threadIdx.x >> 5, r0 = 2 * N * warp + ((threadIdx.x >> 4) & 1);
+    const int t0 = blk * kGroup + r0;
+    const int page = __ldg(call.cache.block_table + (long long)b * call.d.max_blocks + blk);
+    uint2 x[N][2];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int pos = t0 + 2 * i;
+      const uint16_t* r = pos < before ? ring_row(pos) : new_row(pos);
+      x[i][0] = ld8_ring(r + l.g0);
+      x[i][1] = ld8_ring(r + l.g1);
+    }
+    turn<N>(x, t0);
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) m = larger(larger(m, x[i][k].x), x[i][k].y);
+    m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+    if ((threadIdx.x & 31) == 0) share[warp] = m;
+    __syncthreads();  // and every row of the ring has been read
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) m = max(m, share[w]);
+    if (blk >= s.L / kGroup - 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int pos = t0 + 2 * i;
+        if (pos >= before) {
+          st8(ring_row(pos) + l.g0, x[i][0]);
+          st8(ring_row(pos) + l.g1, x[i][1]);
+        }
+      }
+    }
+    if ((unsigned)page >= (unsigned)call.cache.n_pages) {
+      if (threadIdx.x == 0) set_flag(call.cache, KVQ_FLAG_BAD_PAGE);
+      return;
+    }
+    const float amax = widen<BF16>(m).x;
+    const float scale = m ? fminf(fmaxf(__fdiv_rn(amax, kMaxCode), 0x1p-60f), 0x1p60f) : 1.0f;
+    const float inv = __frcp_rn(scale);
+    const long long at = (long long)page * call.d.hkv + h;
+    if (threadIdx.x == 0) call.cache.scales[2 * at + (KEY ? 0 : 1)] = scale;
+    uint8_t* codes = (KEY ? call.cache.k_codes : call.cache.v_codes) + at * (kGroup * kHeadDim);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint8_t* r = codes + (r0 + 2 * i) * kHeadDim;
+      *reinterpret_cast<uint32_t*>(r + l.g0) = codes_of<BF16>(x[i][0], scale, inv);
+      *reinterpret_cast<uint32_t*>(r + l.g1) = codes_of<BF16>(x[i][1], scale, inv);
+    }
+  }
+
+  __device__ __forceinline__ void block(int blk, uint32_t* share) const {
+    if (blk * kGroup + kGroup <= s.L) whole_block(blk, share);
+    else open_block(blk);
+  }
+};
 
 // Blocks that hold new tokens of a sequence.
 __device__ __forceinline__ int blocks_of(const Seq& s) {
@@ -266,7 +314,8 @@ __device__ __forceinline__ Seq append_seq(const AppendCall& call, int b) {
 constexpr int kPerLane = 4;
 
 template <bool BF16>
-__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part) {
+__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part,
+                                        uint32_t* share) {
   const int lane = threadIdx.x & 31;
 #pragma unroll 1
   for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kPerLane) {
@@ -309,11 +358,12 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
     int heir = done - ((done - first) & 1);
     if (before % kGroup == 0 || heir <= first || heir * kGroup >= q.L) heir = -1;
     if (blk == heir) return;
+#pragma unroll 1
     for (;;) {
-      if (part & 1) block_task<BF16, false>(call, q, b, blk, part >> 1);
-      else block_task<BF16, true>(call, q, b, blk, part >> 1);
+      if (part & 1) Task<BF16, false>(call, q, b, part >> 1).block(blk, share);
+      else Task<BF16, true>(call, q, b, part >> 1).block(blk, share);
       if (blk != first || heir < 0) return;
-      __syncwarp();
+      __syncthreads();  // `share` is written again
       blk = heir;
       heir = -1;
     }
@@ -324,6 +374,20 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
 template <bool BF16>
 __device__ __forceinline__ void query_task(const AppendCall& call, int row, int h0) {
   const int lane = threadIdx.x & 31, half = lane >> 4;
+  const Lane l = lane_of(lane & 15, call.p.rot_dim >> 1, call.p.paired);
+  const uint16_t* src = call.p.q + row * call.p.q_stride[0];
+  uint16_t* dst = call.p.q_out + row * call.p.q_out_stride[0];
+  uint2 x[kQueryHeads / 2][2];
+#pragma unroll
+  for (int i = 0; i < kQueryHeads / 2; ++i) {
+    const int h = h0 + 2 * i + half;
+    if (h < call.d.hq) {
+      // (in place: no read-only path)
+      const uint16_t* r = src + h * call.p.q_stride[1];
+      x[i][0] = *reinterpret_cast<const uint2*>(r + l.g0);
+      x[i][1] = *reinterpret_cast<const uint2*>(r + l.g1);
+    }
+  }
   int pos = -1;
 #pragma unroll 1
   for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kPerLane) {
@@ -340,20 +404,6 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
     }
   }
   if (pos < 0) return;
-  const Lane l = lane_of(lane & 15, call.p.rot_dim >> 1, call.p.paired);
-  const uint16_t* src = call.p.q + row * call.p.q_stride[0];
-  uint16_t* dst = call.p.q_out + row * call.p.q_out_stride[0];
-  uint2 x[kQueryHeads / 2][2];
-#pragma unroll
-  for (int i = 0; i < kQueryHeads / 2; ++i) {
-    const int h = h0 + 2 * i + half;
-    if (h < call.d.hq) {
-      // (in place: no read-only path)
-      const uint16_t* r = src + h * call.p.q_stride[1];
-      x[i][0] = *reinterpret_cast<const uint2*>(r + l.g0);
-      x[i][1] = *reinterpret_cast<const uint2*>(r + l.g1);
-    }
-  }
   if (l.rotate) {
     const Angles t = angles_of(call.p, l, table_row(call, row, pos));
 #pragma unroll
@@ -370,22 +420,22 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
   }
 }
 
-// Tasks of blocks, then of queries, a warp each; the last CTA looks over the batch's
-// sizes for the flag word.
+// CTAs of blocks, then of queries; the last CTA looks over the batch's sizes for the flag
+// word.
 template <bool BF16>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, 8)
 append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) {
-  const int warp = threadIdx.x >> 5;
+  __shared__ uint32_t share[kWarps];
   if (blockIdx.x == gridDim.x - 1) {
     for (int b = threadIdx.x; b < call.d.batch; b += 32 * kWarps) {
       const Seq s = append_seq(call, b);
       if (s.bad) set_flag(call.cache, s.bad);
     }
   } else if ((int)blockIdx.x < kv_ctas) {
-    const int task = blockIdx.x * kWarps + warp, parts = 2 * call.d.hkv;
-    kv_task<BF16>(call, task / parts, task % parts);
+    const int parts = 2 * call.d.hkv, unit = (int)blockIdx.x / parts;
+    kv_task<BF16>(call, unit, (int)blockIdx.x - unit * parts, share);
   } else {
-    const int task = ((int)blockIdx.x - kv_ctas) * kWarps + warp;
+    const int task = ((int)blockIdx.x - kv_ctas) * kWarps + ((int)threadIdx.x >> 5);
     const int row = task / groups;
     if (row < call.batch.n_tokens) query_task<BF16>(call, row, (task - row * groups) * kQueryHeads);
   }
@@ -397,8 +447,7 @@ cudaError_t launch_append(const AppendCall& call, cudaStream_t stream) {
   // A sequence of n new tokens touches at most (n - 1) / 32 + 2 blocks.
   const long long tokens = call.batch.n_tokens;
   const long long seqs = tokens < call.d.batch ? tokens : call.d.batch;
-  const long long units = tokens / kGroup + 2 * seqs;
-  const int kv_ctas = (int)((units * 2 * call.d.hkv + kWarps - 1) / kWarps);
+  const int kv_ctas = (int)((tokens / kGroup + 2 * seqs) * 2 * call.d.hkv);
   const int groups = (call.d.hq + kQueryHeads - 1) / kQueryHeads;
   const int q_ctas = call.p.q ? (int)((tokens * groups + kWarps - 1) / kWarps) : 0;
   const int grid = kv_ctas + q_ctas + 1;
