@@ -902,8 +902,8 @@ kvq_status kvq_adjust_logits(const kvq_adjust_params* p, void* stream) {
   if ((const void*)p->out == p->logits &&
       (p->dtype != KVQ_F32 || (p->rows > 1 && p->logits_stride != p->out_stride)))
     return fail(KVQ_ERR_ARG, "in place, logits must be fp32 with the stride of out");
-  if (p->n_history < 0 || p->n_bias < 0)
-    return fail(KVQ_ERR_SHAPE, "n_history and n_bias must be >= 0");
+  if (p->n_history < 0 || p->n_bias < 0 || p->n_history >= (1 << 30) || p->n_bias >= (1 << 30))
+    return fail(KVQ_ERR_SHAPE, "n_history and n_bias must be in [0, 2^30)");
   if ((p->history && !p->history_starts) || (p->n_history && !p->history))
     return fail(KVQ_ERR_ARG, "history and history_starts come together");
   if (((p->bias_ids || p->bias_values) && !p->bias_starts) ||

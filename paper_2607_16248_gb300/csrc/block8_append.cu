@@ -76,10 +76,12 @@ __device__ __forceinline__ Lane lane_of(int c, int r, bool paired) {
   return l;
 }
 
+// (Out of line, as the other seldom way below: in their places they filled the instruction
+// cache, and a prompt of 8191 tokens took 62 us.)
 // x1 c - x2 s (or x1 c + x2 s with s negated) rounded to odd: exact products as two fp32
 // numbers each, their sum as one and what it leaves.  Correct unless the low parts'
 // own sum, 2^-48 of the products, decides.
-__device__ __forceinline__ float rotate_odd(float x1, float c, float x2, float s) {
+__device__ __noinline__ float rotate_odd(float x1, float c, float x2, float s) {
   const float p = __fmul_rn(x1, c), q = __fmul_rn(x2, s);
   const float ep = __fmaf_rn(x1, c, -p), eq = __fmaf_rn(x2, s, -q);
   const float d = __fsub_rn(p, q);
@@ -172,13 +174,16 @@ __device__ __forceinline__ uint32_t to_codes(float x, float y, float z, float w)
       __nv_cvt_float2_to_fp8x2(make_float2(z, w), __NV_SATFINITE, __NV_E4M3);
   return (uint32_t)a | ((uint32_t)b << 16);
 }
+__device__ __noinline__ uint32_t exact_codes(float x, float y, float z, float w, float scale) {
+  return to_codes(__fdiv_rn(x, scale), __fdiv_rn(y, scale), __fdiv_rn(z, scale),
+                  __fdiv_rn(w, scale));
+}
 template <bool BF16>
 __device__ __forceinline__ uint32_t codes_of(uint2 v, float scale, float inv) {
   const float2 x = widen<BF16>(v.x), y = widen<BF16>(v.y);
   const float a = x.x * inv, b = x.y * inv, c = y.x * inv, d = y.y * inv;
   if (near_border(a) || near_border(b) || near_border(c) || near_border(d))
-    return to_codes(__fdiv_rn(x.x, scale), __fdiv_rn(x.y, scale), __fdiv_rn(y.x, scale),
-                    __fdiv_rn(y.y, scale));
+    return exact_codes(x.x, x.y, y.x, y.y, scale);
   return to_codes(a, b, c, d);
 }
 
@@ -309,61 +314,63 @@ __device__ __forceinline__ Seq append_seq(const AppendCall& call, int b) {
   return s;
 }
 
-// A warp looks through the batch 128 sequences at a time, four neighbours a lane: the
-// loads of a step are on their way together.
-constexpr int kPerLane = 4;
+// What a CTA's warps tell one another.
+struct Share {
+  uint32_t m[kWarps];
+  int sum[kWarps];
+  Seq s;
+  int b, left;
+};
 
+// Keys or values of unit `unit` (the batch's blocks with new tokens, in order).  The warps
+// look through 32 sequences each.
 template <bool BF16>
-__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part,
-                                        uint32_t* share) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part, Share& sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll 1
-  for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kPerLane) {
-    Seq s[kPerLane];
-    int mine = 0;
-#pragma unroll
-    for (int k = 0; k < kPerLane; ++k) {
-      s[k] = append_seq(call, b0 + kPerLane * lane + k);
-      mine += blocks_of(s[k]);
-    }
+  for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kWarps) {
+    const int b = b0 + 32 * warp + lane;
+    const Seq s = append_seq(call, b);
+    const int mine = blocks_of(s);
     int inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += y;
     }
-    const int all = __shfl_sync(0xffffffffu, inc, 31);
+    if (lane == 31) sh.sum[warp] = inc;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w == warp) before = all;
+      all += sh.sum[w];
+    }
     if (unit >= all) {
       unit -= all;
+      __syncthreads();
       continue;
     }
-    const int at = __ffs(__ballot_sync(0xffffffffu, inc > unit)) - 1;
-    // the lane that has the unit picks its sequence
-    int left = unit - (inc - mine), k = 0;
-    Seq q = s[0];
-#pragma unroll
-    for (int i = 0; i < kPerLane - 1; ++i)
-      if (k == i && left >= blocks_of(s[i])) {
-        left -= blocks_of(s[i]);
-        q = s[i + 1];
-        k = i + 1;
-      }
-    q.row = __shfl_sync(0xffffffffu, q.row, at);
-    q.n = __shfl_sync(0xffffffffu, q.n, at);
-    q.L = __shfl_sync(0xffffffffu, q.L, at);
-    const int b = b0 + kPerLane * at + __shfl_sync(0xffffffffu, k, at);
-    const int before = q.L - q.n, first = before / kGroup, done = q.L / kGroup;
-    int blk = first + __shfl_sync(0xffffffffu, left, at);
+    const int left = unit - before - (inc - mine);
+    if (left >= 0 && left < mine) {
+      sh.s = s;
+      sh.b = b;
+      sh.left = left;
+    }
+    __syncthreads();
+    const Seq q = sh.s;
+    const int old = q.L - q.n, first = old / kGroup, done = q.L / kGroup;
+    int blk = first + sh.left;
     // the block whose ring slots hold the first rows of a begun block that is completed
     int heir = done - ((done - first) & 1);
-    if (before % kGroup == 0 || heir <= first || heir * kGroup >= q.L) heir = -1;
+    if (old % kGroup == 0 || heir <= first || heir * kGroup >= q.L) heir = -1;
     if (blk == heir) return;
 #pragma unroll 1
     for (;;) {
-      if (part & 1) Task<BF16, false>(call, q, b, part >> 1).block(blk, share);
-      else Task<BF16, true>(call, q, b, part >> 1).block(blk, share);
+      if (part & 1) Task<BF16, false>(call, q, sh.b, part >> 1).block(blk, sh.m);
+      else Task<BF16, true>(call, q, sh.b, part >> 1).block(blk, sh.m);
       if (blk != first || heir < 0) return;
-      __syncthreads();  // `share` is written again
+      __syncthreads();  // sh.m is written again
       blk = heir;
       heir = -1;
     }
@@ -388,22 +395,26 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
       x[i][1] = *reinterpret_cast<const uint2*>(r + l.g1);
     }
   }
-  int pos = -1;
+  int b = -1;
+  if (!call.batch.starts) {
+    b = row / call.batch.max_new;
+  } else {
 #pragma unroll 1
-  for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kPerLane) {
-    int mine = -1;
-#pragma unroll
-    for (int k = 0; k < kPerLane; ++k) {
-      const Seq s = append_seq(call, b0 + kPerLane * lane + k);
-      if (mine < 0 && row >= s.row && row < s.row + s.n) mine = s.L - s.n + row - s.row;
+    for (int b0 = 0; b0 < call.d.batch; b0 += 32) {
+      const int i = b0 + lane;
+      const bool mine = i < call.d.batch && row >= __ldg(call.batch.starts + i) &&
+                        row < __ldg(call.batch.starts + i + 1);
+      const unsigned who = __ballot_sync(0xffffffffu, mine);
+      if (who) {
+        b = b0 + __ffs(who) - 1;
+        break;
+      }
     }
-    const unsigned who = __ballot_sync(0xffffffffu, mine >= 0);
-    if (who) {
-      pos = __shfl_sync(0xffffffffu, mine, __ffs(who) - 1);
-      break;
-    }
+    if (b < 0) return;
   }
-  if (pos < 0) return;
+  const Seq s = append_seq(call, b);
+  if (s.n == 0) return;
+  const int pos = s.L - s.n + row - s.row;
   if (l.rotate) {
     const Angles t = angles_of(call.p, l, table_row(call, row, pos));
 #pragma unroll
@@ -425,7 +436,7 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
 template <bool BF16>
 __global__ void __launch_bounds__(32 * kWarps, 8)
 append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) {
-  __shared__ uint32_t share[kWarps];
+  __shared__ Share share;
   if (blockIdx.x == gridDim.x - 1) {
     for (int b = threadIdx.x; b < call.d.batch; b += 32 * kWarps) {
       const Seq s = append_seq(call, b);

@@ -104,7 +104,7 @@ Plan plan_of(const Dims8& d, int max_new, int ctas) {
   p.many = rows > kFewRows;
   // beside longer ones, single tokens alone are short: more columns would cost them products
   const int most = p.many ? d.gq : (int)rows;
-  p.few = most <= 8 ? 8 : most <= 16 ? 16 : 32;
+  p.few = (most + 7) & ~7;
   p.chunk = rows > kOneTileRows ? 2 * kOneTileRows : kOneTileRows;
   // the kernels run one behind the other
   p.total = parts_bytes(ctas, p.many ? p.chunk : p.few);

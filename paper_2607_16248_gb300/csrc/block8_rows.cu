@@ -21,6 +21,8 @@
 // from the ring; bf16 ones go to fp16 times a power of two, which acts as their scale.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "block8_plan.cuh"
 
 namespace kvq {
@@ -30,23 +32,26 @@ namespace {
 
 constexpr int kTok = 5;            // 32 tokens a unit
 constexpr int kItemCost = 4;       // of an item in units: queries, merge, results
-constexpr int kWarps = 8;
+constexpr int kMergers = 4;        // warps whose results change hands at a time
 constexpr int kHalfPage = kGroup * kHeadDim;  // bytes of a block's keys (or values)
 constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
 constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
 constexpr float kNone = -1e30f;    // the maximum before any token
 constexpr long long kWaitCycles = 4000000000LL;  // bound of a wait (~2 s)
 
+// Warps a CTA: as many as their registers allow (an item's results and queries), since a
+// warp's block is a chain of latencies: a ragged batch of 32 single tokens takes ... with 8.
 template <int NT>
 struct Smem {
-  static constexpr int kSlots = NT == 4 ? 2 : 3;
+  static constexpr int kWarps = NT <= 2 ? 12 : 8, kSlots = 2;
   unsigned char page[kWarps][kSlots][2 * kHalfPage];
-  float4 merge[kWarps / 2][NT * 8][32];
+  float4 merge[kMergers][NT * 8][32];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];
   float2 scale[kWarps][kSlots];
   uint64_t full[kWarps][kSlots];
   int scan[32];
   Start start;
+  Walk<kTok, kItemCost> ahead[kWarps];  // the item whose blocks are being fetched
 };
 
 __device__ __forceinline__ uint32_t sptr(const void* p) {
@@ -97,16 +102,16 @@ struct Rows {
 
 // The softmax of a block's scores s[half of 16 tokens][nt][4], and its weights as B.
 // t0: the block's first token; edge: some row may not see some token.
-template <int NT>
+template <int N, int NT>
 __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
-                                        float (&s)[2][NT][4], int t0, bool edge, float sk,
-                                        float sv, uint32_t (&w)[2][NT][2]) {
+                                        float (&s)[2][N][4], int t0, bool edge, float sk,
+                                        float sv, uint32_t (&w)[2][N][2]) {
   const int gid = (threadIdx.x & 31) >> 2;
   if (edge) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = t0 + 16 * h + 8 * (i >> 1) + gid, pos = rows.pos[n][i & 1];
@@ -117,7 +122,7 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
   const float lsv = log2_fast(sv), inv = 1.0f / sv;
   bool up = false;
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
+  for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
@@ -125,7 +130,7 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
     }
   if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
@@ -143,7 +148,7 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
       }
   }
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+  for (int n = 0; n < N; ++n) {
     float y[2][4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -167,16 +172,16 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
   }
 }
 
-// One block of codes in shared memory.
-template <int NT>
+// One block of codes in shared memory; the first N of the item's row groups are in use.
+template <int N, int NT>
 __device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
                                       const unsigned char* page, float2 scale, int t0, bool edge) {
   const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-  float s[2][NT][4];
+  float s[2][N][4];
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[h][n][i] = 0.0f;
   const unsigned char* kr = page + gid * kHeadDim;
@@ -193,13 +198,13 @@ __device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const 
         const uint32_t a0 = wide_lo(xw[k]), a1 = wide_lo(yw[k]);
         const uint32_t a2 = wide_hi(xw[k]), a3 = wide_hi(yw[k]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < N; ++n)
           mma(s[h][n], a0, a1, a2, a3, st.q[n][4 * c + k][0], st.q[n][4 * c + k][1]);
       }
     }
   }
-  uint32_t w[2][NT][2];
-  weights<NT>(p, st, rows, s, t0, edge, scale.x, scale.y, w);
+  uint32_t w[2][N][2];
+  weights<N, NT>(p, st, rows, s, t0, edge, scale.x, scale.y, w);
   const unsigned char* vb = page + kHalfPage;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -222,7 +227,7 @@ __device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const 
         const uint32_t v = __byte_perm(word(1, 0), word(1, 1), z ? 0x7362 : 0x5140);
         const uint32_t a0 = wide_lo(u), a1 = wide_hi(u), a2 = wide_lo(v), a3 = wide_hi(v);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < N; ++n)
           mma(st.o[n][2 * k + z], a0, a1, a2, a3, w[h][n][0], w[h][n][1]);
       }
     }
@@ -295,7 +300,7 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
     }
   }
   uint32_t w[2][NT][2];
-  weights<NT>(p, st, rows, s, t0, true, 1.0f / fk, 1.0f / fv, w);
+  weights<NT, NT>(p, st, rows, s, t0, true, 1.0f / fk, 1.0f / fv, w);
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -376,21 +381,13 @@ __device__ __forceinline__ void load_queries(const AttnParams& p, const Seq& q, 
   }
 }
 
-// A warp's blocks over all items of the share, in order, ahead of their use.
-struct Feed {
-  Walk<kTok, kItemCost> w;
-  bool more;
-  int i, entry;        // next unit of the item; this lane's table entry of 32 units
-  int i_entry;         // the unit of lane 0's entry
-};
-
 template <int NT, bool BF16>
-__global__ void __launch_bounds__(32 * kWarps, 1)
+__global__ void __launch_bounds__(32 * Smem<NT>::kWarps, 1)
 rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map,
             const __grid_constant__ CUtensorMap v_map) {
   extern __shared__ __align__(1024) unsigned char raw[];
   Smem<NT>& sm = *reinterpret_cast<Smem<NT>*>(raw);
-  constexpr int kSlots = Smem<NT>::kSlots;
+  constexpr int kSlots = Smem<NT>::kSlots, kWarps = Smem<NT>::kWarps;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   if (tid == 0) p.splits[blockIdx.x].valid = 0;
   if (lane == 0) {
@@ -408,34 +405,54 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
   const auto whole_units = [](const Walk<kTok, kItemCost>& w) {
     return w.s.tile(w.s.n - 1) * kGroup + kGroup > w.q.L ? min(w.i1, w.s.n - 1) : w.i1;
   };
-  Feed f;
-  f.w.begin(p, sm.start, u0, u1);
-  f.more = f.w.next(p);
-  f.i = f.w.i0 + warp;
-  f.i_entry = -1;
-  // The next block of this warp into slot `slot`.
+  // This warp's next block, over all items of the share: its item is in shared memory (its
+  // fields would take registers from the results), `next` its unit, `limit` the item's last,
+  // `entry` this lane's table entry of the 32 units from `entries` on.
+  Walk<kTok, kItemCost>& ahead = sm.ahead[warp];
+  int next = 0, limit = 0, entry = 0, entries = -1;
+  {
+    Walk<kTok, kItemCost> first;
+    first.begin(p, sm.start, u0, u1);
+    if (first.next(p)) {
+      next = first.i0 + warp;
+      limit = whole_units(first);
+    } else {
+      first.u = first.end;
+    }
+    ahead = first;
+    __syncwarp();
+  }
+  // It goes to slot `slot`.
   const auto feed = [&](int slot) {
-    while (f.more && f.i >= whole_units(f.w)) {
-      f.w.advance(p);
-      f.more = f.w.next(p);
-      f.i = f.w.i0 + warp;
-      f.i_entry = -1;
+    if (next >= limit) {
+      Walk<kTok, kItemCost> f = ahead;
+      while (next >= limit) {
+        if (f.u >= f.end) break;
+        f.advance(p);
+        if (f.next(p)) {
+          next = f.i0 + warp;
+          limit = whole_units(f);
+        }
+      }
+      entries = -1;
+      __syncwarp();
+      ahead = f;
+      __syncwarp();
+      if (next >= limit) return;  // the end of the share
     }
-    if (!f.more) return;
-    if (f.i_entry < 0 || f.i >= f.i_entry + 32 * kWarps) {
-      f.i_entry = f.i;
-      const int i = f.i + kWarps * lane;
-      f.entry = i < whole_units(f.w)
-                    ? __ldg(p.c.cache.block_table + (long long)f.w.b * p.c.d.max_blocks +
-                            f.w.s.tile(i))
-                    : 0;
+    if (entries < 0 || next >= entries + 32 * kWarps) {
+      entries = next;
+      const int i = next + kWarps * lane;
+      entry = i < limit ? __ldg(p.c.cache.block_table + (long long)ahead.b * p.c.d.max_blocks +
+                                ahead.s.tile(i))
+                        : 0;
     }
-    const int page = __shfl_sync(0xffffffffu, f.entry, (f.i - f.i_entry) / kWarps);
-    f.i += kWarps;
+    const int page = __shfl_sync(0xffffffffu, entry, (next - entries) / kWarps);
+    next += kWarps;
     if (lane == 0) {
       const uint32_t bar = sptr(&sm.full[warp][slot]);
       if ((unsigned)page < (unsigned)p.c.cache.n_pages) {
-        const int at = page * p.c.d.hkv + f.w.head;
+        const int at = page * p.c.d.hkv + ahead.head;
         const uint32_t dst = sptr(sm.page[warp][slot]);
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
                      "r"(2 * kHalfPage)
@@ -502,25 +519,32 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
           (((long long)w.b * p.c.d.hkv + w.head) * kRing + (t0 & (kRing - 1))) * kHeadDim;
       tail_block<NT, BF16>(p, st, rows, p.c.cache.k_ring + at, p.c.cache.v_ring + at, t0, w.q.L);
     }
+    const auto blocks = [&](auto used) {
+      constexpr int N = decltype(used)::value;
 #pragma unroll 1
-    for (int i = w.i0 + warp; i < whole; i += kWarps) {
-      const int t0 = w.s.tile(i) * kGroup;
-      if (lost || !wait(slot, phase)) {
-        if (!lost && lane == 0) set_flag(p.c.cache, KVQ_FLAG_WAIT_TIMEOUT);
-        lost = true;
-        break;
+      for (int i = w.i0 + warp; i < whole; i += kWarps) {
+        const int t0 = w.s.tile(i) * kGroup;
+        if (lost || !wait(slot, phase)) {
+          if (!lost && lane == 0) set_flag(p.c.cache, KVQ_FLAG_WAIT_TIMEOUT);
+          lost = true;
+          break;
+        }
+        const float2 scale = sm.scale[warp][slot];
+        if (scale.x > 0.0f) {
+          const bool edge = t0 + kGroup - 1 > w.s.p0 ||
+                            (p.c.window && t0 <= w.s.p1 - p.c.window && t0 + kGroup > p.c.sinks);
+          block<N, NT>(p, st, rows, sm.page[warp][slot], scale, t0, edge);
+        }
+        __syncwarp();
+        feed(slot);
+        if (++slot == kSlots) slot = 0, phase ^= 1;
       }
-      const float2 scale = sm.scale[warp][slot];
-      if (scale.x > 0.0f) {
-        const bool edge = t0 + kGroup - 1 > w.s.p0 ||
-                          (p.c.window && t0 <= w.s.p1 - p.c.window &&
-                           t0 + kGroup > p.c.sinks);
-        block<NT>(p, st, rows, sm.page[warp][slot], scale, t0, edge);
-      }
-      __syncwarp();
-      feed(slot);
-      if (++slot == kSlots) slot = 0, phase ^= 1;
-    }
+    };
+    const int used = (w.q.n * p.c.d.gq + 7) >> 3;
+    if (NT == 1 || used <= 1) blocks(std::integral_constant<int, 1>{});
+    else if (NT == 2 || used == 2) blocks(std::integral_constant<int, NT < 2 ? NT : 2>{});
+    else if (NT == 3 || used == 3) blocks(std::integral_constant<int, NT < 3 ? NT : 3>{});
+    else blocks(std::integral_constant<int, NT>{});
     // The warps' parts of the item meet in shared memory, always in the same order.
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -555,27 +579,33 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
           st.o[n][i][j + 2] *= g;
         }
       }
+    // Four parts at a time go to slots 0 .. 3; two and one to slots that their own warps
+    // were the last to read.
 #pragma unroll
-    for (int k = kWarps / 2; k; k >>= 1) {
-      if (warp >= k && warp < 2 * k) {
+    for (int alive = kWarps; alive > 1;) {
+      const int keep = alive > 2 * kMergers ? alive - kMergers : alive / 2;
+      const bool four = alive - keep == kMergers;
+      if (warp >= keep && warp < alive) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            sm.merge[warp - k][8 * n + i][lane] =
+            sm.merge[four ? warp - keep : warp][8 * n + i][lane] =
                 make_float4(st.o[n][i][0], st.o[n][i][1], st.o[n][i][2], st.o[n][i][3]);
       }
       __syncthreads();
-      if (warp < k) {
+      if (warp < alive - keep) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float4 x = sm.merge[warp][8 * n + i][lane];
+            const float4 x = sm.merge[four ? warp : warp + keep][8 * n + i][lane];
             st.o[n][i][0] += x.x, st.o[n][i][1] += x.y;
             st.o[n][i][2] += x.z, st.o[n][i][3] += x.w;
           }
       }
+      alive = keep;
+      if (alive >= 2 * kMergers) __syncthreads();
     }
     if (warp == 0) {
       const int n_rows = w.q.n * p.c.d.gq;
@@ -654,7 +684,7 @@ cudaError_t launch(const AttnParams& p, int ctas, cudaStream_t stream) {
   const long long rows = (long long)p.c.cache.n_pages * p.c.d.hkv * kGroup;
   if ((e = make_map(&k, p.c.cache.k_codes, rows)) != cudaSuccess) return e;
   if ((e = make_map(&v, p.c.cache.v_codes, rows)) != cudaSuccess) return e;
-  rows_kernel<NT, BF16><<<ctas, 32 * kWarps, sizeof(Smem<NT>), stream>>>(p, k, v);
+  rows_kernel<NT, BF16><<<ctas, 32 * Smem<NT>::kWarps, sizeof(Smem<NT>), stream>>>(p, k, v);
   return cudaGetLastError();
 }
 
@@ -669,6 +699,7 @@ cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream) {
   switch (p.item_rows) {
     case 8: return launch_type<1>(p, ctas, stream);
     case 16: return launch_type<2>(p, ctas, stream);
+    case 24: return launch_type<3>(p, ctas, stream);
     default: return launch_type<4>(p, ctas, stream);
   }
 }
