@@ -667,8 +667,8 @@ kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cach
  * to the type.
  *   q, out      device [n_tokens][n_q_heads][128] with the strides below (as in
  *               kvq_block8_append); they must not overlap.
- *   workspace   device, >= kvq_block8_workspace_bytes(cfg, max_new); needs no
- *               initialisation; calls sharing it must not overlap on the GPU.
+ *   workspace   device, >= kvq_block8_workspace_bytes(cfg, max_new), zeroed once by
+ *               kvq_workspace_init; calls sharing it must not overlap on the GPU.
  * Lengths and starts are read on the device; the call can be captured in a CUDA graph.
  * batch * n_kv_heads * (max_len / 32 + 8) times the row tiles of max_new must be below
  * 2^31 (KVQ_ERR_SHAPE).

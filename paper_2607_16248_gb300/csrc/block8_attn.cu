@@ -9,10 +9,9 @@ namespace block8 {
 
 namespace {
 
-// The partials of a split item to results: the CTAs (c, y) share the rows of the item that
-// CTA c left, a row a warp.  Each lane finds the weights of one of every 32 partials, then
-// the weighted rows are summed in the order of the tokens.  A partial without a seen token
-// weighs nothing, whatever it holds.
+// The chunk kernel's partials to results: the CTAs (c, y) share the rows of the item that CTA c
+// left, a row a warp.  (In that kernel itself it would fall to the CTA that comes last, whose
+// roles have no registers for it.)
 constexpr int kJoinWarps = 8;
 
 template <bool BF16>
@@ -21,53 +20,12 @@ join_kernel(const __grid_constant__ AttnParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const Split sp = p.splits[blockIdx.x];
   if (!sp.valid) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int n = sp.last - (int)blockIdx.x + 1;
   const Seq q = seq_of(p.c.d, p.c.batch, sp.b);
-  const int r = kJoinWarps * blockIdx.y + warp;
+  const int r = kJoinWarps * blockIdx.y + (threadIdx.x >> 5);
   const int row = sp.row_tile * p.item_rows + r;
   if (r >= p.item_rows || row >= q.n * p.c.d.gq) return;
-  const auto slot = [&](int i) {  // row r of the i-th partial
-    return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? sp.inside : 0)) * p.item_rows + r;
-  };
-  constexpr int kMost = (kMaxSplits + 31) / 32;  // partials a lane
-  float2 ml[kMost];
-  float m = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < kMost; ++k) {
-    const int i = 32 * k + lane;
-    ml[k] = i < n ? __ldcg(&p.part_ml[slot(i)]) : make_float2(0.0f, 0.0f);
-    if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float l = 0.0f;
-#pragma unroll
-  for (int k = 0; k < kMost; ++k) {
-    ml[k].x = ml[k].y > 0.0f ? exp2_fast(ml[k].x - m) : 0.0f;
-    l += ml[k].y * ml[k].x;
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  const float f = l > 0.0f ? 1.0f / l : 0.0f;
-  float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-  for (int k = 0; k < kMost; ++k) {
-#pragma unroll 8
-    for (int i = 32 * k; i < min(n, 32 * k + 32); ++i) {
-      const float x = __shfl_sync(0xffffffffu, ml[k].x, i & 31) * f;
-      const float4 v =
-          __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
-      if (x > 0.0f) {
-        out.x = fmaf(v.x, x, out.x);
-        out.y = fmaf(v.y, x, out.y);
-        out.z = fmaf(v.z, x, out.z);
-        out.w = fmaf(v.w, x, out.w);
-      }
-    }
-  }
-  reinterpret_cast<uint2*>(p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row))[lane] =
-      make_uint2(pack16<BF16>(out.x, out.y), pack16<BF16>(out.z, out.w));
+  join_row<BF16>(p, blockIdx.x, sp.inside, sp.last - (int)blockIdx.x + 1, r,
+                 p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row));
 }
 
 cudaError_t launch_join(const AttnParams& p, int ctas, int rows, cudaStream_t stream) {
@@ -94,9 +52,13 @@ struct Plan {
 // Rows up to which an item is one row tile of the chunk kernel, whose two streams then share
 // the tokens.
 constexpr int kOneTileRows = 128;
+// Tickets (zero between calls) at the front, the same for every call that the workspace
+// serves; then partials and splits.
+size_t tickets_bytes(int ctas) { return ((size_t)ctas * sizeof(int) + 255) / 256 * 256; }
 size_t parts_bytes(int ctas, int rows) {
-  return (size_t)2 * ctas * rows * (kHeadDim * sizeof(float) + sizeof(float2)) +
-         (size_t)ctas * sizeof(Split) + 256;
+  return tickets_bytes(ctas) +
+         (size_t)2 * ctas * rows * (kHeadDim * sizeof(float) + sizeof(float2)) +
+         (size_t)ctas * sizeof(Split);
 }
 Plan plan_of(const Dims8& d, int max_new, int ctas) {
   Plan p;
@@ -117,6 +79,8 @@ AttnParams params_of(const AttnCall& call, int ctas, int item_rows, void* worksp
   p.gq_inverse = (uint32_t)((1ull << 32) / call.d.gq + 1);
   p.item_rows = item_rows;
   char* w = static_cast<char*>(workspace);
+  p.tickets = reinterpret_cast<int*>(w);
+  w += tickets_bytes(ctas);
   p.part_o = reinterpret_cast<float*>(w);
   w += (size_t)2 * ctas * item_rows * kHeadDim * sizeof(float);
   p.part_ml = reinterpret_cast<float2*>(w);
@@ -144,8 +108,7 @@ cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cud
   p.max_rows = plan.few;
   cudaError_t e = cudaSuccess;
   if (call.batch.starts || !plan.many) {
-    if ((e = launch_rows(p, sm_count, stream)) != cudaSuccess) return e;
-    if ((e = launch_join(p, sm_count, plan.few, stream)) != cudaSuccess || !plan.many) return e;
+    if ((e = launch_rows(p, sm_count, stream)) != cudaSuccess || !plan.many) return e;
   }
   p = params_of(call, sm_count, plan.chunk, workspace);
   p.min_rows = plan.few + 1;

@@ -201,9 +201,10 @@ __device__ __forceinline__ float ring_factor(const uint16_t* rows, int valid) {
   if constexpr (!BF16) return 1.0f;
   const int lane = threadIdx.x & 31;
   uint32_t x = 0u;
-#pragma unroll 1
-  for (int r = lane >> 4; r < valid; r += 2)
-    x = max(x, largest(*(reinterpret_cast<const uint4*>(rows + r * kHeadDim) + (lane & 15))));
+#pragma unroll 8
+  for (int r = lane >> 4; r < kGroup; r += 2)
+    if (r < valid)
+      x = max(x, largest(*(reinterpret_cast<const uint4*>(rows + r * kHeadDim) + (lane & 15))));
   return lift_of(__reduce_max_sync(0xffffffffu, x));
 }
 // Its rows, the others zero.

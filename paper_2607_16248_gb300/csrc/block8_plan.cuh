@@ -5,7 +5,8 @@
 // 2^TOK tokens that any of its rows sees, after a fixed cost in units.  All items' units
 // lie end to end (sequence, row tile, kv-head) and every CTA takes an equal contiguous
 // share.  An item that several CTAs share leaves partials (unnormalised rows, maximum,
-// sum) that a second kernel joins in the order of the tokens.
+// sum) that are joined in the order of the tokens: by the CTA that comes last, or by a second
+// kernel.
 #pragma once
 
 #include "block8.cuh"
@@ -25,7 +26,8 @@ struct AttnParams {
   int item_rows;            // rows of an item and of a partial
   float* part_o;            // [2 * CTAs][item_rows][128]
   float2* part_ml;          // [2 * CTAs][item_rows]
-  Split* splits;            // [CTAs]
+  Split* splits;            // [CTAs]: for the kernel that joins
+  int* tickets;             // [CTAs]: for CTAs that join, by the item's first CTA
 };
 
 #ifdef __CUDACC__
@@ -231,6 +233,56 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
+}
+
+// Row r of an item's partials to its result, by a warp.  CTA c0 + i left the i-th, CTA c0 in
+// its slot `inside`.  Each lane finds the weights of one of every 32, then the weighted rows
+// are summed in order.  A partial without a seen token weighs nothing, whatever it holds.
+template <bool BF16>
+__device__ __forceinline__ void join_row(const AttnParams& p, int c0, int inside, int n, int r,
+                                         uint16_t* out) {
+  const int lane = threadIdx.x & 31;
+  const auto slot = [&](int i) {
+    return (long long)(2 * (c0 + i) + (i == 0 ? inside : 0)) * p.item_rows + r;
+  };
+  constexpr int kMost = (kMaxSplits + 31) / 32;  // partials a lane
+  float2 ml[kMost];
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = 32 * k + lane;
+    ml[k] = i < n ? __ldcg(&p.part_ml[slot(i)]) : make_float2(0.0f, 0.0f);
+    if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float l = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    ml[k].x = ml[k].y > 0.0f ? exp2_fast(ml[k].x - m) : 0.0f;
+    l += ml[k].y * ml[k].x;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const float f = l > 0.0f ? 1.0f / l : 0.0f;
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+#pragma unroll 8
+    for (int i = 32 * k; i < min(n, 32 * k + 32); ++i) {
+      const float x = __shfl_sync(0xffffffffu, ml[k].x, i & 31) * f;
+      const float4 v =
+          __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
+      if (x > 0.0f) {
+        sum.x = fmaf(v.x, x, sum.x);
+        sum.y = fmaf(v.y, x, sum.y);
+        sum.z = fmaf(v.z, x, sum.z);
+        sum.w = fmaf(v.w, x, sum.w);
+      }
+    }
+  }
+  reinterpret_cast<uint2*>(out)[lane] =
+      make_uint2(pack16<BF16>(sum.x, sum.y), pack16<BF16>(sum.z, sum.w));
 }
 #endif
 

@@ -32,18 +32,19 @@ namespace {
 
 constexpr int kTok = 5;            // 32 tokens a unit
 constexpr int kItemCost = 4;       // of an item in units: queries, merge, results
-constexpr int kMergers = 4;        // warps whose results change hands at a time
 constexpr int kHalfPage = kGroup * kHeadDim;  // bytes of a block's keys (or values)
 constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
 constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
 constexpr float kNone = -1e30f;    // the maximum before any token
 constexpr long long kWaitCycles = 4000000000LL;  // bound of a wait (~2 s)
 
-// Warps a CTA: as many as their registers allow (an item's results and queries), since a
-// warp's block is a chain of latencies: a ragged batch of 32 single tokens takes ... with 8.
+// Eight warps with two slots each: 128 KB of copies on their way in an SM.  More only make
+// everything else wait behind them (ragged batch of 32 single tokens: 198 us; three slots
+// 214, twelve warps 209).
 template <int NT>
 struct Smem {
-  static constexpr int kWarps = NT <= 2 ? 12 : 8, kSlots = 2;
+  static constexpr int kWarps = 8, kSlots = 2;
+  static constexpr int kMergers = 4;  // warps whose results change hands at a time
   unsigned char page[kWarps][kSlots][2 * kHalfPage];
   float4 merge[kMergers][NT * 8][32];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];
@@ -51,6 +52,7 @@ struct Smem {
   uint64_t full[kWarps][kSlots];
   int scan[32];
   Start start;
+  int join;  // this CTA's partial is the item's last
   Walk<kTok, kItemCost> ahead[kWarps];  // the item whose blocks are being fetched
 };
 
@@ -252,24 +254,14 @@ __device__ __forceinline__ uint32_t largest(uint32_t m, const uint4& v) {
   return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
 
-// The block of 16-bit tokens t0 .. L - 1 (fewer than 32), from the ring's rows.
+// The block of 16-bit tokens t0 .. L - 1 (fewer than 32), from the ring's rows; the item's
+// first, so its results are its own.  bf16 elements go to fp16 times powers of two: a key's
+// is its token's, whose scores the same lanes get; a value's that of the lane's 16 channels,
+// whose results the lane holds.
 template <int NT, bool BF16>
 __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
                                         const uint16_t* k, const uint16_t* v, int t0, int L) {
   const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3, valid = L - t0;
-  float fk = 1.0f, fv = 1.0f;
-  if constexpr (BF16) {
-    uint32_t mk = 0u, mv = 0u;
-#pragma unroll 1
-    for (int r = lane >> 4; r < valid; r += 2) {
-      mk = largest(mk, *reinterpret_cast<const uint4*>(k + r * kHeadDim + 8 * (lane & 15)));
-      mv = largest(mv, *reinterpret_cast<const uint4*>(v + r * kHeadDim + 8 * (lane & 15)));
-    }
-    mk = max(mk & 0xffffu, mk >> 16);
-    mv = max(mv & 0xffffu, mv >> 16);
-    fk = lift_of(__reduce_max_sync(0xffffffffu, mk));
-    fv = lift_of(__reduce_max_sync(0xffffffffu, mv));
-  }
   const auto load = [&](const uint16_t* base, int r, int part) {
     return r < valid ? *reinterpret_cast<const uint4*>(base + r * kHeadDim + part)
                      : make_uint4(0u, 0u, 0u, 0u);
@@ -283,52 +275,100 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
       for (int i = 0; i < 4; ++i) s[h][n][i] = 0.0f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+    if (16 * h >= valid) break;  // no token there
+    uint4 x[2][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[e][c] = load(k, 16 * h + 8 * e + gid, 32 * tig + 8 * c);
+    float f[2] = {1.0f, 1.0f};
+    if constexpr (BF16) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) m = largest(m, x[e][c]);
+        m = max(m & 0xffffu, m >> 16);
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        f[e] = lift_of(m);
+      }
+    }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {  // 8 channels: two steps of the product
-      const uint4 x = load(k, 16 * h + gid, 32 * tig + 8 * c);
-      const uint4 y = load(k, 16 * h + 8 + gid, 32 * tig + 8 * c);
-      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+      const uint32_t xw[4] = {x[0][c].x, x[0][c].y, x[0][c].z, x[0][c].w};
+      const uint32_t yw[4] = {x[1][c].x, x[1][c].y, x[1][c].z, x[1][c].w};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t a0 = to_half2<BF16>(xw[2 * i], fk), a1 = to_half2<BF16>(yw[2 * i], fk);
-        const uint32_t a2 = to_half2<BF16>(xw[2 * i + 1], fk),
-                       a3 = to_half2<BF16>(yw[2 * i + 1], fk);
+        const uint32_t a0 = to_half2<BF16>(xw[2 * i], f[0]), a1 = to_half2<BF16>(yw[2 * i], f[1]);
+        const uint32_t a2 = to_half2<BF16>(xw[2 * i + 1], f[0]),
+                       a3 = to_half2<BF16>(yw[2 * i + 1], f[1]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
           mma(s[h][n], a0, a1, a2, a3, st.q[n][2 * c + i][0], st.q[n][2 * c + i][1]);
       }
     }
+    if constexpr (BF16) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[h][n][i] *= 1.0f / f[i >> 1];
+    }
   }
   uint32_t w[2][NT][2];
-  weights<NT, NT>(p, st, rows, s, t0, true, 1.0f / fk, 1.0f / fv, w);
+  weights<NT, NT>(p, st, rows, s, t0, true, 1.0f, 1.0f, w);
+  float fv = 1.0f;
+  if constexpr (BF16) {
+    uint32_t m = 0u;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      if (16 * h >= valid) break;
+      uint4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = load(v, 16 * h + 8 * (i >> 2) + 2 * tig + (i >> 1 & 1), 16 * gid + 8 * (i & 1));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = largest(m, x[i]);
+    }
+    m = max(m & 0xffffu, m >> 16);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    fv = lift_of(m);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (16 * h >= valid) break;
+    uint4 x[2][2][2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i >> 2][i >> 1 & 1][i & 1] =
+          load(v, 16 * h + 8 * (i >> 2) + 2 * tig + (i >> 1 & 1), 16 * gid + 8 * (i & 1));
 #pragma unroll
     for (int c = 0; c < 2; ++c) {  // 8 channels each
-      uint4 x[2][2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          x[i][e] = load(v, 16 * h + 8 * i + 2 * tig + e, 16 * gid + 8 * c);
 #pragma unroll
       for (int k2 = 0; k2 < 4; ++k2) {
         const auto word = [&](int i, int e) {
-          return to_half2<BF16>(k2 == 0   ? x[i][e].x
-                                : k2 == 1 ? x[i][e].y
-                                : k2 == 2 ? x[i][e].z
-                                          : x[i][e].w,
-                                fv);
+          const uint4& y = x[i][e][c];
+          return to_half2<BF16>(k2 == 0 ? y.x : k2 == 1 ? y.y : k2 == 2 ? y.z : y.w, fv);
         };
-        const uint32_t a0 = __byte_perm(word(0, 0), word(0, 1), 0x5410);
-        const uint32_t a1 = __byte_perm(word(0, 0), word(0, 1), 0x7632);
-        const uint32_t a2 = __byte_perm(word(1, 0), word(1, 1), 0x5410);
-        const uint32_t a3 = __byte_perm(word(1, 0), word(1, 1), 0x7632);
+        const uint32_t w00 = word(0, 0), w01 = word(0, 1), w10 = word(1, 0), w11 = word(1, 1);
+        const uint32_t a0 = __byte_perm(w00, w01, 0x5410), a1 = __byte_perm(w00, w01, 0x7632);
+        const uint32_t a2 = __byte_perm(w10, w11, 0x5410), a3 = __byte_perm(w10, w11, 0x7632);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
           mma(st.o[n][4 * c + k2], a0, a1, a2, a3, w[h][n][0], w[h][n][1]);
       }
     }
+  }
+  if constexpr (BF16) {
+    const float g = 1.0f / fv;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st.o[n][i][j] *= g;
+  }
 }
 
 // Queries of an item: row 8 n + gid's channels 32 tig .. 32 tig + 31, bf16 ones times a power
@@ -388,15 +428,15 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
   extern __shared__ __align__(1024) unsigned char raw[];
   Smem<NT>& sm = *reinterpret_cast<Smem<NT>*>(raw);
   constexpr int kSlots = Smem<NT>::kSlots, kWarps = Smem<NT>::kWarps;
+  constexpr int kMergers = Smem<NT>::kMergers;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
-  if (tid == 0) p.splits[blockIdx.x].valid = 0;
   if (lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(warp & 1 ? &k_map : &v_map) : "memory");
     for (int i = 0; i < kSlots; ++i)
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(sptr(&sm.full[warp][i]))
                    : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Shares shares;
   int u0, u1;
   if (!plan_share<kTok, kItemCost>(p, sm.scan, &sm.start, kWarps, shares, u0, u1)) return;
@@ -416,13 +456,34 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     if (first.next(p)) {
       next = first.i0 + warp;
       limit = whole_units(first);
-    } else {
-      first.u = first.end;
     }
     ahead = first;
     __syncwarp();
   }
-  // It goes to slot `slot`.
+  // An item's queries and 16-bit tokens come to L2 ahead of its blocks: behind full rings a
+  // load waits its turn of several microseconds.
+  const auto fetch_small = [&](const Walk<kTok, kItemCost>& f) {
+    if (warp != kWarps - 1) return;
+    const auto line = [](const void* at) {
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+    };
+    if (lane < f.q.n * p.c.d.gq) {
+      const uint16_t* at = p.c.q + row_offset(p, p.c.q_stride, f.q.row, f.head, lane);
+      line(at);
+      line(at + 64);
+    }
+    const int t0 = f.s.tile(f.s.n - 1) * kGroup, lines = 2 * (f.q.L - t0);
+    if (t0 + kGroup > f.q.L && f.i1 == f.s.n) {
+      const long long at =
+          (((long long)f.b * p.c.d.hkv + f.head) * kRing + (t0 & (kRing - 1))) * kHeadDim;
+      for (int i = lane; i < lines; i += 32) {
+        line(p.c.cache.k_ring + at + 64 * i);
+        line(p.c.cache.v_ring + at + 64 * i);
+      }
+    }
+  };
+  fetch_small(ahead);
+  // The next block goes to slot `slot`.
   const auto feed = [&](int slot) {
     if (next >= limit) {
       Walk<kTok, kItemCost> f = ahead;
@@ -432,6 +493,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         if (f.next(p)) {
           next = f.i0 + warp;
           limit = whole_units(f);
+          fetch_small(f);
         }
       }
       entries = -1;
@@ -607,9 +669,9 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
       alive = keep;
       if (alive >= 2 * kMergers) __syncthreads();
     }
+    const int n_rows = w.q.n * p.c.d.gq;
+    const bool direct = w.whole();
     if (warp == 0) {
-      const int n_rows = w.q.n * p.c.d.gq;
-      const bool direct = w.whole();
       const int slot_row = w.slot(u0) * p.item_rows;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -636,9 +698,28 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
             if (gid == 0) p.part_ml[slot_row + r] = make_float2(mm[n][j], ll[n][j]);
           }
         }
-      if (!direct && w.i0 == 0 && lane == 0)
-        p.splits[blockIdx.x] = Split{1, u0 < w.base ? 1 : 0,
-                                     shares.owner(w.base + kItemCost + w.s.n - 1), w.b, 0, w.head};
+    }
+    if (direct) continue;
+    // Whoever brings an item's last partial joins them, in the order of the tokens.  The
+    // tickets are zero between calls.
+    const int c0 = shares.owner(w.base + kItemCost);
+    const int parts = shares.owner(w.base + kItemCost + w.s.n - 1) - c0 + 1;
+    if (warp == 0) {
+      __threadfence();
+      __syncwarp();
+      if (lane == 0) {
+        const bool last = atomicAdd(p.tickets + c0, 1) == parts - 1;
+        if (last) p.tickets[c0] = 0;
+        __threadfence();
+        sm.join = last;
+      }
+    }
+    __syncthreads();
+    if (sm.join) {
+      const int inside = shares.begin(c0) < w.base ? 1 : 0;
+      for (int r = warp; r < n_rows; r += kWarps)
+        join_row<BF16>(p, c0, inside, parts, r,
+                       p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r));
     }
   }
   // copies that are still on their way get their time before the memory goes

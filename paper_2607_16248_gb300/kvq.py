@@ -8,6 +8,7 @@ a missing library or a non-CUDA tensor raises instead of falling back.
 
 import ctypes
 import math
+import struct
 from dataclasses import dataclass
 from pathlib import Path
 
@@ -129,6 +130,7 @@ def lib():
         cfg_p = ctypes.POINTER(_Config)
         cache_p = ctypes.POINTER(_Cache)
         par_p = ctypes.POINTER(_DgapParams)
+        cfg8_p, cache8_p = ctypes.POINTER(_Block8Config), ctypes.POINTER(_Block8Cache)
         sig = {
             "kvq_last_error": (ctypes.c_char_p, []),
             "kvq_version": (I32, []),
@@ -154,10 +156,10 @@ def lib():
             "kvq_chunk_workspace_bytes": (SZ, [cfg_p, I32, I32]),
             "kvq_chunk_attn": (I32, [cfg_p, cache_p, P, P, ctypes.POINTER(_ChunkParams), I32,
                                      I32, P, SZ, P]),
-            "kvq_block8_validate_config": (I32, [P]),
-            "kvq_block8_append": (I32, [P, P, P, P, P]),
-            "kvq_block8_workspace_bytes": (SZ, [P, I32]),
-            "kvq_block8_attn": (I32, [P, P, P, P, P, P, P, SZ, P]),
+            "kvq_block8_validate_config": (I32, [cfg8_p]),
+            "kvq_block8_append": (I32, [cfg8_p, cache8_p, P, P, P]),
+            "kvq_block8_workspace_bytes": (SZ, [cfg8_p, I32]),
+            "kvq_block8_attn": (I32, [cfg8_p, cache8_p, P, P, P, P, P, SZ, P]),
             "kvq_adjust_logits": (I32, [P, P]),
             "kvq_sample_max_vocab": (I32, []),
             "kvq_sample": (I32, [P, I64, P, I64, I32, I32, P, P, P, P, P, P, P]),
@@ -635,6 +637,7 @@ class Block8Cache:
             _dev(tensors[n], dtype, n)
             setattr(self, n, tensors[n])
         self.device = self.scales.device
+        self.dev = self.scales.get_device()
         if block_table is None:
             block_table = torch.full((cfg.batch, cfg.max_blocks), -1, dtype=torch.int32,
                                      device=self.device)
@@ -665,25 +668,36 @@ class Block8Cache:
         self._flags.zero_()
 
 
-def _rows(t, shape, dtype, name, device):
-    """Address and strides (tokens, heads) of a [tokens, heads, 128] tensor."""
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
-    s = t.stride()
-    return _address(t, dtype, name), _Pair(s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0)
+# The calls below pack their structs with these: a ctypes structure's fields cost more to
+# set, one by one, than the smallest calls take on the GPU.
+_BATCH = struct.Struct("@2P2i")             # kvq_block8_batch
+_APPEND = struct.Struct("@7P3i8q")          # kvq_block8_append_params
+_ATTN = struct.Struct("@2if4q")             # kvq_block8_attn_params
+_ADJUST = struct.Struct("@13P3q6i")         # kvq_adjust_params
 
 
-def _list32(t, n, name, device, dtype=torch.int32):
-    """Address of a contiguous 1-d tensor on the device (n elements, or any number)."""
+def _rows(t, n, heads, dtype, name, dev):
+    """Address and strides (tokens, heads) of an [n, heads, 128] tensor on GPU `dev`."""
+    if t.shape != (n, heads, 128):
+        raise ValueError(f"{name} must be [{n}, {heads}, 128]")
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise TypeError(f"{name} must be {dtype} on cuda:{dev}, got {t.dtype} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), s0 if n > 1 else 0, s1 if heads > 1 else 0
+
+
+def _list(t, n, dtype, name, dev):
+    """Address of a contiguous 1-d tensor of n elements (None: any number) on GPU `dev`,
+    0 for None."""
     if t is None:
-        return None
-    if t.dim() != 1 or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name} must be [{'n' if n is None else n}]")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
-    return _address(t, dtype, name)
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise TypeError(f"{name} must be {dtype} on cuda:{dev}, got {t.dtype} on {t.device}")
+    if t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{'n' if n is None else n}]")
+    return t.data_ptr()
 
 
 def _block8_batch(cache, n_tokens, lengths, starts, max_new):
@@ -697,33 +711,27 @@ def _block8_batch(cache, n_tokens, lengths, starts, max_new):
     elif max_new is None:
         max_new = min(n_tokens, cache.cfg.max_len)
     _in_32_bits("n_tokens and max_new", n_tokens, max_new)
-    return _Block8Batch(_list32(lengths, batch, "lengths", cache.device),
-                        _list32(starts, batch + 1, "starts", cache.device), n_tokens, max_new)
+    return _BATCH.pack(_list(lengths, batch, torch.int32, "lengths", cache.dev),
+                       _list(starts, batch + 1, torch.int32, "starts", cache.dev), n_tokens,
+                       max_new), max_new
 
 
-def _stream_on(device, stream):
-    """The stream's handle; the device's own current stream where none is given."""
+def _launch(dev, stream, fn, *args):
+    """fn(*args, stream) with GPU `dev` current, on its current stream where none is given."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device != device:
-        raise ValueError(f"stream must be on {device}")
-    return stream.cuda_stream
-
-
-class _on:
-    """The device as the current one, if it is not."""
-
-    def __init__(self, device):
-        self.device = device
-
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.was != self.device.index:
-            torch.cuda.set_device(self.device)
-
-    def __exit__(self, *exc):
-        if self.was != self.device.index:
-            torch.cuda.set_device(self.was)
+        handle = torch._C._cuda_getCurrentRawStream(dev)
+    elif stream.device.index != dev:
+        raise ValueError(f"stream must be on cuda:{dev}")
+    else:
+        handle = stream.cuda_stream
+    was = torch._C._cuda_getDevice()
+    if was == dev:
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, handle)
+    if status:
+        _check(status)
 
 
 def kvq_block8_append(cache: Block8Cache, k, v, lengths, starts=None, q=None, q_out=None,
@@ -739,37 +747,37 @@ def kvq_block8_append(cache: Block8Cache, k, v, lengths, starts=None, q=None, q_
     2i + 1) instead of (i, i + rot_dim / 2); ``positions`` int32 [tokens] are rows of
     the tables in place of the tokens' places.  Returns q_out (made if None; may be
     q), or None without q."""
-    cfg, dev = cache.cfg, cache.device
-    n = k.shape[0]
-    kv = (n, cfg.n_kv_heads, cfg.head_dim)
-    p = _Block8Append()
-    batch = _block8_batch(cache, n, lengths, starts, max_new)
-    p.k, p.k_stride = _rows(k, kv, cfg.dtype, "k", dev)
-    p.v, p.v_stride = _rows(v, kv, cfg.dtype, "v", dev)
+    cfg, dev = cache.cfg, cache.dev
+    n, dtype = k.shape[0], cfg.dtype
+    batch, _ = _block8_batch(cache, n, lengths, starts, max_new)
+    ka, k0, k1 = _rows(k, n, cfg.n_kv_heads, dtype, "k", dev)
+    va, v0, v1 = _rows(v, n, cfg.n_kv_heads, dtype, "v", dev)
+    qa = q0 = q1 = oa = o0 = o1 = 0
     if q is not None:
-        shape = (n, cfg.n_q_heads, cfg.head_dim)
-        p.q, p.q_stride = _rows(q, shape, cfg.dtype, "q", dev)
+        qa, q0, q1 = _rows(q, n, cfg.n_q_heads, dtype, "q", dev)
         if q_out is None:
-            q_out = _made_on(stream, lambda: torch.empty(shape, dtype=cfg.dtype, device=dev))
-        p.q_out, p.q_out_stride = _rows(q_out, shape, cfg.dtype, "q_out", dev)
+            q_out = _made_on(stream, lambda: torch.empty(q.shape, dtype=dtype,
+                                                         device=cache.device))
+        oa, o0, o1 = _rows(q_out, n, cfg.n_q_heads, dtype, "q_out", dev)
     elif q_out is not None:
         raise ValueError("q_out needs q")
-    if (cos is None) != (sin is None):
-        raise ValueError("cos and sin come together")
-    if cos is not None:
-        if cos.dim() != 2 or cos.shape != sin.shape:
+    ca = sa = pa = n_pos = rot = 0
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
             raise ValueError("cos and sin must both be [n_positions, rot_dim / 2]")
-        if cos.device != dev or sin.device != dev:
-            raise ValueError(f"cos and sin must be on {dev}")
-        p.n_positions, p.rot_dim = cos.shape[0], 2 * cos.shape[1]
-        if p.rot_dim:
-            p.cos = _dev(cos, torch.float32, "cos").value
-            p.sin = _dev(sin, torch.float32, "sin").value
-            p.positions = _list32(positions, n, "positions", dev)
-        p.paired = int(bool(paired))
-    with _on(dev):
-        _check(lib().kvq_block8_append(cache._cfg_ref, cache._c_ref, ctypes.byref(batch),
-                                       ctypes.byref(p), _stream_on(dev, stream)))
+        n_pos, half = cos.shape
+        rot = 2 * half
+        if rot:
+            for t, name in ((cos, "cos"), (sin, "sin")):
+                if t.dtype is not torch.float32 or t.get_device() != dev:
+                    raise TypeError(f"{name} must be float32 on cuda:{dev}")
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous")
+            ca, sa = cos.data_ptr(), sin.data_ptr()
+            pa = _list(positions, n, torch.int32, "positions", dev)
+    params = _APPEND.pack(ka, va, qa, oa, ca, sa, pa, n_pos, rot, 1 if paired else 0,
+                          k0, k1, v0, v1, q0, q1, o0, o1)
+    _launch(dev, stream, lib().kvq_block8_append, cache._cfg_ref, cache._c_ref, batch, params)
     return q_out
 
 
@@ -780,7 +788,7 @@ def block8_workspace(cfg: Block8Config, max_new, device="cuda"):
     n = lib().kvq_block8_workspace_bytes(ctypes.byref(c), max_new)
     if n == 0:
         raise KvqError(1, last_error())
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
 def kvq_block8_attn(cache: Block8Cache, q, lengths, starts=None, max_new=None, window=0, sinks=0,
@@ -790,24 +798,21 @@ def kvq_block8_attn(cache: Block8Cache, q, lengths, starts=None, max_new=None, w
     shape.  lengths, starts as there; ``max_new`` is the most new tokens of any sequence
     (a smaller number serves single tokens and drafts faster).  window, sinks as in
     kvq_chunk_attn."""
-    cfg, dev = cache.cfg, cache.device
+    cfg, dev = cache.cfg, cache.dev
     n = q.shape[0]
-    shape = (n, cfg.n_q_heads, cfg.head_dim)
-    batch = _block8_batch(cache, n, lengths, starts, max_new)
+    batch, max_new = _block8_batch(cache, n, lengths, starts, max_new)
     _in_32_bits("window and sinks", window, sinks)
-    qa, qs = _rows(q, shape, cfg.dtype, "q", dev)
+    qa, q0, q1 = _rows(q, n, cfg.n_q_heads, cfg.dtype, "q", dev)
     if out is None:
-        out = _made_on(stream, lambda: torch.empty(shape, dtype=cfg.dtype, device=dev))
-    oa, os = _rows(out, shape, cfg.dtype, "out", dev)
+        out = _made_on(stream, lambda: torch.empty(q.shape, dtype=cfg.dtype,
+                                                   device=cache.device))
+    oa, o0, o1 = _rows(out, n, cfg.n_q_heads, cfg.dtype, "out", dev)
     if workspace is None:
-        workspace = _made_on(stream, block8_workspace, cfg, batch.max_new, dev)
-    elif workspace.device != dev:
-        raise ValueError(f"workspace must be on {dev}")
-    p = _Block8Attn(window, sinks, softmax_scale, qs, os)
-    with _on(dev):
-        _check(lib().kvq_block8_attn(cache._cfg_ref, cache._c_ref, ctypes.byref(batch), qa, oa,
-                                     ctypes.byref(p), _dev(workspace, torch.uint8, "workspace"),
-                                     workspace.numel(), _stream_on(dev, stream)))
+        workspace = _made_on(stream, block8_workspace, cfg, max_new, cache.device)
+    ws = _list(workspace, None, torch.uint8, "workspace", dev)
+    params = _ATTN.pack(window, sinks, softmax_scale, q0, q1, o0, o1)
+    _launch(dev, stream, lib().kvq_block8_attn, cache._cfg_ref, cache._c_ref, batch, qa, oa,
+            params, ws, workspace.numel())
     return out
 
 
@@ -828,45 +833,53 @@ def kvq_adjust_logits(logits, out=None, history=None, history_starts=None, promp
     prompt_lengths[b] tokens of a history were asked, the others answered.  repetition,
     frequency, presence are fp32 [rows]; mask int32 [n, ceil(vocab / 32)] of bits, row b's
     at mask_rows[b] (None: b).  All on the device."""
-    if logits.dim() != 2:
+    shape = logits.shape
+    if len(shape) != 2:
         raise ValueError("logits must be [rows, vocab]")
-    rows, V = logits.shape
-    dev = logits.device
+    rows, V = shape
+    dev = logits.get_device()
+    if dev < 0:
+        raise TypeError("logits must be a CUDA tensor")
     _in_32_bits("rows and vocab", rows, V)
-    if logits.dtype not in _LOGIT_TYPES:
+    dtype = _LOGIT_TYPES.get(logits.dtype)
+    if dtype is None:
         raise TypeError(f"logits must be float32, float16 or bfloat16, got {logits.dtype}")
-    p = _AdjustParams()
-    p.logits = _address(logits, logits.dtype, "logits")
-    p.dtype = _LOGIT_TYPES[logits.dtype]
+    f32, i32 = torch.float32, torch.int32
     if out is None:
-        out = _made_on(stream, lambda: torch.empty(rows, V, dtype=torch.float32, device=dev))
-    elif out.shape != logits.shape or out.device != dev:
-        raise ValueError("out must have the logits' shape and device")
-    p.out = _address(out, torch.float32, "out")
-    p.logits_stride, p.out_stride, p.rows, p.vocab = logits.stride(0), out.stride(0), rows, V
-    f32 = torch.float32
-    if history is not None:
-        p.history, p.n_history = _list32(history, None, "history", dev), history.shape[0]
-    p.history_starts = _list32(history_starts, rows + 1, "history_starts", dev)
-    p.prompt_lengths = _list32(prompt_lengths, rows, "prompt_lengths", dev)
-    p.repetition = _list32(repetition, rows, "repetition", dev, f32)
-    p.frequency = _list32(frequency, rows, "frequency", dev, f32)
-    p.presence = _list32(presence, rows, "presence", dev, f32)
-    if bias_ids is not None:
-        p.bias_ids, p.n_bias = _list32(bias_ids, None, "bias_ids", dev), bias_ids.shape[0]
-        if bias_values is None or bias_values.shape != bias_ids.shape:
-            raise ValueError("bias_values must have the shape of bias_ids")
-    p.bias_values = _list32(bias_values, None, "bias_values", dev, f32)
-    p.bias_starts = _list32(bias_starts, rows + 1, "bias_starts", dev)
+        out = _made_on(stream, lambda: torch.empty(rows, V, dtype=f32, device=logits.device))
+    elif out.shape != shape:
+        raise ValueError("out must have the logits' shape")
+    elif out.dtype is not f32 or out.get_device() != dev:
+        raise TypeError(f"out must be float32 on cuda:{dev}")
+    z0, z1 = logits.stride()
+    o0, o1 = out.stride()
+    if V > 1 and (z1 != 1 or o1 != 1):
+        raise ValueError("the last dimension of logits and out must be contiguous")
+    n_history = 0 if history is None else history.numel()
+    n_bias = 0 if bias_ids is None else bias_ids.numel()
+    if n_bias and (bias_values is None or bias_values.shape != bias_ids.shape):
+        raise ValueError("bias_values must have the shape of bias_ids")
+    mask_at = n_masks = mask_stride = 0
     if mask is not None:
-        if mask.dim() != 2 or mask.shape[1] < (V + 31) // 32 or mask.device != dev:
-            raise ValueError("mask must be [n, ceil(vocab / 32)] on the logits' device")
-        p.mask, p.n_masks = _address(mask, torch.int32, "mask"), mask.shape[0]
-        p.mask_stride = mask.stride(0)
-    p.mask_rows = _list32(mask_rows, rows, "mask_rows", dev)
-    _in_32_bits("lists", p.n_history, p.n_bias)
-    with _on(dev):
-        _check(lib().kvq_adjust_logits(ctypes.byref(p), _stream_on(dev, stream)))
+        if mask.dim() != 2 or mask.shape[1] < (V + 31) // 32 or mask.stride(1) != 1:
+            raise ValueError("mask must be [n, ceil(vocab / 32)], its rows contiguous")
+        if mask.dtype is not i32 or mask.get_device() != dev:
+            raise TypeError(f"mask must be int32 on cuda:{dev}")
+        mask_at, n_masks, mask_stride = mask.data_ptr(), mask.shape[0], mask.stride(0)
+    _in_32_bits("lists", n_history, n_bias)
+    params = _ADJUST.pack(
+        logits.data_ptr(), out.data_ptr(), _list(history, None, i32, "history", dev),
+        _list(history_starts, rows + 1, i32, "history_starts", dev),
+        _list(prompt_lengths, rows, i32, "prompt_lengths", dev),
+        _list(repetition, rows, f32, "repetition", dev),
+        _list(frequency, rows, f32, "frequency", dev),
+        _list(presence, rows, f32, "presence", dev),
+        _list(bias_ids, None, i32, "bias_ids", dev),
+        _list(bias_values, None, f32, "bias_values", dev),
+        _list(bias_starts, rows + 1, i32, "bias_starts", dev), mask_at,
+        _list(mask_rows, rows, i32, "mask_rows", dev), z0, o0, mask_stride, dtype, rows, V,
+        n_history, n_bias, n_masks)
+    _launch(dev, stream, lib().kvq_adjust_logits, params)
     return out
 
 
