@@ -58,13 +58,12 @@ __device__ __forceinline__ uint32_t narrow(float a, float b) {
 // The two groups of four channels of lane c of 16, and its first pair (r = rot_dim / 2).
 struct Lane {
   int g0, g1, pair;
-  bool rotate, paired;
+  bool rotate;
 };
 __device__ __forceinline__ Lane lane_of(int c, int r, bool paired) {
   Lane l;
   l.pair = 4 * c;
   l.rotate = 4 * c < r;
-  l.paired = paired;
   if (paired || !l.rotate) {
     // pairs side by side; and the channels behind the rotated ones, 8 a lane
     l.g0 = 8 * c;
@@ -138,11 +137,11 @@ __device__ __forceinline__ uint32_t rotate2(float x1, float c1, float x2, float 
   return narrow<BF16>(rotate_odd(x1, c1, x2, s1), rotate_odd(w1, c2, w2, s2));
 }
 
-template <bool BF16, bool KEY>
+template <bool BF16, bool KEY, bool PAIRED>
 __device__ __forceinline__ void rotate(uint2& a, uint2& b, const Lane& l, const Angles& t) {
   const float2 a0 = widen<BF16>(a.x), a1 = widen<BF16>(a.y);
   const float2 b0 = widen<BF16>(b.x), b1 = widen<BF16>(b.y);
-  if (l.paired) {
+  if constexpr (PAIRED) {
     a.x = rotate2<BF16, KEY>(a0.x, t.c.x, a0.y, t.s.x, a0.y, t.c.x, a0.x, -t.s.x);
     a.y = rotate2<BF16, KEY>(a1.x, t.c.y, a1.y, t.s.y, a1.y, t.c.y, a1.x, -t.s.y);
     b.x = rotate2<BF16, KEY>(b0.x, t.c.z, b0.y, t.s.z, b0.y, t.c.z, b0.x, -t.s.z);
@@ -163,9 +162,14 @@ __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
 // Four codes.  A product with 1 / scale is within 2^-22 of the quotient; where it is not
 // that near to a border of the codes (bits 0 .. 19 of the fp32 number at their middle, as
 // long as the code is a normal number), it rounds as the quotient does.
+__device__ __forceinline__ bool in_doubt(float q) {
+  return ((__float_as_uint(q) & 0xfffffu) - 0x7fff8u) <= 16u || fabsf(q) < 0x1p-6f;
+}
+// Below 2^-6 codes are the multiples of 2^-9.
 __device__ __forceinline__ bool near_border(float q) {
-  const uint32_t u = __float_as_uint(q);
-  return ((u & 0xfffffu) - 0x7fff8u) <= 16u || (q != 0.0f && fabsf(q) < 0x1p-6f);
+  const float t = fabsf(q) * 512.0f;
+  if (t >= 8.0f) return ((__float_as_uint(q) & 0xfffffu) - 0x7fff8u) <= 16u;
+  return fabsf(t - rintf(t)) > 0.5f - 0x1p-17f;
 }
 __device__ __forceinline__ uint32_t to_codes(float x, float y, float z, float w) {
   const __nv_fp8x2_storage_t a =
@@ -174,21 +178,25 @@ __device__ __forceinline__ uint32_t to_codes(float x, float y, float z, float w)
       __nv_cvt_float2_to_fp8x2(make_float2(z, w), __NV_SATFINITE, __NV_E4M3);
   return (uint32_t)a | ((uint32_t)b << 16);
 }
-__device__ __noinline__ uint32_t exact_codes(float x, float y, float z, float w, float scale) {
-  return to_codes(__fdiv_rn(x, scale), __fdiv_rn(y, scale), __fdiv_rn(z, scale),
-                  __fdiv_rn(w, scale));
+__device__ __noinline__ uint32_t careful_codes(float x, float y, float z, float w, float scale,
+                                               float inv) {
+  const float a = x * inv, b = y * inv, c = z * inv, d = w * inv;
+  if (near_border(a) || near_border(b) || near_border(c) || near_border(d))
+    return to_codes(__fdiv_rn(x, scale), __fdiv_rn(y, scale), __fdiv_rn(z, scale),
+                    __fdiv_rn(w, scale));
+  return to_codes(a, b, c, d);
 }
 template <bool BF16>
 __device__ __forceinline__ uint32_t codes_of(uint2 v, float scale, float inv) {
   const float2 x = widen<BF16>(v.x), y = widen<BF16>(v.y);
   const float a = x.x * inv, b = x.y * inv, c = y.x * inv, d = y.y * inv;
-  if (near_border(a) || near_border(b) || near_border(c) || near_border(d))
-    return exact_codes(x.x, x.y, y.x, y.y, scale);
+  if (in_doubt(a) || in_doubt(b) || in_doubt(c) || in_doubt(d))
+    return careful_codes(x.x, x.y, y.x, y.y, scale, inv);
   return to_codes(a, b, c, d);
 }
 
 // Keys (KEY) or values of kv-head h of a sequence.
-template <bool BF16, bool KEY>
+template <bool BF16, bool KEY, bool PAIRED>
 struct Task {
   const AppendCall& call;
   const Seq& s;
@@ -224,7 +232,7 @@ struct Task {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int at = pos + 2 * i;
-        if (at >= before && at < s.L) rotate<BF16, true>(x[i][0], x[i][1], l, t[i]);
+        if (at >= before && at < s.L) rotate<BF16, true, PAIRED>(x[i][0], x[i][1], l, t[i]);
       }
     }
   }
@@ -324,7 +332,7 @@ struct Share {
 
 // Keys or values of unit `unit` (the batch's blocks with new tokens, in order).  The warps
 // look through 32 sequences each.
-template <bool BF16>
+template <bool BF16, bool PAIRED>
 __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part, Share& sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll 1
@@ -367,8 +375,8 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
     if (blk == heir) return;
 #pragma unroll 1
     for (;;) {
-      if (part & 1) Task<BF16, false>(call, q, sh.b, part >> 1).block(blk, sh.m);
-      else Task<BF16, true>(call, q, sh.b, part >> 1).block(blk, sh.m);
+      if (part & 1) Task<BF16, false, PAIRED>(call, q, sh.b, part >> 1).block(blk, sh.m);
+      else Task<BF16, true, PAIRED>(call, q, sh.b, part >> 1).block(blk, sh.m);
       if (blk != first || heir < 0) return;
       __syncthreads();  // sh.m is written again
       blk = heir;
@@ -378,7 +386,7 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
 }
 
 // Queries of token `row`, heads h0 .. h0 + 7.
-template <bool BF16>
+template <bool BF16, bool PAIRED>
 __device__ __forceinline__ void query_task(const AppendCall& call, int row, int h0) {
   const int lane = threadIdx.x & 31, half = lane >> 4;
   const Lane l = lane_of(lane & 15, call.p.rot_dim >> 1, call.p.paired);
@@ -418,7 +426,7 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
   if (l.rotate) {
     const Angles t = angles_of(call.p, l, table_row(call, row, pos));
 #pragma unroll
-    for (int i = 0; i < kQueryHeads / 2; ++i) rotate<BF16, false>(x[i][0], x[i][1], l, t);
+    for (int i = 0; i < kQueryHeads / 2; ++i) rotate<BF16, false, PAIRED>(x[i][0], x[i][1], l, t);
   }
 #pragma unroll
   for (int i = 0; i < kQueryHeads / 2; ++i) {
@@ -433,7 +441,7 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
 
 // CTAs of blocks, then of queries; the last CTA looks over the batch's sizes for the flag
 // word.
-template <bool BF16>
+template <bool BF16, bool PAIRED>
 __global__ void __launch_bounds__(32 * kWarps, 8)
 append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) {
   __shared__ Share share;
@@ -444,11 +452,11 @@ append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) 
     }
   } else if ((int)blockIdx.x < kv_ctas) {
     const int parts = 2 * call.d.hkv, unit = (int)blockIdx.x / parts;
-    kv_task<BF16>(call, unit, (int)blockIdx.x - unit * parts, share);
+    kv_task<BF16, PAIRED>(call, unit, (int)blockIdx.x - unit * parts, share);
   } else {
     const int task = ((int)blockIdx.x - kv_ctas) * kWarps + ((int)threadIdx.x >> 5);
     const int row = task / groups;
-    if (row < call.batch.n_tokens) query_task<BF16>(call, row, (task - row * groups) * kQueryHeads);
+    if (row < call.batch.n_tokens) query_task<BF16, PAIRED>(call, row, (task - row * groups) * kQueryHeads);
   }
 }
 
@@ -462,8 +470,11 @@ cudaError_t launch_append(const AppendCall& call, cudaStream_t stream) {
   const int groups = (call.d.hq + kQueryHeads - 1) / kQueryHeads;
   const int q_ctas = call.p.q ? (int)((tokens * groups + kWarps - 1) / kWarps) : 0;
   const int grid = kv_ctas + q_ctas + 1;
-  if (call.d.bf16) append_kernel<true><<<grid, 32 * kWarps, 0, stream>>>(call, kv_ctas, groups);
-  else append_kernel<false><<<grid, 32 * kWarps, 0, stream>>>(call, kv_ctas, groups);
+  const auto kernel = call.d.bf16
+                          ? (call.p.paired ? append_kernel<true, true> : append_kernel<true, false>)
+                          : (call.p.paired ? append_kernel<false, true>
+                                           : append_kernel<false, false>);
+  kernel<<<grid, 32 * kWarps, 0, stream>>>(call, kv_ctas, groups);
   return cudaGetLastError();
 }
 
