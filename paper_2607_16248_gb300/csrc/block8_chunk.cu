@@ -248,7 +248,6 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
   uint64_t* full = key ? s.k_full : s.v_full;
   uint64_t* empty = key ? s.k_empty : s.v_empty;
   const uint8_t* pool = key ? p.c.cache.k_codes : p.c.cache.v_codes;
-  constexpr int kNone = -0x7fffffff - 1;
   uint32_t n = 0;
   ItemWalk w;
   w.begin(p, s.start, u0, u1);
@@ -259,16 +258,17 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
       return t0 <= w.s.p1 && (t0 + kGroup > w.s.lo || t0 < p.c.sinks);
     };
     const auto token = [&](int i) { return w.s.tile(i) * kTile + j * kGroup; };
-    // page of unit i's block; kNone where no codes are read
-    const auto entry = [&](int i) {
-      if (i >= w.i1) return kNone;
+    // whether unit i's block is read as codes, its page (looked at no sooner than needed),
+    // and its place in the pools, -1 for none
+    const auto reads = [&](int i) {
       const int t0 = token(i);
-      return t0 < whole && seen(t0) ? __ldg(table + (t0 >> 5)) : kNone;
+      return i < w.i1 && t0 < whole && seen(t0);
     };
-    // place of a page's block in the pools, -1 for none
-    const auto place = [&](int e) -> int {
+    const auto entry = [&](int i) { return reads(i) ? __ldg(table + (token(i) >> 5)) : -1; };
+    const auto place = [&](int i, int e) -> int {
+      if (!reads(i)) return -1;
       if ((unsigned)e < (unsigned)p.c.cache.n_pages) return e * p.c.d.hkv + w.head;
-      if (e != kNone && lane == 0) set_flag(p.c.cache, KVQ_FLAG_BAD_PAGE);
+      if (lane == 0) set_flag(p.c.cache, KVQ_FLAG_BAD_PAGE);
       return -1;
     };
     const auto prefetch = [&](int e) {
@@ -278,7 +278,7 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
     };
     Codes c;
     float2 scale = make_float2(1.0f, 1.0f);
-    int at0 = -1, at1 = place(entry(w.i0));
+    int at0 = -1, at1 = place(w.i0, entry(w.i0));
     int e[kAhead];  // entries behind at1's
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) e[k] = entry(w.i0 + 1 + k);
@@ -327,7 +327,7 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
         ++n;
       }
       at0 = at1;
-      at1 = place(e[0]);
+      at1 = place(i + 2, e[0]);
       prefetch(e[kAhead - 1]);
 #pragma unroll
       for (int k = 0; k < kAhead - 1; ++k) e[k] = e[k + 1];
