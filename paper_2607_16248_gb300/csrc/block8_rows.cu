@@ -48,6 +48,8 @@ struct Smem {
   unsigned char page[kWarps][kSlots][2 * kHalfPage];
   float4 merge[kMergers][NT * 8][32];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];
+  uint2 q[NT <= 2 ? 1 : NT][8][32];  // queries of more row groups than fit registers
+  float qf[8 * NT];
   float2 scale[kWarps][kSlots];
   uint64_t full[kWarps][kSlots];
   int scan[32];
@@ -90,10 +92,17 @@ __device__ __forceinline__ uint32_t wide_hi(uint32_t v) {
 
 template <int NT>
 struct State {
+  // queries in registers while there is room for them beside the results
+  static constexpr bool kOwnQueries = NT <= 2;
   float m[NT][2], l[NT][2];  // of rows 8 nt + 2 tig, + 1; l of this lane's tokens alone
   float o[NT][8][4];         // channels 16 gid + 2 i (0, 1) and + 1 (2, 3), the same rows
-  uint32_t q[NT][8][2];      // queries of row 8 nt + gid, channels 32 tig ..
+  uint2 q[kOwnQueries ? NT : 1][8];  // of row 8 nt + gid, channels 32 tig ..
+  const uint2* shared_q;             // [NT][8][32] of the CTA
   float f[NT][2];            // factor of a score in the exponent
+  __device__ __forceinline__ uint2 query(int n, int step) const {
+    if constexpr (kOwnQueries) return q[n][step];
+    else return shared_q[(8 * n + step) * 32 + (threadIdx.x & 31)];
+  }
 };
 
 // What masks a block's tokens: the rows' positions.
@@ -190,18 +199,24 @@ __device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const 
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     const unsigned char* at = kr + (((2 * tig + c) ^ gid) << 4);
+    uint4 x[2], y[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint4 x = *reinterpret_cast<const uint4*>(at + h * 16 * kHeadDim);
-      const uint4 y = *reinterpret_cast<const uint4*>(at + (h * 16 + 8) * kHeadDim);
-      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+      x[h] = *reinterpret_cast<const uint4*>(at + h * 16 * kHeadDim);
+      y[h] = *reinterpret_cast<const uint4*>(at + (h * 16 + 8) * kHeadDim);
+    }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t a0 = wide_lo(xw[k]), a1 = wide_lo(yw[k]);
-        const uint32_t a2 = wide_hi(xw[k]), a3 = wide_hi(yw[k]);
+    for (int k = 0; k < 4; ++k) {
+      uint2 q[N];
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-          mma(s[h][n], a0, a1, a2, a3, st.q[n][4 * c + k][0], st.q[n][4 * c + k][1]);
+      for (int n = 0; n < N; ++n) q[n] = st.query(n, 4 * c + k);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t xw = k == 0 ? x[h].x : k == 1 ? x[h].y : k == 2 ? x[h].z : x[h].w;
+        const uint32_t yw = k == 0 ? y[h].x : k == 1 ? y[h].y : k == 2 ? y[h].z : y[h].w;
+        const uint32_t a0 = wide_lo(xw), a1 = wide_lo(yw), a2 = wide_hi(xw), a3 = wide_hi(yw);
+#pragma unroll
+        for (int n = 0; n < N; ++n) mma(s[h][n], a0, a1, a2, a3, q[n].x, q[n].y);
       }
     }
   }
@@ -304,8 +319,10 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
         const uint32_t a2 = to_half2<BF16>(xw[2 * i + 1], f[0]),
                        a3 = to_half2<BF16>(yw[2 * i + 1], f[1]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          mma(s[h][n], a0, a1, a2, a3, st.q[n][2 * c + i][0], st.q[n][2 * c + i][1]);
+        for (int n = 0; n < NT; ++n) {
+          const uint2 q = st.query(n, 2 * c + i);
+          mma(s[h][n], a0, a1, a2, a3, q.x, q.y);
+        }
       }
     }
     if constexpr (BF16) {
@@ -371,45 +388,68 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
   }
 }
 
-// Queries of an item: row 8 n + gid's channels 32 tig .. 32 tig + 31, bf16 ones times a power
-// of two; the rows' factors and positions.
+// Queries of an item's row group n: row 8 n + gid's channels 32 tig .. 32 tig + 31, bf16 ones
+// times a power of two, which is returned.
+template <bool BF16>
+__device__ __forceinline__ float load_group(const AttnParams& p, const Seq& q, int head, int n,
+                                            uint2 (&out)[8]) {
+  const int lane = threadIdx.x & 31, r = 8 * n + (lane >> 2);
+  uint4 x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+  if (r < q.n * p.c.d.gq) {
+    const uint4* src = reinterpret_cast<const uint4*>(
+        p.c.q + row_offset(p, p.c.q_stride, q.row, head, r) + 32 * (lane & 3));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __ldg(src + i);
+  }
+  float f = 1.0f;
+  if constexpr (BF16) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = largest(m, x[i]);
+    m = max(m & 0xffffu, m >> 16);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    f = lift_of(m);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    out[2 * i] = make_uint2(to_half2<BF16>(x[i].x, f), to_half2<BF16>(x[i].y, f));
+    out[2 * i + 1] = make_uint2(to_half2<BF16>(x[i].z, f), to_half2<BF16>(x[i].w, f));
+  }
+  return f;
+}
+
+// An item's queries, its rows' factors and positions, and empty results.  By all threads.
 template <int NT, bool BF16>
-__device__ __forceinline__ void load_queries(const AttnParams& p, const Seq& q, int head,
-                                             State<NT>& st, Rows<NT>& rows) {
-  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-  const int n_rows = q.n * p.c.d.gq;
+__device__ __forceinline__ void begin_item(const AttnParams& p, const Seq& q, int head,
+                                           Smem<NT>& sm, State<NT>& st, Rows<NT>& rows) {
+  const int lane = threadIdx.x & 31, tig = lane & 3;
+  if constexpr (!State<NT>::kOwnQueries) {
+    const int warp = threadIdx.x >> 5;
+    if (warp < NT) {  // (nobody reads the last item's any more: its parts have met)
+      uint2 x[8];
+      const float f = load_group<BF16>(p, q, head, warp, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sm.q[warp][i][lane] = x[i];
+      if (tig == 0) sm.qf[8 * warp + (lane >> 2)] = f;
+    }
+    __syncthreads();
+    st.shared_q = &sm.q[0][0][0];
+  }
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = 8 * n + gid;
-    uint4 x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (r < n_rows) {
-      const uint4* src = reinterpret_cast<const uint4*>(
-          p.c.q + row_offset(p, p.c.q_stride, q.row, head, r) + 32 * tig);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __ldg(src + i);
-    }
     float f = 1.0f;
-    if constexpr (BF16) {
-      uint32_t m = 0u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) m = largest(m, x[i]);
-      m = max(m & 0xffffu, m >> 16);
-      m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-      m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      f = lift_of(m);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      st.q[n][2 * i][0] = to_half2<BF16>(x[i].x, f);
-      st.q[n][2 * i][1] = to_half2<BF16>(x[i].y, f);
-      st.q[n][2 * i + 1][0] = to_half2<BF16>(x[i].z, f);
-      st.q[n][2 * i + 1][1] = to_half2<BF16>(x[i].w, f);
-    }
+    if constexpr (State<NT>::kOwnQueries) f = load_group<BF16>(p, q, head, n, st.q[n]);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      st.f[n][j] = p.c.scale_log2 / (BF16 ? __shfl_sync(0xffffffffu, f, 8 * tig + 4 * j) : 1.0f);
+      float g = 1.0f;
+      if constexpr (BF16) {
+        if constexpr (State<NT>::kOwnQueries) g = __shfl_sync(0xffffffffu, f, 8 * tig + 4 * j);
+        else g = sm.qf[8 * n + 2 * tig + j];
+      }
+      st.f[n][j] = p.c.scale_log2 / g;
       rows.pos[n][j] = q.L - q.n + token_of_row(p, 8 * n + 2 * tig + j);
       st.m[n][j] = kNone;
       st.l[n][j] = 0.0f;
@@ -573,7 +613,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
   for (; w.next(p); w.advance(p)) {
     State<NT> st;
     Rows<NT> rows;
-    load_queries<NT, BF16>(p, w.q, w.head, st, rows);
+    begin_item<NT, BF16>(p, w.q, w.head, sm, st, rows);
     const int whole = whole_units(w);
     if (warp == kWarps - 1 && whole < w.i1) {
       const int t0 = w.s.tile(whole) * kGroup;
