@@ -24,8 +24,8 @@ join_kernel(const __grid_constant__ AttnParams p) {
   const int r = kJoinWarps * blockIdx.y + (threadIdx.x >> 5);
   const int row = sp.row_tile * p.item_rows + r;
   if (r >= p.item_rows || row >= q.n * p.c.d.gq) return;
-  join_row<BF16>(p, blockIdx.x, sp.inside, sp.last - (int)blockIdx.x + 1, r,
-                 p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row));
+  put_row<BF16>(p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row),
+                join_row(p, blockIdx.x, sp.inside, sp.last - (int)blockIdx.x + 1, r, 0, 1));
 }
 
 cudaError_t launch_join(const AttnParams& p, int ctas, int rows, cudaStream_t stream) {
@@ -98,7 +98,7 @@ long long attn_most_units(const Dims8& d, int max_new) {
   const Plan plan = plan_of(d, max_new, 1);
   const long long tiles =
       plan.many ? ((long long)max_new * d.gq + plan.chunk - 1) / plan.chunk : 1;
-  return (long long)d.batch * d.hkv * (d.max_blocks + 8) * tiles;
+  return (long long)d.batch * d.hkv * ((long long)d.max_blocks * kMostWeight + 16) * tiles;
 }
 
 cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream) {

@@ -674,7 +674,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
     }
     if (!direct && w.i0 == 0 && threadIdx.x == 0)
       p.splits[blockIdx.x] =
-          Split{1, u0 < w.base ? 1 : 0, shares.owner(w.base + kItemCost + w.s.n - 1), w.b,
+          Split{1, u0 < w.base ? 1 : 0, shares.owner(w.last_unit()), w.b,
                 w.row_tile, w.head};
     if (!meet_softmax(s, met)) return;  // s.m, s.l and both accumulators may be written again
     ++items;

@@ -2,7 +2,8 @@
 //
 // An item is one row tile of one (sequence, kv-head): rows t * gq + head of the sequence's
 // new tokens t and the gq heads that share the kv-head.  Its units are the tiles of
-// 2^TOK tokens that any of its rows sees, after a fixed cost in units.  All items' units
+// 2^TOK tokens that any of its rows sees, after a fixed cost in units; a tile counts as many
+// units as the kernel says it takes for the item's rows (`weight`).  All items' units
 // lie end to end (sequence, row tile, kv-head) and every CTA takes an equal contiguous
 // share.  An item that several CTAs share leaves partials (unnormalised rows, maximum,
 // sum) that are joined in the order of the tokens: by the CTA that comes last, or by a second
@@ -18,6 +19,8 @@ namespace block8 {
 struct Split {
   int valid, inside, last, b, row_tile, head;
 };
+
+constexpr int kMostWeight = 7;  // units of a block with four groups of eight rows
 
 struct AttnParams {
   AttnCall c;
@@ -95,6 +98,15 @@ struct Start {
   int b, row_tile, head, step;
 };
 
+// Units of a token tile for a sequence's rows.  Few rows: each row group more is more
+// products, and what a block takes beside its bytes shows while bytes and products share
+// the time (16 chats with one to five drafts: 148 us by blocks alone, CTAs between 92 and
+// 145 us busy).
+template <int TOK>
+__device__ __forceinline__ int weight(const AttnParams& p, const Seq& q) {
+  if constexpr (TOK == 7) return 1;
+  else return kMostWeight - 4 + min((q.n * p.c.d.gq + 7) >> 3, 4);
+}
 // Units of all sequences, this CTA's share and where it begins, by all threads of the CTA
 // (at most 32 warps).  At least `least` units a CTA.  Ends behind a barrier; false where
 // the CTA has no share.
@@ -106,9 +118,9 @@ __device__ __forceinline__ bool plan_share(const AttnParams& p, int* scan, Start
   const int b0 = min(p.c.d.batch, tid * per), b1 = min(p.c.d.batch, b0 + per);
   const auto units = [&](const Seq& q) {
     int n = 0;
-    const int tiles = row_tiles(p, q);
+    const int tiles = row_tiles(p, q), wt = weight<TOK>(p, q);
 #pragma unroll 1
-    for (int t = 0; t < tiles; ++t) n += (span_of<TOK>(p, q, t).n + COST) * p.c.d.hkv;
+    for (int t = 0; t < tiles; ++t) n += (span_of<TOK>(p, q, t).n * wt + COST) * p.c.d.hkv;
     return n;
   };
   int mine = 0;
@@ -150,7 +162,7 @@ __device__ __forceinline__ bool plan_share(const AttnParams& p, int* scan, Start
       const int tiles = row_tiles(p, q);
 #pragma unroll 1
       for (int t = 0; t < tiles; ++t) {
-        const int n = span_of<TOK>(p, q, t).n + COST;
+        const int n = span_of<TOK>(p, q, t).n * weight<TOK>(p, q) + COST;
         if (u0 >= at && u0 < at + n * p.c.d.hkv) {
           start->b = b;
           start->row_tile = t;
@@ -172,7 +184,8 @@ struct Walk {
   int b, row_tile, head;
   Seq q;                  // the item's sequence
   Span s;
-  int i0, i1;             // the item's tiles in this share
+  int wt;                 // units of a tile
+  int i0, i1;             // the item's tiles in this share: those whose first unit lies there
   __device__ __forceinline__ void begin(const AttnParams& p, const Start& st, int u0, int u1) {
     u = u0;
     end = u1;
@@ -183,21 +196,29 @@ struct Walk {
     if (u < end) {
       q = attn_seq(p, b);
       s = span_of<TOK>(p, q, row_tile);
+      wt = weight<TOK>(p, q);
     }
   }
+  // The first tile that begins at unit x of the item or behind it.
+  __device__ __forceinline__ int tile_from(int x) const {
+    return TOK == 7 ? x : (int)((uint32_t)(x + wt - 1) / (uint32_t)wt);
+  }
+  // The item's first unit, and the last tile's.
+  __device__ __forceinline__ int first_unit() const { return base + COST; }
+  __device__ __forceinline__ int last_unit() const { return base + COST + (s.n - 1) * wt; }
   // The current item's part of the share; false at the end.
   __device__ __forceinline__ bool next(const AttnParams& p) {
     while (u < end) {
-      const int local = u - base, stop = min(s.n + COST, local + end - u);
-      i0 = max(local - COST, 0);
-      i1 = stop - COST;
+      const int local = u - base, stop = min(s.n * wt + COST, local + end - u);
+      i0 = tile_from(max(local - COST, 0));
+      i1 = tile_from(max(stop - COST, 0));
       if (i1 > i0) return true;
-      advance(p);  // nothing but a piece of the item's fixed cost
+      advance(p);  // nothing but a piece of the item's fixed cost or of a tile
     }
     return false;
   }
   __device__ __forceinline__ void advance(const AttnParams& p) {
-    base += s.n + COST;
+    base += s.n * wt + COST;
     u = min(base, end);
     if (++head < p.c.d.hkv || u >= end) return;
     head = 0;
@@ -208,6 +229,7 @@ struct Walk {
       } while (q.n == 0);  // the share ends behind another item
     }
     s = span_of<TOK>(p, q, row_tile);
+    wt = weight<TOK>(p, q);
   }
   __device__ __forceinline__ bool whole() const { return i0 == 0 && i1 == s.n; }
   // Slot of the CTA's partial: 0 for the item that its share begins in.
@@ -235,25 +257,39 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   }
 }
 
-// Row r of an item's partials to its result, by a warp.  CTA c0 + i left the i-th, CTA c0 in
-// its slot `inside`.  Each lane finds the weights of one of every 32, then the weighted rows
-// are summed in order.  A partial without a seen token weighs nothing, whatever it holds.
-template <bool BF16>
-__device__ __forceinline__ void join_row(const AttnParams& p, int c0, int inside, int n, int r,
-                                         uint16_t* out) {
+// Row r of an item's partials, weighted and summed in order, by a warp: those numbered first,
+// first + step, ...  CTA c0 + i left the i-th, CTA c0 in its slot `inside`.  Returns this
+// lane's four channels of the sum over these, over the whole softmax' sum.  The rows are on
+// their way with their statistics: sixteen at a time.  A partial without a seen token weighs
+// nothing, whatever it holds.
+__device__ __forceinline__ float4 join_row(const AttnParams& p, int c0, int inside, int n, int r,
+                                           int first, int step) {
   const int lane = threadIdx.x & 31;
   const auto slot = [&](int i) {
     return (long long)(2 * (c0 + i) + (i == 0 ? inside : 0)) * p.item_rows + r;
   };
   constexpr int kMost = (kMaxSplits + 31) / 32;  // partials a lane
+  constexpr int kTogether = 16;
   float2 ml[kMost];
-  float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
     const int i = 32 * k + lane;
     ml[k] = i < n ? __ldcg(&p.part_ml[slot(i)]) : make_float2(0.0f, 0.0f);
-    if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
   }
+  float4 v[kTogether];
+  const auto load = [&](int i0) {
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j) {
+      const int i = i0 + j * step;
+      if (i < n)
+        v[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
+    }
+  };
+  load(first);
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k)
+    if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
 #pragma unroll
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   float l = 0.0f;
@@ -266,23 +302,31 @@ __device__ __forceinline__ void join_row(const AttnParams& p, int c0, int inside
   for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
   const float f = l > 0.0f ? 1.0f / l : 0.0f;
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+  for (int i0 = first; i0 < n; i0 += kTogether * step) {
+    if (i0 > first) load(i0);
 #pragma unroll
-  for (int k = 0; k < kMost; ++k) {
-#pragma unroll 8
-    for (int i = 32 * k; i < min(n, 32 * k + 32); ++i) {
-      const float x = __shfl_sync(0xffffffffu, ml[k].x, i & 31) * f;
-      const float4 v =
-          __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
-      if (x > 0.0f) {
-        sum.x = fmaf(v.x, x, sum.x);
-        sum.y = fmaf(v.y, x, sum.y);
-        sum.z = fmaf(v.z, x, sum.z);
-        sum.w = fmaf(v.w, x, sum.w);
+    for (int j = 0; j < kTogether; ++j) {
+      const int i = i0 + j * step;
+      float w = ml[0].x;  // of the lane's partial in i's group of 32
+#pragma unroll
+      for (int k = 1; k < kMost; ++k)
+        if ((i >> 5) == k) w = ml[k].x;
+      const float x = __shfl_sync(0xffffffffu, w, i & 31) * f;
+      if (i < n && x > 0.0f) {
+        sum.x = fmaf(v[j].x, x, sum.x);
+        sum.y = fmaf(v[j].y, x, sum.y);
+        sum.z = fmaf(v[j].z, x, sum.z);
+        sum.w = fmaf(v[j].w, x, sum.w);
       }
     }
   }
-  reinterpret_cast<uint2*>(out)[lane] =
-      make_uint2(pack16<BF16>(sum.x, sum.y), pack16<BF16>(sum.z, sum.w));
+  return sum;
+}
+template <bool BF16>
+__device__ __forceinline__ void put_row(uint16_t* out, float4 x) {
+  reinterpret_cast<uint2*>(out)[threadIdx.x & 31] =
+      make_uint2(pack16<BF16>(x.x, x.y), pack16<BF16>(x.z, x.w));
 }
 #endif
 

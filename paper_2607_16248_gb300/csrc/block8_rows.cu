@@ -31,7 +31,7 @@ namespace block8 {
 namespace {
 
 constexpr int kTok = 5;            // 32 tokens a unit
-constexpr int kItemCost = 4;       // of an item in units: queries, merge, results
+constexpr int kItemCost = 16;      // of an item in units (a block's are 4 to 7): queries, merge
 constexpr int kHalfPage = kGroup * kHeadDim;  // bytes of a block's keys (or values)
 constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
 constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
@@ -479,7 +479,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
   }
   Shares shares;
   int u0, u1;
-  if (!plan_share<kTok, kItemCost>(p, sm.scan, &sm.start, kWarps, shares, u0, u1)) return;
+  if (!plan_share<kTok, kItemCost>(p, sm.scan, &sm.start, 4 * kWarps, shares, u0, u1)) return;
 
   // Units of an item before the 16-bit ones are whole blocks; warp w takes every eighth.
   const auto whole_units = [](const Walk<kTok, kItemCost>& w) {
@@ -742,8 +742,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     if (direct) continue;
     // Whoever brings an item's last partial joins them, in the order of the tokens.  The
     // tickets are zero between calls.
-    const int c0 = shares.owner(w.base + kItemCost);
-    const int parts = shares.owner(w.base + kItemCost + w.s.n - 1) - c0 + 1;
+    const int c0 = shares.owner(w.first_unit()), parts = shares.owner(w.last_unit()) - c0 + 1;
     if (warp == 0) {
       __threadfence();
       __syncwarp();
@@ -757,9 +756,21 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     __syncthreads();
     if (sm.join) {
       const int inside = shares.begin(c0) < w.base ? 1 : 0;
-      for (int r = warp; r < n_rows; r += kWarps)
-        join_row<BF16>(p, c0, inside, parts, r,
-                       p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r));
+      // of rows fewer than warps, each has several: every other, or every fourth partial
+      const int share = n_rows <= 2 ? 4 : n_rows <= 4 ? 2 : 1, k = warp & (share - 1);
+      for (int r = warp / share; r < n_rows; r += kWarps / share) {
+        float4 x = join_row(p, c0, inside, parts, r, k, share);
+        if (share > 1) {  // (the merge's slots are free: all warps are behind their barrier)
+          if (k) sm.merge[0][warp][lane] = x;
+          asm volatile("bar.sync %0, %1;" ::"r"(1 + r), "r"(32 * share) : "memory");
+          if (k) continue;
+          for (int i = 1; i < share; ++i) {
+            const float4 y = sm.merge[0][warp + i][lane];
+            x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+          }
+        }
+        put_row<BF16>(p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r), x);
+      }
     }
   }
   // copies that are still on their way get their time before the memory goes
