@@ -24,8 +24,8 @@ join_kernel(const __grid_constant__ AttnParams p) {
   const int r = kJoinWarps * blockIdx.y + (threadIdx.x >> 5);
   const int row = sp.row_tile * p.item_rows + r;
   if (r >= p.item_rows || row >= q.n * p.c.d.gq) return;
-  put_row<BF16>(p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row),
-                join_row(p, blockIdx.x, sp.inside, sp.last - (int)blockIdx.x + 1, r, 0, 1));
+  join_row<BF16>(p, blockIdx.x, sp.inside, sp.last - (int)blockIdx.x + 1, r,
+                 p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row));
 }
 
 cudaError_t launch_join(const AttnParams& p, int ctas, int rows, cudaStream_t stream) {

@@ -10,6 +10,8 @@
 // kernel.
 #pragma once
 
+#include <type_traits>
+
 #include "block8.cuh"
 
 namespace kvq {
@@ -184,7 +186,7 @@ struct Walk {
   int b, row_tile, head;
   Seq q;                  // the item's sequence
   Span s;
-  int wt;                 // units of a tile
+  std::conditional_t<TOK == 7, std::integral_constant<int, 1>, int> wt;  // units of a tile
   int i0, i1;             // the item's tiles in this share: those whose first unit lies there
   __device__ __forceinline__ void begin(const AttnParams& p, const Start& st, int u0, int u1) {
     u = u0;
@@ -196,7 +198,7 @@ struct Walk {
     if (u < end) {
       q = attn_seq(p, b);
       s = span_of<TOK>(p, q, row_tile);
-      wt = weight<TOK>(p, q);
+      if constexpr (TOK != 7) wt = weight<TOK>(p, q);
     }
   }
   // The first tile that begins at unit x of the item or behind it.
@@ -229,7 +231,7 @@ struct Walk {
       } while (q.n == 0);  // the share ends behind another item
     }
     s = span_of<TOK>(p, q, row_tile);
-    wt = weight<TOK>(p, q);
+    if constexpr (TOK != 7) wt = weight<TOK>(p, q);
   }
   __device__ __forceinline__ bool whole() const { return i0 == 0 && i1 == s.n; }
   // Slot of the CTA's partial: 0 for the item that its share begins in.
@@ -257,39 +259,25 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   }
 }
 
-// Row r of an item's partials, weighted and summed in order, by a warp: those numbered first,
-// first + step, ...  CTA c0 + i left the i-th, CTA c0 in its slot `inside`.  Returns this
-// lane's four channels of the sum over these, over the whole softmax' sum.  The rows are on
-// their way with their statistics: sixteen at a time.  A partial without a seen token weighs
-// nothing, whatever it holds.
-__device__ __forceinline__ float4 join_row(const AttnParams& p, int c0, int inside, int n, int r,
-                                           int first, int step) {
+// Row r of an item's partials to its result, by a warp.  CTA c0 + i left the i-th, CTA c0 in
+// its slot `inside`.  Each lane finds the weights of one of every 32, then the weighted rows
+// are summed in order.  A partial without a seen token weighs nothing, whatever it holds.
+template <bool BF16>
+__device__ __forceinline__ void join_row(const AttnParams& p, int c0, int inside, int n, int r,
+                                         uint16_t* out) {
   const int lane = threadIdx.x & 31;
   const auto slot = [&](int i) {
     return (long long)(2 * (c0 + i) + (i == 0 ? inside : 0)) * p.item_rows + r;
   };
   constexpr int kMost = (kMaxSplits + 31) / 32;  // partials a lane
-  constexpr int kTogether = 16;
   float2 ml[kMost];
+  float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
     const int i = 32 * k + lane;
     ml[k] = i < n ? __ldcg(&p.part_ml[slot(i)]) : make_float2(0.0f, 0.0f);
-  }
-  float4 v[kTogether];
-  const auto load = [&](int i0) {
-#pragma unroll
-    for (int j = 0; j < kTogether; ++j) {
-      const int i = i0 + j * step;
-      if (i < n)
-        v[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
-    }
-  };
-  load(first);
-  float m = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < kMost; ++k)
     if (ml[k].y > 0.0f) m = fmaxf(m, ml[k].x);
+  }
 #pragma unroll
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   float l = 0.0f;
@@ -302,31 +290,23 @@ __device__ __forceinline__ float4 join_row(const AttnParams& p, int c0, int insi
   for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
   const float f = l > 0.0f ? 1.0f / l : 0.0f;
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 1
-  for (int i0 = first; i0 < n; i0 += kTogether * step) {
-    if (i0 > first) load(i0);
 #pragma unroll
-    for (int j = 0; j < kTogether; ++j) {
-      const int i = i0 + j * step;
-      float w = ml[0].x;  // of the lane's partial in i's group of 32
-#pragma unroll
-      for (int k = 1; k < kMost; ++k)
-        if ((i >> 5) == k) w = ml[k].x;
-      const float x = __shfl_sync(0xffffffffu, w, i & 31) * f;
-      if (i < n && x > 0.0f) {
-        sum.x = fmaf(v[j].x, x, sum.x);
-        sum.y = fmaf(v[j].y, x, sum.y);
-        sum.z = fmaf(v[j].z, x, sum.z);
-        sum.w = fmaf(v[j].w, x, sum.w);
+  for (int k = 0; k < kMost; ++k) {
+#pragma unroll 8
+    for (int i = 32 * k; i < min(n, 32 * k + 32); ++i) {
+      const float x = __shfl_sync(0xffffffffu, ml[k].x, i & 31) * f;
+      const float4 v =
+          __ldcg(reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + lane);
+      if (x > 0.0f) {
+        sum.x = fmaf(v.x, x, sum.x);
+        sum.y = fmaf(v.y, x, sum.y);
+        sum.z = fmaf(v.z, x, sum.z);
+        sum.w = fmaf(v.w, x, sum.w);
       }
     }
   }
-  return sum;
-}
-template <bool BF16>
-__device__ __forceinline__ void put_row(uint16_t* out, float4 x) {
-  reinterpret_cast<uint2*>(out)[threadIdx.x & 31] =
-      make_uint2(pack16<BF16>(x.x, x.y), pack16<BF16>(x.z, x.w));
+  reinterpret_cast<uint2*>(out)[lane] =
+      make_uint2(pack16<BF16>(sum.x, sum.y), pack16<BF16>(sum.z, sum.w));
 }
 #endif
 

@@ -756,21 +756,9 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     __syncthreads();
     if (sm.join) {
       const int inside = shares.begin(c0) < w.base ? 1 : 0;
-      // of rows fewer than warps, each has several: every other, or every fourth partial
-      const int share = n_rows <= 2 ? 4 : n_rows <= 4 ? 2 : 1, k = warp & (share - 1);
-      for (int r = warp / share; r < n_rows; r += kWarps / share) {
-        float4 x = join_row(p, c0, inside, parts, r, k, share);
-        if (share > 1) {  // (the merge's slots are free: all warps are behind their barrier)
-          if (k) sm.merge[0][warp][lane] = x;
-          asm volatile("bar.sync %0, %1;" ::"r"(1 + r), "r"(32 * share) : "memory");
-          if (k) continue;
-          for (int i = 1; i < share; ++i) {
-            const float4 y = sm.merge[0][warp + i][lane];
-            x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
-          }
-        }
-        put_row<BF16>(p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r), x);
-      }
+      for (int r = warp; r < n_rows; r += kWarps)
+        join_row<BF16>(p, c0, inside, parts, r,
+                       p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r));
     }
   }
   // copies that are still on their way get their time before the memory goes
