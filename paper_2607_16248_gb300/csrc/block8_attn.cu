@@ -10,22 +10,71 @@ namespace block8 {
 namespace {
 
 // The chunk kernel's partials to results: the CTAs (c, y) share the rows of the item that CTA c
-// left, a row a warp.  (In that kernel itself it would fall to the CTA that comes last, whose
-// roles have no registers for it.)
-constexpr int kJoinWarps = 8;
+// left.  (In that kernel itself it would fall to the CTA that comes last, whose roles have no
+// registers for it.)  Up to four partials: eight rows a warp, four lanes a row, so that eight
+// loads a lane are on their way (y = 0, 8, ...: 64 rows a CTA); more: a row a warp (join_row).
+constexpr int kJoinWarps = 8, kFewParts = 4;
 
 template <bool BF16>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 join_kernel(const __grid_constant__ AttnParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const Split sp = p.splits[blockIdx.x];
-  if (!sp.valid) return;
+  const int n = sp.last - (int)blockIdx.x + 1;
+  if (!sp.valid || (n <= kFewParts && (blockIdx.y & 7))) return;
   const Seq q = seq_of(p.c.d, p.c.batch, sp.b);
-  const int r = kJoinWarps * blockIdx.y + (threadIdx.x >> 5);
-  const int row = sp.row_tile * p.item_rows + r;
-  if (r >= p.item_rows || row >= q.n * p.c.d.gq) return;
-  join_row<BF16>(p, blockIdx.x, sp.inside, sp.last - (int)blockIdx.x + 1, r,
-                 p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, row));
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n_rows = min(p.item_rows, q.n * p.c.d.gq - sp.row_tile * p.item_rows);
+  const auto result = [&](int r) {
+    return p.c.out + row_offset(p, p.c.out_stride, q.row, sp.head, sp.row_tile * p.item_rows + r);
+  };
+  if (n > kFewParts) {
+    const int r = kJoinWarps * blockIdx.y + warp;
+    if (r < n_rows) join_row<BF16>(p, blockIdx.x, sp.inside, n, r, result(r));
+    return;
+  }
+  const int r = kJoinWarps * ((int)blockIdx.y + warp) + (lane >> 2);
+  if (r >= n_rows) return;
+  const auto slot = [&](int i) {
+    return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? sp.inside : 0)) * p.item_rows + r;
+  };
+  float2 ml[kFewParts];
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    ml[i] = i < n ? __ldcg(&p.part_ml[slot(i)]) : make_float2(0.0f, 0.0f);
+    if (ml[i].y > 0.0f) m = fmaxf(m, ml[i].x);
+  }
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    ml[i].x = ml[i].y > 0.0f ? exp2_fast(ml[i].x - m) : 0.0f;
+    l += ml[i].y * ml[i].x;
+  }
+  const float f = l > 0.0f ? 1.0f / l : 0.0f;
+  float4 out[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) out[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int i = 0; i < kFewParts; ++i) {
+    const float x = ml[i].x * f;
+    if (!(x > 0.0f)) continue;
+    const float4* src =
+        reinterpret_cast<const float4*>(p.part_o + slot(i) * kHeadDim) + (lane & 3);
+    float4 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __ldcg(src + 4 * j);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      out[j].x = fmaf(v[j].x, x, out[j].x);
+      out[j].y = fmaf(v[j].y, x, out[j].y);
+      out[j].z = fmaf(v[j].z, x, out[j].z);
+      out[j].w = fmaf(v[j].w, x, out[j].w);
+    }
+  }
+  uint2* dst = reinterpret_cast<uint2*>(result(r)) + (lane & 3);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    dst[4 * j] = make_uint2(pack16<BF16>(out[j].x, out[j].y), pack16<BF16>(out[j].z, out[j].w));
 }
 
 cudaError_t launch_join(const AttnParams& p, int ctas, int rows, cudaStream_t stream) {

@@ -15,6 +15,11 @@
 // s_v as 2^(x + log2 s_v) with the running maximum taken of that, and the sum of the
 // softmax as that of w / s_v (block8_rows.cu has the same).  bf16 queries and ring rows go
 // to fp16 times a power of two.
+//
+// What bounds it.  Two prompts of 8191 tokens (32 heads over 8): 1.04 ms, 1.06 PFLOP/s of a
+// cuBLAS product's 1.92.  Without the exponentials it takes 0.96, without the conversion of
+// codes 0.93: softmax and loading warps share the issue slots, and the chain of a step
+// (scores, softmax, weights, product) is not hidden whole by the other stream's.
 #include "block8_plan.cuh"
 #include "chunk_core.cuh"
 

@@ -18,7 +18,14 @@
 // fp32.  So neither scale rounds a code, and weights stay within fp16 whatever the scales.
 //
 // The tokens behind the last whole block are a block of 16-bit elements that one warp loads
-// from the ring; bf16 ones go to fp16 times a power of two, which acts as their scale.
+// from the ring; bf16 ones go to fp16 times a power of two.
+//
+// What bounds it.  HBM where there is enough to read: 32 ragged chats of 2k to 32k tokens,
+// query groups of eight, bf16: 188 us, 5.9 TB/s; without the arithmetic 171.  Drafts of one
+// to five tokens in 16 chats of 8k to 32k (one to three row groups): 122 us, 5.6 TB/s.  One
+// chat of 32k: 27 us, of which the cache's bytes take 9 at 7.4 TB/s; the others are the chain
+// of launch, plan (2.1), table (1.2), first block (1.3), merge (1.0), partial and ticket
+// (1.7), and the join (2.4 to 6).
 #include <cuda.h>
 
 #include <type_traits>

@@ -113,3 +113,71 @@ def test_infinities_and_bad_lists(kvq_lib):
         got = kvq.kvq_adjust_logits(z, history=flat(hist), history_starts=starts(hist),
                                     repetition=torch.tensor([rep], device="cuda"))
         assert torch.equal(got[:, 3:], z[:, 3:])
+
+
+@pytest.mark.parametrize("dtype,V,pad", [("bf16", 140001, 0), ("fp16", 140003, 5), ("fp32", 140002, 1)])
+def test_large_calls(kvq_lib, dtype, V, pad):
+    """More than 2^23 logits with short lists: streamed, then patched.  One row names more
+    tokens than are counted at a time, one none, one every token of a stretch."""
+    rows, rng = 61, np.random.default_rng(V)
+    z = torch.randn(rows, V + pad, device="cuda",
+                    generator=torch.Generator("cuda").manual_seed(V)).to(TYPES[dtype])[:, :V]
+    hist = [rng.integers(0, V, 100).tolist() for _ in range(rows)]
+    hist[3] = (rng.random(20000) ** 3 * V).astype(int).tolist()
+    hist[4] = []
+    hist[5] = list(range(100, 5300)) * 2 + [V - 1, 0]
+    prompt = [len(h) // 2 for h in hist]
+    bias = [[(int(i), float(np.float32(x))) for i, x in zip(rng.integers(0, V, 30),
+                                                            rng.normal(0, 5, 30))]
+            for _ in range(rows)]
+    bias[4] = [(7, 1.0), (7, 2.0), (V - 1, 3.0)]
+    allowed = rng.random((2, V)) < 0.5
+    which = [-1, 0, 1] + [i % 2 for i in range(rows - 3)]
+    args = dict(history=flat(hist), history_starts=starts(hist),
+                prompt_lengths=torch.tensor(prompt, dtype=torch.int32, device="cuda"),
+                repetition=torch.full((rows,), 1.25, device="cuda"),
+                frequency=torch.full((rows,), 0.5, device="cuda"),
+                presence=torch.full((rows,), 0.25, device="cuda"),
+                bias_ids=flat([[i for i, _ in x] for x in bias]),
+                bias_values=flat([[v for _, v in x] for x in bias], torch.float32),
+                bias_starts=starts(bias))
+    masked = dict(args, mask=packed(allowed),
+                  mask_rows=torch.tensor(which, dtype=torch.int32, device="cuda"))
+    out = torch.full((rows, V + 2), 7.0, device="cuda")
+    got = kvq.kvq_adjust_logits(z, out=out[:, 1:V + 1], **masked)
+    zz = z.double().cpu().numpy()
+    want = np.stack([block8.adjust(zz[b], hist[b], prompt[b], 1.25, 0.5, 0.25, bias[b],
+                                   allowed[which[b]] if which[b] >= 0 else None)
+                     for b in range(rows)])
+    check(got, want, np.abs(zz).max() * 1.6 + 20 + 0.5 * 400)
+    assert (out[:, 0] == 7.0).all() and (out[:, V + 1] == 7.0).all()
+    assert torch.equal(got, kvq.kvq_adjust_logits(z, **masked))
+    if dtype == "fp32":     # in its place: with a mask, and with nothing to stream
+        for kw in (masked, args):
+            want = kvq.kvq_adjust_logits(z, **kw)
+            same = z.clone()
+            kvq.kvq_adjust_logits(same, out=same, **kw)
+            assert torch.equal(same, want)
+
+
+def test_a_vocabulary_of_several_slices(kvq_lib):
+    rng = np.random.default_rng(8)
+    V = (1 << 23) + 12345
+    z = torch.randn(1, V, device="cuda", generator=torch.Generator("cuda").manual_seed(8))
+    hist = [rng.integers(0, V, 3000).tolist() + [0, V - 1]]
+    got = kvq.kvq_adjust_logits(z, history=flat(hist), history_starts=starts(hist),
+                                presence=torch.ones(1, device="cuda"))
+    want = z.clone()
+    ids = torch.tensor(sorted(set(hist[0])), device="cuda")
+    want[0, ids] -= 1.0
+    assert torch.equal(got, want)
+
+
+def test_small_in_place_without_a_mask(kvq_lib):
+    z = torch.randn(3, 500, device="cuda")
+    hist = [[1, 2, 2], [499], []]
+    args = dict(history=flat(hist), history_starts=starts(hist),
+                frequency=torch.ones(3, device="cuda"))
+    want = kvq.kvq_adjust_logits(z, **args)
+    kvq.kvq_adjust_logits(z, out=z, **args)
+    assert torch.equal(z, want)

@@ -341,3 +341,66 @@ def test_many_sequences_of_one_token(kvq_lib):
     out = kvq.kvq_block8_attn(cache, q, lengths)
     # one weight, 2^7 in fp16 exactly, over its own sum
     assert torch.equal(out, v.expand(2000, 2, 128)) and cache.flags() == 0
+
+
+def test_more_new_tokens_than_said(kvq_lib):
+    cfg = kvq.Block8Config(2, 2, 1, 96)
+    cache = kvq.Block8Cache(cfg, n_pages=1)
+    k, v, q = (torch.randn(6, h, 128).half().cuda() for h in (1, 1, 2))
+    args = dict(starts=ints([0, 2, 6]), max_new=3)
+    kvq.kvq_block8_append(cache, k, v, ints([2, 4]), **args)
+    assert cache.flags() == kvq.FLAG_BAD_BATCH and (cache.k_ring[1] == 0).all()
+    assert torch.equal(cache.v_ring[0, 0, :2], v[:2, 0])
+    cache.clear_flags()
+    out = torch.full((6, 2, 128), 7.0, dtype=torch.float16, device="cuda")
+    kvq.kvq_block8_attn(cache, q, ints([2, 4]), out=out, **args)
+    assert cache.flags() == kvq.FLAG_BAD_BATCH
+    assert (out[2:] == 7.0).all() and not (out[:2] == 7.0).any()
+
+
+@pytest.mark.parametrize("counts", [[1], [20], [90]])
+def test_the_largest_cache(kvq_lib, counts):
+    """2^31 - 32 tokens of which a window is seen."""
+    top, n = 2 ** 31 - 32, counts[0]
+    cfg = kvq.Block8Config(1, 4, 1, top)
+    cache = kvq.Block8Cache(cfg, n_pages=16)
+    for L in (top, top - 5):
+        first = (L - 256) // 32
+        blocks = list(range(first, L // 32))
+        cache.map_blocks(0, blocks, range(len(blocks)))
+        g = torch.Generator().manual_seed(16)
+        start = 32 * first
+        rows = torch.randn(2, L - start, 1, 128, generator=g).half()
+        k, v = rows.cuda()
+        kvq.kvq_block8_append(cache, k, v, ints([L]), starts=ints([0, L - start]))
+        q = torch.randn(n, 4, 128, generator=g).half().cuda()
+        out = kvq.kvq_block8_attn(cache, q, ints([L]), max_new=n, window=100)
+        seen = []
+        for i in (0, 1):
+            s = block8.Sequence()
+            s.append(np64(rows[i][:, 0]), L - start)
+            seen.append(s.seen())
+        check(cfg, out, q, [L - start], counts, [[seen]], 100)
+        assert cache.flags() == 0
+
+
+def test_short_and_long_sequences_of_every_size(kvq_lib):
+    """One call with sequences of each row group count and longer ones; twice the same bits."""
+    counts = [1, 2, 3, 5, 6, 8, 9, 33, 70, 4, 7, 128]
+    lengths = [64 + 37 * i for i in range(len(counts))]
+    lengths[-1] = 500
+    cfg, cache, seen = filled("fp16", len(counts), 1, lengths, 512, seed=17)
+    q = torch.randn(sum(counts), cfg.n_q_heads, 128,
+                    generator=torch.Generator().manual_seed(18)).half().cuda()
+    starts = ints(np.concatenate([[0], np.cumsum(counts)]))
+    outs = [kvq.kvq_block8_attn(cache, q, ints(lengths), starts=starts, max_new=128)
+            for _ in range(3)]
+    check(cfg, outs[0], q, lengths, counts, seen)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    short = [b for b, n in enumerate(counts) if n <= 8]
+    few = [counts[b] if b in short else 0 for b in range(len(counts))]
+    rows = torch.cat([q[sum(counts[:b]):sum(counts[:b + 1])] for b in short])
+    starts = ints(np.concatenate([[0], np.cumsum(few)]))
+    out = kvq.kvq_block8_attn(cache, rows, ints(lengths), starts=starts, max_new=8)
+    check(cfg, out, rows, lengths, few, seen)
+    assert cache.flags() == 0
