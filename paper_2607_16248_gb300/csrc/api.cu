@@ -823,7 +823,7 @@ kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cach
   trace("kvq_block8_append batch %d tokens %d heads %d/%d rot %d%s %s", cfg->batch, n,
         cfg->n_q_heads, cfg->n_kv_heads, p->rot_dim, p->paired ? " paired" : "",
         call.d.bf16 ? "bf16" : "fp16");
-  return cuda_status(block8::launch_append(call, static_cast<cudaStream_t>(stream)),
+  return cuda_status(block8::launch_append(call, sm_count(), static_cast<cudaStream_t>(stream)),
                      "kvq_block8_append launch");
 }
 

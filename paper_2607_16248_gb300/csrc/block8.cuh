@@ -34,7 +34,7 @@ struct AttnCall {
   long long q_stride[2], out_stride[2];
 };
 
-cudaError_t launch_append(const AppendCall& call, cudaStream_t stream);
+cudaError_t launch_append(const AppendCall& call, int sm_count, cudaStream_t stream);
 size_t attn_workspace_bytes(const Dims8& d, int max_new, int sm_count);
 // The most units of work that a call's kernels can count.
 long long attn_most_units(const Dims8& d, int max_new);

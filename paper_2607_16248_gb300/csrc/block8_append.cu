@@ -27,12 +27,15 @@
 
 #include <cuda_fp8.h>
 
+#include <algorithm>
+
 namespace kvq {
 namespace block8 {
 
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kPlaces = 8;      // CTAs an SM
 constexpr int kQueryHeads = 8;  // heads of a query task
 
 __device__ __forceinline__ uint2 ld8(const uint16_t* p) {
@@ -335,10 +338,11 @@ struct Share {
   int b, left;
 };
 
-// Keys or values of unit `unit` (the batch's blocks with new tokens, in order).  The warps
-// look through 32 sequences each.
+// Parts `part` .. end - 1 (2 h: keys of kv-head h, 2 h + 1: its values) of unit `unit` (the
+// batch's blocks with new tokens, in order).  The warps look through 32 sequences each.
 template <bool BF16, bool PAIRED>
-__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part, Share& sh) {
+__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part, int end,
+                                        Share& sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll 1
   for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kWarps) {
@@ -378,15 +382,20 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
     int heir = done - ((done - first) & 1);
     if (old % kGroup == 0 || heir <= first || heir * kGroup >= q.L) heir = -1;
     if (blk == heir) return;
+    const int seq = sh.b;
 #pragma unroll 1
-    for (;;) {
-      if (part & 1) Task<BF16, false, PAIRED>(call, q, sh.b, part >> 1).block(blk, sh.m);
-      else Task<BF16, true, PAIRED>(call, q, sh.b, part >> 1).block(blk, sh.m);
-      if (blk != first || heir < 0) return;
-      __syncthreads();  // sh.m is written again
-      blk = heir;
-      heir = -1;
+    for (; part < end; ++part) {
+#pragma unroll 1
+      for (int at = blk;;) {
+        if (part & 1) Task<BF16, false, PAIRED>(call, q, seq, part >> 1).block(at, sh.m);
+        else Task<BF16, true, PAIRED>(call, q, seq, part >> 1).block(at, sh.m);
+        if (at != first || heir < 0) break;
+        __syncthreads();  // sh.m is written again
+        at = heir;
+      }
+      if (part + 1 < end) __syncthreads();
     }
+    return;
   }
 }
 
@@ -447,8 +456,8 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
 // CTAs of blocks, then of queries; the last CTA looks over the batch's sizes for the flag
 // word.
 template <bool BF16, bool PAIRED>
-__global__ void __launch_bounds__(32 * kWarps, 8)
-append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) {
+__global__ void __launch_bounds__(32 * kWarps, kPlaces)
+append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int parts, int groups) {
   __shared__ Share share;
   if (blockIdx.x == gridDim.x - 1) {
     for (int b = threadIdx.x; b < call.d.batch; b += 32 * kWarps) {
@@ -456,8 +465,9 @@ append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) 
       if (s.bad) set_flag(call.cache, s.bad);
     }
   } else if ((int)blockIdx.x < kv_ctas) {
-    const int parts = 2 * call.d.hkv, unit = (int)blockIdx.x / parts;
-    kv_task<BF16, PAIRED>(call, unit, (int)blockIdx.x - unit * parts, share);
+    const int all = 2 * call.d.hkv, shares = (all + parts - 1) / parts;
+    const int unit = (int)blockIdx.x / shares, part = ((int)blockIdx.x - unit * shares) * parts;
+    kv_task<BF16, PAIRED>(call, unit, part, min(part + parts, all), share);
   } else {
     const int task = ((int)blockIdx.x - kv_ctas) * kWarps + ((int)threadIdx.x >> 5);
     const int row = task / groups;
@@ -467,11 +477,19 @@ append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int groups) 
 
 }  // namespace
 
-cudaError_t launch_append(const AppendCall& call, cudaStream_t stream) {
-  // A sequence of n new tokens touches at most (n - 1) / 32 + 2 blocks.
+cudaError_t launch_append(const AppendCall& call, int sm_count, cudaStream_t stream) {
+  // A sequence of n new tokens touches at most (n + 30) / 32 + 1 blocks.
   const long long tokens = call.batch.n_tokens;
   const long long seqs = tokens < call.d.batch ? tokens : call.d.batch;
-  const int kv_ctas = (int)((tokens / kGroup + 2 * seqs) * 2 * call.d.hkv);
+  const long long units = std::min(tokens / kGroup + 2 * seqs,
+                                   seqs * ((call.batch.max_new + 30LL) / kGroup + 1));
+  // One part a CTA, or as many as leave four CTAs for each place on the GPU: a large batch's
+  // CTAs look for their sequences longer than they take for a part (8192 single tokens of 8
+  // kv-heads: 0.51 ms, 4.8 with a part each; 1024: 37 us and 103).
+  const int all = 2 * call.d.hkv;
+  const int parts =
+      (int)std::max(1LL, std::min<long long>(all, units * all / (4LL * kPlaces * sm_count)));
+  const int kv_ctas = (int)(units * ((all + parts - 1) / parts));
   const int groups = (call.d.hq + kQueryHeads - 1) / kQueryHeads;
   const int q_ctas = call.p.q ? (int)((tokens * groups + kWarps - 1) / kWarps) : 0;
   const int grid = kv_ctas + q_ctas + 1;
@@ -479,7 +497,7 @@ cudaError_t launch_append(const AppendCall& call, cudaStream_t stream) {
                           ? (call.p.paired ? append_kernel<true, true> : append_kernel<true, false>)
                           : (call.p.paired ? append_kernel<false, true>
                                            : append_kernel<false, false>);
-  kernel<<<grid, 32 * kWarps, 0, stream>>>(call, kv_ctas, groups);
+  kernel<<<grid, 32 * kWarps, 0, stream>>>(call, kv_ctas, parts, groups);
   return cudaGetLastError();
 }
 

@@ -226,3 +226,14 @@ def test_attention_long(kvq_lib):
     w.append([8000, 4001], n_positions=8224)
     w.check_attention(w.append([1, 1], n_positions=8224), max_new=1)
     w.check_attention(w.append([150, 7], n_positions=8224), max_new=150)
+
+
+def test_append_large_batch(kvq_lib):
+    """So many blocks that a CTA takes several heads, some of them begun before."""
+    rng = np.random.default_rng(21)
+    w = World(1500, 4, 4, 128, "fp16", seed=21)
+    for _ in range(2):
+        counts = np.where(rng.random(1500) < 0.1, 0, rng.integers(1, 41, 1500)).tolist()
+        w.append(counts, rot=32)
+    w.check_state()
+    assert w.cache.flags() == 0
