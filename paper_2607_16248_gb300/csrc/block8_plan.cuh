@@ -84,11 +84,26 @@ __device__ __forceinline__ int row_tiles(const AttnParams& p, const Seq& q) {
                  : 0;
 }
 
-// CTA c's share of the units: [begin(c), begin(c + 1)), equal to within one.
+// CTA c's share of the units: [begin(c), begin(c + 1)).
+// Over all items: equal to within one unit.  Over items of one size (`even`), each divided
+// among as many CTAs (`parts`): a share that crosses from an item to the next costs its CTA
+// the next one's queries, merge and partial, 4 us of one chat's 27.
 struct Shares {
-  int q, r, n;  // units = n q + r over n CTAs
-  __device__ __forceinline__ int begin(int c) const { return c * q + min(c, r); }
+  int q, r, n;      // units = n q + r over n CTAs
+  int even, parts;  // an item's units, 0: shares over all items
+  __device__ __forceinline__ int begin(int c) const {
+    if (even) {
+      const int i = (int)((uint32_t)c / (uint32_t)parts);
+      return i * even + (int)((uint32_t)((c - i * parts) * even) / (uint32_t)parts);
+    }
+    return c * q + min(c, r);
+  }
   __device__ __forceinline__ int owner(int u) const {
+    if (even) {
+      const int i = (int)((uint32_t)u / (uint32_t)even);
+      return i * parts + (int)(((uint32_t)(u - i * even + 1) * (uint32_t)parts - 1u) /
+                               (uint32_t)even);
+    }
     const int wide = (q + 1) * r;  // units of the CTAs that have q + 1
     return u < wide ? (int)((uint32_t)u / (uint32_t)(q + 1))
                     : r + (int)((uint32_t)(u - wide) / (uint32_t)q);
@@ -139,6 +154,12 @@ __device__ __forceinline__ bool plan_share(const AttnParams& p, int* scan, Start
     if (lane >= o) inc += y;
   }
   if (lane == 31) scan[warp] = inc;
+  // few sequences' items of one size: that size (in a place that no warp's sum has)
+  if (TOK != 7 && warp == 0) {
+    const int size = mine / p.c.d.hkv, most = __reduce_max_sync(0xffffffffu, size);
+    const bool one = __all_sync(0xffffffffu, size == 0 || size == most);
+    if (lane == 0) scan[31] = one && p.c.d.batch <= 32 && most < 1 << 20 ? most : 0;
+  }
   __syncthreads();
   int warps = lane < threads / 32 ? scan[lane] : 0;
 #pragma unroll
@@ -151,6 +172,18 @@ __device__ __forceinline__ bool plan_share(const AttnParams& p, int* scan, Start
   if (warp == 0) before = 0;
   before += inc - mine;
   shares.n = min((int)gridDim.x, (int)(((uint32_t)total + least - 1) / (uint32_t)least));
+  shares.even = 0;
+  if (TOK != 7 && scan[31]) {
+    // as many CTAs an item as there are, or as have `least` units; unless a tenth of the GPU
+    // would be left
+    const int size = scan[31], items = (int)((uint32_t)total / (uint32_t)size);
+    const int fill = (int)gridDim.x / items, need = max(size / least, 1);
+    if (fill >= 1 && (need <= fill || fill * items * 10 >= (int)gridDim.x * 9)) {
+      shares.even = size;
+      shares.parts = min(fill, need);
+      shares.n = shares.parts * items;
+    }
+  }
   if ((int)blockIdx.x >= shares.n) return false;
   shares.q = (int)((uint32_t)total / (uint32_t)shares.n);
   shares.r = total - shares.q * shares.n;

@@ -404,3 +404,19 @@ def test_short_and_long_sequences_of_every_size(kvq_lib):
     out = kvq.kvq_block8_attn(cache, rows, ints(lengths), starts=starts, max_new=8)
     check(cfg, out, rows, lengths, few, seen)
     assert cache.flags() == 0
+
+
+@pytest.mark.parametrize("batch,hkv,L,n", [(1, 1, 2100, 1), (1, 2, 1030, 3), (1, 8, 333, 1),
+                                           (3, 2, 512, 2), (4, 1, 95, 1), (2, 3, 700, 8)])
+def test_items_of_one_size(kvq_lib, batch, hkv, L, n):
+    """Sequences of equal length, each item divided among as many CTAs."""
+    cfg, cache, seen = filled("fp16", batch, hkv, [L] * batch, (L + 31) // 32 * 32, seed=L)
+    q = torch.randn(batch * n, cfg.n_q_heads, 128,
+                    generator=torch.Generator().manual_seed(L)).half().cuda()
+    ws = kvq.block8_workspace(cfg, n)
+    outs = [kvq.kvq_block8_attn(cache, q, ints([L] * batch), workspace=ws) for _ in range(3)]
+    check(cfg, outs[0], q, [L] * batch, [n] * batch, seen)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    out = kvq.kvq_block8_attn(cache, q, ints([L] * batch), workspace=ws, window=65, sinks=3)
+    check(cfg, out, q, [L] * batch, [n] * batch, seen, 65, 3)
+    assert (ws[:4 * 152] == 0).all() and cache.flags() == 0
