@@ -846,6 +846,7 @@ kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache*
   if ((s = check_block8_batch(*cfg, batch)) != KVQ_OK) return s;
   if (!p) return fail(KVQ_ERR_ARG, "params is NULL");
   if (!q || !out) return fail(KVQ_ERR_ARG, "q / out is NULL");
+  if (q == out) return fail(KVQ_ERR_ARG, "q and out must not overlap");
   const int n = batch->n_tokens;
   if ((s = check_block8_rows("q", q, p->q_stride, n, cfg->n_q_heads, false)) != KVQ_OK ||
       (s = check_block8_rows("out", out, p->out_stride, n, cfg->n_q_heads, true)) != KVQ_OK)

@@ -471,7 +471,8 @@ append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int parts, i
   } else {
     const int task = ((int)blockIdx.x - kv_ctas) * kWarps + ((int)threadIdx.x >> 5);
     const int row = task / groups;
-    if (row < call.batch.n_tokens) query_task<BF16, PAIRED>(call, row, (task - row * groups) * kQueryHeads);
+    if (row < call.batch.n_tokens)
+      query_task<BF16, PAIRED>(call, row, (task - row * groups) * kQueryHeads);
   }
 }
 

@@ -730,7 +730,8 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
             const float f = ll[n][j] > 0.0f ? 1.0f / ll[n][j] : 0.0f;
             uint32_t x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = pack16<BF16>(st.o[n][i][j] * f, st.o[n][i][j + 2] * f);
+            for (int i = 0; i < 8; ++i)
+              x[i] = pack16<BF16>(st.o[n][i][j] * f, st.o[n][i][j + 2] * f);
             uint4* dst = reinterpret_cast<uint4*>(
                 p.c.out + row_offset(p, p.c.out_stride, w.q.row, w.head, r) + 16 * gid);
             dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
@@ -782,8 +783,8 @@ cudaError_t make_map(CUtensorMap* map, const void* base, long long rows) {
   if (!encode) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult r;
-    const cudaError_t e =
-        cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &r);
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
+                                                           cudaEnableDefault, &r);
     if (e != cudaSuccess) return e;
     if (r != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
     encode = reinterpret_cast<Encode>(fn);

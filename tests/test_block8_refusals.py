@@ -72,7 +72,8 @@ def _append(L, cfg=None, cache=None, lengths=FAKE, starts=FAKE, n=4, max_new=4, 
 
 def test_append_refusals(L):
     for status, kw in (
-            (ARG, dict(lengths=None)), (ALIGN, dict(lengths=FAKE + 2)), (ALIGN, dict(starts=FAKE + 1)),
+            (ARG, dict(lengths=None)), (ALIGN, dict(lengths=FAKE + 2)),
+            (ALIGN, dict(starts=FAKE + 1)),
             (SHAPE, dict(n=0)), (SHAPE, dict(n=2 ** 26)), (ARG, dict(max_new=0)),
             (ARG, dict(max_new=1025)), (SHAPE, dict(starts=None, n=5)), (ARG, dict(k=None)),
             (ARG, dict(v=None)), (ARG, dict(q=None)), (ARG, dict(q_out=None)),
@@ -90,7 +91,7 @@ def test_append_refusals(L):
         assert kvq.last_error()
 
 
-def _attn(L, q=FAKE, out=FAKE, window=0, sinks=0, scale=0.0, qs=(1024, 128), os=(1024, 128),
+def _attn(L, q=FAKE, out=FAKE + 4096, window=0, sinks=0, scale=0.0, qs=(1024, 128), os=(1024, 128),
           ws=FAKE, max_new=4, ws_bytes=None, cfg=None, cache=None, n=4):
     c = cfg or _cfg()
     batch = kvq._Block8Batch(FAKE, FAKE, n, max_new)
@@ -104,9 +105,11 @@ def _attn(L, q=FAKE, out=FAKE, window=0, sinks=0, scale=0.0, qs=(1024, 128), os=
 def test_attn_refusals(L):
     assert _attn(L) == CAPACITY and "workspace" in kvq.last_error()    # all else is in order
     for status, kw in (
-            (ARG, dict(q=None)), (ARG, dict(out=None)), (ALIGN, dict(q=FAKE + 2)),
-            (ALIGN, dict(out=FAKE + 8)), (ARG, dict(window=-1)), (ARG, dict(sinks=-1)),
-            (ARG, dict(scale=-1.0)), (ARG, dict(scale=float("nan"))), (ARG, dict(scale=float("inf"))),
+            (ARG, dict(q=None)), (ARG, dict(out=None)), (ARG, dict(out=FAKE)),
+            (ALIGN, dict(q=FAKE + 2)), (ALIGN, dict(out=FAKE + 8)), (ARG, dict(window=-1)),
+            (ARG, dict(sinks=-1)),
+            (ARG, dict(scale=-1.0)), (ARG, dict(scale=float("nan"))),
+            (ARG, dict(scale=float("inf"))),
             (ALIGN, dict(qs=(1020, 128))), (ARG, dict(qs=(-8, 128))), (ARG, dict(os=(64, 128))),
             (ARG, dict(os=(1024, 0))), (ARG, dict(ws=None)), (ALIGN, dict(ws=FAKE + 4)),
             (ARG, dict(max_new=2000)), (ARG, dict(cache=_cache(scales=None))),
@@ -172,7 +175,8 @@ def test_oracle_by_hand():
     assert block8.to_type(1.0 + 2.0 ** -11, "fp16") == 1.0        # a tie goes to the even one
     assert block8.to_type(1.0 + 3 * 2.0 ** -11, "fp16") == 1.0 + 2.0 ** -9
     assert block8.to_type(465.0, "e4m3") == 448.0 and block8.to_type(17.0, "e4m3") == 16.0
-    assert block8.to_type(2.0 ** -10, "e4m3") == 0.0 and block8.to_type(-2.0 ** -9, "e4m3") == -2.0 ** -9
+    assert block8.to_type(2.0 ** -10, "e4m3") == 0.0
+    assert block8.to_type(-2.0 ** -9, "e4m3") == -2.0 ** -9
     # torch's conversion goes by way of fp32, as a code's definition does
     grid = np.array([block8.to_type(block8.to_type(x, "fp32"), "e4m3")
                      for x in np.linspace(-460, 460, 3001)])

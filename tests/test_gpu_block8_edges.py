@@ -295,7 +295,8 @@ def test_bad_batches_are_left_alone(kvq_lib, starts, lengths, flag):
 
 def test_queries_ahead_of_the_first_token(kvq_lib):
     cfg, cache, seen = filled("fp16", 2, 1, [3, 0], 64, seed=13)
-    q = torch.randn(80, cfg.n_q_heads, 128, generator=torch.Generator().manual_seed(5)).half().cuda()
+    q = torch.randn(80, cfg.n_q_heads, 128,
+                    generator=torch.Generator().manual_seed(5)).half().cuda()
     for starts, max_new in (([0, 5, 10], 8), ([0, 40, 80], 40)):
         n = [starts[1], starts[2] - starts[1]]
         out = kvq.kvq_block8_attn(cache, q[:starts[2]], ints([3, 0]), starts=ints(starts),
@@ -420,3 +421,17 @@ def test_items_of_one_size(kvq_lib, batch, hkv, L, n):
     out = kvq.kvq_block8_attn(cache, q, ints([L] * batch), workspace=ws, window=65, sinks=3)
     check(cfg, out, q, [L] * batch, [n] * batch, seen, 65, 3)
     assert (ws[:4 * 152] == 0).all() and cache.flags() == 0
+
+
+def test_positions_outside_the_tables(kvq_lib):
+    """They take the nearest row, and the flag says so."""
+    w = World(1, 4, 2, 128, "fp16", seed=22)
+    w.append([60], n_positions=64)
+    assert w.cache.flags() == 0
+    w.append([20], n_positions=64)
+    w.check_state()
+    assert w.cache.flags() == kvq.FLAG_BAD_BATCH
+    w.cache.clear_flags()
+    w.append([3], positions=[-1, 5, 2 ** 31 - 1], n_positions=64)
+    w.check_state()
+    assert w.cache.flags() == kvq.FLAG_BAD_BATCH

@@ -92,7 +92,8 @@ class Loop:
             got = z[b].double().cpu().numpy()
             assert np.array_equal(np.isinf(got), np.isinf(want))
             ok = np.isfinite(want)
-            assert (np.abs(got[ok] - want[ok]) <= 6 * 2.0 ** -24 * (np.abs(want[ok]).max() + 1)).all()
+            bound = 6 * 2.0 ** -24 * (np.abs(want[ok]).max() + 1)
+            assert (np.abs(got[ok] - want[ok]) <= bound).all()
         u = torch.rand(3, V, generator=self.g).cuda()
         token = kvq.kvq_sample(z, u, torch.full((3,), 0.9, device="cuda"))["token"].tolist()
         assert token[0] % 2 == 0 and token[2] % 2 == 0
