@@ -710,7 +710,8 @@ def _block8_batch(cache, n_tokens, lengths, starts, max_new):
         max_new = n_tokens // batch
     elif max_new is None:
         max_new = min(n_tokens, cache.cfg.max_len)
-    _in_32_bits("n_tokens and max_new", n_tokens, max_new)
+    if not (0 <= n_tokens <= 2147483647 and 0 <= max_new <= 2147483647):
+        raise ValueError(f"n_tokens and max_new must be in [0, 2^31) (got {n_tokens}, {max_new})")
     return _BATCH.pack(_list(lengths, batch, torch.int32, "lengths", cache.dev),
                        _list(starts, batch + 1, torch.int32, "starts", cache.dev), n_tokens,
                        max_new), max_new

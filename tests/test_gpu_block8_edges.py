@@ -435,3 +435,25 @@ def test_positions_outside_the_tables(kvq_lib):
     w.append([3], positions=[-1, 5, 2 ** 31 - 1], n_positions=64)
     w.check_state()
     assert w.cache.flags() == kvq.FLAG_BAD_BATCH
+
+
+def test_two_calls_at_once(kvq_lib):
+    """Two layers on two streams, workspaces of their own: single tokens beside a chunk."""
+    made = [filled("fp16", 2, 2, [900, 700], 928, seed=30 + i) for i in range(2)]
+    g = torch.Generator().manual_seed(31)
+    counts = ([1, 1], [120, 90])
+    args, want = [], []
+    for (cfg, cache, _), n in zip(made, counts):
+        q = torch.randn(sum(n), cfg.n_q_heads, 128, generator=g).half().cuda()
+        kw = dict(starts=ints([0, n[0], sum(n)]), max_new=max(n),
+                  workspace=kvq.block8_workspace(cfg, max(n)))
+        args.append((cache, q, ints([900, 700]), kw))
+        want.append(kvq.kvq_block8_attn(*args[-1][:3], **kw))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        got = [kvq.kvq_block8_attn(*a[:3], stream=s, **a[3]) for a, s in zip(args, streams)]
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for (cfg, _, seen), n, out, a in zip(made, counts, want, args):
+        check(cfg, out, a[1], [900, 700], n, seen)
