@@ -13,8 +13,9 @@
 // columns of the results), so a lane's 16 codes become 32 neighbouring bytes.  A block's
 // scales reach the softmax instead: scores times s_k in the exponent's factor, weights times
 // s_v as 2^(x + log2 s_v) with the running maximum taken of that, and the sum of the
-// softmax as that of w / s_v (block8_rows.cu has the same).  bf16 queries and ring rows go
-// to fp16 times a power of two.
+// softmax as that of w / s_v (block8_rows.cu has the same).  bf16 queries go to fp16 times a
+// power of two, and so do the rows of the open block, keys and values of both types, each
+// times its own: what one row holds, seen or not, does not touch the others.
 //
 // What bounds it.  Two prompts of 8191 tokens (32 heads over 8): 1.04 ms, 1.06 PFLOP/s of a
 // cuBLAS product's 1.92.  Without the exponentials it takes 0.96, without the conversion of
@@ -69,9 +70,11 @@ using chunk::tc_commit;
 using chunk::tile_at;
 using chunk::tile_desc;
 using chunk::tm_load32;
+using chunk::tm_load8;
 using chunk::tm_load_wait;
 using chunk::tm_store16;
 using chunk::tm_store32;
+using chunk::tm_store8;
 using chunk::tm_store_wait;
 using chunk::unpair;
 using chunk::warp_arrive;
@@ -98,7 +101,8 @@ struct Smem {
   Start start;
   uint32_t tmem;
   int abort;
-  float4 scale[kScaleTiles][4];        // a block's s_k, log2 s_v, 1 / s_v
+  float4 scale[kScaleTiles][4];        // a block's s_k, log2 s_v, 1 / s_v; 1 for the open one
+  float2 open[kScaleTiles][kGroup];    // its tokens' s_k, log2 s_v
   float qf[2][2][kTile];               // [item][stream]: 1 / the factor of a row's queries
   float m[kTile], l[kTile];            // stream 1's statistics of a shared row tile
 };
@@ -200,36 +204,40 @@ __device__ __forceinline__ void restore_codes(const Codes& c, int k, unsigned ch
   st16(tile, tile_at(half, row, chunk + 1 - half), half ? lo : hi);
 }
 
-// The factor that the elements of the block that is not whole get (`valid` rows).
-template <bool BF16>
-__device__ __forceinline__ float ring_factor(const uint16_t* rows, int valid) {
-  if constexpr (!BF16) return 1.0f;
-  const int lane = threadIdx.x & 31;
-  uint32_t x = 0u;
-#pragma unroll 8
-  for (int r = lane >> 4; r < kGroup; r += 2)
-    if (r < valid)
-      x = max(x, largest(*(reinterpret_cast<const uint4*>(rows + r * kHeadDim) + (lane & 15))));
-  return lift_of(__reduce_max_sync(0xffffffffu, x));
-}
-// Its rows, the others zero.
-template <bool BF16>
-__device__ __forceinline__ void ring_block(const uint16_t* rows, int valid, float f,
-                                           unsigned char* tile, int j) {
+// The open block's rows (`valid` of them, the others zero) by a warp, four at a time, 16
+// lanes a row.  The keys' warp also finds the values' factors and leaves both in `open`.
+template <bool BF16, bool KEY>
+__device__ __forceinline__ void open_block(const uint16_t* rows, const uint16_t* values, int valid,
+                                           unsigned char* tile, int j, float2* open) {
   const int lane = threadIdx.x & 31, m = lane & 15;
-#pragma unroll 1
-  for (int h = 0; h < 32; h += 8) {
-    uint4 v[4];
+  const auto load = [&](const uint16_t* base, int r) {
+    return r < valid ? *(reinterpret_cast<const uint4*>(base + r * kHeadDim) + m)
+                     : make_uint4(0u, 0u, 0u, 0u);
+  };
+  const auto row_lift = [&](const uint4& v, bool key) {
+    uint32_t x = largest(v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int o = 8; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return key ? key_lift<BF16>(x) : value_lift<BF16>(x);
+  };
+#pragma unroll 1
+  for (int h = 0; h < 32; h += 4) {
+    uint4 v[2], u[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       const int r = h + 2 * i + (lane >> 4);
-      v[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (r < valid) v[i] = *(reinterpret_cast<const uint4*>(rows + r * kHeadDim) + m);
+      v[i] = load(rows, r);
+      if (KEY) u[i] = load(values, r);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      st16(tile, tile_at(m >> 3, 32 * j + h + 2 * i + (lane >> 4), m & 7),
-           to_half8<BF16>(v[i], f));
+    for (int i = 0; i < 2; ++i) {
+      const int r = h + 2 * i + (lane >> 4), e = row_lift(v[i], KEY);
+      st16(tile, tile_at(m >> 3, 32 * j + r, m & 7), lifted8<BF16>(v[i], pow2(e)));
+      if (KEY) {
+        const int ev = row_lift(u[i], false);
+        if (m == 0) open[r] = make_float2(pow2(-e), (float)-ev);
+      }
+    }
   }
 }
 __device__ __forceinline__ void zero_block(unsigned char* tile, int j) {
@@ -296,8 +304,7 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
       unsigned char* tile = tiles[buf];
       if (i >= w.i0) {
         if (!warp_wait(s, &empty[buf], ((n >> 1) & 1) ^ 1)) return;
-        float2 sc = scale;
-        bool none = false;  // the block counts for nothing
+        bool none = false, open = false;  // the block counts for nothing; is the open one
         if (at0 < 0) {
           const int ta = token(i);
           none = !(ta >= whole && ta < w.q.L && seen(ta));
@@ -307,18 +314,21 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
             const long long at =
                 (((long long)w.b * p.c.d.hkv + w.head) * kRing + (ta & (kRing - 1))) * kHeadDim;
             const int valid = w.q.L - ta;
-            const float fv = ring_factor<BF16>(p.c.cache.v_ring + at, valid);
-            const float fk = key ? ring_factor<BF16>(p.c.cache.k_ring + at, valid) : 1.0f;
-            sc = make_float2(1.0f / fk, 1.0f / fv);
-            ring_block<BF16>((key ? p.c.cache.k_ring : p.c.cache.v_ring) + at, valid,
-                             key ? fk : fv, tile, j);
+            const uint16_t* v = p.c.cache.v_ring + at;
+            if (key)
+              open_block<BF16, true>(p.c.cache.k_ring + at, v, valid, tile, j,
+                                     s.open[n & (kScaleTiles - 1)]);
+            else
+              open_block<BF16, false>(v, v, valid, tile, j, nullptr);
+            open = true;
           }
         }
         // (the scores' product waits for the keys' warps alone: they write all of it)
         if (key && lane == 0)
           s.scale[n & (kScaleTiles - 1)][j] =
-              none ? make_float4(1.0f, -INFINITY, 1.0f, 0.0f)
-                   : make_float4(sc.x, log2_fast(sc.y), 1.0f / sc.y, 0.0f);
+              none   ? make_float4(1.0f, -INFINITY, 1.0f, 0.0f)
+              : open ? make_float4(1.0f, 0.0f, 0.0f, 1.0f)
+                     : make_float4(scale.x, log2_fast(scale.y), 1.0f / scale.y, 0.0f);
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -460,6 +470,45 @@ __device__ __forceinline__ void mask_row(uint32_t ts, int hi, int lo, int sink) 
   tm_store_wait();
 }
 
+// The scores of the open block, 32 columns: the best of a thread's row by x + log2 s_v, and the
+// others against it, x - x_best + log2 s_v - log2 s_best (at most 0), in their place.  Returns
+// the best's x + log2 s_v and the sum of 2^(the others) / s_v.  Few steps come here, so the
+// numbers stay in tensor memory, eight at a time.
+__device__ __forceinline__ float2 open_scores(uint32_t ts, const float2* open, float sl) {
+  float best = -INFINITY, best_lv = 0.0f, sum = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < kGroup; c += 8) {
+    uint32_t r[8];
+    tm_load8(ts + c, r);
+    tm_load_wait();
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const float2 s = open[c + n];
+      const float x = __uint_as_float(r[n]) * fmaxf(s.x * sl, kLeastFactor);
+      if ((x - best) + (s.y - best_lv) > 0.0f) best = x, best_lv = s.y;
+      r[n] = __float_as_uint(x);
+    }
+    tm_store8(ts + c, r);
+  }
+  tm_store_wait();
+  if (best == -INFINITY) best = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < kGroup; c += 8) {
+    uint32_t r[8];
+    tm_load8(ts + c, r);
+    tm_load_wait();
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const float lv = open[c + n].y, y = (__uint_as_float(r[n]) - best) + (lv - best_lv);
+      sum += exp2_fast(y - lv);
+      r[n] = __float_as_uint(y);
+    }
+    tm_store8(ts + c, r);
+  }
+  tm_store_wait();
+  return make_float2(best + best_lv, sum);
+}
+
 template <bool BF16>
 __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u0, int u1,
                                              const Shares& shares, int two) {
@@ -515,13 +564,23 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
         // the last token behind the window, -1 if there is none (positions and windows
         // each reach 2^31)
         const int behind = p.c.window ? max(max(pos, 0) - p.c.window, -1) : -1;
-        if (!whole) mask_row(sb, (valid ? pos : -1) - t0, behind - t0, p.c.sinks - t0);
-        const float4* sc = &s.scale[(nt + (st >> two)) & (kScaleTiles - 1)][2 * half];
+        const int slot = (nt + (st >> two)) & (kScaleTiles - 1);
+        const float4* sc = &s.scale[slot][2 * half];
+        // the block that is open, -1 for none (it ends behind every row's position: no step
+        // with it is whole); what its scores give waits in the warp's place for results
+        const int open = whole ? -1 : sc[0].w != 0.0f ? 0 : sc[1].w != 0.0f ? 1 : -1;
+        float2* kept = reinterpret_cast<float2*>(s.stage[warp]) + (threadIdx.x & 31);
+        if (!whole) {
+          mask_row(sb, (valid ? pos : -1) - t0, behind - t0, p.c.sinks - t0);
+          if (open >= 0) *kept = open_scores(sb + 32 * open, s.open[slot], sl);
+        }
         uint32_t r[2][32];
         tm_load32(sb, r[0]);
         tm_load32(sb + 32, r[1]);
-        const float2 f = make_float2(sc[0].x * sl, sc[1].x * sl);
-        const float2 lv = make_float2(sc[0].y, sc[1].y);
+        float2 f = make_float2(sc[0].x * sl, sc[1].x * sl);
+        float2 lv = make_float2(sc[0].y, sc[1].y);
+        if (open == 0) f.x = 1.0f, lv.x = kept->x;
+        if (open == 1) f.y = 1.0f, lv.y = kept->x;
         tm_load_wait();
         float mc[2];
 #pragma unroll
@@ -555,6 +614,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
           }
         }
         const float base = row.m == -INFINITY ? 0.0f : kLiftLog2 - row.m;
+        if (open >= 0) row.l = fmaf(kept->y, exp2_fast(base + kept->x), row.l);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const float fc = c ? f.y : f.x, oc = base + (c ? lv.y : lv.x);

@@ -292,6 +292,42 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   }
 }
 
+// Elements of the open block go to fp16 times 2^lift, the power that takes their row's largest
+// magnitude to [2^14, 2^15): a row's elements are exact down to 2^-24 of that, and two rows
+// share nothing.  Keys: of bits from 2^-100 on.  Values: from 2^-80 on, so that sums of
+// 2^lift stay within fp32; rows of nothing as if they were the smallest, so that their
+// weights count beside any others' (a weight is held with its value's scale in it).
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+template <bool BF16>
+__device__ __forceinline__ int lift_log2(uint32_t bits, int least) {
+  const float m = BF16 ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half(bits));
+  const int e = max((int)(__float_as_uint(m) >> 23) - 127, least);
+  return BF16 ? 14 - e : max(14 - e, 0);  // (fp16's smallest would not stand 2^-1)
+}
+template <bool BF16>
+__device__ __forceinline__ int key_lift(uint32_t bits) {
+  return bits ? lift_log2<BF16>(bits, -100) : 0;
+}
+template <bool BF16>
+__device__ __forceinline__ int value_lift(uint32_t bits) {
+  return bits ? lift_log2<BF16>(bits, -80) : 60;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t lifted2(uint32_t u, float f) {
+  if constexpr (BF16)
+    return pack16<false>(__uint_as_float(u << 16) * f, __uint_as_float(u & 0xffff0000u) * f);
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u));
+  return pack16<false>(x.x * f, x.y * f);
+}
+template <bool BF16>
+__device__ __forceinline__ uint4 lifted8(const uint4& v, float f) {
+  return make_uint4(lifted2<BF16>(v.x, f), lifted2<BF16>(v.y, f), lifted2<BF16>(v.z, f),
+                    lifted2<BF16>(v.w, f));
+}
+// A score's factor in the exponent is at least this: masked scores are -inf, and their product
+// with 0 would be NaN; no score is large enough to show the difference.
+constexpr float kLeastFactor = 0x1p-126f;
+
 // Row r of an item's partials to its result, by a warp.  CTA c0 + i left the i-th, CTA c0 in
 // its slot `inside`.  Each lane finds the weights of one of every 32, then the weighted rows
 // are summed in order.  A partial without a seen token weighs nothing, whatever it holds.

@@ -1,0 +1,142 @@
+"""Attention over the block-8 cache at the ends of its inputs' range: open blocks (16-bit
+tokens in the ring) whose elements lie far apart.
+
+Tolerance: a weight is rounded to fp16, its score to fp32, as in test_gpu_block8.py: 2^-11 +
+2^-14 of sum p |v| and half a step of the result (at least half of fp16's smallest, 2^-25).
+An open token's elements are good to 2^-40 of its largest (2^-25 of fp16's smallest beside 2^15),
+which the random ones here leave far below that; small weights to 2^-32 of the largest product
+of weight and value scale: L 2^-30 of the row's largest p |v| is added where sizes are mixed."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import block8
+from paper_2607_16248_gb300 import kvq
+from test_gpu_block8 import HALF_STEP, TYPES, np64
+from test_gpu_block8_edges import ints, table_of
+
+pytestmark = pytest.mark.gpu
+
+# query heads a kv-head, new tokens, sequences (so many that a warp has several blocks)
+KINDS = {"chunk64": (32, 2, 1), "chunk80": (4, 20, 1), "chunk280": (4, 70, 1),
+         "many64": (32, 2, 160)}
+
+
+def rounded(x, dtype):
+    """The finite elements in the 16-bit type."""
+    return np.where(np.isfinite(x), block8.to_type(np.where(np.isfinite(x), x, 0.0), dtype), x)
+
+
+class Case:
+    """Keys and values (fp64 [L, 128]) of one kv-head put in by hand, for each of a number of
+    sequences."""
+
+    def __init__(self, dtype, gq, k, v, batch=1):
+        self.dtype, L, blocks = dtype, len(k), len(k) // 32
+        self.cfg = kvq.Block8Config(batch, gq, 1, (L + 31) // 32 * 32, TYPES[dtype])
+        self.cache = kvq.Block8Cache(self.cfg, n_pages=max(1, blocks),
+                                     block_table=table_of(self.cfg, [list(range(blocks))] * batch))
+        self.seen = []
+        for i, (x, pool, slots) in enumerate(((k, self.cache.k_codes, self.cache.k_ring),
+                                              (v, self.cache.v_codes, self.cache.v_ring))):
+            rows = rounded(x, dtype)
+            out, codes = rows.copy(), np.zeros((max(1, blocks), 1, 32, 128))
+            scales, ring = np.ones(max(1, blocks)), np.zeros((64, 128))
+            for j in range(blocks):
+                codes[j, 0], scales[j] = block8.quantize(rows[32 * j:32 * j + 32])
+                out[32 * j:32 * j + 32] = codes[j, 0] * scales[j]
+            for p in range(32 * blocks, L):
+                ring[p % 64] = rows[p]
+            pool.copy_(torch.tensor(codes).to(torch.float8_e4m3fn))
+            self.cache.scales[:, 0, i] = torch.tensor(scales).float().cuda()
+            slots[:, 0] = torch.tensor(ring).to(TYPES[dtype]).cuda()
+            self.seen.append(out)
+        self.L = L
+
+    def attend(self, q, window=0, sinks=0, scale=0.0, mixed=False, unseen=()):
+        """q fp64 [n, gq, 128]; rows of queries that see none of `unseen` are compared."""
+        n, L = len(q), self.L
+        q, batch = torch.tensor(q).to(TYPES[self.dtype]), self.cfg.batch
+        out = kvq.kvq_block8_attn(self.cache, q.cuda().repeat(batch, 1, 1), ints([L] * batch),
+                                  max_new=n, window=window, sinks=sinks, softmax_scale=scale)
+        k, v = (x.copy() for x in self.seen)
+        k[list(unseen)] = 0.0
+        want, size = block8.attend(np64(q), k, v, float(np.float32(scale)) or None, window, sinks)
+        rows = [t for t in range(n) if all(self.hidden(L - n + t, j, window, sinks)
+                                           for j in unseen)]
+        got = np64(out).reshape(batch, n, *out.shape[1:])[:, rows]
+        want, size = want[rows], size[rows]
+        tol = (2.0 ** -11 + 2.0 ** -14) * size + HALF_STEP[self.dtype] * np.abs(want)
+        if self.dtype == "fp16":
+            tol = tol + 2.0 ** -25
+        if mixed:
+            tol = tol + L * 2.0 ** -30 * size.max(-1, keepdims=True)
+        err = np.abs(got - want)
+        assert len(rows) and np.isfinite(got).all()
+        assert (err <= tol).all(), float((err / tol).max())
+        assert self.cache.flags() == 0
+        return out
+
+    @staticmethod
+    def hidden(p, j, window, sinks):
+        return j > p or bool(window and j <= p - window and j >= sinks)
+
+
+def randn(seed, *shape):
+    return np.random.default_rng(seed).standard_normal(shape)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 2.0 ** 60, 2.0 ** 127])
+@pytest.mark.parametrize("where", ["later", "behind"])
+def test_unseen_keys_of_the_open_block(kvq_lib, kind, bad, where):
+    """A key in the ring that is later than a query, or behind every query's window."""
+    gq, n, batch = KINDS[kind]
+    if where == "behind" and n > 4:
+        n = 9
+    L, window = (32 * 20 + 13, 0) if where == "later" else (32 * 20 + 29, 11)
+    k, v, q = randn(1, L, 128), randn(2, L, 128), randn(3, n, gq, 128)
+    at = [L - 1] if where == "later" else [32 * 20, 32 * 20 + 3]
+    k[at] = bad
+    Case("bf16", gq, k, v, batch).attend(q, window=window, unseen=at)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_keys_of_the_open_block_far_apart(kvq_lib, kind):
+    """Seen keys of 2^-60 to 2^30 in one open block (the large ones in channels in which the
+    queries hold nothing, so that no score is large)."""
+    gq, n, batch = KINDS[kind]
+    L = 32 * 20 + 27
+    k, v, q = randn(4, L, 128), randn(5, L, 128), randn(6, n, gq, 128)
+    k[-20:] *= 2.0 ** np.linspace(-60, 0, 20)[:, None]
+    k[-25, 100:] *= 2.0 ** 30
+    q[..., 100:] = 0.0
+    Case("bf16", gq, k, v, batch).attend(q)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("dtype,big", [("bf16", 2.0 ** 60), ("bf16", 2.0 ** 120),
+                                       ("fp16", 2.0 ** 13)])
+def test_a_later_value_of_the_open_block_is_large(kvq_lib, kind, dtype, big):
+    """Finite values that a query does not see, or that count for little, leave what it does
+    see as it is."""
+    gq, n, batch = KINDS[kind]
+    small = 1.0 if dtype == "bf16" else 2.0 ** -10
+    L = 32 * 20 + 17
+    k, v, q = randn(7, L, 128), small * randn(8, L, 128), randn(9, n, gq, 128)
+    v[-1] = big * randn(10, 128)
+    case = Case(dtype, gq, k, v, batch)
+    case.attend(q, unseen=[L - 1])
+    case.attend(q, mixed=True)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("L", [1, 17, 50, 32 * 20 + 1, 32 * 20 + 31])
+@pytest.mark.parametrize("dtype,size", [("bf16", 2.0 ** -40), ("bf16", 2.0 ** 40),
+                                        ("fp16", 2.0 ** -14), ("fp16", 2.0 ** -18)])
+def test_values_of_one_size_beside_an_open_block(kvq_lib, kind, L, dtype, size):
+    gq, n, batch = KINDS[kind]
+    n = min(n, L)
+    k, v, q = 2.0 * randn(11, L, 128), size * randn(12, L, 128), randn(13, n, gq, 128)
+    Case(dtype, gq, k, v, batch).attend(q)
