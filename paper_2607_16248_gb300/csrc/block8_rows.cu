@@ -18,7 +18,8 @@
 // fp32.  So neither scale rounds a code, and weights stay within fp16 whatever the scales.
 //
 // The tokens behind the last whole block are a block of 16-bit elements that one warp loads
-// from the ring; bf16 ones go to fp16 times a power of two.
+// from the ring.  Values, and bf16 keys, go to fp16 times a power of two, each token's its own:
+// what one token holds, seen or not, does not touch the others.
 //
 // What bounds it.  HBM where there is enough to read: 32 ragged chats of 2k to 32k tokens,
 // query groups of eight, bf16: 188 us, 5.9 TB/s; without the arithmetic 171.  Drafts of one
@@ -276,10 +277,70 @@ __device__ __forceinline__ uint32_t largest(uint32_t m, const uint4& v) {
   return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
 
+// The softmax of the open block's scores, in which every token has factors of its own: ks and
+// 2^lift, of tokens 16 h + 8 i + gid.  The reference is the row's best token by x + log2 of its
+// value's factor, whose two parts stay apart until the weights are written: so is their sum
+// exact where scores are large.
+template <int NT>
+__device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
+                                             const Rows<NT>& rows, float (&s)[2][NT][4], int t0,
+                                             const float (&ks)[2][2], const int (&lift)[2][2],
+                                             uint32_t (&w)[2][NT][2], float (&unit)[NT][2]) {
+  const int gid = (threadIdx.x & 31) >> 2;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float y[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float best = -INFINITY, best_lv = 0.0f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int t = t0 + 16 * h + 8 * i + gid, pos = rows.pos[n][j];
+          float x = s[h][n][j + 2 * i] * fmaxf(ks[h][i] * st.f[n][j], kLeastFactor);
+          if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks)) x = -INFINITY;
+          const float lv = (float)-lift[h][i];
+          if ((x - best) + (lv - best_lv) > 0.0f) best = x, best_lv = lv;
+          y[h][j + 2 * i] = x;
+        }
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        const float x = __shfl_xor_sync(0xffffffffu, best, o);
+        const float lv = __shfl_xor_sync(0xffffffffu, best_lv, o);
+        const float d = (x - best) + (lv - best_lv);
+        if (d > 0.0f || (d == 0.0f && x > best)) best = x, best_lv = lv;
+      }
+      unit[n][j] = 1.0f;
+      if (best == -INFINITY) {  // no token is seen
+        best = 0.0f;
+      } else {
+        const float m = best + best_lv;
+        unit[n][j] = exp2_fast((best - m) + best_lv);
+        st.m[n][j] = m;
+      }
+      float sum = 0.0f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float lv = (float)-lift[h][i];
+          const float x = exp2_fast((y[h][j + 2 * i] - best) + (lv - best_lv) + kLift);
+          sum = fmaf(x, pow2(lift[h][i]), sum);
+          y[h][j + 2 * i] = x;
+        }
+      st.l[n][j] = sum * unit[n][j];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        w[h][n][i] = transpose(pack16<false>(y[h][2 * i], y[h][2 * i + 1]));
+  }
+}
+
 // The block of 16-bit tokens t0 .. L - 1 (fewer than 32), from the ring's rows; the item's
-// first, so its results are its own.  bf16 elements go to fp16 times powers of two: a key's
-// is its token's, whose scores the same lanes get; a value's that of the lane's 16 channels,
-// whose results the lane holds.
+// first, so its results are its own.
 template <int NT, bool BF16>
 __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
                                         const uint16_t* k, const uint16_t* v, int t0, int L) {
@@ -288,7 +349,17 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
     return r < valid ? *reinterpret_cast<const uint4*>(base + r * kHeadDim + part)
                      : make_uint4(0u, 0u, 0u, 0u);
   };
-  float s[2][NT][4];
+  // the largest magnitude of a row of which four lanes hold a quarter each
+  const auto row_largest = [&](const uint4 (&x)[4]) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) m = largest(m, x[c]);
+    m = max(m & 0xffffu, m >> 16);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  };
+  float s[2][NT][4], ks[2][2] = {{1.0f, 1.0f}, {1.0f, 1.0f}};
+  int lift[2][2] = {{0, 0}, {0, 0}};
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -300,20 +371,23 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
     if (16 * h >= valid) break;  // no token there
     uint4 x[2][4];
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[e][c] = load(v, 16 * h + 8 * e + gid, 32 * tig + 8 * c);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      lift[h][e] = value_lift<BF16>(row_largest(x[e]));
 #pragma unroll
       for (int c = 0; c < 4; ++c) x[e][c] = load(k, 16 * h + 8 * e + gid, 32 * tig + 8 * c);
+    }
     float f[2] = {1.0f, 1.0f};
     if constexpr (BF16) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        uint32_t m = 0u;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) m = largest(m, x[e][c]);
-        m = max(m & 0xffffu, m >> 16);
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        f[e] = lift_of(m);
+        const int z = key_lift<BF16>(row_largest(x[e]));
+        f[e] = pow2(z);
+        ks[h][e] = pow2(-z);
       }
     }
 #pragma unroll
@@ -332,33 +406,10 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
         }
       }
     }
-    if constexpr (BF16) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][n][i] *= 1.0f / f[i >> 1];
-    }
   }
   uint32_t w[2][NT][2];
-  weights<NT, NT>(p, st, rows, s, t0, true, 1.0f, 1.0f, w);
-  float fv = 1.0f;
-  if constexpr (BF16) {
-    uint32_t m = 0u;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (16 * h >= valid) break;
-      uint4 x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[i] = load(v, 16 * h + 8 * (i >> 2) + 2 * tig + (i >> 1 & 1), 16 * gid + 8 * (i & 1));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = largest(m, x[i]);
-    }
-    m = max(m & 0xffffu, m >> 16);
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    fv = lift_of(m);
-  }
+  float unit[NT][2];
+  tail_weights<NT>(p, st, rows, s, t0, ks, lift, w, unit);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if (16 * h >= valid) break;
@@ -367,13 +418,19 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
     for (int i = 0; i < 8; ++i)
       x[i >> 2][i >> 1 & 1][i & 1] =
           load(v, 16 * h + 8 * (i >> 2) + 2 * tig + (i >> 1 & 1), 16 * gid + 8 * (i & 1));
+    float f[2][2];  // of rows 8 i + 2 tig + e: lanes 4 (2 tig + e) know them
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        f[i][e] = pow2(__shfl_sync(0xffffffffu, lift[h][i], 8 * tig + 4 * e));
 #pragma unroll
     for (int c = 0; c < 2; ++c) {  // 8 channels each
 #pragma unroll
       for (int k2 = 0; k2 < 4; ++k2) {
         const auto word = [&](int i, int e) {
           const uint4& y = x[i][e][c];
-          return to_half2<BF16>(k2 == 0 ? y.x : k2 == 1 ? y.y : k2 == 2 ? y.z : y.w, fv);
+          return lifted2<BF16>(k2 == 0 ? y.x : k2 == 1 ? y.y : k2 == 2 ? y.z : y.w, f[i][e]);
         };
         const uint32_t w00 = word(0, 0), w01 = word(0, 1), w10 = word(1, 0), w11 = word(1, 1);
         const uint32_t a0 = __byte_perm(w00, w01, 0x5410), a1 = __byte_perm(w00, w01, 0x7632);
@@ -384,15 +441,12 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
       }
     }
   }
-  if constexpr (BF16) {
-    const float g = 1.0f / fv;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) st.o[n][i][j] *= g;
-  }
+      for (int j = 0; j < 4; ++j) st.o[n][i][j] *= unit[n][j & 1];
 }
 
 // Queries of an item's row group n: row 8 n + gid's channels 32 tig .. 32 tig + 31, bf16 ones

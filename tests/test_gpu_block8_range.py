@@ -1,5 +1,6 @@
 """Attention over the block-8 cache at the ends of its inputs' range: open blocks (16-bit
-tokens in the ring) whose elements lie far apart.
+tokens in the ring) whose elements lie far apart.  By both kernels: up to 32 query rows a
+kv-head, and more, of one row tile and of two.
 
 Tolerance: a weight is rounded to fp16, its score to fp32, as in test_gpu_block8.py: 2^-11 +
 2^-14 of sum p |v| and half a step of the result (at least half of fp16's smallest, 2^-25).
@@ -19,7 +20,9 @@ from test_gpu_block8_edges import ints, table_of
 pytestmark = pytest.mark.gpu
 
 # query heads a kv-head, new tokens, sequences (so many that a warp has several blocks)
-KINDS = {"chunk64": (32, 2, 1), "chunk80": (4, 20, 1), "chunk280": (4, 70, 1),
+KINDS = {"rows8": (4, 2, 1), "rows16": (4, 3, 1), "rows24": (8, 3, 1), "rows32": (8, 4, 1),
+         "many8": (4, 2, 160), "many24": (8, 3, 160), "many32": (8, 4, 160),
+         "chunk64": (32, 2, 1), "chunk80": (4, 20, 1), "chunk280": (4, 70, 1),
          "many64": (32, 2, 160)}
 
 
@@ -129,6 +132,7 @@ def test_a_later_value_of_the_open_block_is_large(kvq_lib, kind, dtype, big):
     case = Case(dtype, gq, k, v, batch)
     case.attend(q, unseen=[L - 1])
     case.attend(q, mixed=True)
+    case.attend(q[-1:], window=1)
 
 
 @pytest.mark.parametrize("kind", list(KINDS))
