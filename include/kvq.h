@@ -676,7 +676,7 @@ kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cach
 typedef struct kvq_block8_attn_params {
   int32_t window;      /* newest tokens seen, the query's own included; 0: all */
   int32_t sinks;       /* with a window: first tokens that stay visible, >= 0 */
-  float softmax_scale; /* 0 selects 1/sqrt(128) */
+  float softmax_scale; /* at most 2^127; 0 selects 1/sqrt(128) */
   int64_t q_stride[2];
   int64_t out_stride[2];
 } kvq_block8_attn_params;

@@ -853,8 +853,8 @@ kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache*
     return s;
   if (p->window < 0 || p->sinks < 0)
     return fail(KVQ_ERR_ARG, "window and sinks must be >= 0 (got %d, %d)", p->window, p->sinks);
-  if (!(p->softmax_scale >= 0.0f) || isinf(p->softmax_scale))
-    return fail(KVQ_ERR_ARG, "softmax_scale must be finite and >= 0");
+  if (!(p->softmax_scale >= 0.0f) || p->softmax_scale > 0x1p127f)  // times log2 e it is finite
+    return fail(KVQ_ERR_ARG, "softmax_scale must be in [0, 2^127]");
   const block8::Dims8 d = block8_dims(*cfg);
   if (block8::attn_most_units(d, batch->max_new) >= (1LL << 31))
     return fail(KVQ_ERR_SHAPE, "batch * n_kv_heads * max_len and max_new give too many tiles");

@@ -577,7 +577,7 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
         uint32_t r[2][32];
         tm_load32(sb, r[0]);
         tm_load32(sb + 32, r[1]);
-        float2 f = make_float2(sc[0].x * sl, sc[1].x * sl);
+        float2 f = make_float2(fmaxf(sc[0].x * sl, kLeastFactor), fmaxf(sc[1].x * sl, kLeastFactor));
         float2 lv = make_float2(sc[0].y, sc[1].y);
         if (open == 0) f.x = 1.0f, lv.x = kept->x;
         if (open == 1) f.y = 1.0f, lv.y = kept->x;

@@ -139,13 +139,14 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
         }
   }
   const float lsv = log2_fast(sv), inv = 1.0f / sv;
+  const auto factor = [&](int n, int j) { return fmaxf(sk * st.f[n][j], kLeastFactor); };
   bool up = false;
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
-      up |= fmaf(mx, sk * st.f[n][j], lsv - st.m[n][j]) > kLag;
+      up |= fmaf(mx, factor(n, j), lsv - st.m[n][j]) > kLag;
     }
   if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
@@ -155,7 +156,7 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
         float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float m = fmaxf(st.m[n][j], fmaf(mx, sk * st.f[n][j], lsv));
+        const float m = fmaxf(st.m[n][j], fmaf(mx, factor(n, j), lsv));
         const float f = exp2_fast(st.m[n][j] - m);
         st.m[n][j] = m;
         st.l[n][j] *= f;
@@ -171,7 +172,7 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
     float y[2][4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float f = sk * st.f[n][j], c = lsv + kLift - st.m[n][j];
+      const float f = factor(n, j), c = lsv + kLift - st.m[n][j];
       float sum = 0.0f;
 #pragma unroll
       for (int h = 0; h < 2; ++h)

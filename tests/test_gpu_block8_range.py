@@ -1,6 +1,6 @@
 """Attention over the block-8 cache at the ends of its inputs' range: open blocks (16-bit
-tokens in the ring) whose elements lie far apart.  By both kernels: up to 32 query rows a
-kv-head, and more, of one row tile and of two.
+tokens in the ring) whose elements lie far apart, and factors of scores that leave fp32.  By both
+kernels: up to 32 query rows a kv-head, and more, of one row tile and of two.
 
 Tolerance: a weight is rounded to fp16, its score to fp32, as in test_gpu_block8.py: 2^-11 +
 2^-14 of sum p |v| and half a step of the result (at least half of fp16's smallest, 2^-25).
@@ -144,3 +144,25 @@ def test_values_of_one_size_beside_an_open_block(kvq_lib, kind, L, dtype, size):
     n = min(n, L)
     k, v, q = 2.0 * randn(11, L, 128), size * randn(12, L, 128), randn(13, n, gq, 128)
     Case(dtype, gq, k, v, batch).attend(q)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("q_size,k_size", [(-85, -40), (-90, -55), (-100, -100), (-30, -110),
+                                           (60, -120)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_factors_below_fp32(kvq_lib, kind, q_size, k_size, window):
+    """Scores of nothing: every visible token counts the same, masked ones not at all."""
+    gq, n, batch = KINDS[kind]
+    L = 32 * 20 + 21
+    k, v, q = randn(17, L, 128), randn(18, L, 128), randn(19, n, gq, 128)
+    Case("bf16", gq, k * 2.0 ** k_size, v, batch).attend(q * 2.0 ** q_size, window=window)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("scale", [1e-38, 1e-44])
+def test_the_smallest_softmax_scales(kvq_lib, kind, dtype, scale):
+    gq, n, batch = KINDS[kind]
+    L = 32 * 20 + 21
+    Case(dtype, gq, 0.01 * randn(20, L, 128), randn(21, L, 128), batch).attend(
+        randn(22, n, gq, 128), scale=scale)
