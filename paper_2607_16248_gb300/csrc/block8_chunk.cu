@@ -102,9 +102,9 @@ struct Smem {
   uint32_t tmem;
   int abort;
   float4 scale[kScaleTiles][4];        // a block's s_k, log2 s_v, 1 / s_v; 1 for the open one
-  float2 open[kScaleTiles][kGroup];    // its tokens' s_k, log2 s_v
+  float2 open[kScaleTiles][kGroup];    // its tokens' s_k (from the keys' warp), log2 s_v
   float qf[2][2][kTile];               // [item][stream]: 1 / the factor of a row's queries
-  float m[kTile], l[kTile];            // stream 1's statistics of a shared row tile
+  float m[kTile], l[kTile], unit[kTile];  // stream 1's statistics of a shared row tile
 };
 
 // Waits are bounded: after the limit, or once another role has given up, they return
@@ -204,38 +204,33 @@ __device__ __forceinline__ void restore_codes(const Codes& c, int k, unsigned ch
   st16(tile, tile_at(half, row, chunk + 1 - half), half ? lo : hi);
 }
 
-// The open block's rows (`valid` of them, the others zero) by a warp, four at a time, 16
-// lanes a row.  The keys' warp also finds the values' factors and leaves both in `open`.
+// The open block's rows (`valid` of them, the others zero) by a warp, 16 lanes a row, so many at
+// a time that two waits for memory do; what becomes of their factors in `open`: a key's in x,
+// log2 of a value's in y.
 template <bool BF16, bool KEY>
-__device__ __forceinline__ void open_block(const uint16_t* rows, const uint16_t* values, int valid,
-                                           unsigned char* tile, int j, float2* open) {
+__device__ __forceinline__ void open_block(const uint16_t* rows, int valid, unsigned char* tile,
+                                           int j, float2* open) {
   const int lane = threadIdx.x & 31, m = lane & 15;
-  const auto load = [&](const uint16_t* base, int r) {
-    return r < valid ? *(reinterpret_cast<const uint4*>(base + r * kHeadDim) + m)
-                     : make_uint4(0u, 0u, 0u, 0u);
-  };
-  const auto row_lift = [&](const uint4& v, bool key) {
-    uint32_t x = largest(v);
-#pragma unroll
-    for (int o = 8; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
-    return key ? key_lift<BF16>(x) : value_lift<BF16>(x);
-  };
 #pragma unroll 1
-  for (int h = 0; h < 32; h += 4) {
-    uint4 v[2], u[2];
+  for (int h = 0; h < 32; h += 16) {
+    uint4 v[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 8; ++i) {
       const int r = h + 2 * i + (lane >> 4);
-      v[i] = load(rows, r);
-      if (KEY) u[i] = load(values, r);
+      v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < valid) v[i] = *(reinterpret_cast<const uint4*>(rows + r * kHeadDim) + m);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = h + 2 * i + (lane >> 4), e = row_lift(v[i], KEY);
+    for (int i = 0; i < 8; ++i) {
+      const int r = h + 2 * i + (lane >> 4);
+      uint32_t x = largest(v[i]);
+#pragma unroll
+      for (int o = 8; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+      const int e = KEY ? key_lift<BF16>(x) : value_lift<BF16>(x);
       st16(tile, tile_at(m >> 3, 32 * j + r, m & 7), lifted8<BF16>(v[i], pow2(e)));
-      if (KEY) {
-        const int ev = row_lift(u[i], false);
-        if (m == 0) open[r] = make_float2(pow2(-e), (float)-ev);
+      if (m == 0) {
+        if (KEY) open[r].x = pow2(-e);
+        else open[r].y = (float)-e;
       }
     }
   }
@@ -314,16 +309,15 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
             const long long at =
                 (((long long)w.b * p.c.d.hkv + w.head) * kRing + (ta & (kRing - 1))) * kHeadDim;
             const int valid = w.q.L - ta;
-            const uint16_t* v = p.c.cache.v_ring + at;
-            if (key)
-              open_block<BF16, true>(p.c.cache.k_ring + at, v, valid, tile, j,
-                                     s.open[n & (kScaleTiles - 1)]);
-            else
-              open_block<BF16, false>(v, v, valid, tile, j, nullptr);
+            float2* factors = s.open[n & (kScaleTiles - 1)];
+            if (key) open_block<BF16, true>(p.c.cache.k_ring + at, valid, tile, j, factors);
+            else open_block<BF16, false>(p.c.cache.v_ring + at, valid, tile, j, factors);
             open = true;
           }
+          c = Codes{};  // (nothing is in it: so it takes no registers from the lines above)
         }
-        // (the scores' product waits for the keys' warps alone: they write all of it)
+        // (the scores' product waits for the keys' warps alone: they write all of it; the values'
+        // factors of the open block are waited for)
         if (key && lane == 0)
           s.scale[n & (kScaleTiles - 1)][j] =
               none   ? make_float4(1.0f, -INFINITY, 1.0f, 0.0f)
@@ -415,9 +409,13 @@ __device__ __forceinline__ void issue_role(const AttnParams& p, Smem& s, int u0,
 // Softmax, results
 // ---------------------------------------------------------------------------
 
+// The running maximum of x + log2 s_v is m + e: e is 0 until it passes kFar (from then on
+// log2 s_v alone, and every step goes by differences of scores, which are exact where it counts).
+// l: lifted sum of w / s_v.
 struct Row {
-  float m, l;  // running maximum of x + log2 s_v, lifted sum of w / s_v
+  float m, e, l;
 };
+constexpr float kFar = 32768.0f;  // rounded to fp32, a sum with m is good to 2^-9
 
 // A warp's 32 rows, from row r0 of the sequence and row `row` of the tile on: 16 lanes a row.
 template <bool BF16>
@@ -470,43 +468,72 @@ __device__ __forceinline__ void mask_row(uint32_t ts, int hi, int lo, int sink) 
   tm_store_wait();
 }
 
-// The scores of the open block, 32 columns: the best of a thread's row by x + log2 s_v, and the
-// others against it, x - x_best + log2 s_v - log2 s_best (at most 0), in their place.  Returns
-// the best's x + log2 s_v and the sum of 2^(the others) / s_v.  Few steps come here, so the
-// numbers stay in tensor memory, eight at a time.
-__device__ __forceinline__ float2 open_scores(uint32_t ts, const float2* open, float sl) {
-  float best = -INFINITY, best_lv = 0.0f, sum = 0.0f;
+// A step in which tokens have factors of their own (the open block's: w of its scale is 1), or
+// in which scores are so large that only their differences are fit for fp32 (`far`): the best of a
+// thread's row by x + log2 s_v first, then all weights against it.  Returns the row and what the
+// results so far have to be multiplied with.  Few steps come here, so the numbers stay in tensor
+// memory, 16 at a time, and the code out of the others' way.
+__device__ __noinline__ float4 apart_step(uint32_t sb, const float4* sc, const float2* open,
+                                          float sl, bool first, bool far, float row_m,
+                                          float row_e, float l) {
+  // s_k, log2 s_v of columns c .. c + 15, one or each: the first's place and its distance to the next
+  const auto factors = [&](int c, int& stride) {
+    stride = sc[c >> 5].w != 0.0f ? 1 : 0;
+    return stride ? open + (c & 31) : reinterpret_cast<const float2*>(sc + (c >> 5));
+  };
+  float best = -INFINITY, best_lv = 0.0f;
 #pragma unroll 1
-  for (int c = 0; c < kGroup; c += 8) {
+  for (int c = 0; c < kStep; c += 8) {
     uint32_t r[8];
-    tm_load8(ts + c, r);
+    int stride;
+    const float2* f = factors(c, stride);
+    tm_load8(sb + c, r);
     tm_load_wait();
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
-      const float2 s = open[c + n];
-      const float x = __uint_as_float(r[n]) * fmaxf(s.x * sl, kLeastFactor);
+      const float2 s = f[n * stride];
+      const float x = __fmul_rn(__uint_as_float(r[n]), fmaxf(s.x * sl, kLeastFactor));
       if ((x - best) + (s.y - best_lv) > 0.0f) best = x, best_lv = s.y;
       r[n] = __float_as_uint(x);
     }
-    tm_store8(ts + c, r);
+    tm_store8(sb + c, r);
   }
   tm_store_wait();
-  if (best == -INFINITY) best = 0.0f;
+  // (-inf - -inf is NaN, and no reason for a new maximum)
+  const float d = (best - row_m) + (best_lv - row_e);
+  float z = 1.0f;
+  if (first || d > kRescaleLog2) {
+    const float sum = best + best_lv;
+    const bool split = far || fabsf(sum) > kFar;
+    z = exp2_fast(-d);
+    l = first ? 0.0f : l * z;
+    row_m = split ? best : sum;
+    row_e = split ? best_lv : 0.0f;
+  }
+  const float m = row_m == -INFINITY ? 0.0f : row_m, e = row_e - kLiftLog2;
 #pragma unroll 1
-  for (int c = 0; c < kGroup; c += 8) {
-    uint32_t r[8];
-    tm_load8(ts + c, r);
+  for (int c = 0; c < kStep; c += 16) {
+    uint32_t r[2][8], h[8];
+    int stride;
+    const float2* f = factors(c, stride);
+    tm_load8(sb + c, r[0]);
+    tm_load8(sb + c + 8, r[1]);
     tm_load_wait();
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const float lv = open[c + n].y, y = (__uint_as_float(r[n]) - best) + (lv - best_lv);
-      sum += exp2_fast(y - lv);
-      r[n] = __float_as_uint(y);
+    for (int n = 0; n < 16; n += 2) {
+      const float lv0 = f[n * stride].y, lv1 = f[(n + 1) * stride].y;
+      const float y0 = (__uint_as_float(r[n >> 3][n & 7]) - m) + (lv0 - e);
+      const float y1 = (__uint_as_float(r[n >> 3][(n & 7) + 1]) - m) + (lv1 - e);
+      const float w0 = exp2_fast(y0), w1 = exp2_fast(y1);
+      if (w0 > 0.0f) l = fmaf(w0, exp2_fast(-lv0), l);
+      if (w1 > 0.0f) l = fmaf(w1, exp2_fast(-lv1), l);
+      h[n >> 1] = pack16<false>(w0, w1);
     }
-    tm_store8(ts + c, r);
+    // (words 8 c / 16 ..: what stood there has been read)
+    tm_store8(sb + (c >> 1), h);
   }
   tm_store_wait();
-  return make_float2(best + best_lv, sum);
+  return make_float4(row_m, row_e, l, z);
 }
 
 template <bool BF16>
@@ -545,7 +572,8 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
     const bool valid = g < rows;
     const bool live = g_warp < rows;  // the warp has a row
     const int pos = w.q.L - w.q.n + token_of_row(p, g);
-    Row row{-INFINITY, 0.0f};
+    Row row{-INFINITY, 0.0f, 0.0f};
+    bool far = false;  // a row of the warp has its maximum beyond kFar
     float sl = p.c.scale_log2;
     const int steps = (w.i1 - w.i0) << two;
 #pragma unroll 1
@@ -558,86 +586,102 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
         if (BF16 && st == 0) sl *= s.qf[items & 1][two ? x : 0][lane_row];
         const int half = two ? st & 1 : x;
         const int t0 = w.s.tile(w.i0 + (st >> two)) * kTile + kStep * half;
-        // every token of the step is seen by every row of the item
-        const bool whole = w.s.p0 >= t0 + kStep - 1 &&
+        // every token of the step is seen by every row of the item, and nothing is special
+        const bool whole = !far && w.s.p0 >= t0 + kStep - 1 &&
                            (!p.c.window || t0 > w.s.p1 - p.c.window || t0 <= p.c.sinks - kStep);
-        // the last token behind the window, -1 if there is none (positions and windows
-        // each reach 2^31)
-        const int behind = p.c.window ? max(max(pos, 0) - p.c.window, -1) : -1;
         const int slot = (nt + (st >> two)) & (kScaleTiles - 1);
         const float4* sc = &s.scale[slot][2 * half];
-        // the block that is open, -1 for none (it ends behind every row's position: no step
-        // with it is whole); what its scores give waits in the warp's place for results
-        const int open = whole ? -1 : sc[0].w != 0.0f ? 0 : sc[1].w != 0.0f ? 1 : -1;
-        float2* kept = reinterpret_cast<float2*>(s.stage[warp]) + (threadIdx.x & 31);
+        // The product before this step's has to be in: the next scores are issued behind it;
+        // an item's last step has none behind.
+        const auto rescale = [&](float z) {
+          if (st + 1 < steps ? !warp_wait(s, &s.s_full[x][b ^ 1], ((ns + 1) >> 1) & 1)
+                             : !warp_wait(s, &s.o_last[x], lasts & 1))
+            return false;
+          tc_after();
+          rescale_row(to, z);
+          return true;
+        };
         if (!whole) {
+          // the last token behind the window, -1 if there is none (positions and windows
+          // each reach 2^31)
+          const int behind = p.c.window ? max(max(pos, 0) - p.c.window, -1) : -1;
           mask_row(sb, (valid ? pos : -1) - t0, behind - t0, p.c.sinks - t0);
-          if (open >= 0) *kept = open_scores(sb + 32 * open, s.open[slot], sl);
+          // (the open block ends behind every row's position: no step with it is whole)
+          if (far || sc[0].w != 0.0f || sc[1].w != 0.0f) goto apart;
         }
-        uint32_t r[2][32];
-        tm_load32(sb, r[0]);
-        tm_load32(sb + 32, r[1]);
-        float2 f = make_float2(fmaxf(sc[0].x * sl, kLeastFactor), fmaxf(sc[1].x * sl, kLeastFactor));
-        float2 lv = make_float2(sc[0].y, sc[1].y);
-        if (open == 0) f.x = 1.0f, lv.x = kept->x;
-        if (open == 1) f.y = 1.0f, lv.y = kept->x;
-        tm_load_wait();
-        float mc[2];
+        {
+          uint32_t r[2][32];
+          tm_load32(sb, r[0]);
+          tm_load32(sb + 32, r[1]);
+          const float2 f =
+              make_float2(fmaxf(sc[0].x * sl, kLeastFactor), fmaxf(sc[1].x * sl, kLeastFactor));
+          const float2 lv = make_float2(sc[0].y, sc[1].y);
+          tm_load_wait();
+          float mc[2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const uint32_t* y = r[c];
-          float a = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-          float d = fmaxf(__uint_as_float(y[2]), __uint_as_float(y[3]));
+          for (int c = 0; c < 2; ++c) {
+            const uint32_t* y = r[c];
+            float a = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+            float d = fmaxf(__uint_as_float(y[2]), __uint_as_float(y[3]));
 #pragma unroll
-          for (int n = 4; n < 32; n += 4) {
-            a = fmaxf(fmaxf(a, __uint_as_float(y[n])), __uint_as_float(y[n + 1]));
-            d = fmaxf(fmaxf(d, __uint_as_float(y[n + 2])), __uint_as_float(y[n + 3]));
+            for (int n = 4; n < 32; n += 4) {
+              a = fmaxf(fmaxf(a, __uint_as_float(y[n])), __uint_as_float(y[n + 1]));
+              d = fmaxf(fmaxf(d, __uint_as_float(y[n + 2])), __uint_as_float(y[n + 3]));
+            }
+            mc[c] = fmaxf(a, d);
           }
-          mc[c] = fmaxf(a, d);
-        }
-        const float mx = fmaxf(fmaf(mc[0], f.x, lv.x), fmaf(mc[1], f.y, lv.y));
-        if (st == 0) {
-          row.m = mx;
-        } else {
-          const bool up = mx > row.m + kRescaleLog2;
-          if (__any_sync(0xffffffffu, up)) {
-            const float z = up ? exp2_fast(row.m - mx) : 1.0f;
-            if (up) row.m = mx;
-            row.l *= z;
-            // The product before this step's has to be in: the next scores are issued
-            // behind it; an item's last step has none behind.
-            if (st + 1 < steps ? !warp_wait(s, &s.s_full[x][b ^ 1], ((ns + 1) >> 1) & 1)
-                               : !warp_wait(s, &s.o_last[x], lasts & 1))
-              return;
-            tc_after();
-            rescale_row(to, z);
+          const float mx = fmaxf(fmaf(mc[0], f.x, lv.x), fmaf(mc[1], f.y, lv.y));
+          if (st == 0) {
+            far = __any_sync(0xffffffffu, mx > -INFINITY && fabsf(mx) > kFar);
+            if (far) goto apart;
+            row.m = mx;
+          } else {
+            const bool up = mx > row.m + kRescaleLog2;
+            if (__any_sync(0xffffffffu, up)) {
+              far = __any_sync(0xffffffffu, up && fabsf(mx) > kFar);
+              if (far) goto apart;
+              const float z = up ? exp2_fast(row.m - mx) : 1.0f;
+              if (up) row.m = mx;
+              row.l *= z;
+              if (!rescale(z)) return;
+            }
           }
-        }
-        const float base = row.m == -INFINITY ? 0.0f : kLiftLog2 - row.m;
-        if (open >= 0) row.l = fmaf(kept->y, exp2_fast(base + kept->x), row.l);
+          const float base = row.m == -INFINITY ? 0.0f : kLiftLog2 - row.m;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const float fc = c ? f.y : f.x, oc = base + (c ? lv.y : lv.x);
-          const uint64_t sl2 = pair(fc, fc), of = pair(oc, oc);
-          uint64_t acc[2] = {0ull, 0ull};
-          uint32_t h[16];
+          for (int c = 0; c < 2; ++c) {
+            const float fc = c ? f.y : f.x, oc = base + (c ? lv.y : lv.x);
+            const uint64_t sl2 = pair(fc, fc), of = pair(oc, oc);
+            uint64_t acc[2] = {0ull, 0ull};
+            uint32_t h[16];
 #pragma unroll
-          for (int n = 0; n < 16; ++n) {
+            for (int n = 0; n < 16; ++n) {
+              float y0, y1;
+              unpair(fma2(pair(__uint_as_float(r[c][2 * n]), __uint_as_float(r[c][2 * n + 1])),
+                          sl2, of),
+                     y0, y1);
+              y0 = exp2_fast(y0);
+              y1 = exp2_fast(y1);
+              acc[n & 1] = add2(acc[n & 1], pair(y0, y1));
+              h[n] = pack16<false>(y0, y1);
+            }
+            tm_store16(sb + 16 * c, h);
             float y0, y1;
-            unpair(fma2(pair(__uint_as_float(r[c][2 * n]), __uint_as_float(r[c][2 * n + 1])), sl2,
-                        of),
-                   y0, y1);
-            y0 = exp2_fast(y0);
-            y1 = exp2_fast(y1);
-            acc[n & 1] = add2(acc[n & 1], pair(y0, y1));
-            h[n] = pack16<false>(y0, y1);
+            unpair(add2(acc[0], acc[1]), y0, y1);
+            row.l = fmaf(y0 + y1, sc[c].z, row.l);
           }
-          tm_store16(sb + 16 * c, h);
-          float y0, y1;
-          unpair(add2(acc[0], acc[1]), y0, y1);
-          row.l = fmaf(y0 + y1, sc[c].z, row.l);
+          tm_store_wait();
         }
-        tm_store_wait();
+        if (false) {  // (behind the others' code, so that theirs stays in one piece)
+        apart:
+          const uint32_t t = nt + (st >> two);
+          if (!warp_wait(s, &s.v_full[t & 1], (t >> 1) & 1)) return;
+          const float4 next =
+              apart_step(sb, sc, s.open[slot], sl, st == 0, far, row.m, row.e, row.l);
+          row = Row{next.x, next.y, next.z};
+          far |= __any_sync(0xffffffffu, row.e != 0.0f ||
+                                             (row.m > -INFINITY && fabsf(row.m) > kFar)) != 0;
+          if (st > 0 && __any_sync(0xffffffffu, next.w != 1.0f) && !rescale(next.w)) return;
+        }
       }
       tc_before();
       warp_arrive(&s.p_ready[x][b]);
@@ -661,14 +705,23 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
     if (!warp_wait(s, &s.o_full[x], items & 1)) return;
     if (!two && x == 0 && !warp_wait(s, &s.o_full[1], items & 1)) return;
     tc_after();
+    // one number again for the maximum; what it leaves of the two goes to the results
+    float unit = 1.0f;
+    if (far && row.m > -INFINITY) {
+      const float m = row.m + row.e;
+      unit = exp2_fast((row.m - m) + row.e);
+      row.l *= unit;
+      row.m = m;
+    }
     if (!two && x == 1) {
       s.m[lane_row] = row.m;
       s.l[lane_row] = row.l;
+      s.unit[lane_row] = unit;
     }
     if (!two && !meet_softmax(s, met)) return;
     const bool direct = w.whole();
     if ((two || x == 0) && live) {
-      float f0 = 1.0f, f1 = 0.0f, m = row.m, l = row.l;
+      float f0 = unit, f1 = 0.0f, m = row.m, l = row.l;
       if (!two) {
         const float m1 = s.m[lane_row], l1 = s.l[lane_row];
         m = fmaxf(row.m, m1);
@@ -677,6 +730,8 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
           f1 = exp2_fast(m1 - m);
         }
         l = row.l * f0 + l1 * f1;
+        f0 *= unit;
+        f1 *= s.unit[lane_row];
       }
       const float scale = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
       f0 *= scale;

@@ -16,6 +16,10 @@
 // times s_v is 2^(x + log2 s_v): the running maximum is taken of x + log2 s_v, fp16 weights
 // are w = 2^(x + log2 s_v - m + kLift), and the sum of the softmax is that of w / s_v, in
 // fp32.  So neither scale rounds a code, and weights stay within fp16 whatever the scales.
+// The maximum is kept in its two parts, m = x_max and e = log2 s_v there, and a weight's
+// exponent is (x - m) + (log2 s_v + kLift - e) with x rounded: the difference of two scores
+// is exact where it counts, however large they are.  In one sum with x, a product's rounding
+// and that of kLift - m passed fp16's range from scores of 2^28 on.
 //
 // The tokens behind the last whole block are a block of 16-bit elements that one warp loads
 // from the ring.  Values, and bf16 keys, go to fp16 times a power of two, each token's its own:
@@ -29,6 +33,7 @@
 // (1.7), and the join (2.4).
 #include <cuda.h>
 
+#include <cfloat>
 #include <type_traits>
 
 #include "block8_plan.cuh"
@@ -43,7 +48,7 @@ constexpr int kItemCost = 16;      // of an item in units (a block's are 4 to 7)
 constexpr int kHalfPage = kGroup * kHeadDim;  // bytes of a block's keys (or values)
 constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
 constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
-constexpr float kNone = -1e30f;    // the maximum before any token
+constexpr float kNone = -FLT_MAX;  // the maximum before any token
 constexpr long long kWaitCycles = 4000000000LL;  // bound of a wait (~2 s)
 
 // Eight warps with two slots each: 128 KB of copies on their way in an SM.  More only make
@@ -82,6 +87,23 @@ __device__ __forceinline__ uint32_t transpose(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// Two fp32 operations at once.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 v;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n"
+      " mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(v.x), "=f"(v.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return v;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 v;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n"
+      " add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(v.x), "=f"(v.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return v;
+}
 // Codes 2 i, 2 i + 1 of a word as fp16.
 __device__ __forceinline__ uint32_t wide_lo(uint32_t v) {
   uint32_t r;
@@ -102,7 +124,8 @@ template <int NT>
 struct State {
   // queries in registers while there is room for them beside the results
   static constexpr bool kOwnQueries = NT <= 2;
-  float m[NT][2], l[NT][2];  // of rows 8 nt + 2 tig, + 1; l of this lane's tokens alone
+  float m[NT][2], e[NT][2];  // of rows 8 nt + 2 tig, + 1
+  float l[NT][2];            // of this lane's tokens alone
   float o[NT][8][4];         // channels 16 gid + 2 i (0, 1) and + 1 (2, 3), the same rows
   uint2 q[kOwnQueries ? NT : 1][8];  // of row 8 nt + gid, channels 32 tig ..
   const uint2* shared_q;             // [NT][8][32] of the CTA
@@ -114,39 +137,49 @@ struct State {
 };
 
 // What masks a block's tokens: the rows' positions.
-template <int NT>
 struct Rows {
-  int pos[NT][2];
+  int first;  // of row 0
+  __device__ __forceinline__ int pos(const AttnParams& p, int n, int j) const {
+    return first + token_of_row(p, 8 * n + 2 * (threadIdx.x & 3) + j);
+  }
 };
 
 // The softmax of a block's scores s[half of 16 tokens][nt][4], and its weights as B.
 // t0: the block's first token; edge: some row may not see some token.
 template <int N, int NT>
-__device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
+__device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, const Rows& rows,
                                         float (&s)[2][N][4], int t0, bool edge, float sk,
                                         float sv, uint32_t (&w)[2][N][2]) {
   const int gid = (threadIdx.x & 31) >> 2;
   if (edge) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+      for (int j = 0; j < 2; ++j) {
+        const int pos = rows.pos(p, n, j);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = t0 + 16 * h + 8 * (i >> 1) + gid, pos = rows.pos[n][i & 1];
-          if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks))
-            s[h][n][i] = -INFINITY;
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int t = t0 + 16 * h + 8 * i + gid;
+            if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks))
+              s[h][n][j + 2 * i] = -INFINITY;
+          }
+      }
   }
   const float lsv = log2_fast(sv), inv = 1.0f / sv;
   const auto factor = [&](int n, int j) { return fmaxf(sk * st.f[n][j], kLeastFactor); };
+  // how far a score of row j of group n is above the reference
+  const auto above = [&](int n, int j, float s) {
+    return __fsub_rn(__fmul_rn(s, factor(n, j)), st.m[n][j]) + (lsv - st.e[n][j]);
+  };
   bool up = false;
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
-      up |= fmaf(mx, factor(n, j), lsv - st.m[n][j]) > kLag;
+      up |= above(n, j, mx) > kLag;
     }
   if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
@@ -156,9 +189,13 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
         float mx = fmaxf(fmaxf(s[0][n][j], s[0][n][j + 2]), fmaxf(s[1][n][j], s[1][n][j + 2]));
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float m = fmaxf(st.m[n][j], fmaf(mx, factor(n, j), lsv));
-        const float f = exp2_fast(st.m[n][j] - m);
-        st.m[n][j] = m;
+        const float d = above(n, j, mx);
+        float f = 1.0f;
+        if (d > 0.0f) {
+          f = exp2_fast(-d);
+          st.m[n][j] = __fmul_rn(mx, factor(n, j));
+          st.e[n][j] = lsv;
+        }
         st.l[n][j] *= f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -169,32 +206,29 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    float y[2][4];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float f = factor(n, j), c = lsv + kLift - st.m[n][j];
-      float sum = 0.0f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float x = exp2_fast(fmaf(s[h][n][j + 2 * i], f, c));
-          y[h][j + 2 * i] = x;
-          sum += x;
-        }
-      st.l[n][j] = fmaf(sum, inv, st.l[n][j]);
-    }
+    const float2 f = make_float2(factor(n, 0), factor(n, 1));
+    const float2 c = make_float2(lsv + kLift - st.e[n][0], lsv + kLift - st.e[n][1]);
+    float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        w[h][n][i] = transpose(pack16<false>(y[h][2 * i], y[h][2 * i + 1]));
+      for (int i = 0; i < 2; ++i) {
+        // (m by single subtractions: a packed one would be fused with the product)
+        const float2 x = mul2(make_float2(s[h][n][2 * i], s[h][n][2 * i + 1]), f);
+        float2 y = add2(make_float2(__fsub_rn(x.x, st.m[n][0]), __fsub_rn(x.y, st.m[n][1])), c);
+        y.x = exp2_fast(y.x);
+        y.y = exp2_fast(y.y);
+        sum = add2(sum, y);
+        w[h][n][i] = transpose(pack16<false>(y.x, y.y));
+      }
+    st.l[n][0] = fmaf(sum.x, inv, st.l[n][0]);
+    st.l[n][1] = fmaf(sum.y, inv, st.l[n][1]);
   }
 }
 
 // One block of codes in shared memory; the first N of the item's row groups are in use.
 template <int N, int NT>
-__device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
+__device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const Rows& rows,
                                       const unsigned char* page, float2 scale, int t0, bool edge) {
   const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   float s[2][N][4];
@@ -280,26 +314,26 @@ __device__ __forceinline__ uint32_t largest(uint32_t m, const uint4& v) {
 
 // The softmax of the open block's scores, in which every token has factors of its own: ks and
 // 2^lift, of tokens 16 h + 8 i + gid.  The reference is the row's best token by x + log2 of its
-// value's factor, whose two parts stay apart until the weights are written: so is their sum
-// exact where scores are large.
+// value's factor.
 template <int NT>
 __device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
-                                             const Rows<NT>& rows, float (&s)[2][NT][4], int t0,
+                                             const Rows& rows, float (&s)[2][NT][4], int t0,
                                              const float (&ks)[2][2], const int (&lift)[2][2],
-                                             uint32_t (&w)[2][NT][2], float (&unit)[NT][2]) {
+                                             uint32_t (&w)[2][NT][2]) {
   const int gid = (threadIdx.x & 31) >> 2;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     float y[2][4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+      const int pos = rows.pos(p, n, j);
       float best = -INFINITY, best_lv = 0.0f;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int t = t0 + 16 * h + 8 * i + gid, pos = rows.pos[n][j];
-          float x = s[h][n][j + 2 * i] * fmaxf(ks[h][i] * st.f[n][j], kLeastFactor);
+          const int t = t0 + 16 * h + 8 * i + gid;
+          float x = __fmul_rn(s[h][n][j + 2 * i], fmaxf(ks[h][i] * st.f[n][j], kLeastFactor));
           if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks)) x = -INFINITY;
           const float lv = (float)-lift[h][i];
           if ((x - best) + (lv - best_lv) > 0.0f) best = x, best_lv = lv;
@@ -312,13 +346,11 @@ __device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
         const float d = (x - best) + (lv - best_lv);
         if (d > 0.0f || (d == 0.0f && x > best)) best = x, best_lv = lv;
       }
-      unit[n][j] = 1.0f;
-      if (best == -INFINITY) {  // no token is seen
-        best = 0.0f;
+      if (best > -INFINITY) {  // a token is seen
+        st.m[n][j] = best;
+        st.e[n][j] = best_lv;
       } else {
-        const float m = best + best_lv;
-        unit[n][j] = exp2_fast((best - m) + best_lv);
-        st.m[n][j] = m;
+        best = 0.0f;
       }
       float sum = 0.0f;
 #pragma unroll
@@ -330,7 +362,7 @@ __device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
           sum = fmaf(x, pow2(lift[h][i]), sum);
           y[h][j + 2 * i] = x;
         }
-      st.l[n][j] = sum * unit[n][j];
+      st.l[n][j] = sum;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -343,7 +375,7 @@ __device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
 // The block of 16-bit tokens t0 .. L - 1 (fewer than 32), from the ring's rows; the item's
 // first, so its results are its own.
 template <int NT, bool BF16>
-__device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, const Rows<NT>& rows,
+__device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, const Rows& rows,
                                         const uint16_t* k, const uint16_t* v, int t0, int L) {
   const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3, valid = L - t0;
   const auto load = [&](const uint16_t* base, int r, int part) {
@@ -409,8 +441,7 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
     }
   }
   uint32_t w[2][NT][2];
-  float unit[NT][2];
-  tail_weights<NT>(p, st, rows, s, t0, ks, lift, w, unit);
+  tail_weights<NT>(p, st, rows, s, t0, ks, lift, w);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if (16 * h >= valid) break;
@@ -442,12 +473,6 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
       }
     }
   }
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) st.o[n][i][j] *= unit[n][j & 1];
 }
 
 // Queries of an item's row group n: row 8 n + gid's channels 32 tig .. 32 tig + 31, bf16 ones
@@ -486,7 +511,7 @@ __device__ __forceinline__ float load_group(const AttnParams& p, const Seq& q, i
 // An item's queries, its rows' factors and positions, and empty results.  By all threads.
 template <int NT, bool BF16>
 __device__ __forceinline__ void begin_item(const AttnParams& p, const Seq& q, int head,
-                                           Smem<NT>& sm, State<NT>& st, Rows<NT>& rows) {
+                                           Smem<NT>& sm, State<NT>& st, Rows& rows) {
   const int lane = threadIdx.x & 31, tig = lane & 3;
   if constexpr (!State<NT>::kOwnQueries) {
     const int warp = threadIdx.x >> 5;
@@ -500,6 +525,7 @@ __device__ __forceinline__ void begin_item(const AttnParams& p, const Seq& q, in
     __syncthreads();
     st.shared_q = &sm.q[0][0][0];
   }
+  rows.first = q.L - q.n;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     float f = 1.0f;
@@ -512,8 +538,8 @@ __device__ __forceinline__ void begin_item(const AttnParams& p, const Seq& q, in
         else g = sm.qf[8 * n + 2 * tig + j];
       }
       st.f[n][j] = p.c.scale_log2 / g;
-      rows.pos[n][j] = q.L - q.n + token_of_row(p, 8 * n + 2 * tig + j);
       st.m[n][j] = kNone;
+      st.e[n][j] = 0.0f;
       st.l[n][j] = 0.0f;
     }
 #pragma unroll
@@ -674,7 +700,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
 #pragma unroll 1
   for (; w.next(p); w.advance(p)) {
     State<NT> st;
-    Rows<NT> rows;
+    Rows rows;
     begin_item<NT, BF16>(p, w.q, w.head, sm, st, rows);
     const int whole = whole_units(w);
     if (warp == kWarps - 1 && whole < w.i1) {
@@ -717,9 +743,14 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         float l = st.l[n][j];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        // one number for the maximum from here on; what it leaves of the two goes to sum and
+        // results
+        const float m = st.m[n][j] + st.e[n][j];
+        st.e[n][j] += st.m[n][j] - m;
+        st.m[n][j] = m;
         if (gid == 0) {
-          sm.m[warp][8 * n + 2 * tig + j] = st.m[n][j];
-          sm.l[warp][8 * n + 2 * tig + j] = l;
+          sm.m[warp][8 * n + 2 * tig + j] = m;
+          sm.l[warp][8 * n + 2 * tig + j] = l * exp2_fast(st.e[n][j]);
         }
       }
     __syncthreads();
@@ -736,7 +767,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         for (int k = 0; k < kWarps; ++k) l = fmaf(sm.l[k][r], exp2_fast(sm.m[k][r] - m), l);
         mm[n][j] = m;
         ll[n][j] = l;
-        const float g = exp2_fast(st.m[n][j] - m);
+        const float g = exp2_fast((st.m[n][j] - m) + st.e[n][j]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           st.o[n][i][j] *= g;

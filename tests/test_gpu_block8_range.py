@@ -1,6 +1,6 @@
 """Attention over the block-8 cache at the ends of its inputs' range: open blocks (16-bit
-tokens in the ring) whose elements lie far apart, and factors of scores that leave fp32.  By both
-kernels: up to 32 query rows a kv-head, and more, of one row tile and of two.
+tokens in the ring) whose elements lie far apart, factors of scores that leave fp32, very large
+scores.  By both kernels: up to 32 query rows a kv-head, and more, of one row tile and of two.
 
 Tolerance: a weight is rounded to fp16, its score to fp32, as in test_gpu_block8.py: 2^-11 +
 2^-14 of sum p |v| and half a step of the result (at least half of fp16's smallest, 2^-25).
@@ -166,3 +166,63 @@ def test_the_smallest_softmax_scales(kvq_lib, kind, dtype, scale):
     L = 32 * 20 + 21
     Case(dtype, gq, 0.01 * randn(20, L, 128), randn(21, L, 128), batch).attend(
         randn(22, n, gq, 128), scale=scale)
+
+
+# Keys are 448 times a power of two in every channel, so that codes, scales and the sum
+# over the channels are exact and tokens of one kind have the same score to the bit.
+LARGE = {"fp16": ((8.0, 4096.0, 0.0), (128.0, 65504.0, 0.0), (8.0, 4096.0, 1000.0)),
+         "bf16": ((8.0, 4096.0, 0.0), (2.0 ** 50, 2.0 ** 50, 0.0), (2.0 ** 40, 2.0 ** 55, 1e3))}
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("dtype,i", [(t, i) for t in LARGE for i in range(3)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("L", [32 * 5, 32 * 20 + 14, 32 * 70 + 9])
+def test_large_scores(kvq_lib, kind, dtype, i, sign, L):
+    """Scores of 2^28 and far beyond: equal ones share the weight, the largest takes it all."""
+    gq, n, batch = KINDS[kind]
+    step, q_size, scale = LARGE[dtype][i]
+    q = np.full((n, gq, 128), sign * q_size)
+    v = randn(23, L, 128)
+    k = np.full((L, 128), 448.0 * step)
+    Case(dtype, gq, k, v, batch).attend(q, scale=scale)                      # all equal
+    Case(dtype, gq, -k, v, batch).attend(q, scale=scale, window=70, sinks=2)
+    half = np.arange(L) % 64 < 32
+    if sign > 0:
+        # the blocks' scales differ, and so do the values'
+        k[half] *= 0.5
+        v[~half] *= 8.0
+        Case(dtype, gq, k, v, batch).attend(q, scale=scale)
+        # one token above all others, in a block and in the open one
+        for at in (40, L - n - 1):
+            k = np.full((L, 128), 224.0 * step)
+            k[at] = 448.0 * step
+            Case(dtype, gq, k, v, batch).attend(q, scale=scale)
+    # some queries' scores are large, the others' are not
+    q = q.copy()
+    q[::2, ::2] = 2.0 ** -6 / step
+    Case(dtype, gq, np.full((L, 128), 448.0 * step), v, batch).attend(q, scale=scale)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_scores_grow_along_the_text(kvq_lib, kind):
+    """The reference moves from ordinary scores to very large ones, block by block."""
+    gq, n, batch = KINDS[kind]
+    L = 32 * 40 + 9
+    k = 7.0 * 2.0 ** (np.arange(L) // 64)[:, None] * np.ones((L, 128))
+    v, q = randn(24, L, 128), np.ones((n, gq, 128))
+    v *= 2.0 ** (np.arange(L) // 32 % 3 * 4)[:, None]
+    Case("bf16", gq, k, v, batch).attend(q, mixed=True)
+    Case("bf16", gq, k[::-1].copy(), v, batch).attend(q, mixed=True)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("L", [32 * 20, 32 * 20 + 14])
+def test_scores_far_below_zero(kvq_lib, kind, L):
+    """Queries that see nothing of the open block or of a step, all scores about -300."""
+    gq, n, batch = KINDS[kind]
+    k, v, q = -27.0 + randn(25, L, 128), randn(26, L, 128), np.ones((n, gq, 128))
+    for dtype in ("fp16", "bf16"):
+        case = Case(dtype, gq, k, v, batch)
+        case.attend(q)
+        case.attend(q, window=33, sinks=3)
