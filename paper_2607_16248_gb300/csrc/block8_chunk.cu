@@ -235,6 +235,17 @@ __device__ __forceinline__ void open_block(const uint16_t* rows, int valid, unsi
     }
   }
 }
+// Whether a block's values are all zero; for a warp of the keys (the values' loads it
+// just before, so it is near).
+__device__ __forceinline__ bool no_value(const uint8_t* codes) {
+  uint32_t any = 0u;
+#pragma unroll 2
+  for (int k = 0; k < 8; ++k) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>(codes + 512 * k) + (threadIdx.x & 31));
+    any |= x.x | x.y | x.z | x.w;
+  }
+  return !__any_sync(0xffffffffu, (any & 0x7f7f7f7fu) != 0u);
+}
 __device__ __forceinline__ void zero_block(unsigned char* tile, int j) {
   const int lane = threadIdx.x & 31, m = lane & 15;
 #pragma unroll 1
@@ -318,6 +329,9 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
         }
         // (the scores' product waits for the keys' warps alone: they write all of it; the values'
         // factors of the open block are waited for)
+        if (key && at0 >= 0 && scale.y == 1.0f &&
+            no_value(p.c.cache.v_codes + (long long)at0 * (kGroup * kHeadDim)))
+          scale.y = kNoValue;
         if (key && lane == 0)
           s.scale[n & (kScaleTiles - 1)][j] =
               none   ? make_float4(1.0f, -INFINITY, 1.0f, 0.0f)

@@ -310,7 +310,7 @@ __device__ __forceinline__ int key_lift(uint32_t bits) {
 }
 template <bool BF16>
 __device__ __forceinline__ int value_lift(uint32_t bits) {
-  return bits ? lift_log2<BF16>(bits, -80) : 60;
+  return bits ? lift_log2<BF16>(bits, -80) : 60;  // 2^-60: kNoValue
 }
 template <bool BF16>
 __device__ __forceinline__ uint32_t lifted2(uint32_t u, float f) {
@@ -324,6 +324,10 @@ __device__ __forceinline__ uint4 lifted8(const uint4& v, float f) {
   return make_uint4(lifted2<BF16>(v.x, f), lifted2<BF16>(v.y, f), lifted2<BF16>(v.z, f),
                     lifted2<BF16>(v.w, f));
 }
+// What stands for the scale of a block whose values are all zero.  By the format it is 1, but a
+// weight is held with its value's scale in it, and beside small values those of a large
+// scale would lose the others' bits.
+constexpr float kNoValue = 0x1p-60f;
 // A score's factor in the exponent is at least this: masked scores are -inf, and their product
 // with 0 would be NaN; no score is large enough to show the difference.
 constexpr float kLeastFactor = 0x1p-126f;

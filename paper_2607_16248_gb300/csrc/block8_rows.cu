@@ -226,6 +226,17 @@ __device__ __forceinline__ void weights(const AttnParams& p, State<NT>& st, cons
   }
 }
 
+// Whether a block's values are all zero; for a warp.
+__device__ __forceinline__ bool no_value(const unsigned char* codes) {
+  uint32_t any = 0u;
+#pragma unroll
+  for (int k = 0; k < kHalfPage / 512; ++k) {
+    const uint4 x = reinterpret_cast<const uint4*>(codes + 512 * k)[threadIdx.x & 31];
+    any |= x.x | x.y | x.z | x.w;
+  }
+  return !__any_sync(0xffffffffu, (any & 0x7f7f7f7fu) != 0u);
+}
+
 // One block of codes in shared memory; the first N of the item's row groups are in use.
 template <int N, int NT>
 __device__ __forceinline__ void block(const AttnParams& p, State<NT>& st, const Rows& rows,
@@ -719,8 +730,9 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
           lost = true;
           break;
         }
-        const float2 scale = sm.scale[warp][slot];
+        float2 scale = sm.scale[warp][slot];
         if (scale.x > 0.0f) {
+          if (scale.y == 1.0f && no_value(sm.page[warp][slot] + kHalfPage)) scale.y = kNoValue;
           const bool edge = t0 + kGroup - 1 > w.s.p0 ||
                             (p.c.window && t0 <= w.s.p1 - p.c.window && t0 + kGroup > p.c.sinks);
           block<N, NT>(p, st, rows, sm.page[warp][slot], scale, t0, edge);

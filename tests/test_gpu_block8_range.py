@@ -147,6 +147,23 @@ def test_values_of_one_size_beside_an_open_block(kvq_lib, kind, L, dtype, size):
 
 
 @pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("L", [32 * 20, 32 * 20 + 20])
+@pytest.mark.parametrize("dtype,size", [("bf16", 2.0 ** -40), ("bf16", 1.0), ("bf16", 2.0 ** 40),
+                                        ("fp16", 2.0 ** -14), ("fp16", 1.0)])
+def test_blocks_and_tokens_of_no_value(kvq_lib, kind, L, dtype, size):
+    """A block whose values are all zero has scale 1; its weights count all the same."""
+    gq, n, batch = KINDS[kind]
+    k, v, q = 2.0 * randn(14, L, 128), size * randn(15, L, 128), randn(16, n, gq, 128)
+    v[32:64] = 0.0
+    v[-7:-3] = 0.0
+    Case(dtype, gq, k, v, batch).attend(q)
+    # a block of scale 1 that does hold something
+    v[64:96] *= 448.0 / np.abs(v[64:96]).max() if size == 1.0 else 1.0
+    v[64, 3] = 448.0 if size == 1.0 else v[64, 3]
+    Case(dtype, gq, k, v, batch).attend(q, mixed=True)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
 @pytest.mark.parametrize("q_size,k_size", [(-85, -40), (-90, -55), (-100, -100), (-30, -110),
                                            (60, -120)])
 @pytest.mark.parametrize("window", [0, 40])
