@@ -670,8 +670,9 @@ kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cach
  *   workspace   device, >= kvq_block8_workspace_bytes(cfg, max_new), zeroed once by
  *               kvq_workspace_init; calls sharing it must not overlap on the GPU.
  * Lengths and starts are read on the device; the call can be captured in a CUDA graph.
- * batch * n_kv_heads * (7 max_len / 32 + 16) times the row tiles of max_new must be below
- * 2^31 (KVQ_ERR_SHAPE).
+ * batch * n_kv_heads * (7 max_len / 32 + 16) must be below 2^31, and with more than 32 rows
+ * r = max_new * n_q_heads / n_kv_heads so must batch * n_kv_heads * (max_len / 128 + 3) times
+ * r / 256 (r / 128 up to 128 rows), quotients rounded up (KVQ_ERR_SHAPE).
  */
 typedef struct kvq_block8_attn_params {
   int32_t window;      /* newest tokens seen, the query's own included; 0: all */

@@ -143,11 +143,15 @@ AttnParams params_of(const AttnCall& call, int ctas, int item_rows, void* worksp
 size_t attn_workspace_bytes(const Dims8& d, int max_new, int sm_count) {
   return plan_of(d, max_new, sm_count).total;
 }
+// Each kernel counts all of its items' units in 32 bits: the first a row tile a sequence, in
+// blocks, the second row tiles of `chunk` rows in tiles of 128 tokens.
 long long attn_most_units(const Dims8& d, int max_new) {
   const Plan plan = plan_of(d, max_new, 1);
-  const long long tiles =
-      plan.many ? ((long long)max_new * d.gq + plan.chunk - 1) / plan.chunk : 1;
-  return (long long)d.batch * d.hkv * ((long long)d.max_blocks * kMostWeight + 16) * tiles;
+  const long long pairs = (long long)d.batch * d.hkv, blocks = d.max_blocks;
+  const long long few = pairs * (blocks * kMostWeight + kRowsItemCost);
+  if (!plan.many) return few;
+  const long long tiles = ((long long)max_new * d.gq + plan.chunk - 1) / plan.chunk;
+  return std::max(few, pairs * tiles * ((blocks + 3) / 4 + kChunkItemCost));
 }
 
 cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream) {

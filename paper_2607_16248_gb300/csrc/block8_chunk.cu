@@ -80,7 +80,7 @@ using chunk::unpair;
 using chunk::warp_arrive;
 
 constexpr int kTok = 7;       // tiles of 128 tokens
-constexpr int kItemCost = 3;  // of an item in tiles
+constexpr int kItemCost = kChunkItemCost;
 constexpr int kScaleTiles = 8;  // tiles whose scales are kept: loading is at most five ahead
 constexpr int kRegsLoad = 104, kRegsSoftmax = 112;
 static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kLoadWarps * kRegsLoad + 4 * kRegsIssue) <=

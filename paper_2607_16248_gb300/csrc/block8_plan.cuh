@@ -23,6 +23,9 @@ struct Split {
 };
 
 constexpr int kMostWeight = 7;  // units of a block with four groups of eight rows
+// Fixed cost of an item in units.  Few rows (a block's are 4 to 7): queries, merge.  Many
+// (units are tiles of 128 tokens): queries in, results out, the pipeline's filling.
+constexpr int kRowsItemCost = 16, kChunkItemCost = 3;
 
 struct AttnParams {
   AttnCall c;

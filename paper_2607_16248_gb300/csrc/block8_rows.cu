@@ -44,7 +44,7 @@ namespace block8 {
 namespace {
 
 constexpr int kTok = 5;            // 32 tokens a unit
-constexpr int kItemCost = 16;      // of an item in units (a block's are 4 to 7): queries, merge
+constexpr int kItemCost = kRowsItemCost;
 constexpr int kHalfPage = kGroup * kHeadDim;  // bytes of a block's keys (or values)
 constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
 constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
