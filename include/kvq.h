@@ -597,7 +597,11 @@ typedef struct kvq_block8_cache {
  * outside all ranges are left alone, and so is a sequence without new tokens.
  * Ranges that are out of order, reach outside [0, n_tokens] or hold more than max_new
  * tokens set KVQ_FLAG_BAD_BATCH, a length above max_len sets KVQ_FLAG_OVERFLOW; the
- * calls leave such a sequence's rows and cache alone.
+ * calls leave such a sequence's rows and cache alone.  Behind a start out of order the
+ * ranges of other sequences may overlap.  They are appended in order, each as a whole,
+ * until their blocks with new tokens would be more than s ((max_new + 30) / 32 + 1) or
+ * n_tokens / 32 + 2 s in all, s = min(batch, n_tokens); a row of q goes by the first
+ * that takes it, and in a row of attention's outputs their results mix.
  */
 typedef struct kvq_block8_batch {
   const int32_t* lengths; /* device [batch]: tokens of each sequence, new ones included */

@@ -338,12 +338,14 @@ struct Share {
   int b, left;
 };
 
-// Parts `part` .. end - 1 (2 h: keys of kv-head h, 2 h + 1: its values) of unit `unit` (the
-// batch's blocks with new tokens, in order).  The warps look through 32 sequences each.
+// Parts `part` .. end - 1 (2 h: keys of kv-head h, 2 h + 1: its values) of unit `unit` of
+// `units` (the batch's blocks with new tokens, in order).  The warps look through 32 sequences
+// each.  Where ranges overlap there may be more blocks than units: a sequence that does not
+// fit is left alone whole.
 template <bool BF16, bool PAIRED>
-__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int part, int end,
-                                        Share& sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int units, int part,
+                                        int end, Share& sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, place = unit;
 #pragma unroll 1
   for (int b0 = 0; b0 < call.d.batch; b0 += 32 * kWarps) {
     const int b = b0 + 32 * warp + lane;
@@ -377,6 +379,7 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
     __syncthreads();
     const Seq q = sh.s;
     const int old = q.L - q.n, first = old / kGroup, done = q.L / kGroup;
+    if (place - sh.left + blocks_of(q) > units) return;
     int blk = first + sh.left;
     // the block whose ring slots hold the first rows of a begun block that is completed
     int heir = done - ((done - first) & 1);
@@ -399,9 +402,19 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int pa
   }
 }
 
+// The blocks of sequences 0 .. n - 1, for a warp.
+__device__ __noinline__ long long blocks_until(const AppendCall& call, int n) {
+  long long sum = 0;
+#pragma unroll 1
+  for (int b = threadIdx.x & 31; b < n; b += 32) sum += blocks_of(append_seq(call, b));
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
+}
+
 // Queries of token `row`, heads h0 .. h0 + 7.
 template <bool BF16, bool PAIRED>
-__device__ __forceinline__ void query_task(const AppendCall& call, int row, int h0) {
+__device__ __forceinline__ void query_task(const AppendCall& call, int units, int row, int h0) {
   const int lane = threadIdx.x & 31, half = lane >> 4;
   const Lane l = lane_of(lane & 15, call.p.rot_dim >> 1, call.p.paired);
   const uint16_t* src = call.p.q + row * call.p.q_stride[0];
@@ -417,24 +430,31 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
       x[i][1] = *reinterpret_cast<const uint2*>(r + l.g1);
     }
   }
-  int b = -1;
+  // the first sequence that takes the row (they may share it only behind a start out of order)
+  Seq s{0, 0, 0, 0};
   if (!call.batch.starts) {
-    b = row / call.batch.max_new;
+    s = append_seq(call, row / call.batch.max_new);
   } else {
+    bool ordered = true;
 #pragma unroll 1
-    for (int b0 = 0; b0 < call.d.batch; b0 += 32) {
+    for (int b0 = 0; b0 < call.d.batch && s.n == 0; b0 += 32) {
       const int i = b0 + lane;
-      const bool mine = i < call.d.batch && row >= __ldg(call.batch.starts + i) &&
-                        row < __ldg(call.batch.starts + i + 1);
-      const unsigned who = __ballot_sync(0xffffffffu, mine);
-      if (who) {
-        b = b0 + __ffs(who) - 1;
-        break;
+      bool mine = false, down = false;
+      if (i < call.d.batch) {
+        const int begin = __ldg(call.batch.starts + i), end = __ldg(call.batch.starts + i + 1);
+        mine = row >= begin && row < end;
+        down = end < begin;
+      }
+      ordered = ordered && !__any_sync(0xffffffffu, down);
+      unsigned who = __ballot_sync(0xffffffffu, mine);
+#pragma unroll 1
+      for (; who && s.n == 0; who &= who - 1) {
+        const int b = b0 + __ffs(who) - 1;
+        s = append_seq(call, b);
+        if (s.n && !ordered && blocks_until(call, b + 1) > units) return;  // nor do later ones
       }
     }
-    if (b < 0) return;
   }
-  const Seq s = append_seq(call, b);
   if (s.n == 0) return;
   const int pos = s.L - s.n + row - s.row;
   if (l.rotate) {
@@ -457,7 +477,8 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int row, int 
 // word.
 template <bool BF16, bool PAIRED>
 __global__ void __launch_bounds__(32 * kWarps, kPlaces)
-append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int parts, int groups) {
+append_kernel(const __grid_constant__ AppendCall call, int units, int kv_ctas, int parts,
+              int groups) {
   __shared__ Share share;
   if (blockIdx.x == gridDim.x - 1) {
     for (int b = threadIdx.x; b < call.d.batch; b += 32 * kWarps) {
@@ -467,19 +488,20 @@ append_kernel(const __grid_constant__ AppendCall call, int kv_ctas, int parts, i
   } else if ((int)blockIdx.x < kv_ctas) {
     const int all = 2 * call.d.hkv, shares = (all + parts - 1) / parts;
     const int unit = (int)blockIdx.x / shares, part = ((int)blockIdx.x - unit * shares) * parts;
-    kv_task<BF16, PAIRED>(call, unit, part, min(part + parts, all), share);
+    kv_task<BF16, PAIRED>(call, unit, units, part, min(part + parts, all), share);
   } else {
     const int task = ((int)blockIdx.x - kv_ctas) * kWarps + ((int)threadIdx.x >> 5);
     const int row = task / groups;
     if (row < call.batch.n_tokens)
-      query_task<BF16, PAIRED>(call, row, (task - row * groups) * kQueryHeads);
+      query_task<BF16, PAIRED>(call, units, row, (task - row * groups) * kQueryHeads);
   }
 }
 
 }  // namespace
 
 cudaError_t launch_append(const AppendCall& call, int sm_count, cudaStream_t stream) {
-  // A sequence of n new tokens touches at most (n + 30) / 32 + 1 blocks.
+  // A sequence of n new tokens touches at most (n + 30) / 32 + 1 blocks (no two the same rows,
+  // unless a start is out of order).
   const long long tokens = call.batch.n_tokens;
   const long long seqs = tokens < call.d.batch ? tokens : call.d.batch;
   const long long units = std::min(tokens / kGroup + 2 * seqs,
@@ -498,7 +520,7 @@ cudaError_t launch_append(const AppendCall& call, int sm_count, cudaStream_t str
                           ? (call.p.paired ? append_kernel<true, true> : append_kernel<true, false>)
                           : (call.p.paired ? append_kernel<false, true>
                                            : append_kernel<false, false>);
-  kernel<<<grid, 32 * kWarps, 0, stream>>>(call, kv_ctas, parts, groups);
+  kernel<<<grid, 32 * kWarps, 0, stream>>>(call, (int)units, kv_ctas, parts, groups);
   return cudaGetLastError();
 }
 
