@@ -710,7 +710,7 @@ __device__ __forceinline__ void load_role(const Params& p, Smem& s, int u0, int 
       if (i >= w.i1) return kNone;
       const int t0 = token(i);
       if (t0 >= lq || !seen(t0)) return kNone;
-      return table ? __ldg(table + (t0 >> 5)) : t0 >> 5;
+      return table ? max(__ldg(table + (t0 >> 5)), kNone + 1) : t0 >> 5;  // (as much outside)
     };
     const auto address = [&](int e) -> const char* {
       if (e >= 0 && e < limit) return base + (long long)e * stride;
