@@ -21,8 +21,9 @@
 // is exact where it counts, however large they are.  In one sum with x, a product's rounding
 // and that of kLift - m passed fp16's range from scores of 2^28 on.
 //
-// The tokens behind the last whole block are a block of 16-bit elements that one warp loads
-// from the ring.  Values, and bf16 keys, go to fp16 times a power of two, each token's its own:
+// The tokens behind the last whole block are a block of 16-bit elements that two warps take
+// from the ring, 16 tokens each, by asynchronous copies ahead of the item: behind full rings each
+// load waits for microseconds, and their largest magnitudes make two passes.  Values, and bf16 keys, go to fp16 times a power of two, each token's its own:
 // what one token holds, seen or not, does not touch the others.
 //
 // What bounds it.  HBM where there is enough to read: 32 ragged chats of 2k to 32k tokens,
@@ -62,6 +63,7 @@ struct Smem {
   float4 merge[kMergers][NT * 8][32];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];
   uint2 q[NT <= 2 ? 1 : NT][8][32];  // queries of more row groups than fit registers
+  uint4 tail[2][2][16][16];  // 16 open tokens' keys and values each: chunk c of row r at c ^ r mod 8
   float qf[8 * NT];
   float2 scale[kWarps][kSlots];
   uint64_t full[kWarps][kSlots];
@@ -323,33 +325,31 @@ __device__ __forceinline__ uint32_t largest(uint32_t m, const uint4& v) {
   return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
 
-// The softmax of the open block's scores, in which every token has factors of its own: ks and
-// 2^lift, of tokens 16 h + 8 i + gid.  The reference is the row's best token by x + log2 of its
+// The softmax of the scores of 16 open tokens from t0 on, each of which has factors of its own: ks
+// and 2^lift, of tokens 8 i + gid.  The reference is the row's best token by x + log2 of its
 // value's factor.
 template <int NT>
 __device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
-                                             const Rows& rows, float (&s)[2][NT][4], int t0,
-                                             const float (&ks)[2][2], const int (&lift)[2][2],
-                                             uint32_t (&w)[2][NT][2]) {
+                                             const Rows& rows, float (&s)[NT][4], int t0,
+                                             const float (&ks)[2], const int (&lift)[2],
+                                             uint32_t (&w)[NT][2]) {
   const int gid = (threadIdx.x & 31) >> 2;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    float y[2][4];
+    float y[4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int pos = rows.pos(p, n, j);
       float best = -INFINITY, best_lv = 0.0f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int t = t0 + 16 * h + 8 * i + gid;
-          float x = __fmul_rn(s[h][n][j + 2 * i], fmaxf(ks[h][i] * st.f[n][j], kLeastFactor));
-          if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks)) x = -INFINITY;
-          const float lv = (float)-lift[h][i];
-          if ((x - best) + (lv - best_lv) > 0.0f) best = x, best_lv = lv;
-          y[h][j + 2 * i] = x;
-        }
+      for (int i = 0; i < 2; ++i) {
+        const int t = t0 + 8 * i + gid;
+        float x = __fmul_rn(s[n][j + 2 * i], fmaxf(ks[i] * st.f[n][j], kLeastFactor));
+        if (t > pos || (p.c.window && t <= pos - p.c.window && t >= p.c.sinks)) x = -INFINITY;
+        const float lv = (float)-lift[i];
+        if ((x - best) + (lv - best_lv) > 0.0f) best = x, best_lv = lv;
+        y[j + 2 * i] = x;
+      }
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
         const float x = __shfl_xor_sync(0xffffffffu, best, o);
@@ -365,34 +365,54 @@ __device__ __forceinline__ void tail_weights(const AttnParams& p, State<NT>& st,
       }
       float sum = 0.0f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float lv = (float)-lift[h][i];
-          const float x = exp2_fast((y[h][j + 2 * i] - best) + (lv - best_lv) + kLift);
-          sum = fmaf(x, pow2(lift[h][i]), sum);
-          y[h][j + 2 * i] = x;
-        }
+      for (int i = 0; i < 2; ++i) {
+        const float lv = (float)-lift[i];
+        const float x = exp2_fast((y[j + 2 * i] - best) + (lv - best_lv) + kLift);
+        sum = fmaf(x, pow2(lift[i]), sum);
+        y[j + 2 * i] = x;
+      }
       st.l[n][j] = sum;
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        w[h][n][i] = transpose(pack16<false>(y[h][2 * i], y[h][2 * i + 1]));
+    for (int i = 0; i < 2; ++i) w[n][i] = transpose(pack16<false>(y[2 * i], y[2 * i + 1]));
   }
 }
 
-// The block of 16-bit tokens t0 .. L - 1 (fewer than 32), from the ring's rows; the item's
-// first, so its results are its own.
+// An item's open tokens: the first one's position, and how many.
+__device__ __forceinline__ int2 open_tokens(const Walk<kTok, kItemCost>& w) {
+  const int t0 = w.s.tile(w.s.n - 1) * kGroup;
+  return make_int2(t0, w.q.L - t0);
+}
+// The ring's rows of 16 of an item's open tokens (from the t-th on) on their way to shared
+// memory, by a warp; rows behind the last are zero.
+__device__ __forceinline__ void fetch_tail(const AttnParams& p, const Walk<kTok, kItemCost>& w,
+                                           int t, uint4 (&tail)[2][16][16]) {
+  const int lane = threadIdx.x & 31, c = lane & 15;
+  const int2 open = open_tokens(w);
+  const long long at =
+      (((long long)w.b * p.c.d.hkv + w.head) * kRing + ((open.x + t) & (kRing - 1))) * kHeadDim;
+#pragma unroll 1
+  for (int r = lane >> 4; r < 16; r += 2) {
+    const bool valid = t + r < open.y;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint16_t* src = (i ? p.c.cache.v_ring : p.c.cache.k_ring) + at + 8 * c +
+                            (valid ? r * kHeadDim : 0);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                       sptr(&tail[i][r][c ^ (r & 7)])),
+                   "l"(src), "r"(valid ? 16 : 0)
+                   : "memory");
+    }
+  }
+}
+
+// 16 open tokens from t0 on, from shared memory; the warp's first of the item, so its results are
+// its own.
 template <int NT, bool BF16>
 __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, const Rows& rows,
-                                        const uint16_t* k, const uint16_t* v, int t0, int L) {
-  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3, valid = L - t0;
-  const auto load = [&](const uint16_t* base, int r, int part) {
-    return r < valid ? *reinterpret_cast<const uint4*>(base + r * kHeadDim + part)
-                     : make_uint4(0u, 0u, 0u, 0u);
-  };
+                                           const uint4 (&tail)[2][16][16], int t0) {
+  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const auto load = [&](int i, int r, int chunk) { return tail[i][r][chunk ^ (r & 7)]; };
   // the largest magnitude of a row of which four lanes hold a quarter each
   const auto row_largest = [&](const uint4 (&x)[4]) {
     uint32_t m = 0u;
@@ -402,86 +422,70 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
   };
-  float s[2][NT][4], ks[2][2] = {{1.0f, 1.0f}, {1.0f, 1.0f}};
-  int lift[2][2] = {{0, 0}, {0, 0}};
+  float s[NT][4], ks[2] = {1.0f, 1.0f}, f[2] = {1.0f, 1.0f};
+  int lift[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int i = 0; i < 4; ++i) s[n][i] = 0.0f;
+  uint4 x[2][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[h][n][i] = 0.0f;
+  for (int e = 0; e < 2; ++e) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (16 * h >= valid) break;  // no token there
-    uint4 x[2][4];
+    for (int c = 0; c < 4; ++c) x[e][c] = load(1, 8 * e + gid, 4 * tig + c);
+    lift[e] = value_lift<BF16>(row_largest(x[e]));
+  }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+  for (int e = 0; e < 2; ++e) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x[e][c] = load(v, 16 * h + 8 * e + gid, 32 * tig + 8 * c);
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      lift[h][e] = value_lift<BF16>(row_largest(x[e]));
-#pragma unroll
-      for (int c = 0; c < 4; ++c) x[e][c] = load(k, 16 * h + 8 * e + gid, 32 * tig + 8 * c);
-    }
-    float f[2] = {1.0f, 1.0f};
+    for (int c = 0; c < 4; ++c) x[e][c] = load(0, 8 * e + gid, 4 * tig + c);
     if constexpr (BF16) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int z = key_lift<BF16>(row_largest(x[e]));
-        f[e] = pow2(z);
-        ks[h][e] = pow2(-z);
-      }
+      const int z = key_lift<BF16>(row_largest(x[e]));
+      f[e] = pow2(z);
+      ks[e] = pow2(-z);
     }
+  }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {  // 8 channels: two steps of the product
-      const uint32_t xw[4] = {x[0][c].x, x[0][c].y, x[0][c].z, x[0][c].w};
-      const uint32_t yw[4] = {x[1][c].x, x[1][c].y, x[1][c].z, x[1][c].w};
+  for (int c = 0; c < 4; ++c) {  // 8 channels: two steps of the product
+    const uint32_t xw[4] = {x[0][c].x, x[0][c].y, x[0][c].z, x[0][c].w};
+    const uint32_t yw[4] = {x[1][c].x, x[1][c].y, x[1][c].z, x[1][c].w};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t a0 = to_half2<BF16>(xw[2 * i], f[0]), a1 = to_half2<BF16>(yw[2 * i], f[1]);
-        const uint32_t a2 = to_half2<BF16>(xw[2 * i + 1], f[0]),
-                       a3 = to_half2<BF16>(yw[2 * i + 1], f[1]);
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t a0 = to_half2<BF16>(xw[2 * i], f[0]), a1 = to_half2<BF16>(yw[2 * i], f[1]);
+      const uint32_t a2 = to_half2<BF16>(xw[2 * i + 1], f[0]),
+                     a3 = to_half2<BF16>(yw[2 * i + 1], f[1]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const uint2 q = st.query(n, 2 * c + i);
-          mma(s[h][n], a0, a1, a2, a3, q.x, q.y);
-        }
+      for (int n = 0; n < NT; ++n) {
+        const uint2 q = st.query(n, 2 * c + i);
+        mma(s[n], a0, a1, a2, a3, q.x, q.y);
       }
     }
   }
-  uint32_t w[2][NT][2];
+  uint32_t w[NT][2];
   tail_weights<NT>(p, st, rows, s, t0, ks, lift, w);
+  uint4 v[2][2][2];
+  float g[2][2];  // of rows 8 i + 2 tig + e: lanes 4 (2 tig + e) know them
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (16 * h >= valid) break;
-    uint4 x[2][2][2];
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i >> 2][i >> 1 & 1][i & 1] =
-          load(v, 16 * h + 8 * (i >> 2) + 2 * tig + (i >> 1 & 1), 16 * gid + 8 * (i & 1));
-    float f[2][2];  // of rows 8 i + 2 tig + e: lanes 4 (2 tig + e) know them
+    for (int e = 0; e < 2; ++e) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int c = 0; c < 2; ++c) v[i][e][c] = load(1, 8 * i + 2 * tig + e, 2 * gid + c);
+      g[i][e] = pow2(__shfl_sync(0xffffffffu, lift[i], 8 * tig + 4 * e));
+    }
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        f[i][e] = pow2(__shfl_sync(0xffffffffu, lift[h][i], 8 * tig + 4 * e));
+  for (int c = 0; c < 2; ++c) {  // 8 channels each
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {  // 8 channels each
+    for (int k = 0; k < 4; ++k) {
+      const auto word = [&](int i, int e) {
+        const uint4& y = v[i][e][c];
+        return lifted2<BF16>(k == 0 ? y.x : k == 1 ? y.y : k == 2 ? y.z : y.w, g[i][e]);
+      };
+      const uint32_t w00 = word(0, 0), w01 = word(0, 1), w10 = word(1, 0), w11 = word(1, 1);
+      const uint32_t a0 = __byte_perm(w00, w01, 0x5410), a1 = __byte_perm(w00, w01, 0x7632);
+      const uint32_t a2 = __byte_perm(w10, w11, 0x5410), a3 = __byte_perm(w10, w11, 0x7632);
 #pragma unroll
-      for (int k2 = 0; k2 < 4; ++k2) {
-        const auto word = [&](int i, int e) {
-          const uint4& y = x[i][e][c];
-          return lifted2<BF16>(k2 == 0 ? y.x : k2 == 1 ? y.y : k2 == 2 ? y.z : y.w, f[i][e]);
-        };
-        const uint32_t w00 = word(0, 0), w01 = word(0, 1), w10 = word(1, 0), w11 = word(1, 1);
-        const uint32_t a0 = __byte_perm(w00, w01, 0x5410), a1 = __byte_perm(w00, w01, 0x7632);
-        const uint32_t a2 = __byte_perm(w10, w11, 0x5410), a3 = __byte_perm(w10, w11, 0x7632);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-          mma(st.o[n][4 * c + k2], a0, a1, a2, a3, w[h][n][0], w[h][n][1]);
-      }
+      for (int n = 0; n < NT; ++n) mma(st.o[n][4 * c + k], a0, a1, a2, a3, w[n][0], w[n][1]);
     }
   }
 }
@@ -589,39 +593,44 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
   // `entry` this lane's table entry of the 32 units from `entries` on.
   Walk<kTok, kItemCost>& ahead = sm.ahead[warp];
   int next = 0, limit = 0, entry = 0, entries = -1;
+  bool some;  // the share has a tile
   {
     Walk<kTok, kItemCost> first;
     first.begin(p, sm.start, u0, u1);
-    if (first.next(p)) {
+    some = first.next(p);
+    if (some) {
       next = first.i0 + warp;
       limit = whole_units(first);
     }
     ahead = first;
     __syncwarp();
   }
-  // An item's queries and 16-bit tokens come to L2 ahead of its blocks: behind full rings a
-  // load waits its turn of several microseconds.
+  // An item's queries come to L2 ahead of its blocks, its open tokens to shared memory if that
+  // is free (`held`: the first unit of the item whose tokens it has): behind full rings a load
+  // waits its turn of several microseconds.  The last two warps, which never have more blocks
+  // than the others, take 16 open tokens each.
+  const int half = warp - (kWarps - 2);
+  const auto has_tail = [&](const Walk<kTok, kItemCost>& f) {
+    const int open = open_tokens(f).y;
+    return half >= 0 && f.i1 == f.s.n && open < kGroup && open > 16 * half;
+  };
+  int held = -1;
   const auto fetch_small = [&](const Walk<kTok, kItemCost>& f) {
-    if (warp != kWarps - 1) return;
+    if (half < 0) return;
     const auto line = [](const void* at) {
       asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
     };
-    if (lane < f.q.n * p.c.d.gq) {
+    if (half && lane < f.q.n * p.c.d.gq) {
       const uint16_t* at = p.c.q + row_offset(p, p.c.q_stride, f.q.row, f.head, lane);
       line(at);
       line(at + 64);
     }
-    const int t0 = f.s.tile(f.s.n - 1) * kGroup, lines = 2 * (f.q.L - t0);
-    if (t0 + kGroup > f.q.L && f.i1 == f.s.n) {
-      const long long at =
-          (((long long)f.b * p.c.d.hkv + f.head) * kRing + (t0 & (kRing - 1))) * kHeadDim;
-      for (int i = lane; i < lines; i += 32) {
-        line(p.c.cache.k_ring + at + 64 * i);
-        line(p.c.cache.v_ring + at + 64 * i);
-      }
+    if (held < 0 && has_tail(f)) {
+      fetch_tail(p, f, 16 * half, sm.tail[half]);
+      held = f.base;
     }
   };
-  fetch_small(ahead);
+  if (some) fetch_small(ahead);
   // The next block goes to slot `slot`.
   const auto feed = [&](int slot) {
     if (next >= limit) {
@@ -714,11 +723,19 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     Rows rows;
     begin_item<NT, BF16>(p, w.q, w.head, sm, st, rows);
     const int whole = whole_units(w);
-    if (warp == kWarps - 1 && whole < w.i1) {
-      const int t0 = w.s.tile(whole) * kGroup;
-      const long long at =
-          (((long long)w.b * p.c.d.hkv + w.head) * kRing + (t0 & (kRing - 1))) * kHeadDim;
-      tail_block<NT, BF16>(p, st, rows, p.c.cache.k_ring + at, p.c.cache.v_ring + at, t0, w.q.L);
+    if (has_tail(w)) {
+      const auto copied = [] {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+      };
+      copied();
+      if (held != w.base) {  // (another item's, or none)
+        fetch_tail(p, w, 16 * half, sm.tail[half]);
+        copied();
+      }
+      tail_block<NT, BF16>(p, st, rows, sm.tail[half], open_tokens(w).x + 16 * half);
+      held = -1;
+      __syncwarp();
     }
     const auto blocks = [&](auto used) {
       constexpr int N = decltype(used)::value;
