@@ -768,6 +768,22 @@ kvq_status kvq_selftest_wait_timeout(uint32_t* flag, void* stream);
 kvq_status kvq_selftest_chunk_wait_timeout(int32_t role, uint32_t* flag, void* stream);
 
 /*
+ * kvq_selftest_block8_wait_timeout — kvq_block8_attn with waits of ~10 ms (1 to 2 s there) and
+ * an arrival left out in each CTA that has enough to do: by the few-rows kernel a warp's
+ * second block is awaited but not copied, by the many-rows kernel a quarter of the second
+ * tile of keys is not reported.  The waits run out, KVQ_FLAG_WAIT_TIMEOUT is set in the
+ * cache's flags, `out` is not valid, and the workspace is as any call leaves it.
+ * fp16, groups of up to 8, max_new times the group at most 8 or more than 32
+ * (KVQ_ERR_UNSUPPORTED).
+ */
+kvq_status kvq_selftest_block8_wait_timeout(const kvq_block8_config* cfg,
+                                            const kvq_block8_cache* cache,
+                                            const kvq_block8_batch* batch, const uint16_t* q,
+                                            uint16_t* out,
+                                            const kvq_block8_attn_params* params,
+                                            void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Offline drift metrics (Sec. 4.1 "Adaptive recovery-window selection",
  * Sec. 4.2 "Offline supervision and calibration").  Tooling for paired
  * traces: each row holds one decode step's FP16-cache logits z_fp and

@@ -836,10 +836,10 @@ size_t kvq_block8_workspace_bytes(const kvq_block8_config* cfg, int32_t max_new)
   return block8::attn_workspace_bytes(block8_dims(*cfg), max_new, sm_count());
 }
 
-kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
-                           const kvq_block8_batch* batch, const uint16_t* q, uint16_t* out,
-                           const kvq_block8_attn_params* p, void* workspace, size_t ws_bytes,
-                           void* stream) {
+static kvq_status block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
+                              const kvq_block8_batch* batch, const uint16_t* q, uint16_t* out,
+                              const kvq_block8_attn_params* p, void* workspace, size_t ws_bytes,
+                              void* stream, bool selftest) {
   kvq_status s = check_block8_config(cfg);
   if (s != KVQ_OK) return s;
   if ((s = check_block8_cache(*cfg, cache)) != KVQ_OK) return s;
@@ -883,9 +883,31 @@ kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache*
   trace("kvq_block8_attn batch %d tokens %d max_new %d window %d sinks %d heads %d/%d %s",
         cfg->batch, n, batch->max_new, call.window, call.sinks, d.hq, d.hkv,
         d.bf16 ? "bf16" : "fp16");
-  return cuda_status(
-      block8::launch_attn(call, sm_count(), workspace, static_cast<cudaStream_t>(stream)),
-      "kvq_block8_attn launch");
+  return cuda_status(block8::launch_attn(call, sm_count(), workspace,
+                                         static_cast<cudaStream_t>(stream), selftest),
+                     "kvq_block8_attn launch");
+}
+
+kvq_status kvq_block8_attn(const kvq_block8_config* cfg, const kvq_block8_cache* cache,
+                           const kvq_block8_batch* batch, const uint16_t* q, uint16_t* out,
+                           const kvq_block8_attn_params* p, void* workspace, size_t ws_bytes,
+                           void* stream) {
+  return block8_attn(cfg, cache, batch, q, out, p, workspace, ws_bytes, stream, false);
+}
+
+kvq_status kvq_selftest_block8_wait_timeout(const kvq_block8_config* cfg,
+                                            const kvq_block8_cache* cache,
+                                            const kvq_block8_batch* batch, const uint16_t* q,
+                                            uint16_t* out, const kvq_block8_attn_params* p,
+                                            void* workspace, size_t ws_bytes, void* stream) {
+  if (cfg && batch && (cfg->dtype != KVQ_F16 || (long long)cfg->n_q_heads > 8LL * cfg->n_kv_heads))
+    return fail(KVQ_ERR_UNSUPPORTED, "the self-test takes fp16 and groups of up to 8");
+  if (cfg && batch && cfg->n_kv_heads > 0) {
+    const long long rows = (long long)batch->max_new * (cfg->n_q_heads / cfg->n_kv_heads);
+    if (rows > 8 && rows <= 32)
+      return fail(KVQ_ERR_UNSUPPORTED, "the self-test takes up to 8 rows or more than 32");
+  }
+  return block8_attn(cfg, cache, batch, q, out, p, workspace, ws_bytes, stream, true);
 }
 
 kvq_status kvq_adjust_logits(const kvq_adjust_params* p, void* stream) {

@@ -38,7 +38,9 @@ cudaError_t launch_append(const AppendCall& call, int sm_count, cudaStream_t str
 size_t attn_workspace_bytes(const Dims8& d, int max_new, int sm_count);
 // The most units of work that a call's kernels can count.
 long long attn_most_units(const Dims8& d, int max_new);
-cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream);
+// selftest: with a short limit and an arrival that never comes, so that a wait runs out.
+cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream,
+                        bool selftest = false);
 
 #ifdef __CUDACC__
 // The rows [row, row + n) of sequence b, which has L tokens with them; n is 0 where it

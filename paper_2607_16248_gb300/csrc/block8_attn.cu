@@ -154,19 +154,20 @@ long long attn_most_units(const Dims8& d, int max_new) {
   return std::max(few, pairs * tiles * ((blocks + 3) / 4 + kChunkItemCost));
 }
 
-cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream) {
+cudaError_t launch_attn(const AttnCall& call, int sm_count, void* workspace, cudaStream_t stream,
+                        bool selftest) {
   const Plan plan = plan_of(call.d, call.batch.max_new, sm_count);
   AttnParams p = params_of(call, sm_count, plan.few, workspace);
   p.min_rows = 1;
   p.max_rows = plan.few;
   cudaError_t e = cudaSuccess;
   if (call.batch.starts || !plan.many) {
-    if ((e = launch_rows(p, sm_count, stream)) != cudaSuccess || !plan.many) return e;
+    if ((e = launch_rows(p, sm_count, stream, selftest)) != cudaSuccess || !plan.many) return e;
   }
   p = params_of(call, sm_count, plan.chunk, workspace);
   p.min_rows = plan.few + 1;
   p.max_rows = 1 << 30;
-  if ((e = launch_chunk(p, sm_count, stream)) != cudaSuccess) return e;
+  if ((e = launch_chunk(p, sm_count, stream, selftest)) != cudaSuccess) return e;
   const int rows = (int)std::min<long long>(plan.chunk, (long long)call.batch.max_new * call.d.gq);
   return launch_join(p, sm_count, rows, stream);
 }

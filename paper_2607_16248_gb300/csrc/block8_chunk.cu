@@ -99,7 +99,7 @@ struct Smem {
   int scan[32];
   ItemWalk walk[kSoftmaxWarps][2];     // a softmax warp's item and the next one
   Start start;
-  uint32_t tmem;
+  uint32_t tmem, limit;                // cycles of a bounded wait
   int abort;
   float4 scale[kScaleTiles][4];        // a block's s_k, log2 s_v, 1 / s_v; 1 for the open one
   float2 open[kScaleTiles][kGroup];    // its tokens' s_k (from the keys' warp), log2 s_v
@@ -115,7 +115,7 @@ __device__ __forceinline__ bool warp_wait(Smem& s, uint64_t* b, uint32_t parity)
     const uint32_t t0 = (uint32_t)clock();
 #pragma unroll 1
     while (!(ok = bar_try(b, parity))) {
-      if (*reinterpret_cast<volatile int*>(&s.abort) || (uint32_t)clock() - t0 > kWaitLimit) {
+      if (*reinterpret_cast<volatile int*>(&s.abort) || (uint32_t)clock() - t0 > s.limit) {
         *reinterpret_cast<volatile int*>(&s.abort) = 1;
         break;
       }
@@ -259,7 +259,7 @@ __device__ __forceinline__ void zero_block(unsigned char* tile, int j) {
 // is on its way.  The keys' warps leave the block's scales beside the tile.
 constexpr int kAhead = 2;
 
-template <bool BF16>
+template <bool BF16, bool TEST>
 __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, int u1, int j,
                                           bool key) {
   const int lane = threadIdx.x & 31;
@@ -346,7 +346,7 @@ __device__ __forceinline__ void load_role(const AttnParams& p, Smem& s, int u0, 
       if (key && at1 >= 0) scale = __ldg(reinterpret_cast<const float2*>(p.c.cache.scales) + at1);
       if (i >= w.i0) {
         fence_async();
-        warp_arrive(&full[buf]);
+        if (!TEST || !key || j != 1 || n != 1) warp_arrive(&full[buf]);
         ++n;
       }
       at0 = at1;
@@ -819,7 +819,8 @@ __device__ __forceinline__ void softmax_role(const AttnParams& p, Smem& s, int u
 // Kernel
 // ---------------------------------------------------------------------------
 
-template <bool BF16>
+// TEST: a short bound of the waits, and an arrival for the second tile of keys is left out.
+template <bool BF16, bool TEST>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_kernel(const __grid_constant__ AttnParams p) {
   extern __shared__ __align__(1024) unsigned char raw[];
@@ -844,6 +845,7 @@ chunk_kernel(const __grid_constant__ AttnParams p) {
     bar_init(&s.q_full, 4 << two);
     bar_init(&s.meet, kSoftmaxWarps);
     s.abort = 0;
+    s.limit = TEST ? kWaitLimit / 100 : kWaitLimit;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -867,7 +869,7 @@ chunk_kernel(const __grid_constant__ AttnParams p) {
     __syncwarp();
   } else if (warp < kIssueWarp) {
     chunk::regs_up<kRegsLoad>();
-    load_role<BF16>(p, s, u0, u1, warp & 3, warp < kSoftmaxWarps + 4);
+    load_role<BF16, TEST>(p, s, u0, u1, warp & 3, warp < kSoftmaxWarps + 4);
     __syncwarp();
   } else {
     chunk::regs_down<kRegsIssue>();
@@ -879,28 +881,31 @@ chunk_kernel(const __grid_constant__ AttnParams p) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
-template <bool BF16>
+template <bool BF16, bool TEST>
 cudaError_t launch(const AttnParams& p, int ctas, cudaStream_t stream) {
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = once_per_device(done, [] {
     const cudaError_t e = cudaFuncSetAttribute(
-        chunk_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+        chunk_kernel<BF16, TEST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
     if (e != cudaSuccess) return e;
     // the register shares wait for registers that a smaller launch would lack
     cudaFuncAttributes attr;
-    const cudaError_t ea = cudaFuncGetAttributes(&attr, chunk_kernel<BF16>);
+    const cudaError_t ea = cudaFuncGetAttributes(&attr, chunk_kernel<BF16, TEST>);
     if (ea != cudaSuccess) return ea;
     return attr.numRegs < kRegsLaunch ? cudaErrorInvalidConfiguration : cudaSuccess;
   });
   if (e != cudaSuccess) return e;
-  chunk_kernel<BF16><<<ctas, kThreads, sizeof(Smem), stream>>>(p);
+  chunk_kernel<BF16, TEST><<<ctas, kThreads, sizeof(Smem), stream>>>(p);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_chunk(const AttnParams& p, int ctas, cudaStream_t stream) {
-  return p.c.d.bf16 ? launch<true>(p, ctas, stream) : launch<false>(p, ctas, stream);
+cudaError_t launch_chunk(const AttnParams& p, int ctas, cudaStream_t stream, bool selftest) {
+  if (selftest)
+    return p.c.d.bf16 ? cudaErrorNotSupported : launch<false, true>(p, ctas, stream);
+  return p.c.d.bf16 ? launch<true, false>(p, ctas, stream)
+                    : launch<false, false>(p, ctas, stream);
 }
 
 }  // namespace block8

@@ -388,8 +388,8 @@ __device__ __forceinline__ void join_row(const AttnParams& p, int c0, int inside
 
 // Launchers of the kernels: few rows (block8_rows.cu), many (block8_chunk.cu).
 constexpr int kFewRows = 32;
-cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream);
-cudaError_t launch_chunk(const AttnParams& p, int ctas, cudaStream_t stream);
+cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream, bool selftest);
+cudaError_t launch_chunk(const AttnParams& p, int ctas, cudaStream_t stream, bool selftest);
 
 }  // namespace block8
 }  // namespace kvq

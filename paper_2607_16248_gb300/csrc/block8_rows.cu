@@ -51,6 +51,7 @@ constexpr float kLift = 7.0f;      // weights stay below 2^(kLift + kLag)
 constexpr float kLag = 8.0f;       // how far a score may pass the running maximum
 constexpr float kNone = -FLT_MAX;  // the maximum before any token
 constexpr long long kWaitCycles = 4000000000LL;  // bound of a wait (~2 s)
+constexpr long long kTestCycles = 20000000LL;    // in the self-test (~10 ms)
 
 // Eight warps with two slots each: 128 KB of copies on their way in an SM.  More only make
 // everything else wait behind them (ragged batch of 32 single tokens: 198 us; three slots
@@ -564,7 +565,8 @@ __device__ __forceinline__ void begin_item(const AttnParams& p, const Seq& q, in
   }
 }
 
-template <int NT, bool BF16>
+// TEST: a short bound, and no copies of the third warp's second block.
+template <int NT, bool BF16, bool TEST>
 __global__ void __launch_bounds__(32 * Smem<NT>::kWarps, 1)
 rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map,
             const __grid_constant__ CUtensorMap v_map) {
@@ -631,6 +633,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     }
   };
   if (some) fetch_small(ahead);
+  int fed = 0;  // TEST: this warp's blocks
   // The next block goes to slot `slot`.
   const auto feed = [&](int slot) {
     if (next >= limit) {
@@ -667,6 +670,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
                      "r"(2 * kHalfPage)
                      : "memory");
+        if (TEST && warp == 2 && fed++ == 1) return;
         asm volatile(
             "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], "
             "[%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -709,7 +713,7 @@ rows_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     bool ok = arrived(i, parity);
     if (!ok) {
       const long long begun = clock64();
-      while (!(ok = arrived(i, parity)) && clock64() - begun < kWaitCycles) {
+      while (!(ok = arrived(i, parity)) && clock64() - begun < (TEST ? kTestCycles : kWaitCycles)) {
       }
     }
     return __all_sync(0xffffffffu, ok) != 0;
@@ -915,19 +919,19 @@ cudaError_t make_map(CUtensorMap* map, const void* base, long long rows) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int NT, bool BF16>
+template <int NT, bool BF16, bool TEST = false>
 cudaError_t launch(const AttnParams& p, int ctas, cudaStream_t stream) {
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = once_per_device(done, [] {
-    return cudaFuncSetAttribute(rows_kernel<NT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)sizeof(Smem<NT>));
+    return cudaFuncSetAttribute(rows_kernel<NT, BF16, TEST>,
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<NT>));
   });
   if (e != cudaSuccess) return e;
   CUtensorMap k, v;
   const long long rows = (long long)p.c.cache.n_pages * p.c.d.hkv * kGroup;
   if ((e = make_map(&k, p.c.cache.k_codes, rows)) != cudaSuccess) return e;
   if ((e = make_map(&v, p.c.cache.v_codes, rows)) != cudaSuccess) return e;
-  rows_kernel<NT, BF16><<<ctas, 32 * Smem<NT>::kWarps, sizeof(Smem<NT>), stream>>>(p, k, v);
+  rows_kernel<NT, BF16, TEST><<<ctas, 32 * Smem<NT>::kWarps, sizeof(Smem<NT>), stream>>>(p, k, v);
   return cudaGetLastError();
 }
 
@@ -938,7 +942,10 @@ cudaError_t launch_type(const AttnParams& p, int ctas, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream) {
+cudaError_t launch_rows(const AttnParams& p, int ctas, cudaStream_t stream, bool selftest) {
+  if (selftest)
+    return p.item_rows == 8 && !p.c.d.bf16 ? launch<1, false, true>(p, ctas, stream)
+                                           : cudaErrorNotSupported;
   switch (p.item_rows) {
     case 8: return launch_type<1>(p, ctas, stream);
     case 16: return launch_type<2>(p, ctas, stream);

@@ -38,6 +38,7 @@ EXPORTS = (
     "kvq_sample_max_vocab", "kvq_sample", "dgap_workspace_bytes",
     "dgap_restore", "kvq_drift_max_vocab", "kvq_drift_metrics", "kvq_drift_window",
     "kvq_selftest_wait_timeout", "kvq_selftest_chunk_wait_timeout",
+    "kvq_selftest_block8_wait_timeout",
 )
 NOALLOC_SCRATCH_BYTES = 4 << 20
 
@@ -168,6 +169,7 @@ def lib():
             "kvq_drift_max_vocab": (I32, []),
             "kvq_selftest_wait_timeout": (I32, [P, P]),
             "kvq_selftest_chunk_wait_timeout": (I32, [I32, P, P]),
+            "kvq_selftest_block8_wait_timeout": (I32, [cfg8_p, cache8_p, P, P, P, P, P, SZ, P]),
             "kvq_drift_metrics": (I32, [P, P, I32, I32, ctypes.POINTER(_DriftParams),
                                         P, P, P, P, P, P]),
             "kvq_drift_window": (I32, [P, I32, I32, F32, P, P, P]),
@@ -1060,6 +1062,20 @@ def selftest_wait_timeout(stream=None):
     flag = torch.zeros(1, dtype=torch.int32, device="cuda")
     _check(lib().kvq_selftest_wait_timeout(_dev(flag, torch.int32, "flag"), _stream(stream)))
     return flag
+
+
+def selftest_block8_wait_timeout(cache: Block8Cache, q, lengths, workspace, stream=None):
+    """kvq_selftest_block8_wait_timeout: kvq_block8_attn whose waits run out, as many new tokens
+    for each sequence; the flag is in ``cache.flags()``."""
+    n = q.shape[0]
+    batch, _ = _block8_batch(cache, n, lengths, None, None)
+    out = torch.empty_like(q)
+    qa, q0, q1 = _rows(q, n, cache.cfg.n_q_heads, cache.cfg.dtype, "q", cache.dev)
+    oa, o0, o1 = _rows(out, n, cache.cfg.n_q_heads, cache.cfg.dtype, "out", cache.dev)
+    ws = _list(workspace, None, torch.uint8, "workspace", cache.dev)
+    _launch(cache.dev, stream, lib().kvq_selftest_block8_wait_timeout, cache._cfg_ref,
+            cache._c_ref, batch, qa, oa, _ATTN.pack(0, 0, 0.0, q0, q1, o0, o1), ws,
+            workspace.numel())
 
 
 def selftest_chunk_wait_timeout(role, stream=None):
