@@ -581,7 +581,7 @@ typedef struct kvq_block8_config {
 typedef struct kvq_block8_cache {
   uint8_t* k_codes;           /* [n_pages][n_kv_heads][32][128] e4m3 */
   uint8_t* v_codes;           /* the same */
-  float* scales;              /* [n_pages][n_kv_heads][2]: keys', values'; > 0 */
+  float* scales;              /* [n_pages][n_kv_heads][2]: keys', values'; 2^-90 .. 2^90 */
   uint16_t* k_ring;           /* [batch][n_kv_heads][64][128] */
   uint16_t* v_ring;           /* the same */
   const int32_t* block_table; /* [batch][max_len / 32]: a block's page; entries of
@@ -665,10 +665,12 @@ kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cach
  * of the call sees are not read and need not be mapped.  In the others a key may be
  * anything where a query does not see it; values have to be finite for all of them.
  * A block mapped outside [0, n_pages) counts as unseen and sets KVQ_FLAG_BAD_PAGE.
- * Codes are exact in the fp16 operands, scales meet fp32 numbers, and bf16 queries and
- * ring rows go to fp16 times a power of two; the softmax weights (times their block's
- * value scale) are rounded once to fp16.  Sums, maxima and outputs are fp32, rounded once
- * to the type.
+ * Codes are exact in the fp16 operands, scales meet fp32 numbers; bf16 queries and keys and
+ * all values of the open block (the tokens in the ring) go to fp16 times a power of two,
+ * each row its own, so an element is good to 2^-40 of its row's largest (or of 2^-100, values
+ * 2^-80); the softmax weights (times their value's scale) are rounded once to fp16.  Sums,
+ * maxima and outputs are fp32, outputs rounded once to the type.  Scores may be as large as
+ * fp32 holds; their differences are those of the scores rounded to fp32.
  *   q, out      device [n_tokens][n_q_heads][128] with the strides below (as in
  *               kvq_block8_append); they must not overlap.
  *   workspace   device, >= kvq_block8_workspace_bytes(cfg, max_new), zeroed once by

@@ -243,3 +243,21 @@ def test_scores_far_below_zero(kvq_lib, kind, L):
         case = Case(dtype, gq, k, v, batch)
         case.attend(q)
         case.attend(q, window=33, sinks=3)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("L", [32 * 20, 32 * 20 + 14])
+@pytest.mark.parametrize("ks,vs", [(90, 90), (-90, -90), (90, -90), (0, -90), (-90, 0)])
+def test_scales_that_a_caller_chose(kvq_lib, kind, L, ks, vs):
+    """Blocks that somebody else filled may have scales of 2^-90 to 2^90."""
+    gq, n, batch = KINDS[kind]
+    ks, vs, blocks = 2.0 ** ks, 2.0 ** vs, L // 32
+    k, v, q = randn(27, L, 128), randn(28, L, 128), randn(29, n, gq, 128)
+    k[32 * blocks:] *= 128.0 * ks       # (about what the blocks hold)
+    v[32 * blocks:] *= 128.0 * vs
+    case = Case("bf16", gq, k, v, batch)
+    for i, to in ((0, ks), (1, vs)):
+        by = to / np64(case.cache.scales[:, 0, i])
+        case.cache.scales[:, 0, i] = to
+        case.seen[i][:32 * blocks] *= by.repeat(32)[:, None]
+    case.attend(2.0 * q / (128.0 * ks))
