@@ -402,14 +402,27 @@ __device__ __forceinline__ void kv_task(const AppendCall& call, int unit, int un
   }
 }
 
-// The blocks of sequences 0 .. n - 1, for a warp.
-__device__ __noinline__ long long blocks_until(const AppendCall& call, int n) {
-  long long sum = 0;
+// The first sequence that takes token `row`, for a warp: one whose range holds it, that is
+// appended and whose blocks fit (kv_task).  Where a start is out of order; n is 0 for none.
+__device__ __forceinline__ Seq taker_of(const AppendCall& call, int units, int row) {
+  const int lane = threadIdx.x & 31;
+  long long blocks = 0;
 #pragma unroll 1
-  for (int b = threadIdx.x & 31; b < n; b += 32) sum += blocks_of(append_seq(call, b));
+  for (int b0 = 0; b0 < call.d.batch; b0 += 32) {
+    const Seq s = append_seq(call, b0 + lane);
+    long long until = blocks_of(s);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, until, o);
+      if (lane >= o) until += y;
+    }
+    until += blocks;
+    const unsigned who = __ballot_sync(
+        0xffffffffu, s.n > 0 && row >= s.row && row < s.row + s.n && until <= units);
+    if (who) return append_seq(call, b0 + __ffs(who) - 1);
+    blocks = __shfl_sync(0xffffffffu, until, 31);
+  }
+  return Seq{0, 0, 0, 0};
 }
 
 // Queries of token `row`, heads h0 .. h0 + 7.
@@ -430,31 +443,31 @@ __device__ __forceinline__ void query_task(const AppendCall& call, int units, in
       x[i][1] = *reinterpret_cast<const uint2*>(r + l.g1);
     }
   }
-  // the first sequence that takes the row (they may share it only behind a start out of order)
-  Seq s{0, 0, 0, 0};
+  int b = -1;
+  bool down = false;  // a start is out of order
   if (!call.batch.starts) {
-    s = append_seq(call, row / call.batch.max_new);
+    b = row / call.batch.max_new;
   } else {
-    bool ordered = true;
 #pragma unroll 1
-    for (int b0 = 0; b0 < call.d.batch && s.n == 0; b0 += 32) {
+    for (int b0 = 0; b0 < call.d.batch; b0 += 32) {
       const int i = b0 + lane;
-      bool mine = false, down = false;
+      bool mine = false;
       if (i < call.d.batch) {
         const int begin = __ldg(call.batch.starts + i), end = __ldg(call.batch.starts + i + 1);
         mine = row >= begin && row < end;
-        down = end < begin;
+        down |= end < begin;
       }
-      ordered = ordered && !__any_sync(0xffffffffu, down);
-      unsigned who = __ballot_sync(0xffffffffu, mine);
-#pragma unroll 1
-      for (; who && s.n == 0; who &= who - 1) {
-        const int b = b0 + __ffs(who) - 1;
-        s = append_seq(call, b);
-        if (s.n && !ordered && blocks_until(call, b + 1) > units) return;  // nor do later ones
+      const unsigned who = __ballot_sync(0xffffffffu, mine);
+      if (who) {
+        b = b0 + __ffs(who) - 1;
+        break;
       }
     }
+    if (b < 0) return;
   }
+  Seq s = append_seq(call, b);
+  if (call.batch.starts && (s.n == 0 || __any_sync(0xffffffffu, down)))
+    s = taker_of(call, units, row);
   if (s.n == 0) return;
   const int pos = s.L - s.n + row - s.row;
   if (l.rotate) {
