@@ -17,10 +17,12 @@
 // power of two, and so do the rows of the open block, keys and values of both types, each
 // times its own: what one row holds, seen or not, does not touch the others.
 //
-// What bounds it.  Two prompts of 8191 tokens (32 heads over 8): 1.04 ms, 1.06 PFLOP/s of a
-// cuBLAS product's 1.92.  Without the exponentials it takes 0.96, without the conversion of
-// codes 0.93: softmax and loading warps share the issue slots, and the chain of a step
-// (scores, softmax, weights, product) is not hidden whole by the other stream's.
+// What bounds it.  Two prompts of 8191 tokens (32 heads over 8): 1.07 ms, 1.03 PFLOP/s of a
+// cuBLAS product's 1.92 (bf16: 1.24).  When it took 1.04, it was 0.96 without the exponentials
+// and 0.93 without the conversion of codes: softmax and loading warps share the issue slots,
+// and the chain of a step (scores, softmax, weights, product) is not hidden whole by the other
+// stream's.  The ordinary step's code has to stay in one piece: with the open block's in its
+// midst 1.17 ms, with that of large scores too 1.27.
 #include "block8_plan.cuh"
 #include "chunk_core.cuh"
 

@@ -800,7 +800,8 @@ def kvq_block8_attn(cache: Block8Cache, q, lengths, starts=None, max_new=None, w
     has appended: q [tokens, n_q_heads, 128] (rotated; strided views too) -> out of that
     shape.  lengths, starts as there; ``max_new`` is the most new tokens of any sequence
     (a smaller number serves single tokens and drafts faster).  window, sinks as in
-    kvq_chunk_attn."""
+    kvq_chunk_attn.  Without a ``workspace`` (block8_workspace of that max_new or more) each
+    call makes and zeroes one."""
     cfg, dev = cache.cfg, cache.dev
     n = q.shape[0]
     batch, max_new = _block8_batch(cache, n, lengths, starts, max_new)
