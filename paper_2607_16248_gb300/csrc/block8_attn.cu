@@ -113,7 +113,8 @@ Plan plan_of(const Dims8& d, int max_new, int ctas) {
   Plan p;
   const long long rows = (long long)max_new * d.gq;
   p.many = rows > kFewRows;
-  // beside longer ones, single tokens alone are short: more columns would cost them products
+  // beside longer ones, single tokens alone: with more row groups the first kernel has fewer
+  // registers to spare and its queries in shared memory (drafts beside a chunk are the second's)
   const int most = p.many ? d.gq : (int)rows;
   p.few = (most + 7) & ~7;
   p.chunk = rows > kOneTileRows ? 2 * kOneTileRows : kOneTileRows;
