@@ -667,8 +667,8 @@ kvq_status kvq_block8_append(const kvq_block8_config* cfg, const kvq_block8_cach
  * A block mapped outside [0, n_pages) counts as unseen and sets KVQ_FLAG_BAD_PAGE.
  * Codes are exact in the fp16 operands, scales meet fp32 numbers; bf16 queries and keys and
  * all values of the open block (the tokens in the ring) go to fp16 times a power of two,
- * each row its own, so an element is good to 2^-40 of its row's largest (or of 2^-100, values
- * 2^-80); the softmax weights (times their value's scale) are rounded once to fp16.  Sums,
+ * each row its own, so an element is good to 2^-40 of its row's largest (or of 2^-100), a
+ * value to 2^-33 (or of 2^-80); the softmax weights (times their value's scale) are rounded once to fp16.  Sums,
  * maxima and outputs are fp32, outputs rounded once to the type.  Scores may be as large as
  * fp32 holds; their differences are those of the scores rounded to fp32.
  *   q, out      device [n_tokens][n_q_heads][128] with the strides below (as in

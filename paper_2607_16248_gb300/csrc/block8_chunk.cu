@@ -225,10 +225,16 @@ __device__ __forceinline__ void open_block(const uint16_t* rows, int valid, unsi
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int r = h + 2 * i + (lane >> 4);
-      uint32_t x = largest(v[i]);
+      uint32_t most = largest(v[i]), least = 0xffffu;
 #pragma unroll
-      for (int o = 8; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
-      const int e = KEY ? key_lift<BF16>(x) : value_lift<BF16>(x);
+      for (int o = 8; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+      if (!KEY) {
+        least = least2(least2(least2(least2(~0u, v[i].x), v[i].y), v[i].z), v[i].w);
+        least = min(least & 0xffffu, least >> 16);
+#pragma unroll
+        for (int o = 8; o; o >>= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
+      }
+      const int e = KEY ? key_lift<BF16>(most) : value_lift<BF16>(most, least);
       st16(tile, tile_at(m >> 3, 32 * j + r, m & 7), lifted8<BF16>(v[i], pow2(e)));
       if (m == 0) {
         if (KEY) open[r].x = pow2(-e);

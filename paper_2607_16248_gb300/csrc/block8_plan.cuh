@@ -295,25 +295,33 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   }
 }
 
-// Elements of the open block go to fp16 times 2^lift, the power that takes their row's largest
-// magnitude to [2^14, 2^15): a row's elements are exact down to 2^-24 of that, and two rows
-// share nothing.  Keys: of bits from 2^-100 on.  Values: from 2^-80 on, so that sums of
-// 2^lift stay within fp32; rows of nothing as if they were the smallest, so that their
-// weights count beside any others' (a weight is held with its value's scale in it).
+// Elements of the open block go to fp16 times 2^lift, and two rows share nothing.  Keys: their
+// row's largest magnitude to 2^14, bits from 2^-100 on; elements are exact down to 2^-24 of
+// the largest.  Values, bits from 2^-80 on (sums of 2^lift stay within fp32): to 2^8, where the
+// codes are, because an element shares fp16's range with its weight, which has 2^-lift in it
+// (with 2^14 a first token without a value cost the newest ones theirs); higher, up to 2^14,
+// where the row's smallest element would lose bits.  Rows of nothing as if they were the
+// smallest, so that their weights count beside any others'.
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 template <bool BF16>
-__device__ __forceinline__ int lift_log2(uint32_t bits, int least) {
+__device__ __forceinline__ int exponent_of(uint32_t bits) {
   const float m = BF16 ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half(bits));
-  const int e = max((int)(__float_as_uint(m) >> 23) - 127, least);
-  return BF16 ? 14 - e : max(14 - e, 0);  // (fp16's smallest would not stand 2^-1)
+  return (int)(__float_as_uint(m) >> 23) - 127;
 }
 template <bool BF16>
 __device__ __forceinline__ int key_lift(uint32_t bits) {
-  return bits ? lift_log2<BF16>(bits, -100) : 0;
+  const int lift = bits ? 14 - max(exponent_of<BF16>(bits), -100) : 0;
+  return BF16 ? lift : max(lift, 0);  // (fp16's smallest would not stand 2^-1)
+}
+// (least: the smallest magnitude but 0, less 1; 0xffff for none)
+__device__ __forceinline__ uint32_t least2(uint32_t m, uint32_t x) {
+  return __vminu2(m, __vsub2(x & 0x7fff7fffu, 0x00010001u));
 }
 template <bool BF16>
-__device__ __forceinline__ int value_lift(uint32_t bits) {
-  return bits ? lift_log2<BF16>(bits, -80) : 60;  // 2^-60: kNoValue
+__device__ __forceinline__ int value_lift(uint32_t most, uint32_t least) {
+  if (!most) return 60;  // 2^-60: kNoValue
+  const int e = max(exponent_of<BF16>(most), -80);
+  return min(14 - e, max(8 - e, (BF16 ? -17 : -14) - exponent_of<BF16>(least + 1)));
 }
 template <bool BF16>
 __device__ __forceinline__ uint32_t lifted2(uint32_t u, float f) {

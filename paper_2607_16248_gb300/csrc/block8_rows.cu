@@ -414,14 +414,23 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
                                            const uint4 (&tail)[2][16][16], int t0) {
   const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const auto load = [&](int i, int r, int chunk) { return tail[i][r][chunk ^ (r & 7)]; };
-  // the largest magnitude of a row of which four lanes hold a quarter each
-  const auto row_largest = [&](const uint4 (&x)[4]) {
+  // the largest magnitude of a row of which four lanes hold a quarter each, and the least (least2)
+  const auto row_most = [&](const uint4 (&x)[4]) {
     uint32_t m = 0u;
 #pragma unroll
     for (int c = 0; c < 4; ++c) m = largest(m, x[c]);
     m = max(m & 0xffffu, m >> 16);
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  };
+  const auto row_least = [&](const uint4 (&x)[4]) {
+    uint32_t m = ~0u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      m = least2(least2(least2(least2(m, x[c].x), x[c].y), x[c].z), x[c].w);
+    m = min(m & 0xffffu, m >> 16);
+    m = min(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    return min(m, __shfl_xor_sync(0xffffffffu, m, 2));
   };
   float s[NT][4], ks[2] = {1.0f, 1.0f}, f[2] = {1.0f, 1.0f};
   int lift[2];
@@ -434,14 +443,14 @@ __device__ __forceinline__ void tail_block(const AttnParams& p, State<NT>& st, c
   for (int e = 0; e < 2; ++e) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) x[e][c] = load(1, 8 * e + gid, 4 * tig + c);
-    lift[e] = value_lift<BF16>(row_largest(x[e]));
+    lift[e] = value_lift<BF16>(row_most(x[e]), row_least(x[e]));
   }
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) x[e][c] = load(0, 8 * e + gid, 4 * tig + c);
     if constexpr (BF16) {
-      const int z = key_lift<BF16>(row_largest(x[e]));
+      const int z = key_lift<BF16>(row_most(x[e]));
       f[e] = pow2(z);
       ks[e] = pow2(-z);
     }

@@ -4,9 +4,10 @@ scores.  By both kernels: up to 32 query rows a kv-head, and more, of one row ti
 
 Tolerance: a weight is rounded to fp16, its score to fp32, as in test_gpu_block8.py: 2^-11 +
 2^-14 of sum p |v| and half a step of the result (at least half of fp16's smallest, 2^-25).
-An open token's elements are good to 2^-40 of its largest (2^-25 of fp16's smallest beside 2^15),
-which the random ones here leave far below that; small weights to 2^-32 of the largest product
-of weight and value scale: L 2^-30 of the row's largest p |v| is added where sizes are mixed."""
+An open token's elements are good to 2^-40 of its largest, values to 2^-33 (2^-25 of fp16's
+smallest beside 2^15 and 2^8), far below that for the random ones here; small weights to 2^-32
+of the largest product of weight and value scale: L 2^-30 of the row's largest p |v| is added
+where sizes are mixed."""
 
 import numpy as np
 import pytest
@@ -261,3 +262,22 @@ def test_scales_that_a_caller_chose(kvq_lib, kind, L, ks, vs):
         case.cache.scales[:, 0, i] = to
         case.seen[i][:32 * blocks] *= by.repeat(32)[:, None]
     case.attend(2.0 * q / (128.0 * ks))
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("L", [32 * 20, 32 * 20 + 18, 32 * 20 + 31])
+@pytest.mark.parametrize("dtype,size", [("fp16", 2.0 ** 12), ("fp16", 1.0), ("bf16", 1.0),
+                                        ("bf16", 2.0 ** -30)])
+def test_first_token_without_value(kvq_lib, kind, L, dtype, size):
+    """A first token with all but 1e-5 of the weight and no value, in a block with values like
+    the others': the result is the newest tokens, open ones among them, to the bits that
+    weights keep down to 2^-21 of the largest."""
+    gq, n, batch = KINDS[kind]
+    u = np.sign(randn(30, 128))
+    k, v = randn(31, L, 128), size * randn(32, L, 128)
+    k -= (k @ u)[:, None] * u / 128
+    k[0], v[0] = 13.0 * np.sqrt(128) / 128 * u, 0.0
+    q = u + 0.3 * randn(33, n, gq, 128)
+    case = Case(dtype, gq, k, v, batch)
+    case.attend(q, window=17, sinks=1)
+    case.attend(q, window=300, sinks=1)
