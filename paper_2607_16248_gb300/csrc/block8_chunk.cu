@@ -17,7 +17,7 @@
 // power of two, and so do the rows of the open block, keys and values of both types, each
 // times its own: what one row holds, seen or not, does not touch the others.
 //
-// What bounds it.  Two prompts of 8191 tokens (32 heads over 8): 1.07 ms, 1.03 PFLOP/s of a
+// What bounds it.  Two prompts of 8191 tokens (32 heads over 8): 1.08 ms, 1.02 PFLOP/s of a
 // cuBLAS product's 1.92 (bf16: 1.24).  When it took 1.04, it was 0.96 without the exponentials
 // and 0.93 without the conversion of codes: softmax and loading warps share the issue slots,
 // and the chain of a step (scores, softmax, weights, product) is not hidden whole by the other
@@ -206,35 +206,35 @@ __device__ __forceinline__ void restore_codes(const Codes& c, int k, unsigned ch
   st16(tile, tile_at(half, row, chunk + 1 - half), half ? lo : hi);
 }
 
-// The open block's rows (`valid` of them, the others zero) by a warp, 16 lanes a row, so many at
-// a time that two waits for memory do; what becomes of their factors in `open`: a key's in x,
-// log2 of a value's in y.
+// The open block's rows (`valid` of them, the others zero) by a warp, 16 lanes a row, as many at
+// a time as fit registers, since each time waits for memory; what becomes of their factors in
+// `open`: a key's in x, log2 of a value's in y.
 template <bool BF16, bool KEY>
 __device__ __forceinline__ void open_block(const uint16_t* rows, int valid, unsigned char* tile,
                                            int j, float2* open) {
   const int lane = threadIdx.x & 31, m = lane & 15;
+  constexpr int N = KEY ? 8 : 4;  // (values' least magnitudes take some too)
 #pragma unroll 1
-  for (int h = 0; h < 32; h += 16) {
-    uint4 v[8];
+  for (int h = 0; h < 32; h += 2 * N) {
+    uint4 v[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int r = h + 2 * i + (lane >> 4);
       v[i] = make_uint4(0u, 0u, 0u, 0u);
       if (r < valid) v[i] = *(reinterpret_cast<const uint4*>(rows + r * kHeadDim) + m);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int r = h + 2 * i + (lane >> 4);
-      uint32_t most = largest(v[i]), least = 0xffffu;
-#pragma unroll
-      for (int o = 8; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+      // the row's largest magnitude, and (values) above it what its least (least2) lacks to 0xffff
+      uint32_t x = largest(v[i]);
       if (!KEY) {
-        least = least2(least2(least2(least2(~0u, v[i].x), v[i].y), v[i].z), v[i].w);
-        least = min(least & 0xffffu, least >> 16);
-#pragma unroll
-        for (int o = 8; o; o >>= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
+        uint32_t y = least2(least2(least2(least2(~0u, v[i].x), v[i].y), v[i].z), v[i].w);
+        x |= ~min(y & 0xffffu, y >> 16) << 16;
       }
-      const int e = KEY ? key_lift<BF16>(most) : value_lift<BF16>(most, least);
+#pragma unroll
+      for (int o = 8; o; o >>= 1) x = __vmaxu2(x, __shfl_xor_sync(0xffffffffu, x, o));
+      const int e = KEY ? key_lift<BF16>(x) : value_lift<BF16>(x & 0xffffu, ~x >> 16);
       st16(tile, tile_at(m >> 3, 32 * j + r, m & 7), lifted8<BF16>(v[i], pow2(e)));
       if (m == 0) {
         if (KEY) open[r].x = pow2(-e);

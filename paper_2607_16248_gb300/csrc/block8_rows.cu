@@ -28,7 +28,7 @@
 //
 // What bounds it.  HBM where there is enough to read: 32 ragged chats of 2k to 32k tokens,
 // query groups of eight, bf16: 183 us, 6.1 TB/s; without the arithmetic 171.  Drafts of one
-// to five tokens in 16 chats of 8k to 32k (one to three row groups): 125 us, 5.4 TB/s, three
+// to five tokens in 16 chats of 8k to 32k (one to three row groups): 124 us, 5.5 TB/s, two
 // of them the open tokens' own factors.  One chat of 32k: 24.6 us, of which the cache's bytes
 // take 9 at 7.4 TB/s; the others are the chain of launch, plan (2.6), table (1.3), first block
 // (1.4), merge (1.1), partial and ticket (1.7), and the join (4).
